@@ -266,6 +266,121 @@ int chunkkv_decode_attention_static(const chunkkv_problem *prob, int32_t compact
                                     const void *q, const void *k, const void *v, float *out, float *lse,
                                     void *stream);
 
+/* ---- Caches in pages: from the compressed prompt on ------------------------------------------------------------
+ * Generation goes on behind Algorithm 1's K', V' (Eq. 1 sizes that cache, Section 4.4 times decoding over it): every
+ * step adds a token to the cache of every head, attends over it, and a cache that has to keep its budget gives up a
+ * token for it.  The calls below do that over pools of pages, so that sequences grow and shrink without moving:
+ *   chunkkv_paged_compact            a selection's rows and the window into pages (chunkkv_compact's form for them)
+ *   chunkkv_paged_append             head norms, position rotation and storing of new tokens
+ *   chunkkv_paged_decode_attention   attention of one new token per sequence, accumulating what every slot received
+ *   chunkkv_paged_evict              keeps the slots that received most, in place
+ *
+ * A layer's K and V are a pool each, with the same layout: page i starts at element i*stride_page, in it row r of
+ * kv-head h at h*stride_head + r*stride_tok, d contiguous elements.  Both [n_pages][Hkv][page_tokens][d] and
+ * [n_pages][page_tokens][Hkv][d] fit.  Rows are 16-byte aligned.  The tokens of a (sequence, kv-head) are in SLOTS
+ * 0 .. kv_len-1: slot s is row s % page_tokens of page page_table[b][s / page_tokens].  Slots carry no order: attention
+ * does not need one, and the position of a slot's token is in token_pos.  Device arrays:
+ *   page_table    int32 [B][table_pitch], shared by all heads and layers; entries of pages without slots are not read.
+ *                 An entry outside [0, n_pages) is a page that is not there: nothing is stored in it, its slots are
+ *                 left out of the attention and are not moved; no call reads or writes outside the pools for it
+ *   kv_len        int32 [B][Hkv], clamped to [0, max_tokens_b]
+ *   token_pos     int32 [B][Hkv][slot_pitch]    position of every slot's token
+ *   token_weight  float [B][Hkv][slot_pitch]    attention it has received, summed over the steps and the g query heads
+ *                 of its kv-head (and what the window queries gave it, where chunkkv_paged_compact was told)
+ * Rows, positions and weights of slots that hold no token are never read for a result, whatever bits they are, and stay
+ * as they are.  Two sequences may share pages that are only read; a page that is written must belong to one.
+ * Calls with n_layers take host arrays of n_layers pool pointers, and kv_len, token_pos, token_weight with a leading
+ * dimension [n_layers].  Conventions, errors and streams as above; all of the calls can be captured into a graph, the
+ * host arrays are then those of the capture.  A workspace may be shared by calls that run one after the other.
+ *
+ * Limits: head_dim 64 or 128; up to 256 query heads per kv-head; page_tokens a multiple of 16 up to 4096; max_tokens_b up
+ * to 2^24; rows of a page up to 4 MB apart.  max_tokens is what launches and workspaces are sized by: a bound of every
+ * kv_len of the sequence, lengths included that a call is going to write; the closer, the better the launches.        */
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim;
+  int32_t dtype;                /* chunkkv_dtype: of queries, new tokens and pages                             */
+  float softmax_scale;          /* 0 selects 1/sqrt(head_dim)                                                  */
+  int32_t page_tokens;          /* slots of a page                                                             */
+  int32_t n_pages;              /* pages of a pool, >= 1                                                       */
+  int32_t table_pitch;          /* entries of a row of page_table, >= max_b ceil(max_tokens_b / page_tokens)   */
+  int32_t slot_pitch;           /* entries of a row of token_pos and token_weight, >= max_b max_tokens_b       */
+  int64_t stride_page, stride_head, stride_tok;   /* elements                                                  */
+  const int32_t *max_tokens;    /* host[batch]                                                                 */
+} chunkkv_pages;
+
+/* Algorithm 1's gather (chunkkv_compact) into pages, for n_layers layers: for every layer l, sequence and kv-head the
+ * rows named by the selection of group l / reuse, in ascending order, then the window rows, go to slots 0, 1, ...
+ *   prob         geometry of the full caches, window, chunk, n_keep, flags; its out_* fields are not used
+ *   k, v         HOST arrays of n_layers full caches;  k_pages, v_pages   HOST arrays of n_layers pools
+ *   sel_*        as in chunkkv_compress_stack, ceil(n_layers / reuse) groups (chunkkv_chunk_topk writes one)
+ *   token_importance  NULL, or a HOST array of ceil(n_layers / reuse) device arrays as chunkkv_score writes them
+ *                ([B][Hkv][score_cap*chunk]): the weight a prefix token starts with.  Without it weights start at 0;
+ *                window tokens always do
+ *   kv_len       written: the rows stored, n_keep_b + w (whole-chunk mode: as many as the selection keeps)
+ *   token_pos    NULL, or written: the token's index in the full cache;  token_weight  NULL, or written
+ * prob and pages have to agree on batch, heads, head_dim and dtype, and n_keep_b + w <= max_tokens_b
+ * (CHUNKKV_ERR_SHAPE).  A malformed selection entry stores nothing; slots it should have filled stay as they are.      */
+int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *pages, int32_t n_layers, int32_t reuse,
+                          const void *const *k, const void *const *v, const int32_t *sel_chunk, const int32_t *sel_len,
+                          const int32_t *sel_count, const float *const *token_importance, const int32_t *page_table,
+                          void *const *k_pages, void *const *v_pages, int32_t *kv_len, int32_t *token_pos,
+                          float *token_weight, void *stream);
+
+/* New tokens: their queries and keys are normalised per head and rotated by position, keys and values stored in the
+ * next slots.  T = sum_b n_new_b tokens, those of sequence 0 first.  For a head's row x of q or k (all in fp32, rounded
+ * to the storage type once):
+ *   y = x * 1/sqrt(mean(x^2) + eps) * norm                                   (norm NULL: y = x)
+ *   with r = rotary_dim and a_i = positions[t] * inv_freq[i], 0 <= i < r/2, the pair (y_i, y_{i+r/2}), or with
+ *   `interleaved` (y_2i, y_2i+1), becomes (y_i cos a_i - y_j sin a_i, y_j cos a_i + y_i sin a_i); elements from r on stay.
+ *   Product and reduction to a revolution are in double: 3 * 2^-25 of a revolution at a position of 2^31, 2^-34 at 2^20.
+ * Values, and with neither norm nor rotation keys and queries too, are copied bit by bit.
+ *   n_new        HOST int32 [batch], each >= 0
+ *   q, k, v      device rows [T][heads][d] with a token stride in elements, heads contiguous: rows of a fused projection
+ *                fit.  q may be NULL (then q_out and q_norm too): keys and values only
+ *   positions    device int32 [T]
+ *   q_norm, k_norm   device [d] in the storage type, or NULL
+ *   inv_freq     device float [rotary_dim / 2], or NULL with rotary_dim 0; rotary_dim a multiple of 16, <= head_dim
+ *   q_out        device [T][Hq][d];  must not alias an input
+ *   kv_len       read: tokens before;  kv_len_out  written: tokens after; may be kv_len itself
+ *   token_pos, token_weight   NULL, or written for the new slots (the position; 0)
+ * A token past max_tokens_b is not stored and not counted; its query is computed all the same.
+ * One launch per 128 sequences, two where kv_len_out is kv_len and a sequence has more than one new token.              */
+int chunkkv_paged_append(const chunkkv_pages *pages, const int32_t *n_new, const void *q, int64_t q_stride_tok,
+                         const void *k, int64_t k_stride_tok, const void *v, int64_t v_stride_tok,
+                         const int32_t *positions, const void *q_norm, const void *k_norm, float eps,
+                         const float *inv_freq, int32_t rotary_dim, int32_t interleaved, void *q_out,
+                         const int32_t *page_table, void *k_pages, void *v_pages, const int32_t *kv_len,
+                         int32_t *kv_len_out, int32_t *token_pos, float *token_weight, void *stream);
+
+/* chunkkv_decode_attention over pages: query head i of sequence b attends to all kv_len slots of kv-head i / g.
+ *   kv_len        NULL: max_tokens_b slots in every head.  0 slots give out = 0 and lse = -inf
+ *   q             device [B][Hq][d], 16-byte aligned;  out  device float [B][Hq][d];  lse  NULL or device float [B][Hq]
+ *   token_weight  NULL, or += for every slot the sum over the g heads of its softmax weight, in fp32, in a fixed order
+ *   workspace     chunkkv_paged_decode_workspace_bytes(pages, token_weight != NULL) bytes (0 = invalid), contents scratch
+ * Precision as chunkkv_decode_attention: products and sums in fp32, softmax weights exact to fp32 (fp16: to 2^-72 of
+ * the largest).  Slots that hold no token may hold any bits; a NaN or an infinity in a slot that does gives undefined
+ * outputs of its kv-head's query heads.  The same call on the same inputs gives the same bits.                           */
+size_t chunkkv_paged_decode_workspace_bytes(const chunkkv_pages *pages, int32_t with_weights);
+int chunkkv_paged_decode_attention(const chunkkv_pages *pages, const int32_t *page_table, const int32_t *kv_len,
+                                   const void *q, const void *k_pages, const void *v_pages, float *out, float *lse,
+                                   float *token_weight, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Eviction by accumulated attention weight, in place: of a (layer, sequence, kv-head) with n > budget_b slots the
+ * budget_b first ones stay in the order (protected first, weight descending, slot ascending); protected are the tokens
+ * of the `recent` newest positions, position > max position - recent.  Kept slots below budget_b stay where they are; the
+ * others move, in ascending order, into the slots below budget_b that became free, in ascending order: rows, positions
+ * and weights of a moved slot are copied, everything else stays as it was, and kv_len becomes budget_b.  A head of
+ * budget_b slots or fewer is left alone.  Weights must not be NaN; -0 counts as +0.
+ *   budget     HOST int32 [batch], each >= 0;  recent >= 0 and <= every budget (CHUNKKV_ERR_SHAPE)
+ *   k_pages, v_pages   HOST arrays of n_layers pools
+ *   kv_len, token_pos, token_weight   [n_layers]..., read and written
+ *   workspace  chunkkv_paged_evict_workspace_bytes(pages, n_layers, budget) bytes (0 = invalid), contents scratch
+ * A row that would move from or to a page that is not there is not moved (its position and weight are).                  */
+size_t chunkkv_paged_evict_workspace_bytes(const chunkkv_pages *pages, int32_t n_layers, const int32_t *budget);
+int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int32_t *budget, int32_t recent,
+                        const int32_t *page_table, void *const *k_pages, void *const *v_pages, int32_t *kv_len,
+                        int32_t *token_pos, float *token_weight, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Scoring has two implementations with the same results (to rounding; both keep logits, exponentials and sums in
  * fp32): a single pass over K (bf16 and fp16 caches of head_dim 128, 65 to 256 window rows per kv-head, chunk
  * sizes 5, 10 and 20; not used when token_importance is requested) and a general two-pass one.
@@ -278,8 +393,9 @@ int chunkkv_decode_attention_static(const chunkkv_problem *prob, int32_t compact
  * milliseconds and the number of launches:
  *   0 score pass 0 (softmax statistics) or the single-pass kernel   1 statistics merge
  *   2 score pass 1 (importance, chunk sums) or the single-pass row reduction
- *   3 chunk sums for c larger than a key tile   4 chunk selection   5 compaction, or selection and
- *     compaction where one kernel does both (short launches; then none under 4)   6 decode attention
+ *   3 chunk sums for c larger than a key tile   4 chunk selection, and that of slots to keep   5 compaction, or selection
+ *     and compaction where one kernel does both (short launches; then none under 4), the storing of new tokens and the
+ *     moving of kept slots in pages   6 decode attention
  * total_ms and launches are host arrays of CHUNKKV_TIMING_KINDS entries.  Process-wide and not thread-safe:
  * one measurement at a time, no compression calls from other threads meanwhile.  It changes no result.   */
 #define CHUNKKV_TIMING_KINDS 7

@@ -23,6 +23,8 @@ SYMBOLS = ("chunkkv_status_string", "chunkkv_workspace_bytes", "chunkkv_score", 
            "chunkkv_compact", "chunkkv_compress_stack", "chunkkv_score_lse", "chunkkv_compress_stack_lse",
            "chunkkv_compress_layer", "chunkkv_workspace_bytes_hybrid", "chunkkv_compress_stack_hybrid", "chunkkv_jaccard", "chunkkv_decode_workspace_bytes", "chunkkv_decode_attention",
            "chunkkv_decode_attention_static", "chunkkv_quality_workspace_bytes", "chunkkv_quality_metrics",
+           "chunkkv_paged_compact", "chunkkv_paged_append", "chunkkv_paged_decode_workspace_bytes", "chunkkv_paged_decode_attention",
+           "chunkkv_paged_evict_workspace_bytes", "chunkkv_paged_evict",
            "chunkkv_timing_begin",
            "chunkkv_timing_end")
 TIMING_KINDS = ("score_stats", "stats_merge", "score_colsum", "chunk_sums", "chunk_topk", "compact", "decode")
@@ -136,6 +138,75 @@ class Problem(_KeepsStruct):
         return cp
 
 
+class _CPages(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("softmax_scale", C.c_float), ("page_tokens", C.c_int32), ("n_pages", C.c_int32), ("table_pitch", C.c_int32), ("slot_pitch", C.c_int32),
+        ("stride_page", C.c_int64), ("stride_head", C.c_int64), ("stride_tok", C.c_int64), ("max_tokens", C.POINTER(C.c_int32)),
+    ]
+
+
+@dataclass
+class Pages(_KeepsStruct):
+    """Python mirror of chunkkv_pages (see include/chunkkv.h for the meaning of every field).  Without strides the pools are
+    [n_pages][n_kv_heads][page_tokens][head_dim]; without pitches the arrays are as wide as max_tokens needs."""
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    dtype: int
+    page_tokens: int
+    n_pages: int
+    max_tokens: Sequence[int]
+    stride_page: int = 0
+    stride_head: int = 0
+    stride_tok: int = 0
+    table_pitch: int = 0
+    slot_pitch: int = 0
+    softmax_scale: float = 0.0
+
+    def __post_init__(self):
+        if self.stride_tok == 0:
+            self.stride_tok = self.head_dim
+            self.stride_head = self.page_tokens * self.head_dim
+            self.stride_page = self.n_kv_heads * self.stride_head
+        most = max([1] + [int(n) for n in self.max_tokens])
+        if self.table_pitch == 0:
+            self.table_pitch = -(-most // max(1, self.page_tokens))
+        if self.slot_pitch == 0:
+            self.slot_pitch = most
+
+    @property
+    def batch(self) -> int:
+        return len(self.max_tokens)
+
+    def pool_elements(self) -> int:
+        """Elements from the start of a pool to the end of its last row."""
+        return ((self.n_pages - 1) * self.stride_page + (self.n_kv_heads - 1) * self.stride_head
+                + (self.page_tokens - 1) * self.stride_tok + self.head_dim)
+
+    # As the struct of a Problem: kept with the numbers it holds, which are compared on every call.
+    def _c(self):
+        now = (self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype, self.page_tokens, self.n_pages, self.stride_page, self.stride_head,
+               self.stride_tok, self.table_pitch, self.slot_pitch, self.softmax_scale, tuple(self.max_tokens))
+        kept = getattr(self, "_kept", None)
+        if kept is None or kept[0] != now:
+            cp = self.as_c()
+            plain = tuple(tuple(map(int, x)) if isinstance(x, tuple) else float(x) if isinstance(x, float) else int(x) for x in now)
+            kept = self._kept = (plain, cp, C.byref(cp))
+        return kept[2]
+
+    def __getstate__(self):
+        return self.__dict__.copy()
+
+    def as_c(self):
+        B = self.batch
+        most = (C.c_int32 * B)(*[int(x) for x in self.max_tokens])
+        cp = _CPages(B, self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype, self.softmax_scale, self.page_tokens, self.n_pages,
+                     self.table_pitch, self.slot_pitch, self.stride_page, self.stride_head, self.stride_tok, most)
+        cp._keep = most
+        return cp
+
+
 _lib = None
 
 
@@ -190,6 +261,21 @@ def load_library(path: Optional[str] = None):
     lib.chunkkv_quality_workspace_bytes.argtypes = [C.POINTER(_CProblem)]
     lib.chunkkv_quality_metrics.restype = C.c_int
     lib.chunkkv_quality_metrics.argtypes = [C.POINTER(_CProblem), i32p, vp, vp, vp, vp, vp, f32p, f32p, vp, C.c_size_t, vp]
+    lib.chunkkv_paged_compact.restype = C.c_int
+    lib.chunkkv_paged_compact.argtypes = [C.POINTER(_CProblem), C.POINTER(_CPages), C.c_int32, C.c_int32, C.POINTER(vp), C.POINTER(vp), i32p, i32p,
+                                          i32p, C.POINTER(vp), i32p, C.POINTER(vp), C.POINTER(vp), i32p, i32p, f32p, vp]
+    lib.chunkkv_paged_append.restype = C.c_int
+    lib.chunkkv_paged_append.argtypes = [C.POINTER(_CPages), i32p, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32p, vp, vp, C.c_float, f32p, C.c_int32,
+                                         C.c_int32, vp, i32p, vp, vp, i32p, i32p, i32p, f32p, vp]
+    lib.chunkkv_paged_decode_workspace_bytes.restype = C.c_size_t
+    lib.chunkkv_paged_decode_workspace_bytes.argtypes = [C.POINTER(_CPages), C.c_int32]
+    lib.chunkkv_paged_decode_attention.restype = C.c_int
+    lib.chunkkv_paged_decode_attention.argtypes = [C.POINTER(_CPages), i32p, i32p, vp, vp, vp, f32p, f32p, f32p, vp, C.c_size_t, vp]
+    lib.chunkkv_paged_evict_workspace_bytes.restype = C.c_size_t
+    lib.chunkkv_paged_evict_workspace_bytes.argtypes = [C.POINTER(_CPages), C.c_int32, i32p]
+    lib.chunkkv_paged_evict.restype = C.c_int
+    lib.chunkkv_paged_evict.argtypes = [C.POINTER(_CPages), C.c_int32, i32p, C.c_int32, i32p, C.POINTER(vp), C.POINTER(vp), i32p, i32p, f32p, vp,
+                                        C.c_size_t, vp]
     lib.chunkkv_decode_attention_static.restype = C.c_int
     lib.chunkkv_decode_attention_static.argtypes = [C.POINTER(_CProblem), C.c_int32, i32p, vp, vp, vp, f32p, f32p, vp]
     _lib = lib
@@ -356,6 +442,136 @@ def chunkkv_decode_attention_static(prob: Problem, compacted: bool, kv_len, q, k
     _check(load_library().chunkkv_decode_attention_static(
         cp, 1 if compacted else 0, _ptr(kv_len), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
         _stream(stream)), "chunkkv_decode_attention_static")
+
+
+# ---- caches in pages ----
+# A wrong size here is a read or a write out of bounds on the device, so sizes, types and devices are compared with the
+# handle's before the call (0.1 us a tensor).
+_KINDS = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}
+
+
+def _need(where: str, device: int, name: str, t: Optional[torch.Tensor], kind, elements: int, strided: bool = False) -> None:
+    if t is None:
+        return
+    if t.dtype != kind:
+        raise ValueError(f"{where}: {name} is {t.dtype}, not {kind}")
+    if t.get_device() != device:
+        raise ValueError(f"{where}: {name} is on device {t.get_device()}, the call runs on {device}")
+    if not strided and (t.numel() < elements or not t.is_contiguous()):
+        raise ValueError(f"{where}: {name} has {t.numel()} elements{'' if t.is_contiguous() else ', not contiguous'}; {elements} are needed")
+
+
+def _need_pool(where: str, device: int, name: str, t: torch.Tensor, pages: Pages) -> None:
+    _need(where, device, name, t, _KINDS.get(pages.dtype), 0, True)
+    room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+    if room < pages.pool_elements():
+        raise ValueError(f"{where}: {name} has {room} elements, the pages reach to {pages.pool_elements()}")
+
+
+def _new_rows(where: str, device: int, name: str, t: torch.Tensor, kind, tokens: int, heads: int, dim: int) -> int:
+    """Token stride of [tokens][heads][dim] rows."""
+    _need(where, device, name, t, kind, 0, True)
+    if tuple(t.shape) != (tokens, heads, dim) or (tokens and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim))):
+        raise ValueError(f"{where}: {name} is {tuple(t.shape)} with strides {t.stride()}, not [{tokens}][{heads}][{dim}] with contiguous heads")
+    return t.stride(0) if tokens > 1 else max(t.stride(0), heads * dim)
+
+
+def _pointers(ts):
+    return (C.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
+
+
+def chunkkv_paged_compact(prob: Problem, pages: Pages, reuse: int, k: Sequence, v: Sequence, sel_chunk, sel_len, sel_count, token_importance,
+                          page_table, k_pages: Sequence, v_pages: Sequence, kv_len, token_pos, token_weight, stream=None) -> None:
+    where, n, dev = "chunkkv_paged_compact", len(k), torch.cuda.current_device()
+    heads = pages.batch * pages.n_kv_heads
+    groups = -(-n // max(1, reuse))
+    if not len(v) == len(k_pages) == len(v_pages) == n or (token_importance is not None and len(token_importance) != groups):
+        raise ValueError(f"{where}: lists of {n}, {len(v)}, {len(k_pages)} and {len(v_pages)} layers")
+    for name, t, kind, each in (("sel_chunk", sel_chunk, torch.int32, groups * heads * prob.sel_cap), ("sel_len", sel_len, torch.int32, groups * heads * prob.sel_cap),
+                                ("sel_count", sel_count, torch.int32, groups * heads), ("page_table", page_table, torch.int32, pages.batch * pages.table_pitch),
+                                ("kv_len", kv_len, torch.int32, n * heads), ("token_pos", token_pos, torch.int32, n * heads * pages.slot_pitch),
+                                ("token_weight", token_weight, torch.float32, n * heads * pages.slot_pitch)):
+        _need(where, dev, name, t, kind, each)
+    for t in token_importance or ():
+        _need(where, dev, "token_importance", t, torch.float32, heads * prob.score_cap * prob.chunk)
+    for name, ts in (("k_pages", k_pages), ("v_pages", v_pages)):
+        for t in ts:
+            _need_pool(where, dev, name, t, pages)
+    for name, ts in (("k", k), ("v", v)):
+        for t in ts:
+            _need(where, dev, name, t, _KINDS.get(prob.dtype), 0, True)
+    _check(load_library().chunkkv_paged_compact(
+        prob._c(), pages._c(), n, reuse, _pointers(k), _pointers(v), _ptr(sel_chunk), _ptr(sel_len), _ptr(sel_count),
+        None if token_importance is None else _pointers(token_importance), _ptr(page_table), _pointers(k_pages), _pointers(v_pages), _ptr(kv_len),
+        _ptr(token_pos), _ptr(token_weight), _stream(stream)), where)
+
+
+def chunkkv_paged_append(pages: Pages, n_new: Sequence[int], q, k, v, positions, q_norm, k_norm, eps: float, inv_freq, interleaved: bool, q_out,
+                         page_table, k_pages, v_pages, kv_len, kv_len_out, token_pos, token_weight, stream=None) -> None:
+    """q, k, v: [tokens][heads][head_dim], views of a fused projection among them; rotary_dim is twice inv_freq's length."""
+    where, dev, kind = "chunkkv_paged_append", torch.cuda.current_device(), _KINDS.get(pages.dtype)
+    if len(n_new) != pages.batch:
+        raise ValueError(f"{where}: n_new has {len(n_new)} entries for {pages.batch} sequences")
+    new = (C.c_int32 * len(n_new))(*[int(x) for x in n_new])
+    tokens, heads, d = max(0, sum(new)), pages.batch * pages.n_kv_heads, pages.head_dim
+    q_tok = 0 if q is None else _new_rows(where, dev, "q", q, kind, tokens, pages.n_q_heads, d)
+    k_tok, v_tok = (_new_rows(where, dev, name, t, kind, tokens, pages.n_kv_heads, d) for name, t in (("k", k), ("v", v)))
+    for name, t, of, each in (("positions", positions, torch.int32, tokens), ("q_norm", q_norm, kind, d), ("k_norm", k_norm, kind, d),
+                              ("q_out", q_out, kind, tokens * pages.n_q_heads * d), ("page_table", page_table, torch.int32, pages.batch * pages.table_pitch),
+                              ("kv_len", kv_len, torch.int32, heads), ("kv_len_out", kv_len_out, torch.int32, heads), ("inv_freq", inv_freq, torch.float32, 0),
+                              ("token_pos", token_pos, torch.int32, heads * pages.slot_pitch), ("token_weight", token_weight, torch.float32, heads * pages.slot_pitch)):
+        _need(where, dev, name, t, of, each)
+    _need_pool(where, dev, "k_pages", k_pages, pages)
+    _need_pool(where, dev, "v_pages", v_pages, pages)
+    _check(load_library().chunkkv_paged_append(
+        pages._c(), new, _ptr(q), q_tok, _ptr(k), k_tok, _ptr(v), v_tok, _ptr(positions), _ptr(q_norm), _ptr(k_norm), eps, _ptr(inv_freq),
+        0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, _ptr(q_out), _ptr(page_table), _ptr(k_pages), _ptr(v_pages), _ptr(kv_len),
+        _ptr(kv_len_out), _ptr(token_pos), _ptr(token_weight), _stream(stream)), where)
+
+
+def chunkkv_paged_decode_workspace_bytes(pages: Pages, with_weights: bool = False) -> int:
+    return int(load_library().chunkkv_paged_decode_workspace_bytes(pages._c(), 1 if with_weights else 0))
+
+
+def chunkkv_paged_decode_attention(pages: Pages, page_table, kv_len, q, k_pages, v_pages, out, lse, token_weight, workspace, stream=None) -> None:
+    where, dev, kind = "chunkkv_paged_decode_attention", torch.cuda.current_device(), _KINDS.get(pages.dtype)
+    rows, heads = pages.batch * pages.n_q_heads, pages.batch * pages.n_kv_heads
+    for name, t, of, each in (("page_table", page_table, torch.int32, pages.batch * pages.table_pitch), ("kv_len", kv_len, torch.int32, heads),
+                              ("q", q, kind, rows * pages.head_dim), ("out", out, torch.float32, rows * pages.head_dim), ("lse", lse, torch.float32, rows),
+                              ("token_weight", token_weight, torch.float32, heads * pages.slot_pitch)):
+        _need(where, dev, name, t, of, each)
+    _need_pool(where, dev, "k_pages", k_pages, pages)
+    _need_pool(where, dev, "v_pages", v_pages, pages)
+    _check(load_library().chunkkv_paged_decode_attention(
+        pages._c(), _ptr(page_table), _ptr(kv_len), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(out), _ptr(lse), _ptr(token_weight), _ptr(workspace),
+        _bytes(workspace), _stream(stream)), where)
+
+
+def chunkkv_paged_evict_workspace_bytes(pages: Pages, n_layers: int, budget: Sequence[int]) -> int:
+    return int(load_library().chunkkv_paged_evict_workspace_bytes(pages._c(), n_layers, _budgets("chunkkv_paged_evict_workspace_bytes", pages, budget)))
+
+
+def _budgets(where: str, pages: Pages, budget: Sequence[int]):
+    if len(budget) != pages.batch:
+        raise ValueError(f"{where}: budget has {len(budget)} entries for {pages.batch} sequences")
+    return (C.c_int32 * len(budget))(*[int(x) for x in budget])
+
+
+def chunkkv_paged_evict(pages: Pages, budget: Sequence[int], recent: int, page_table, k_pages: Sequence, v_pages: Sequence, kv_len, token_pos,
+                        token_weight, workspace, stream=None) -> None:
+    where, n, dev = "chunkkv_paged_evict", len(k_pages), torch.cuda.current_device()
+    if len(v_pages) != n:
+        raise ValueError(f"{where}: lists of {n} and {len(v_pages)} layers")
+    heads = n * pages.batch * pages.n_kv_heads
+    for name, t, of, each in (("page_table", page_table, torch.int32, pages.batch * pages.table_pitch), ("kv_len", kv_len, torch.int32, heads),
+                              ("token_pos", token_pos, torch.int32, heads * pages.slot_pitch), ("token_weight", token_weight, torch.float32, heads * pages.slot_pitch)):
+        _need(where, dev, name, t, of, each)
+    for name, ts in (("k_pages", k_pages), ("v_pages", v_pages)):
+        for t in ts:
+            _need_pool(where, dev, name, t, pages)
+    _check(load_library().chunkkv_paged_evict(
+        pages._c(), n, _budgets(where, pages, budget), recent, _ptr(page_table), _pointers(k_pages), _pointers(v_pages), _ptr(kv_len), _ptr(token_pos),
+        _ptr(token_weight), _ptr(workspace), _bytes(workspace), _stream(stream)), where)
 
 
 def chunkkv_timing_begin(max_records: int = 4096) -> None:

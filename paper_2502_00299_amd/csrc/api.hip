@@ -64,29 +64,25 @@ struct Plan {
 };
 
 // ---- optional per-kernel timing (chunkkv_timing_begin / chunkkv_timing_end) -----------------------
-enum Kind { kStats = 0, kCombine, kColsum, kChunkSums, kTopk, kCompact, kDecode, kKinds };
-static_assert(kKinds == CHUNKKV_TIMING_KINDS, "timing kinds of the header");
 struct Timing {
   bool on = false;
   int cap = 0, used = 0;
   hipEvent_t *ev = nullptr;  // 2 per record
   int *kind = nullptr;
 } g_timing;
+}  // namespace
 
-struct Timed {  // records an event pair around one launch when timing is on
-  hipStream_t s;
-  int slot = -1;
-  Timed(int kind, hipStream_t stream) : s(stream) {
-    if (g_timing.on && g_timing.used < g_timing.cap) {
-      slot = g_timing.used++;
-      g_timing.kind[slot] = kind;
-      (void)hipEventRecord(g_timing.ev[2 * slot], s);
-    }
+Timed::Timed(int kind, hipStream_t stream) : s(stream) {
+  if (g_timing.on && g_timing.used < g_timing.cap) {
+    slot = g_timing.used++;
+    g_timing.kind[slot] = kind;
+    (void)hipEventRecord(g_timing.ev[2 * slot], s);
   }
-  ~Timed() {
-    if (slot >= 0) (void)hipEventRecord(g_timing.ev[2 * slot + 1], s);
-  }
-};
+}
+Timed::~Timed() {
+  if (slot >= 0) (void)hipEventRecord(g_timing.ev[2 * slot + 1], s);
+}
+namespace {
 
 // ---- device-resident scratch for chunkkv_decode_attention_static ---------------------------------
 // One array per GPU the library runs on, held until the process ends.  Its name is only a host-side
@@ -116,6 +112,7 @@ int static_scratch(void **out) {
 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+}  // namespace
 int check_problem(const chunkkv_problem *p, bool need_out) {
   if (!p) return CHUNKKV_ERR_NULL;
   if (!p->seqlen || !p->n_keep || !p->kv_base) return CHUNKKV_ERR_NULL;
@@ -153,8 +150,7 @@ int check_problem(const chunkkv_problem *p, bool need_out) {
   return CHUNKKV_OK;
 }
 
-bool misaligned(const void *p) { return ((uintptr_t)p & 15) != 0; }
-
+namespace {
 // Do the single-pass kernels score a group with this chunk size (no log-sum-exps, no token importance asked for)?
 bool takes_one_pass(const chunkkv_problem *p, const Plan &pl, int chunk) {
   return !(p->flags & CHUNKKV_FLAG_TWO_PASS) && pl.n_periods_fit && single_pass_ok(p->dtype, p->head_dim, (p->n_q_heads / p->n_kv_heads) * p->window, chunk);

@@ -244,6 +244,20 @@ __device__ __forceinline__ int find_sequence(const ScoreArgs &a, int &x) {
   return seq;
 }
 
+// ---- host side, shared by the entry points (api.hip) ----
+int check_problem(const chunkkv_problem *p, bool need_out);
+inline bool misaligned(const void *p) { return ((uintptr_t)p & 15) != 0; }
+// Kinds of chunkkv_timing_end, and the event pair around one launch while timing is on.
+enum Kind { kStats = 0, kCombine, kColsum, kChunkSums, kTopk, kCompact, kDecode, kKinds };
+static_assert(kKinds == CHUNKKV_TIMING_KINDS, "timing kinds of the header");
+struct Timed {
+  hipStream_t s;
+  int slot = -1;
+  Timed(int kind, hipStream_t stream);
+  ~Timed();
+  Timed(const Timed &) = delete;
+};
+
 // Geometry of the scoring kernels for one (dtype, head_dim, row count).
 struct ScoreGeom {
   int row_bytes;   // head_dim * sizeof(element)

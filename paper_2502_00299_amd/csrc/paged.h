@@ -1,0 +1,135 @@
+// Caches in pages: what the kernels of paged_*.hip and their entry points share.
+#pragma once
+#include "internal.h"
+
+namespace ckv {
+
+constexpr int kPagedBatch = 128;        // sequences per launch: their tables travel as kernel arguments
+constexpr int kPagedMaxTokens = 1 << 24;
+constexpr int kPagedMaxGroup = 256;     // query heads per kv-head
+
+// A pool of pages, strides in bytes.  Slots are addressed by blocks of 16: a page is a whole number of them, so a block
+// never crosses pages, whatever the page size is.
+struct PageGeom {
+  int64_t page, head, tok;
+  const int32_t *table;                 // [batch_total][pitch]
+  int32_t pitch, n_pages;
+  uint32_t blocks, magic;               // 16-row blocks of a page; ceil(2^32 / blocks), not used for one
+};
+
+// Page of block `blk` of a sequence.  Exact: blk < 2^20 and blocks <= 256, so blk times the magic number's excess stays below 2^32.
+__device__ __forceinline__ uint32_t page_of_block(const PageGeom &g, uint32_t blk) {
+  return g.blocks == 1 ? blk : __umulhi(blk, g.magic);
+}
+// Byte offset in a pool of the first row of block `blk` of kv-head h, or -1 where the page is not there.
+__device__ __forceinline__ int64_t block_offset(const PageGeom &g, const int32_t *row, int h, uint32_t blk) {
+  const uint32_t p = page_of_block(g, blk);
+  const int32_t page = row[p];
+  const int64_t at = (int64_t)page * g.page + (int64_t)h * g.head + (int64_t)((blk - p * g.blocks) * 16) * g.tok;
+  return page >= 0 && page < g.n_pages ? at : -1;
+}
+// The same for one slot.
+__device__ __forceinline__ int64_t slot_offset(const PageGeom &g, const int32_t *row, int h, int slot) {
+  const int64_t at = block_offset(g, row, h, (uint32_t)slot >> 4);
+  return at < 0 ? -1 : at + (int64_t)(slot & 15) * g.tok;
+}
+
+// Sequence of entry x of a grid that counts the entries (ranges, tokens) of all sequences of a launch; first[i]: number of
+// the first entry of sequence i, INT32_MAX past the last one.  Two levels, so that at most 22 scalars are compared.
+#define CKV_PAGED_SEQUENCE(ARGS, x, nb) paged_sequence<offsetof(ARGS, first)>(x, nb)
+template <size_t FIRST>
+__device__ __forceinline__ int paged_sequence(int x, int nb) {
+  int lo = 0;
+  if (nb > 16) {
+#pragma unroll
+    for (int i = 16; i < kPagedBatch; i += 16) lo += x >= kernarg_at<int32_t>(FIRST, i) ? 16 : 0;
+  }
+  int b = lo;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) b += x >= kernarg_at<int32_t>(FIRST, lo + i) ? 1 : 0;
+  return b;
+}
+
+struct PagedAppendArgs {
+  PageGeom geom;
+  const void *q, *k, *v;
+  void *q_out, *k_pages, *v_pages;
+  const void *q_norm, *k_norm;
+  const float *inv_freq;
+  const int32_t *positions, *kv_len;
+  int32_t *kv_len_out, *token_pos;
+  float *token_weight;
+  int64_t q_tok, k_tok, v_tok;          // bytes
+  int32_t tokens, token0;               // of the launch; number of its first token
+  int32_t batch0, batch, n_q_heads, n_kv_heads, slot_pitch;
+  int32_t rotary, interleaved, parts;   // parts: wavefronts that share a token's rows
+  int32_t write_len;                    // 1: the last new token of a sequence writes its length
+  float eps;
+  int32_t first[kPagedBatch + 16], max_tokens[kPagedBatch];
+};
+
+struct PagedLenArgs {                   // kv_len_out = min(kv_len + n_new, max_tokens)
+  const int32_t *kv_len;
+  int32_t *kv_len_out;
+  int32_t batch0, batch, n_kv_heads;
+  int32_t n_new[kPagedBatch], max_tokens[kPagedBatch];
+};
+
+struct PagedCompactArgs {
+  PageGeom geom;
+  const void *k[kMaxLayersPerLaunch], *v[kMaxLayersPerLaunch];
+  void *k_pages[kMaxLayersPerLaunch], *v_pages[kMaxLayersPerLaunch];
+  const float *importance[kMaxLayersPerLaunch];   // of the layer's group, or null
+  SeqTable seq;
+  const int32_t *sel_chunk, *sel_len, *sel_count;
+  int32_t *kv_len, *token_pos;
+  float *token_weight;
+  int64_t kv_stride_head, kv_stride_tok;          // elements
+  int64_t imp_pitch;
+  int32_t layer0, reuse, batch0, batch_total, n_kv_heads, window, chunk, elem_bytes, sel_cap, slot_pitch, whole_chunks;
+  int32_t entries;                                // selection entries of a workgroup
+};
+
+struct PagedDecodeArgs {
+  PageGeom geom;
+  const void *q, *k, *v;
+  float *out, *lse, *weight;
+  const int32_t *kv_len;
+  float2 *part_ml;                      // (max in log2 units, sum) of every range and query head: [range][Hq]
+  float *part_o;                        // [range][Hq][d]
+  float *scores;                        // scaled logits in log2 units: first_row * Hq numbers of the sequences before, then [Hq][rows_b]
+  int32_t batch0, batch, n_q_heads, n_kv_heads, group, slot_pitch;
+  float scale_log2e;
+  int32_t direct;                       // 1: every head is one range, the range kernel writes the outputs
+  int32_t first[kPagedBatch + 16];      // number of the first key range of every sequence
+  int32_t first_row[kPagedBatch];       // rows of the sequences before, each rounded up to 32
+  int32_t max_tokens[kPagedBatch];
+};
+constexpr int kPagedMinRange = 128, kPagedMaxRange = 1024;   // rows of a key range
+// Rows of every range of a head with n slots that `splits` ranges share.  From the length that the device knows, so that
+// all ranges have work when max_tokens is far above it.
+__host__ __device__ inline int paged_range_rows(int n, int splits) {
+  const int r = ((n + splits - 1) / splits + 31) & ~31;
+  return r < kPagedMinRange ? kPagedMinRange : r;
+}
+
+struct PagedEvictArgs {
+  PageGeom geom;
+  void *k_pages[kMaxLayersPerLaunch], *v_pages[kMaxLayersPerLaunch];
+  int32_t *kv_len, *token_pos;          // [layer][batch_total][Hkv]..., from the launch's first layer on
+  float *token_weight;
+  int32_t *lists;                       // [layer][batch_total][Hkv][2 * pitch + 1]: slots that move, free slots, their number
+  int32_t pitch;
+  int32_t batch0, batch_total, n_kv_heads, slot_pitch, recent;
+  int32_t row_bytes;
+  int32_t budget[kPagedBatch], max_tokens[kPagedBatch];
+};
+
+int launch_paged_append(int dtype, int head_dim, const PagedAppendArgs &a, hipStream_t s);
+int launch_paged_len(const PagedLenArgs &a, hipStream_t s);
+int launch_paged_compact(int row_bytes, const PagedCompactArgs &a, int n_layers, int batch, hipStream_t s);
+int launch_paged_decode(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s);
+int paged_decode_heads(int dtype, int group);   // query heads of a kv-head that a workgroup serves
+int launch_paged_evict(const PagedEvictArgs &a, int n_layers, int batch, int max_tokens, hipStream_t s);
+
+}  // namespace ckv

@@ -38,12 +38,22 @@ struct Selected {
   int count, kept;   // chunks and tokens
 };
 
+struct NoMore {};
+// A score as it is ranked: fp32 by order_key, a key (1 and up) as it is.
+__device__ __forceinline__ uint32_t rank_key(float x) { return order_key(x); }
+__device__ __forceinline__ uint32_t rank_key(uint32_t x) { return x; }
+template <typename S>
+__device__ __forceinline__ uint32_t bits_of(S x) { return __builtin_bit_cast(uint32_t, x); }
+
 // T: threads of the workgroup, KR: chunks a thread takes at a time, REG: all keys of the head stay in registers (C <= KR T),
-// otherwise every step re-reads the scores.  P candidate tokens, chunk size c; emit(chunk, place, length, token offset) is
-// called once for every selected chunk, by the thread that owns it.
-template <int T, int KR, bool REG, typename Emit>
-__device__ __forceinline__ Selected select_chunks(const float *scores, int P, int c, int n_keep, bool whole_chunks, Emit emit) {
+// otherwise every step re-reads the scores (scores[i]: of chunk i, fp32 or a key).  P candidate tokens, chunk size c; emit(chunk, place,
+// length, token offset) is called once for every selected chunk, by the thread that owns it.  more(ranked, selected), if
+// given, is called instead of it, by all threads: selected(chunk, key) tells which chunks are, and ranked(pred, f) calls
+// f(chunk, rank) for those of a kind; a barrier has to lie between two calls of ranked.
+template <int T, int KR, bool REG, typename Scores, typename Emit, typename More = NoMore>
+__device__ __forceinline__ Selected select_chunks(Scores scores, int P, int c, int n_keep, bool whole_chunks, Emit emit, More more = {}) {
   constexpr int NW = T / 64;
+  using S = std::decay_t<decltype(scores[0])>;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int C = (P + c - 1) / c;
   // exact budget: ceil(n_keep / c) chunks, the lowest-ranked one cut; whole-chunk mode: floor(n_keep / c)
@@ -64,9 +74,9 @@ __device__ __forceinline__ Selected select_chunks(const float *scores, int P, in
   if constexpr (REG) {
 #pragma unroll
     for (int j = 0; j < KR; ++j)
-      kreg[j] = __float_as_uint(scores[j * T + tid < C ? j * T + tid : C - 1]);
+      kreg[j] = bits_of(scores[j * T + tid < C ? j * T + tid : C - 1]);
 #pragma unroll
-    for (int j = 0; j < KR; ++j) kreg[j] = j * T + tid < C ? order_key(__uint_as_float(kreg[j])) : 0u;
+    for (int j = 0; j < KR; ++j) kreg[j] = j * T + tid < C ? rank_key(__builtin_bit_cast(S, kreg[j])) : 0u;
   }
   // f(chunk index, key) for every own chunk, in index order.  Places past the last chunk carry key 0, which ranks below
   // every chunk: they may be counted and listed but are never the threshold or above it.
@@ -77,12 +87,12 @@ __device__ __forceinline__ Selected select_chunks(const float *scores, int P, in
         if (KR <= 4 || j * T < C) f(j * T + tid, kreg[j]);
     } else {
       for (int i0 = tid; i0 < C; i0 += 8 * T) {
-        float x[8];
+        S x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = scores[i0 + j * T < C ? i0 + j * T : C - 1];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (i0 + j * T < C) f(i0 + j * T, order_key(x[j]) - low);
+          if (i0 + j * T < C) f(i0 + j * T, rank_key(x[j]) - low);
       }
     }
   };
@@ -96,7 +106,7 @@ __device__ __forceinline__ Selected select_chunks(const float *scores, int P, in
         int n = 0;
         if (KR <= 4 || i0 + j * T < C) {
           const int i = i0 + j * T + tid;
-          const bool p = REG ? pred(i, kreg[REG ? j : 0]) : i < C && pred(i, order_key(scores[i < C ? i : C - 1]) - low);
+          const bool p = REG ? pred(i, kreg[REG ? j : 0]) : i < C && pred(i, rank_key(scores[i < C ? i : C - 1]) - low);
           own |= p ? 1u << j : 0u;
           n = (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(p));
         }
@@ -150,7 +160,7 @@ __device__ __forceinline__ Selected select_chunks(const float *scores, int P, in
 #pragma unroll
     for (int j = 0; j < KR; ++j) kreg[j] = kreg[j] != 0 ? kreg[j] - low : 0u;
   }
-  const uint32_t tail_key = order_key(scores[C - 1]) - low;
+  const uint32_t tail_key = rank_key(scores[C - 1]) - low;
   const int hi = 32 - __builtin_clz(kmx - low);   // bits [0, hi) may be set
 
   uint32_t thr = 0;    // key and index of the m-th ranked chunk
@@ -229,10 +239,13 @@ __device__ __forceinline__ Selected select_chunks(const float *scores, int P, in
   const int size_trunc = thr_idx == C - 1 ? tail_size : c;
   const int len_trunc = whole_chunks ? size_trunc : n_keep - (total - size_trunc);
 
-  ranked([&](int i, uint32_t key) { return key > thr || (key == thr && i <= thr_idx); },
-         [&](int i, int pos) {
-           emit(i, pos, i == thr_idx ? len_trunc : (i == C - 1 ? tail_size : c), pos * c - (i > thr_idx ? size_trunc - len_trunc : 0));
-         });
+  auto selected = [&](int i, uint32_t key) { return key > thr || (key == thr && i <= thr_idx); };
+  if constexpr (std::is_same_v<More, NoMore>)
+    ranked(selected, [&](int i, int pos) {
+      emit(i, pos, i == thr_idx ? len_trunc : (i == C - 1 ? tail_size : c), pos * c - (i > thr_idx ? size_trunc - len_trunc : 0));
+    });
+  else
+    more(ranked, selected);
   return {m, whole_chunks ? total : n_keep};
 }
 

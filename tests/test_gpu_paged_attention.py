@@ -1,0 +1,157 @@
+"""Attention of one new token over pages, and the weights it accumulates, against float64."""
+import pytest
+import torch
+
+import paper_2502_00299_amd as ckv
+from tests import paged_helpers as H
+
+pytestmark = pytest.mark.gpu
+DEV = H.DEV
+F32, BF16, F16 = ckv.F32, ckv.BF16, ckv.F16
+
+# A logit is a sum of head_dim products, in chains of at most 24 roundings: 24 * 2^-24 * sum |q k| * scale, about 10 for these
+# inputs, is 1.5e-5 nats.  A weight is off by that relatively, its normalisation again; the log-sum-exp by that absolutely.
+LOGIT = 1.5e-5
+PAIR = 2 * LOGIT
+
+
+def run(cache, q, lens, weight=None, lse=True, scratch=0xFF):
+    """out, lse, weight of a call whose workspace holds NaN."""
+    p = cache.pages
+    ws = torch.full((ckv.chunkkv_paged_decode_workspace_bytes(p, weight is not None),), scratch, dtype=torch.uint8, device=DEV)
+    out = torch.full((cache.batch, cache.hq, cache.d), float("nan"), device=DEV)
+    got = torch.full((cache.batch, cache.hq), float("nan"), device=DEV) if lse else None
+    w = None if weight is None else weight.to(DEV)
+    n = None if lens is None else torch.as_tensor(lens, dtype=torch.int32).to(DEV)
+    ckv.chunkkv_paged_decode_attention(p, cache.table.to(DEV), n, q.to(DEV), cache.pool(cache.k)[0], cache.pool(cache.v)[0], out, got, w, ws)
+    return out.cpu(), None if got is None else got.cpu(), None if w is None else w.cpu()
+
+
+def check(cache, q, lens, with_weights=True):
+    want, want_lse, want_weight, top = H.attention(cache, q, lens)
+    before = cache.weight[0].clone()
+    out, lse, weight = run(cache, q, lens, before if with_weights else None)
+    g = cache.hq // cache.hkv
+    for b in range(cache.batch):
+        for h in range(cache.hkv):
+            heads, n = slice(h * g, (h + 1) * g), int(lens[b][h])
+            if torch.isinf(want_lse[b, heads]).any():
+                assert (out[b, heads] == 0).all() and (lse[b, heads] == float("-inf")).all()
+            else:
+                assert float((out[b, heads].double() - want[b, heads]).abs().max()) <= PAIR * float(top[b, h])
+                assert float((lse[b, heads].double() - want_lse[b, heads]).abs().max()) <= LOGIT
+            if with_weights:
+                err = (weight[b, h, :n].double() - (before[b, h, :n].double() + want_weight[b, h, :n])).abs()
+                # the sum of g weights, then its rounding with what was there
+                assert bool((err <= PAIR * want_weight[b, h, :n] + 2.0 ** -24 * (before[b, h, :n].double() + want_weight[b, h, :n])).all())
+                assert H.same_bits(weight[b, h, n:], before[b, h, n:])
+    return out, lse, weight
+
+
+SHAPES = [(8, 2, 128), (7, 1, 128), (4, 4, 64), (16, 2, 64), (6, 2, 128), (20, 1, 128)]
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("hq,hkv,d", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_short_lengths(lib, dtype, hq, hkv, d, weights):
+    """Zero, one, the edges of blocks and steps, in one batch, pages of 16 and of 48 slots."""
+    lens = [0, 1, 2, 15, 16, 17, 31, 32, 33, 48, 63, 65, 127, 128, 129, 160, 200]
+    gen = torch.Generator().manual_seed(hq * 100 + d)
+    for page, first in ((16, False), (48, True)):
+        cache = H.Cache(gen, dtype, hq, hkv, d, page, lens, lens, tokens_first=first)
+        check(cache, (torch.randn((len(lens), hq, d), generator=gen)).to(H.KIND[dtype]), cache.len[0].tolist(), weights)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,page,room", [
+    (BF16, 32, 8, 128, 16, [3001]), (F16, 28, 4, 128, 64, [4000, 17, 900, 1]), (BF16, 14, 2, 64, 4096, [9000, 5]), (F32, 8, 2, 128, 32, [2500, 300]),
+    (F32, 16, 4, 64, 48, [5000]), (F32, 3, 3, 64, 16, [1500, 1500]), (F16, 12, 1, 128, 256, [20011]), (BF16, 2, 2, 128, 16, [40000]), (F32, 12, 2, 128, 112, [7001]),
+])
+def test_key_ranges(lib, dtype, hq, hkv, d, page, room):
+    """Heads cut into several ranges; lengths that differ between heads, below what there is room for, none."""
+    gen = torch.Generator().manual_seed(sum(room))
+    cache = H.Cache(gen, dtype, hq, hkv, d, page, room, room)
+    q = torch.randn((len(room), hq, d), generator=gen).to(H.KIND[dtype])
+    full = [[n] * hkv for n in room]
+    for lens in (full, [[max(0, n - 77 * h - 5) for h in range(hkv)] for n in room], [[n // 9 for h in range(hkv)] for n in room], [[0] * hkv for n in room]):
+        check(cache, q, lens)
+        check(cache, q, lens, False)
+    # no lengths: all there is room for; lengths out of range are clamped
+    a, b, c = (run(cache, q, x, cache.weight[0]) for x in (None, full, [[n + 1000 for _ in x] for n, x in zip(room, full)]))
+    for x, y, z in zip(a, b, c):
+        assert H.same_bits(x, y) and H.same_bits(x, z)
+    d0 = run(cache, q, [[-5] * hkv for _ in room], None)
+    assert (d0[0] == 0).all() and (d0[1] == float("-inf")).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_many_sequences(lib, dtype):
+    """More than a launch's tables hold, most of them short, some empty."""
+    gen = torch.Generator().manual_seed(9)
+    room = [int(x) for x in torch.randint(0, 150, (150,), generator=gen)]
+    room[3], room[131], room[149] = 1300, 2000, 0
+    cache = H.Cache(gen, dtype, 4, 2, 64, 16, room, room)
+    check(cache, torch.randn((150, 4, 64), generator=gen).to(H.KIND[dtype]), cache.len[0].tolist())
+
+
+@pytest.mark.parametrize("batch", [1, 15, 16, 17, 33, 127, 128, 129])
+def test_sequence_of_a_range(lib, batch):
+    gen = torch.Generator().manual_seed(batch)
+    room = [1 + (7 * i) % 60 for i in range(batch)]
+    room[batch // 2] = 700
+    cache = H.Cache(gen, BF16, 2, 1, 64, 16, room, room)
+    check(cache, torch.randn((batch, 2, 64), generator=gen).bfloat16(), cache.len[0].tolist())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_pages_that_are_not_there(lib, dtype):
+    """Their slots are left out, also when nothing else is left; no entry of a page without slots is used."""
+    gen = torch.Generator().manual_seed(4)
+    room = [100, 40, 600, 33]
+    cache = H.Cache(gen, dtype, 8, 2, 128, 16, room, room)
+    cache.table[0, 2] = -1
+    cache.table[0, 6] = cache.n_pages
+    cache.table[1, :3] = 2 ** 31 - 1
+    cache.table[2, 5:30] = -(2 ** 31)
+    check(cache, torch.randn((4, 8, 128), generator=gen).to(H.KIND[dtype]), cache.len[0].tolist())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("scale", [0.0, 3.0, 1e-30])
+def test_scales_and_far_logits(lib, dtype, scale):
+    """Logits of some hundred nats: one slot has all the weight; vanishing ones: all have the same."""
+    gen = torch.Generator().manual_seed(5)
+    cache = H.Cache(gen, dtype, 8, 2, 64, 32, [700, 300], [700, 300], scale=scale)
+    q = torch.randn((2, 8, 64), generator=gen).to(H.KIND[dtype])
+    if scale == 3.0:
+        # the error of a logit grows with the scale: compare where it stays below the bar, on few rows that are far apart
+        cache.k[0][torch.isfinite(cache.k[0])] = 0
+        s, page, row = cache.slots(0, 0, 700)
+        cache.k[0, page[137], :, row[137]] = q[0, 0] / 4
+        want, _, _, top = H.attention(cache, q, cache.len[0].tolist())
+        out, _, _ = run(cache, q, cache.len[0].tolist())
+        assert float((out.double() - want).abs().max()) <= 40 * PAIR * float(top.max())   # sum |q k| * scale up to 4 * 64 * 3 / 2
+        return
+    check(cache, q, cache.len[0].tolist())
+
+
+def test_equal_keys_and_exact_weights(lib):
+    """Equal keys: every slot gets g / n, summed over calls."""
+    gen = torch.Generator().manual_seed(6)
+    cache = H.Cache(gen, BF16, 4, 1, 128, 16, [512], [512])
+    cache.k[0][torch.isfinite(cache.k[0])] = 0.5
+    q, w = torch.randn((1, 4, 128), generator=gen).bfloat16(), torch.zeros_like(cache.weight[0])
+    for i in range(3):
+        _, _, w = run(cache, q, [[512]], w)
+        assert torch.allclose(w[0, 0, :512], torch.tensor((i + 1) * 4 / 512), rtol=1e-6, atol=0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_same_bits_again_and_without_lse(lib, dtype):
+    gen = torch.Generator().manual_seed(7)
+    cache = H.Cache(gen, dtype, 28, 4, 128, 64, [3000, 5, 1111], [3000, 5, 1111])
+    q = torch.randn((3, 28, 128), generator=gen).to(H.KIND[dtype])
+    a, b = run(cache, q, None, cache.weight[0]), run(cache, q, None, cache.weight[0], scratch=0)
+    for x, y in zip(a, b):
+        assert H.same_bits(x, y)
+    assert H.same_bits(run(cache, q, None, None, lse=False)[0], run(cache, q, None, None)[0])
