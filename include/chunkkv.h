@@ -293,7 +293,7 @@ int chunkkv_decode_attention_static(const chunkkv_problem *prob, int32_t compact
  * dimension [n_layers].  Conventions, errors and streams as above; all of the calls can be captured into a graph, the
  * host arrays are then those of the capture.  A workspace may be shared by calls that run one after the other.
  *
- * Limits: head_dim 64 or 128; up to 256 query heads per kv-head; page_tokens a multiple of 16 up to 4096; max_tokens_b up
+ * Limits: head_dim 64 or 128; up to 1023 kv-heads and 256 query heads per kv-head; page_tokens a multiple of 16 up to 4096; max_tokens_b up
  * to 2^24; rows of a page up to 4 MB apart.  max_tokens is what launches and workspaces are sized by: a bound of every
  * kv_len of the sequence, lengths included that a call is going to write; the closer, the better the launches.        */
 typedef struct {

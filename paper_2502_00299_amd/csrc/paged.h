@@ -113,6 +113,35 @@ __host__ __device__ inline int paged_range_rows(int n, int splits) {
   return r < kPagedMinRange ? kPagedMinRange : r;
 }
 
+// Slots of (sequence, kv-head), as the device knows them.
+__device__ __forceinline__ int paged_length(const PagedDecodeArgs &a, int bl, int h) {
+  const int most = CKV_ARG(PagedDecodeArgs, max_tokens, bl);
+  if (a.kv_len == nullptr) return most;
+  const int n = a.kv_len[(int64_t)(a.batch0 + bl) * a.n_kv_heads + h];
+  return n < 0 ? 0 : (n > most ? most : n);
+}
+// Number of key ranges that the launch has for a sequence.
+__device__ __forceinline__ int paged_splits(int bl) {
+  return CKV_ARG(PagedDecodeArgs, first, bl + 1) - CKV_ARG(PagedDecodeArgs, first, bl);
+}
+__device__ __forceinline__ float *head_scores(const PagedDecodeArgs &a, int bl, int hq) {
+  const int64_t rows = (CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31) & ~31;
+  return a.scores + (int64_t)CKV_ARG(PagedDecodeArgs, first_row, bl) * a.n_q_heads + (int64_t)hq * rows;
+}
+// Element e of the state (M, L, o) that this workgroup's key range leaves of query head hq of sequence b.
+template <int HD>
+__device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int hq, int e, float M, float L, float o) {
+  const int64_t slot = (int64_t)blockIdx.x * a.n_q_heads + hq;
+  if (e == 0) a.part_ml[slot] = make_float2(M, L);
+  if (a.direct) {
+    const int64_t head = (int64_t)b * a.n_q_heads + hq;
+    a.out[head * HD + e] = L > 0.f ? o / L : 0.f;
+    if (a.lse != nullptr && e == 0) a.lse[head] = L > 0.f ? (M + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+  } else {
+    a.part_o[slot * HD + e] = o;
+  }
+}
+
 struct PagedEvictArgs {
   PageGeom geom;
   void *k_pages[kMaxLayersPerLaunch], *v_pages[kMaxLayersPerLaunch];
@@ -129,6 +158,7 @@ int launch_paged_append(int dtype, int head_dim, const PagedAppendArgs &a, hipSt
 int launch_paged_len(const PagedLenArgs &a, hipStream_t s);
 int launch_paged_compact(int row_bytes, const PagedCompactArgs &a, int n_layers, int batch, hipStream_t s);
 int launch_paged_decode(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s);
+int launch_paged_mfma(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s);   // 16-bit rows
 int paged_decode_heads(int dtype, int group);   // query heads of a kv-head that a workgroup serves
 int launch_paged_evict(const PagedEvictArgs &a, int n_layers, int batch, int max_tokens, hipStream_t s);
 

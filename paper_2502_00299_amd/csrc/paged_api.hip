@@ -23,7 +23,7 @@ int check_pages(const chunkkv_pages *p) {
   if (!fine_scale(p->softmax_scale)) return CHUNKKV_ERR_SHAPE;
   if (p->dtype != CHUNKKV_F32 && p->dtype != CHUNKKV_BF16 && p->dtype != CHUNKKV_F16) return CHUNKKV_ERR_UNSUPPORTED;
   if (p->head_dim != 64 && p->head_dim != 128) return CHUNKKV_ERR_UNSUPPORTED;
-  if (p->n_q_heads / p->n_kv_heads > kPagedMaxGroup || p->n_kv_heads > 4095) return CHUNKKV_ERR_UNSUPPORTED;   // grids have 65535 rows
+  if (p->n_q_heads / p->n_kv_heads > kPagedMaxGroup || p->n_kv_heads > 1023) return CHUNKKV_ERR_UNSUPPORTED;   // grids have 65535 rows
   if (p->page_tokens < 16 || p->page_tokens > 4096 || p->page_tokens % 16 != 0) return CHUNKKV_ERR_UNSUPPORTED;
   const int esz = elem_bytes(p->dtype);
   if (p->stride_tok < p->head_dim || p->stride_head < 0 || p->stride_page < 0) return CHUNKKV_ERR_SHAPE;

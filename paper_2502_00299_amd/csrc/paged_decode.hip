@@ -46,22 +46,6 @@ __device__ __forceinline__ void widen(const u32x4 &r, float (&f)[EPL]) {
   }
 }
 
-// Slots of (sequence, kv-head), as the device knows them.
-__device__ __forceinline__ int paged_length(const PagedDecodeArgs &a, int bl, int h) {
-  const int most = CKV_ARG(PagedDecodeArgs, max_tokens, bl);
-  if (a.kv_len == nullptr) return most;
-  const int n = a.kv_len[(int64_t)(a.batch0 + bl) * a.n_kv_heads + h];
-  return n < 0 ? 0 : (n > most ? most : n);
-}
-// Number of key ranges that the launch has for a sequence.
-__device__ __forceinline__ int paged_splits(int bl) {
-  return CKV_ARG(PagedDecodeArgs, first, bl + 1) - CKV_ARG(PagedDecodeArgs, first, bl);
-}
-__device__ __forceinline__ float *head_scores(const PagedDecodeArgs &a, int bl, int hq) {
-  const int64_t rows = (CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31) & ~31;
-  return a.scores + (int64_t)CKV_ARG(PagedDecodeArgs, first_row, bl) * a.n_q_heads + (int64_t)hq * rows;
-}
-
 // DT: chunkkv_dtype, HD: head dim, G: query heads of a workgroup, W: 1 = the scores are kept for the weights
 template <int DT, int HD, int G, int W>
 __global__ __launch_bounds__(kThreads) void paged_decode_kernel(PagedDecodeArgs a) {
@@ -204,79 +188,102 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(PagedDecodeArgs 
 #pragma unroll
     for (int e = 0; e < EPL; ++e) acc[e] += s_o[w][j][sg][e] * f;
   }
-  const int64_t hq = (int64_t)h * a.group + j0 + j;
-  const int64_t slot = (int64_t)blockIdx.x * a.n_q_heads + hq;
-  if (sg == 0) a.part_ml[slot] = make_float2(M, L);
-  if (a.direct) {
-    const int64_t head = (int64_t)b * a.n_q_heads + hq;
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) a.out[head * HD + sg * EPL + e] = L > 0.f ? acc[e] / L : 0.f;
-    if (a.lse != nullptr && sg == 0) a.lse[head] = L > 0.f ? (M + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
-  } else {
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) a.part_o[slot * HD + sg * EPL + e] = acc[e];
-  }
+  for (int e = 0; e < EPL; ++e) store_range<HD>(a, b, h * a.group + j0 + j, sg * EPL + e, M, L, acc[e]);
 }
 
-// Join of a head's key ranges: out = sum_r o_r 2^(m_r - M) / sum_r l_r 2^(m_r - M), in range order.  256 threads: HD columns
-// by 256 / HD groups that take every so many-th range.
-template <int HD>
-__device__ __forceinline__ void join_head(const PagedDecodeArgs &a, int bl, int hq, int used, float (*s_acc)[HD + 2]) {
-  constexpr int NG = kThreads / HD;
-  const int col = threadIdx.x % HD, grp = threadIdx.x / HD;
-  const int64_t slot = (int64_t)CKV_ARG(PagedDecodeArgs, first, bl) * a.n_q_heads + hq;
-  float acc = 0.f, m = kNegBig, lsum = 0.f;
-  for (int r = grp; r < used; r += NG) {
-    const float2 p = a.part_ml[slot + (int64_t)r * a.n_q_heads];
-    const float x = a.part_o[(slot + (int64_t)r * a.n_q_heads) * HD + col];
-    const float mm = fmaxf(m, p.x), f0 = __builtin_amdgcn_exp2f(m - mm), f1 = __builtin_amdgcn_exp2f(p.x - mm);
-    acc = acc * f0 + x * f1;
-    lsum = lsum * f0 + p.y * f1;
-    m = mm;
-  }
-  __syncthreads();   // the rows of a head before
-  s_acc[grp][col] = acc;
-  if (col == 0) { s_acc[grp][HD] = lsum; s_acc[grp][HD + 1] = m; }
-  __syncthreads();
-  if (threadIdx.x < HD) {
-    float M = s_acc[0][HD + 1];
+// The launch behind the ranges.
+//
+// Its first `joins` workgroups join a query head each: out = sum_r o_r 2^(m_r - M) / sum_r l_r 2^(m_r - M).  A thread owns four
+// columns and every so many-th range, four of them in flight; the groups of ranges are folded through LDS in order.
+// With weights (W = 1) the others add token_weight[s] += sum_i 2^(x_i(s) - lse_i) to the slots of one key range of one kv-head,
+// heads in order: the scores of the first four heads are on their way while the log-sum-exps are formed from all ranges' pairs.
+template <int HD, int W>
+__global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs a, int joins) {
+  constexpr int TPR = HD / 4, NG = kThreads / TPR, UN = 4;
+  __shared__ float s_acc[NG][HD + 2];
+  __shared__ float s_lse[W != 0 ? kPagedMaxGroup : 1];
+  const int t = threadIdx.x;
+  if (W == 0 || (int)blockIdx.x < joins) {
+    const int bl = blockIdx.x / a.n_q_heads, hq = blockIdx.x % a.n_q_heads, col = t % TPR, grp = t / TPR;
+    const int n = paged_length(a, bl, hq / a.group), rps = paged_range_rows(n, paged_splits(bl)), used = n > 0 ? (n + rps - 1) / rps : 1;
+    const int64_t slot = (int64_t)CKV_ARG(PagedDecodeArgs, first, bl) * a.n_q_heads + hq;
+    const float2 *ml = a.part_ml + slot;
+    const float *po = a.part_o + slot * HD + col * 4;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, m = kNegBig, lsum = 0.f;
+    for (int r0 = grp; r0 < used; r0 += UN * NG) {
+      float2 p[UN];
+      float4 o4[UN];
 #pragma unroll
-    for (int g = 1; g < NG; ++g) M = fmaxf(M, s_acc[g][HD + 1]);
-    float v = 0.f, L = 0.f;
+      for (int u = 0; u < UN; ++u) {
+        const int64_t r = (int64_t)(r0 + u * NG < used ? r0 + u * NG : r0) * a.n_q_heads;
+        p[u] = ml[r];
+        o4[u] = *(const float4 *)(po + r * HD);
+      }
+      float mm = m;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const float f = __builtin_amdgcn_exp2f(s_acc[g][HD + 1] - M);
-      v += s_acc[g][threadIdx.x] * f;
-      L += s_acc[g][HD] * f;
+      for (int u = 0; u < UN; ++u) mm = fmaxf(mm, p[u].x);
+      const float f0 = __builtin_amdgcn_exp2f(m - mm);
+      lsum *= f0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= f0;
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        const float f = r0 + u * NG < used ? __builtin_amdgcn_exp2f(p[u].x - mm) : 0.f;
+        lsum += p[u].y * f;
+        acc[0] += o4[u].x * f; acc[1] += o4[u].y * f; acc[2] += o4[u].z * f; acc[3] += o4[u].w * f;
+      }
+      m = mm;
     }
-    const int64_t head = (int64_t)(a.batch0 + bl) * a.n_q_heads + hq;
-    a.out[head * HD + threadIdx.x] = L > 0.f ? v / L : 0.f;
-    if (a.lse != nullptr && threadIdx.x == 0) a.lse[head] = L > 0.f ? (M + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s_acc[grp][col * 4 + e] = acc[e];
+    if (col == 0) { s_acc[grp][HD] = lsum; s_acc[grp][HD + 1] = m; }
+    __syncthreads();
+    if (t < HD) {
+      float M = s_acc[0][HD + 1];
+#pragma unroll
+      for (int g = 1; g < NG; ++g) M = fmaxf(M, s_acc[g][HD + 1]);
+      float v = 0.f, L = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const float f = __builtin_amdgcn_exp2f(s_acc[g][HD + 1] - M);
+        v += s_acc[g][t] * f;
+        L += s_acc[g][HD] * f;
+      }
+      const int64_t head = (int64_t)(a.batch0 + bl) * a.n_q_heads + hq;
+      a.out[head * HD + t] = L > 0.f ? v / L : 0.f;
+      if (a.lse != nullptr && t == 0) a.lse[head] = L > 0.f ? (M + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+    }
+    return;
   }
-}
-
-// grid: x = query head, y = sequence
-template <int HD>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(PagedDecodeArgs a) {
-  __shared__ float s_acc[kThreads / HD][HD + 2];
-  const int bl = blockIdx.y, hq = blockIdx.x, n = paged_length(a, bl, hq / a.group);
-  const int rps = paged_range_rows(n, paged_splits(bl));
-  join_head<HD>(a, bl, hq, n > 0 ? (n + rps - 1) / rps : 1, s_acc);
-}
-
-// The same with the weights: token_weight[s] += sum_i 2^(x_i(s) - lse_i), heads in order.  A workgroup has one key range of a
-// kv-head: it forms the log-sum-exps of the g heads from all ranges' pairs, adds the weights of its own rows and joins the
-// heads split, split + splits, ...  grid: x = key range, y = kv-head
-template <int HD>
-__global__ __launch_bounds__(kThreads) void paged_weight_kernel(PagedDecodeArgs a) {
-  __shared__ float s_acc[kThreads / HD][HD + 2];
-  __shared__ float s_lse[kPagedMaxGroup];
-  const int h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int bl = CKV_PAGED_SEQUENCE(PagedDecodeArgs, (int)blockIdx.x, a.batch), b = a.batch0 + bl;
-  const int first = CKV_ARG(PagedDecodeArgs, first, bl), split = blockIdx.x - first, splits = paged_splits(bl);
-  const int n = paged_length(a, bl, h), rps = paged_range_rows(n, splits), used = n > 0 ? (n + rps - 1) / rps : 1;
-  const int r0 = split * rps, r1 = r0 + rps < n ? r0 + rps : n;
-  if (r0 < r1) {
+  if constexpr (W != 0) {
+    const int x = blockIdx.x - joins, h = x % a.n_kv_heads, range = x / a.n_kv_heads, lane = t & 63, wave = t >> 6;
+    const int bl = CKV_PAGED_SEQUENCE(PagedDecodeArgs, range, a.batch), b = a.batch0 + bl;
+    const int first = CKV_ARG(PagedDecodeArgs, first, bl), split = range - first, splits = paged_splits(bl);
+    const int n = paged_length(a, bl, h), rps = paged_range_rows(n, splits), used = n > 0 ? (n + rps - 1) / rps : 1;
+    const int r0 = split * rps, len = r0 + rps < n ? rps : n - r0;
+    if (len <= 0) return;
+    constexpr int NR = kPagedMaxRange / kThreads;   // rows of a thread
+    const uint32_t pitch = ((uint32_t)CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31u) & ~31u;
+    const float *scores = head_scores(a, bl, h * a.group) + r0;
+    float *weight = a.weight + ((int64_t)b * a.n_kv_heads + h) * a.slot_pitch + r0;
+    float sx[4][NR], sum[NR];
+    auto load = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          sx[j][i] = kNegBig;
+          if (j0 + j < a.group && t + i * kThreads < len) sx[j][i] = scores[(int64_t)(j0 + j) * pitch + t + i * kThreads];
+        }
+    };
+    load(0);
+    float old[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      sum[i] = 0.f;
+      old[i] = t + i * kThreads < len ? weight[t + i * kThreads] : 0.f;
+    }
     for (int j = wave; j < a.group; j += kThreads / 64) {
       float m = kNegBig, l = 0.f;
       for (int r = lane; r < used; r += 64) {
@@ -292,49 +299,56 @@ __global__ __launch_bounds__(kThreads) void paged_weight_kernel(PagedDecodeArgs 
       if (lane == 0) s_lse[j] = l > 0.f ? M + __builtin_log2f(l) : 3.0e38f;   // no slot is there: no weight
     }
     __syncthreads();
-    float *weight = a.weight + ((int64_t)b * a.n_kv_heads + h) * a.slot_pitch;
-    const int64_t rows = (CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31) & ~31;
-    const float *x = head_scores(a, bl, h * a.group);
-    for (int r = r0 + threadIdx.x; r < r1; r += kThreads) {
-      float sum = 0.f;
-      for (int j = 0; j < a.group; ++j) sum += __builtin_amdgcn_exp2f(x[j * rows + r] - s_lse[j]);
-      weight[r] += sum;
+    for (int j0 = 0;;) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float lse = j0 + j < a.group ? s_lse[j0 + j] : 3.0e38f;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) sum[i] += __builtin_amdgcn_exp2f(sx[j][i] - lse);
+      }
+      j0 += 4;
+      if (j0 >= a.group) break;
+      load(j0);
     }
+#pragma unroll
+    for (int i = 0; i < NR; ++i)
+      if (t + i * kThreads < len) weight[t + i * kThreads] = old[i] + sum[i];
   }
-  if (a.direct) return;
-  for (int j = split; j < a.group; j += splits) join_head<HD>(a, bl, h * a.group + j, used, s_acc);
 }
 
+// Query heads of one kv-head that a workgroup serves.  Matrix cores: 4 or 8; 5 to 7 are one padded batch of 8, not two passes over
+// K and V.  Vector ALU: 1, 2 or 4 (registers).
 int paged_decode_heads(int dtype, int group) {
-  (void)dtype;
+  if (dtype != CHUNKKV_F32) return group > 4 ? 8 : 4;
   return group > 2 ? 4 : group;
 }
 
-template <int DT, int HD>
-int launch_decode_hd(const PagedDecodeArgs &a, hipStream_t s) {
-  const int G = paged_decode_heads(DT, a.group), ranges = a.first[a.batch];
-  const dim3 grid(ranges, a.n_kv_heads, (a.group + G - 1) / G);
-  auto go = [&](auto g) {
-    constexpr int GG = decltype(g)::value;
-    if (a.weight != nullptr) hipLaunchKernelGGL((paged_decode_kernel<DT, HD, GG, 1>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((paged_decode_kernel<DT, HD, GG, 0>), grid, dim3(kThreads), 0, s, a);
-  };
-  if (G == 1) go(std::integral_constant<int, 1>{});
-  else if (G == 2) go(std::integral_constant<int, 2>{});
-  else go(std::integral_constant<int, 4>{});
-  if (hipGetLastError() != hipSuccess) return CHUNKKV_ERR_LAUNCH;
-  if (a.weight != nullptr) hipLaunchKernelGGL((paged_weight_kernel<HD>), dim3(ranges, a.n_kv_heads), dim3(kThreads), 0, s, a);
-  else if (!a.direct) hipLaunchKernelGGL((paged_join_kernel<HD>), dim3(a.n_q_heads, a.batch), dim3(kThreads), 0, s, a);
+template <int HD>
+int launch_decode_hd(int dtype, const PagedDecodeArgs &a, hipStream_t s) {
+  const int G = paged_decode_heads(dtype, a.group), ranges = a.first[a.batch];
+  if (dtype != CHUNKKV_F32) {
+    const int rc = launch_paged_mfma(dtype, HD, a, s);
+    if (rc) return rc;
+  } else {
+    const dim3 grid(ranges, a.n_kv_heads, (a.group + G - 1) / G);
+    auto go = [&](auto g) {
+      constexpr int GG = decltype(g)::value;
+      if (a.weight != nullptr) hipLaunchKernelGGL((paged_decode_kernel<CHUNKKV_F32, HD, GG, 1>), grid, dim3(kThreads), 0, s, a);
+      else hipLaunchKernelGGL((paged_decode_kernel<CHUNKKV_F32, HD, GG, 0>), grid, dim3(kThreads), 0, s, a);
+    };
+    if (G == 1) go(std::integral_constant<int, 1>{});
+    else if (G == 2) go(std::integral_constant<int, 2>{});
+    else go(std::integral_constant<int, 4>{});
+    if (hipGetLastError() != hipSuccess) return CHUNKKV_ERR_LAUNCH;
+  }
+  const int joins = a.direct ? 0 : a.batch * a.n_q_heads;
+  if (a.weight != nullptr) hipLaunchKernelGGL((paged_finish_kernel<HD, 1>), dim3(joins + ranges * a.n_kv_heads), dim3(kThreads), 0, s, a, joins);
+  else if (joins > 0) hipLaunchKernelGGL((paged_finish_kernel<HD, 0>), dim3(joins), dim3(kThreads), 0, s, a, joins);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 
 int launch_paged_decode(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s) {
-  if (head_dim == 128) {
-    if (dtype == CHUNKKV_F32) return launch_decode_hd<CHUNKKV_F32, 128>(a, s);
-    return dtype == CHUNKKV_BF16 ? launch_decode_hd<CHUNKKV_BF16, 128>(a, s) : launch_decode_hd<CHUNKKV_F16, 128>(a, s);
-  }
-  if (dtype == CHUNKKV_F32) return launch_decode_hd<CHUNKKV_F32, 64>(a, s);
-  return dtype == CHUNKKV_BF16 ? launch_decode_hd<CHUNKKV_BF16, 64>(a, s) : launch_decode_hd<CHUNKKV_F16, 64>(a, s);
+  return head_dim == 128 ? launch_decode_hd<128>(dtype, a, s) : launch_decode_hd<64>(dtype, a, s);
 }
 
 }  // namespace ckv
