@@ -9,7 +9,9 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from dataclasses import dataclass
+from operator import attrgetter
 from typing import Optional, Sequence
 
 import torch
@@ -192,8 +194,11 @@ class Pages(_KeepsStruct):
         if kept is None or kept[0] != now:
             cp = self.as_c()
             plain = tuple(tuple(map(int, x)) if isinstance(x, tuple) else float(x) if isinstance(x, float) else int(x) for x in now)
-            kept = self._kept = (plain, cp, C.byref(cp))
+            kept = self._kept = (plain, cp, C.byref(cp), self.pool_elements())
         return kept[2]
+
+    def _pool_elements(self) -> int:   # of the struct that _c() has just returned
+        return self._kept[3]
 
     def __getstate__(self):
         return self.__dict__.copy()
@@ -262,8 +267,8 @@ def load_library(path: Optional[str] = None):
     lib.chunkkv_quality_metrics.restype = C.c_int
     lib.chunkkv_quality_metrics.argtypes = [C.POINTER(_CProblem), i32p, vp, vp, vp, vp, vp, f32p, f32p, vp, C.c_size_t, vp]
     lib.chunkkv_paged_compact.restype = C.c_int
-    lib.chunkkv_paged_compact.argtypes = [C.POINTER(_CProblem), C.POINTER(_CPages), C.c_int32, C.c_int32, C.POINTER(vp), C.POINTER(vp), i32p, i32p,
-                                          i32p, C.POINTER(vp), i32p, C.POINTER(vp), C.POINTER(vp), i32p, i32p, f32p, vp]
+    lib.chunkkv_paged_compact.argtypes = [C.POINTER(_CProblem), C.POINTER(_CPages), C.c_int32, C.c_int32, vp, vp, i32p, i32p, i32p, vp, i32p, vp, vp,
+                                          i32p, i32p, f32p, vp]
     lib.chunkkv_paged_append.restype = C.c_int
     lib.chunkkv_paged_append.argtypes = [C.POINTER(_CPages), i32p, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32p, vp, vp, C.c_float, f32p, C.c_int32,
                                          C.c_int32, vp, i32p, vp, vp, i32p, i32p, i32p, f32p, vp]
@@ -274,8 +279,7 @@ def load_library(path: Optional[str] = None):
     lib.chunkkv_paged_evict_workspace_bytes.restype = C.c_size_t
     lib.chunkkv_paged_evict_workspace_bytes.argtypes = [C.POINTER(_CPages), C.c_int32, i32p]
     lib.chunkkv_paged_evict.restype = C.c_int
-    lib.chunkkv_paged_evict.argtypes = [C.POINTER(_CPages), C.c_int32, i32p, C.c_int32, i32p, C.POINTER(vp), C.POINTER(vp), i32p, i32p, f32p, vp,
-                                        C.c_size_t, vp]
+    lib.chunkkv_paged_evict.argtypes = [C.POINTER(_CPages), C.c_int32, i32p, C.c_int32, i32p, vp, vp, i32p, i32p, f32p, vp, C.c_size_t, vp]
     lib.chunkkv_decode_attention_static.restype = C.c_int
     lib.chunkkv_decode_attention_static.argtypes = [C.POINTER(_CProblem), C.c_int32, i32p, vp, vp, vp, f32p, f32p, vp]
     _lib = lib
@@ -446,87 +450,116 @@ def chunkkv_decode_attention_static(prob: Problem, compacted: bool, kv_len, q, k
 
 # ---- caches in pages ----
 # A wrong size here is a read or a write out of bounds on the device, so sizes, types and devices are compared with the
-# handle's before the call (0.1 us a tensor).
+# handle's before a call.  A decoding step is 5 to 10 us on the device, so the comparisons are written to cost 0.2 us a tensor
+# and 0.1 us a pool of a list.
 _KINDS = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}
+_I32, _F32 = torch.int32, torch.float32
+_get_device, _data_ptr, _nbytes = torch.Tensor.get_device, torch.Tensor.data_ptr, attrgetter("nbytes")
 
 
-def _need(where: str, device: int, name: str, t: Optional[torch.Tensor], kind, elements: int, strided: bool = False) -> None:
-    if t is None:
-        return
-    if t.dtype != kind:
+def _refuse(where: str, dev: int, name: str, t, kind, elements: int):
+    if t.dtype is not kind:
         raise ValueError(f"{where}: {name} is {t.dtype}, not {kind}")
-    if t.get_device() != device:
-        raise ValueError(f"{where}: {name} is on device {t.get_device()}, the call runs on {device}")
-    if not strided and (t.numel() < elements or not t.is_contiguous()):
-        raise ValueError(f"{where}: {name} has {t.numel()} elements{'' if t.is_contiguous() else ', not contiguous'}; {elements} are needed")
+    if t.get_device() != dev:
+        raise ValueError(f"{where}: {name} is on device {t.get_device()}, the call runs on {dev}")
+    raise ValueError(f"{where}: {name} has {t.numel()} elements{'' if t.is_contiguous() else ', not contiguous'}; {elements} are needed")
 
 
-def _need_pool(where: str, device: int, name: str, t: torch.Tensor, pages: Pages) -> None:
-    _need(where, device, name, t, _KINDS.get(pages.dtype), 0, True)
-    room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-    if room < pages.pool_elements():
-        raise ValueError(f"{where}: {name} has {room} elements, the pages reach to {pages.pool_elements()}")
+def _arrays(where: str, dev: int, *arrays):
+    """Checks (name, tensor or None, type, elements) each; -> their addresses."""
+    out = []
+    for name, t, kind, elements in arrays:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not kind or t.get_device() != dev or t.numel() < elements or not t.is_contiguous():
+            _refuse(where, dev, name, t, kind, elements)
+        out.append(t.data_ptr())
+    return out
 
 
-def _new_rows(where: str, device: int, name: str, t: torch.Tensor, kind, tokens: int, heads: int, dim: int) -> int:
+def _pool(where: str, dev: int, name: str, t: torch.Tensor, kind, elements: int) -> int:
+    if t.dtype is not kind or t.get_device() != dev or t.numel() < elements or not t.is_contiguous():
+        # a view of something larger: what counts is the memory behind its first element
+        room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if t.dtype is not kind or t.get_device() != dev or room < elements:
+            _refuse(where, dev, name, t, kind, elements)
+    return t.data_ptr()
+
+
+def _pools(where: str, dev: int, name: str, ts: Sequence, kind, elements: int):
+    """Addresses of the pools of several layers, as an array whose own address the library reads them from."""
+    if len(ts) <= 4 or ts[0].dtype is not kind or set(map(_get_device, ts)) != {dev} or min(map(_nbytes, ts)) < elements * ts[0].element_size():
+        return array("Q", [_pool(where, dev, name, t, kind, elements) for t in ts])
+    return array("Q", map(_data_ptr, ts))
+
+
+def _at(table) -> Optional[int]:
+    return None if table is None else table.buffer_info()[0]
+
+
+def _new_rows(where: str, dev: int, name: str, t: torch.Tensor, kind, tokens: int, heads: int, dim: int) -> int:
     """Token stride of [tokens][heads][dim] rows."""
-    _need(where, device, name, t, kind, 0, True)
-    if tuple(t.shape) != (tokens, heads, dim) or (tokens and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim))):
-        raise ValueError(f"{where}: {name} is {tuple(t.shape)} with strides {t.stride()}, not [{tokens}][{heads}][{dim}] with contiguous heads")
-    return t.stride(0) if tokens > 1 else max(t.stride(0), heads * dim)
+    if t.dtype is not kind or t.get_device() != dev:
+        _refuse(where, dev, name, t, kind, 0)
+    strides = t.stride()
+    if t.shape != (tokens, heads, dim) or (tokens and (strides[2] != 1 or (heads > 1 and strides[1] != dim))):
+        raise ValueError(f"{where}: {name} is {tuple(t.shape)} with strides {strides}, not [{tokens}][{heads}][{dim}] with contiguous heads")
+    return strides[0] if tokens > 1 else max(strides[0], heads * dim)
 
 
-def _pointers(ts):
-    return (C.c_void_p * len(ts))(*[t.data_ptr() for t in ts])
+_last_ints = ((), None)   # the host array of the last call's numbers, found again by the numbers
+
+
+def _ints(xs: Sequence[int]):
+    global _last_ints
+    key = tuple(xs)
+    last = _last_ints
+    if last[0] != key:
+        key = tuple(map(int, key))
+        last = _last_ints = (key, (C.c_int32 * len(key))(*key))
+    return last
 
 
 def chunkkv_paged_compact(prob: Problem, pages: Pages, reuse: int, k: Sequence, v: Sequence, sel_chunk, sel_len, sel_count, token_importance,
                           page_table, k_pages: Sequence, v_pages: Sequence, kv_len, token_pos, token_weight, stream=None) -> None:
     where, n, dev = "chunkkv_paged_compact", len(k), torch.cuda.current_device()
-    heads = pages.batch * pages.n_kv_heads
-    groups = -(-n // max(1, reuse))
+    heads, groups, cp = pages.batch * pages.n_kv_heads, -(-n // max(1, reuse)), pages._c()
     if not len(v) == len(k_pages) == len(v_pages) == n or (token_importance is not None and len(token_importance) != groups):
         raise ValueError(f"{where}: lists of {n}, {len(v)}, {len(k_pages)} and {len(v_pages)} layers")
-    for name, t, kind, each in (("sel_chunk", sel_chunk, torch.int32, groups * heads * prob.sel_cap), ("sel_len", sel_len, torch.int32, groups * heads * prob.sel_cap),
-                                ("sel_count", sel_count, torch.int32, groups * heads), ("page_table", page_table, torch.int32, pages.batch * pages.table_pitch),
-                                ("kv_len", kv_len, torch.int32, n * heads), ("token_pos", token_pos, torch.int32, n * heads * pages.slot_pitch),
-                                ("token_weight", token_weight, torch.float32, n * heads * pages.slot_pitch)):
-        _need(where, dev, name, t, kind, each)
-    for t in token_importance or ():
-        _need(where, dev, "token_importance", t, torch.float32, heads * prob.score_cap * prob.chunk)
-    for name, ts in (("k_pages", k_pages), ("v_pages", v_pages)):
-        for t in ts:
-            _need_pool(where, dev, name, t, pages)
-    for name, ts in (("k", k), ("v", v)):
-        for t in ts:
-            _need(where, dev, name, t, _KINDS.get(prob.dtype), 0, True)
-    _check(load_library().chunkkv_paged_compact(
-        prob._c(), pages._c(), n, reuse, _pointers(k), _pointers(v), _ptr(sel_chunk), _ptr(sel_len), _ptr(sel_count),
-        None if token_importance is None else _pointers(token_importance), _ptr(page_table), _pointers(k_pages), _pointers(v_pages), _ptr(kv_len),
-        _ptr(token_pos), _ptr(token_weight), _stream(stream)), where)
+    sel, slots, kind, room = groups * heads * prob.sel_cap, n * heads * pages.slot_pitch, _KINDS.get(pages.dtype), pages._pool_elements()
+    chunks, lens, count, table, length, pos, weight = _arrays(
+        where, dev, ("sel_chunk", sel_chunk, _I32, sel), ("sel_len", sel_len, _I32, sel), ("sel_count", sel_count, _I32, groups * heads),
+        ("page_table", page_table, _I32, pages.batch * pages.table_pitch), ("kv_len", kv_len, _I32, n * heads), ("token_pos", token_pos, _I32, slots),
+        ("token_weight", token_weight, _F32, slots))
+    given = None if token_importance is None else _pools(where, dev, "token_importance", token_importance, _F32, heads * prob.score_cap * prob.chunk)
+    ks, vs = _pools(where, dev, "k", k, kind, 0), _pools(where, dev, "v", v, kind, 0)
+    kp, vp = _pools(where, dev, "k_pages", k_pages, kind, room), _pools(where, dev, "v_pages", v_pages, kind, room)
+    _check(load_library().chunkkv_paged_compact(prob._c(), cp, n, reuse, _at(ks), _at(vs), chunks, lens, count, _at(given), table, _at(kp), _at(vp), length,
+                                                pos, weight, _stream(stream)), where)
 
 
 def chunkkv_paged_append(pages: Pages, n_new: Sequence[int], q, k, v, positions, q_norm, k_norm, eps: float, inv_freq, interleaved: bool, q_out,
                          page_table, k_pages, v_pages, kv_len, kv_len_out, token_pos, token_weight, stream=None) -> None:
     """q, k, v: [tokens][heads][head_dim], views of a fused projection among them; rotary_dim is twice inv_freq's length."""
     where, dev, kind = "chunkkv_paged_append", torch.cuda.current_device(), _KINDS.get(pages.dtype)
-    if len(n_new) != pages.batch:
-        raise ValueError(f"{where}: n_new has {len(n_new)} entries for {pages.batch} sequences")
-    new = (C.c_int32 * len(n_new))(*[int(x) for x in n_new])
-    tokens, heads, d = max(0, sum(new)), pages.batch * pages.n_kv_heads, pages.head_dim
+    batch, hkv, d, cp = pages.batch, pages.n_kv_heads, pages.head_dim, pages._c()
+    numbers, new = _ints(n_new)
+    if len(numbers) != batch:
+        raise ValueError(f"{where}: n_new has {len(numbers)} entries for {batch} sequences")
+    tokens, heads = max(0, sum(numbers)), batch * hkv
     q_tok = 0 if q is None else _new_rows(where, dev, "q", q, kind, tokens, pages.n_q_heads, d)
-    k_tok, v_tok = (_new_rows(where, dev, name, t, kind, tokens, pages.n_kv_heads, d) for name, t in (("k", k), ("v", v)))
-    for name, t, of, each in (("positions", positions, torch.int32, tokens), ("q_norm", q_norm, kind, d), ("k_norm", k_norm, kind, d),
-                              ("q_out", q_out, kind, tokens * pages.n_q_heads * d), ("page_table", page_table, torch.int32, pages.batch * pages.table_pitch),
-                              ("kv_len", kv_len, torch.int32, heads), ("kv_len_out", kv_len_out, torch.int32, heads), ("inv_freq", inv_freq, torch.float32, 0),
-                              ("token_pos", token_pos, torch.int32, heads * pages.slot_pitch), ("token_weight", token_weight, torch.float32, heads * pages.slot_pitch)):
-        _need(where, dev, name, t, of, each)
-    _need_pool(where, dev, "k_pages", k_pages, pages)
-    _need_pool(where, dev, "v_pages", v_pages, pages)
+    k_tok, v_tok = _new_rows(where, dev, "k", k, kind, tokens, hkv, d), _new_rows(where, dev, "v", v, kind, tokens, hkv, d)
+    at, qn, kn, out, table, length, after, freq, pos, weight = _arrays(
+        where, dev, ("positions", positions, _I32, tokens), ("q_norm", q_norm, kind, d), ("k_norm", k_norm, kind, d),
+        ("q_out", q_out, kind, tokens * pages.n_q_heads * d), ("page_table", page_table, _I32, batch * pages.table_pitch), ("kv_len", kv_len, _I32, heads),
+        ("kv_len_out", kv_len_out, _I32, heads), ("inv_freq", inv_freq, _F32, 0), ("token_pos", token_pos, _I32, heads * pages.slot_pitch),
+        ("token_weight", token_weight, _F32, heads * pages.slot_pitch))
+    room = pages._pool_elements()
     _check(load_library().chunkkv_paged_append(
-        pages._c(), new, _ptr(q), q_tok, _ptr(k), k_tok, _ptr(v), v_tok, _ptr(positions), _ptr(q_norm), _ptr(k_norm), eps, _ptr(inv_freq),
-        0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, _ptr(q_out), _ptr(page_table), _ptr(k_pages), _ptr(v_pages), _ptr(kv_len),
-        _ptr(kv_len_out), _ptr(token_pos), _ptr(token_weight), _stream(stream)), where)
+        cp, new, None if q is None else q.data_ptr(), q_tok, k.data_ptr(), k_tok, v.data_ptr(), v_tok, at, qn, kn, eps, freq,
+        0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, out, table, _pool(where, dev, "k_pages", k_pages, kind, room),
+        _pool(where, dev, "v_pages", v_pages, kind, room), length, after, pos, weight, _stream(stream)), where)
 
 
 def chunkkv_paged_decode_workspace_bytes(pages: Pages, with_weights: bool = False) -> int:
@@ -535,43 +568,39 @@ def chunkkv_paged_decode_workspace_bytes(pages: Pages, with_weights: bool = Fals
 
 def chunkkv_paged_decode_attention(pages: Pages, page_table, kv_len, q, k_pages, v_pages, out, lse, token_weight, workspace, stream=None) -> None:
     where, dev, kind = "chunkkv_paged_decode_attention", torch.cuda.current_device(), _KINDS.get(pages.dtype)
-    rows, heads = pages.batch * pages.n_q_heads, pages.batch * pages.n_kv_heads
-    for name, t, of, each in (("page_table", page_table, torch.int32, pages.batch * pages.table_pitch), ("kv_len", kv_len, torch.int32, heads),
-                              ("q", q, kind, rows * pages.head_dim), ("out", out, torch.float32, rows * pages.head_dim), ("lse", lse, torch.float32, rows),
-                              ("token_weight", token_weight, torch.float32, heads * pages.slot_pitch)):
-        _need(where, dev, name, t, of, each)
-    _need_pool(where, dev, "k_pages", k_pages, pages)
-    _need_pool(where, dev, "v_pages", v_pages, pages)
+    cp, batch = pages._c(), pages.batch
+    rows, heads, room = batch * pages.n_q_heads, batch * pages.n_kv_heads, pages._pool_elements()
+    table, length, qp, op, lp, weight = _arrays(
+        where, dev, ("page_table", page_table, _I32, batch * pages.table_pitch), ("kv_len", kv_len, _I32, heads), ("q", q, kind, rows * pages.head_dim),
+        ("out", out, _F32, rows * pages.head_dim), ("lse", lse, _F32, rows), ("token_weight", token_weight, _F32, heads * pages.slot_pitch))
     _check(load_library().chunkkv_paged_decode_attention(
-        pages._c(), _ptr(page_table), _ptr(kv_len), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(out), _ptr(lse), _ptr(token_weight), _ptr(workspace),
-        _bytes(workspace), _stream(stream)), where)
+        cp, table, length, qp, _pool(where, dev, "k_pages", k_pages, kind, room), _pool(where, dev, "v_pages", v_pages, kind, room), op, lp, weight,
+        _ptr(workspace), _bytes(workspace), _stream(stream)), where)
+
+
+def _budgets(where: str, pages: Pages, budget: Sequence[int]):
+    numbers, host = _ints(budget)
+    if len(numbers) != pages.batch:
+        raise ValueError(f"{where}: budget has {len(numbers)} entries for {pages.batch} sequences")
+    return host
 
 
 def chunkkv_paged_evict_workspace_bytes(pages: Pages, n_layers: int, budget: Sequence[int]) -> int:
     return int(load_library().chunkkv_paged_evict_workspace_bytes(pages._c(), n_layers, _budgets("chunkkv_paged_evict_workspace_bytes", pages, budget)))
 
 
-def _budgets(where: str, pages: Pages, budget: Sequence[int]):
-    if len(budget) != pages.batch:
-        raise ValueError(f"{where}: budget has {len(budget)} entries for {pages.batch} sequences")
-    return (C.c_int32 * len(budget))(*[int(x) for x in budget])
-
-
 def chunkkv_paged_evict(pages: Pages, budget: Sequence[int], recent: int, page_table, k_pages: Sequence, v_pages: Sequence, kv_len, token_pos,
                         token_weight, workspace, stream=None) -> None:
-    where, n, dev = "chunkkv_paged_evict", len(k_pages), torch.cuda.current_device()
+    where, n, dev, kind = "chunkkv_paged_evict", len(k_pages), torch.cuda.current_device(), _KINDS.get(pages.dtype)
     if len(v_pages) != n:
         raise ValueError(f"{where}: lists of {n} and {len(v_pages)} layers")
-    heads = n * pages.batch * pages.n_kv_heads
-    for name, t, of, each in (("page_table", page_table, torch.int32, pages.batch * pages.table_pitch), ("kv_len", kv_len, torch.int32, heads),
-                              ("token_pos", token_pos, torch.int32, heads * pages.slot_pitch), ("token_weight", token_weight, torch.float32, heads * pages.slot_pitch)):
-        _need(where, dev, name, t, of, each)
-    for name, ts in (("k_pages", k_pages), ("v_pages", v_pages)):
-        for t in ts:
-            _need_pool(where, dev, name, t, pages)
-    _check(load_library().chunkkv_paged_evict(
-        pages._c(), n, _budgets(where, pages, budget), recent, _ptr(page_table), _pointers(k_pages), _pointers(v_pages), _ptr(kv_len), _ptr(token_pos),
-        _ptr(token_weight), _ptr(workspace), _bytes(workspace), _stream(stream)), where)
+    cp, heads = pages._c(), n * pages.batch * pages.n_kv_heads
+    room, slots = pages._pool_elements(), heads * pages.slot_pitch
+    table, length, pos, weight = _arrays(where, dev, ("page_table", page_table, _I32, pages.batch * pages.table_pitch), ("kv_len", kv_len, _I32, heads),
+                                         ("token_pos", token_pos, _I32, slots), ("token_weight", token_weight, _F32, slots))
+    kp, vp = _pools(where, dev, "k_pages", k_pages, kind, room), _pools(where, dev, "v_pages", v_pages, kind, room)
+    _check(load_library().chunkkv_paged_evict(cp, n, _budgets(where, pages, budget), recent, table, _at(kp), _at(vp), length, pos, weight, _ptr(workspace),
+                                              _bytes(workspace), _stream(stream)), where)
 
 
 def chunkkv_timing_begin(max_records: int = 4096) -> None:

@@ -50,6 +50,21 @@ __device__ __forceinline__ int paged_sequence(int x, int nb) {
   return b;
 }
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_amdgcn_update_dpp(0.f, x, CTRL, 0xf, 0xf, false);
+}
+// Sum over the LPR lanes that share a row; every lane of the group ends with the same bits.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float x) {
+  x = dpp_add<0xB1>(x);                            // quad_perm [1,0,3,2]
+  x = dpp_add<0x4E>(x);                            // quad_perm [2,3,0,1]
+  if constexpr (LPR >= 8) x = dpp_add<0x141>(x);   // row_half_mirror: the other quad of 8 lanes
+  if constexpr (LPR >= 16) x = dpp_add<0x140>(x);  // row_mirror: the other half of 16 lanes
+  if constexpr (LPR >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
+
 struct PagedAppendArgs {
   PageGeom geom;
   const void *q, *k, *v;
@@ -147,8 +162,9 @@ struct PagedEvictArgs {
   void *k_pages[kMaxLayersPerLaunch], *v_pages[kMaxLayersPerLaunch];
   int32_t *kv_len, *token_pos;          // [layer][batch_total][Hkv]..., from the launch's first layer on
   float *token_weight;
-  int32_t *lists;                       // [layer][batch_total][Hkv][2 * pitch + 1]: slots that move, free slots, their number
+  int32_t *lists;                       // [layer][batch_total][Hkv][1 + 2 * pitch]: number of moves, slots that move, free slots
   int32_t pitch;
+  int32_t apart;                        // 1: the moves are a launch of their own
   int32_t batch0, batch_total, n_kv_heads, slot_pitch, recent;
   int32_t row_bytes;
   int32_t budget[kPagedBatch], max_tokens[kPagedBatch];
@@ -161,5 +177,7 @@ int launch_paged_decode(int dtype, int head_dim, const PagedDecodeArgs &a, hipSt
 int launch_paged_mfma(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s);   // 16-bit rows
 int paged_decode_heads(int dtype, int group);   // query heads of a kv-head that a workgroup serves
 int launch_paged_evict(const PagedEvictArgs &a, int n_layers, int batch, int max_tokens, hipStream_t s);
+bool paged_moves_apart(const PagedEvictArgs &a);   // are there moves enough for a launch of their own
+int launch_paged_move(const PagedEvictArgs &a, int n_layers, int batch, hipStream_t s);
 
 }  // namespace ckv

@@ -2,55 +2,24 @@
 //
 // out_i = sum_s softmax_s(scale * q_i . k_s) v_s over the slots of a kv-head; a head's slots are cut into key ranges, each a
 // workgroup that leaves (maximum, sum, weighted values) of its rows, joined afterwards in range order.
-// This file holds the vector-ALU range kernel and the join.
+// This file holds the range kernel for fp32 pages, on the vector ALU, and the launch behind the ranges; 16-bit pages go to
+// paged_decode_mfma.hip.
 //
-// A row is spread over LPR = d * element size / 16 lanes, 16 bytes each; the lanes of a row reduce their partial dot
-// products with DPP adds, each group of LPR lanes runs its own online softmax over the rows it meets, and groups,
-// wavefronts and ranges are merged by the (max, sum, weighted output) rule, always in the same order.  The addresses of a
-// range's 16-row blocks are looked up once, by one lane each, and kept in LDS.
+// A row is spread over LPR = d / 4 lanes, 16 bytes each; the lanes of a row reduce their partial dot products with DPP adds,
+// each group of LPR lanes runs its own online softmax over the rows it meets, and groups, wavefronts and ranges are merged by
+// the (max, sum, weighted output) rule, always in the same order.  The addresses of a range's 16-row blocks are looked up
+// once, by one lane each, and kept in LDS.  A wavefront has the rows of its next round on their way while it works on one.
 #include "paged.h"
 
 namespace ckv {
 
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr float kNegBig = -1.0e30f, kMasked = -3.0e38f;
 
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x) {
-  return x + __builtin_amdgcn_update_dpp(0.f, x, CTRL, 0xf, 0xf, false);
-}
-// Sum over the LPR lanes that share a row; every lane of the group ends with the same bits.
-template <int LPR>
-__device__ __forceinline__ float row_sum(float x) {
-  x = dpp_add<0xB1>(x);                            // quad_perm [1,0,3,2]
-  x = dpp_add<0x4E>(x);                            // quad_perm [2,3,0,1]
-  if constexpr (LPR >= 8) x = dpp_add<0x141>(x);   // row_half_mirror: the other quad of 8 lanes
-  if constexpr (LPR >= 16) x = dpp_add<0x140>(x);  // row_mirror: the other half of 16 lanes
-  if constexpr (LPR >= 32) x += __shfl_xor(x, 16);
-  return x;
-}
-template <int DT, int EPL>
-__device__ __forceinline__ void widen(const u32x4 &r, float (&f)[EPL]) {
-  if constexpr (DT == CHUNKKV_F32) {
-    f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
-  } else if constexpr (DT == CHUNKKV_BF16) {
-    const bf16x8 x = __builtin_bit_cast(bf16x8, r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)x[i];
-  } else {
-    const f16x8 x = __builtin_bit_cast(f16x8, r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)x[i];
-  }
-}
-
-// DT: chunkkv_dtype, HD: head dim, G: query heads of a workgroup, W: 1 = the scores are kept for the weights
-template <int DT, int HD, int G, int W>
-__global__ __launch_bounds__(kThreads) void paged_decode_kernel(PagedDecodeArgs a) {
-  constexpr int ESZ = DT == CHUNKKV_F32 ? 4 : 2, ROWB = HD * ESZ;
-  constexpr int LPR = ROWB / 16, RPW = 64 / LPR, EPL = 16 / ESZ, U = 4, NW = kThreads / 64;
+// HD: head dim, G: query heads of a workgroup, NW: its wavefronts, W: 1 = the scores are kept for the weights
+template <int HD, int G, int NW, int W>
+__global__ __launch_bounds__(NW * 64) void paged_f32_kernel(PagedDecodeArgs a) {
+  constexpr int LPR = HD / 4, RPW = 64 / LPR, U = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane / LPR, seg = lane % LPR;
   const int h = blockIdx.y, j0 = blockIdx.z * G;
   const int bl = CKV_PAGED_SEQUENCE(PagedDecodeArgs, (int)blockIdx.x, a.batch), b = a.batch0 + bl;
@@ -60,60 +29,62 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(PagedDecodeArgs 
   if (r0 >= n && split > 0) return;   // the join knows how many ranges hold rows
 
   __shared__ int64_t s_block[kPagedMaxRange / 16];
-  for (int i = threadIdx.x; r0 + 16 * i < r1; i += kThreads)
-    s_block[i] = block_offset(a.geom, a.geom.table + (int64_t)b * a.geom.pitch, h, (uint32_t)(r0 / 16 + i));
+  f32x4 q[G];
+#pragma unroll
+  for (int j = 0; j < G; ++j) {
+    q[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (j0 + j < a.group) q[j] = *(const f32x4 *)((const float *)a.q + ((int64_t)b * a.n_q_heads + (int64_t)h * a.group + j0 + j) * HD + seg * 4);
+  }
+  static_assert(kPagedMaxRange / 16 <= 64, "a block per lane of the first wavefront");
+  if ((int)threadIdx.x < kPagedMaxRange / 16 && r0 + 16 * (int)threadIdx.x < r1)
+    s_block[threadIdx.x] = block_offset(a.geom, a.geom.table + (int64_t)b * a.geom.pitch, h, (uint32_t)(r0 / 16 + threadIdx.x));
   __syncthreads();
 
   const char *kbase = (const char *)a.k + seg * 16, *vbase = (const char *)a.v + seg * 16;
-  float qf[G][EPL];
-#pragma unroll
-  for (int j = 0; j < G; ++j) {
-    u32x4 r = {0, 0, 0, 0};
-    if (j0 + j < a.group) r = *(const u32x4 *)((const char *)a.q + ((int64_t)b * a.n_q_heads + (int64_t)h * a.group + j0 + j) * ROWB + seg * 16);
-    widen<DT, EPL>(r, qf[j]);
-  }
-  float m[G], l[G], o[G][EPL];
+  float m[G], l[G];
+  f32x4 o[G];
 #pragma unroll
   for (int j = 0; j < G; ++j) {
     m[j] = kNegBig;
     l[j] = 0.f;
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) o[j][e] = 0.f;
+    o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const float c1 = a.scale_log2e;
-  for (int base = r0 + wave * (U * RPW); base < r1; base += NW * U * RPW) {
-    u32x4 kr[U], vr[U];
-    bool valid[U];
+  f32x4 kn[U], vn[U];
+  auto load = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int row = base + u * RPW + grp;
       const int64_t at = row < r1 ? s_block[(row - r0) >> 4] : -1;
-      valid[u] = at >= 0;
-      kr[u] = vr[u] = u32x4{0, 0, 0, 0};   // rows that are not there count as zeros, whatever is in memory
-      if (valid[u]) {
+      kn[u] = vn[u] = f32x4{0.f, 0.f, 0.f, 0.f};   // rows that are not there count as zeros, whatever is in memory
+      if (at >= 0) {
         const int64_t off = at + (int64_t)(row & 15) * a.geom.tok;
-        kr[u] = __builtin_nontemporal_load((const u32x4 *)(kbase + off));
-        vr[u] = __builtin_nontemporal_load((const u32x4 *)(vbase + off));
+        kn[u] = __builtin_nontemporal_load((const f32x4 *)(kbase + off));
+        vn[u] = __builtin_nontemporal_load((const f32x4 *)(vbase + off));
       }
     }
+  };
+  const int base0 = r0 + wave * (U * RPW);
+  if (base0 < r1) load(base0);
+  for (int base = base0; base < r1; base += NW * U * RPW) {
+    f32x4 kr[U], vr[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) { kr[u] = kn[u]; vr[u] = vn[u]; }
+    if (base + NW * U * RPW < r1) load(base + NW * U * RPW);
     float s[U][G];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float kf[EPL];
-      widen<DT, EPL>(kr[u], kf);
+      const int row = base + u * RPW + grp;
+      const bool there = row < r1 && s_block[(row - r0) >> 4] >= 0;
 #pragma unroll
       for (int j = 0; j < G; ++j) {
-        float d = kf[0] * qf[j][0];
+        float d = kr[u][0] * q[j][0];
 #pragma unroll
-        for (int e = 1; e < EPL; ++e) d = __builtin_fmaf(kf[e], qf[j][e], d);
+        for (int e = 1; e < 4; ++e) d = __builtin_fmaf(kr[u][e], q[j][e], d);
         d = row_sum<LPR>(d);
-        s[u][j] = valid[u] ? d * c1 : kMasked;
+        s[u][j] = there ? d * c1 : kMasked;
       }
-    }
-    if constexpr (W != 0) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int row = base + u * RPW + grp;
+      if constexpr (W != 0) {
 #pragma unroll
         for (int j = 0; j < G; ++j)
           if (seg == j && row < r1 && j0 + j < a.group) head_scores(a, bl, h * a.group + j0 + j)[row] = s[u][j];
@@ -128,24 +99,20 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(PagedDecodeArgs 
         const float m_new = fmaxf(m[j], smax);
         const float f = __builtin_amdgcn_exp2f(m[j] - m_new);
         l[j] *= f;
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) o[j][e] *= f;
+        o[j] *= f;
         m[j] = m_new;
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) s[u][j] = __builtin_amdgcn_exp2f(s[u][j] - m[j]);   // now the weight
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float vf[EPL];
-      widen<DT, EPL>(vr[u], vf);
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int j = 0; j < G; ++j) {
         l[j] += s[u][j];
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) o[j][e] = __builtin_fmaf(s[u][j], vf[e], o[j][e]);
+        for (int e = 0; e < 4; ++e) o[j][e] = __builtin_fmaf(s[u][j], vr[u][e], o[j][e]);
       }
-    }
   }
   // the row groups of the wavefront (lanes that hold the same 16 bytes of a row)
 #pragma unroll
@@ -157,39 +124,36 @@ __global__ __launch_bounds__(kThreads) void paged_decode_kernel(PagedDecodeArgs 
       const float fa = __builtin_amdgcn_exp2f(m[j] - M), fb = __builtin_amdgcn_exp2f(m_o - M);
       l[j] = l[j] * fa + l_o * fb;
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) o[j][e] = o[j][e] * fa + __shfl_xor(o[j][e], x) * fb;
+      for (int e = 0; e < 4; ++e) o[j][e] = o[j][e] * fa + __shfl_xor(o[j][e], x) * fb;
       m[j] = M;
     }
   }
-  // the wavefronts, through LDS: thread (j, seg) folds their states in order
-  __shared__ float s_m[NW][G][LPR], s_l[NW][G][LPR], s_o[NW][G][LPR][EPL];
+  // the wavefronts, through LDS: a thread per element folds their states in order
+  __shared__ float s_m[NW][G], s_l[NW][G];
+  __shared__ f32x4 s_o[NW][G][LPR];
   if (grp == 0) {
 #pragma unroll
     for (int j = 0; j < G; ++j) {
-      s_m[wave][j][seg] = m[j];
-      s_l[wave][j][seg] = l[j];
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) s_o[wave][j][seg][e] = o[j][e];
+      if (seg == 0) { s_m[wave][j] = m[j]; s_l[wave][j] = l[j]; }
+      s_o[wave][j][seg] = o[j];
     }
   }
   __syncthreads();
-  const int t = threadIdx.x, j = t / LPR, sg = t % LPR;
-  if (t >= G * LPR || j0 + j >= a.group) return;
-  float M = s_m[0][j][sg];
+  for (int t = threadIdx.x; t < G * HD; t += NW * 64) {
+    const int j = t / HD, e = t % HD;
+    if (j0 + j >= a.group) break;
+    float M = s_m[0][j];
 #pragma unroll
-  for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][j][sg]);
-  float L = 0.f, acc[EPL];
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][j]);
+    float L = 0.f, acc = 0.f;
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    const float f = __builtin_amdgcn_exp2f(s_m[w][j][sg] - M);
-    L += s_l[w][j][sg] * f;
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) acc[e] += s_o[w][j][sg][e] * f;
+    for (int w = 0; w < NW; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][j] - M);
+      L += s_l[w][j] * f;
+      acc += ((const float *)s_o[w][j])[e] * f;
+    }
+    store_range<HD>(a, b, h * a.group + j0 + j, e, M, L, acc);
   }
-#pragma unroll
-  for (int e = 0; e < EPL; ++e) store_range<HD>(a, b, h * a.group + j0 + j, sg * EPL + e, M, L, acc[e]);
 }
 
 // The launch behind the ranges.
@@ -323,24 +287,31 @@ int paged_decode_heads(int dtype, int group) {
   return group > 2 ? 4 : group;
 }
 
+// Up to two workgroups a CU, at d = 128, the rows of a range are spread over eight wavefronts, so that most have one or two rounds of
+// them to wait for: 300 slots of 8 kv-heads, 4 heads each 12.0 us a call, with four 13.8; at d = 64, where a round is 64 rows, 11187 slots
+// of four sequences 20.1, with four 16.6.
+template <int HD, int G>
+int launch_f32(const PagedDecodeArgs &a, hipStream_t s) {
+  const int ranges = a.first[a.batch];
+  const dim3 grid(ranges, a.n_kv_heads, (a.group + G - 1) / G);
+  const bool wide = HD == 128 && (int64_t)grid.x * grid.y * grid.z <= 512;
+  if (a.weight != nullptr) {
+    if (wide) hipLaunchKernelGGL((paged_f32_kernel<HD, G, 8, 1>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((paged_f32_kernel<HD, G, 4, 1>), grid, dim3(256), 0, s, a);
+  } else {
+    if (wide) hipLaunchKernelGGL((paged_f32_kernel<HD, G, 8, 0>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((paged_f32_kernel<HD, G, 4, 0>), grid, dim3(256), 0, s, a);
+  }
+  return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
+}
+
 template <int HD>
 int launch_decode_hd(int dtype, const PagedDecodeArgs &a, hipStream_t s) {
   const int G = paged_decode_heads(dtype, a.group), ranges = a.first[a.batch];
-  if (dtype != CHUNKKV_F32) {
-    const int rc = launch_paged_mfma(dtype, HD, a, s);
-    if (rc) return rc;
-  } else {
-    const dim3 grid(ranges, a.n_kv_heads, (a.group + G - 1) / G);
-    auto go = [&](auto g) {
-      constexpr int GG = decltype(g)::value;
-      if (a.weight != nullptr) hipLaunchKernelGGL((paged_decode_kernel<CHUNKKV_F32, HD, GG, 1>), grid, dim3(kThreads), 0, s, a);
-      else hipLaunchKernelGGL((paged_decode_kernel<CHUNKKV_F32, HD, GG, 0>), grid, dim3(kThreads), 0, s, a);
-    };
-    if (G == 1) go(std::integral_constant<int, 1>{});
-    else if (G == 2) go(std::integral_constant<int, 2>{});
-    else go(std::integral_constant<int, 4>{});
-    if (hipGetLastError() != hipSuccess) return CHUNKKV_ERR_LAUNCH;
-  }
+  int rc;
+  if (dtype != CHUNKKV_F32) rc = launch_paged_mfma(dtype, HD, a, s);
+  else rc = G == 1 ? launch_f32<HD, 1>(a, s) : (G == 2 ? launch_f32<HD, 2>(a, s) : launch_f32<HD, 4>(a, s));
+  if (rc) return rc;
   const int joins = a.direct ? 0 : a.batch * a.n_q_heads;
   if (a.weight != nullptr) hipLaunchKernelGGL((paged_finish_kernel<HD, 1>), dim3(joins + ranges * a.n_kv_heads), dim3(kThreads), 0, s, a, joins);
   else if (joins > 0) hipLaunchKernelGGL((paged_finish_kernel<HD, 0>), dim3(joins), dim3(kThreads), 0, s, a, joins);

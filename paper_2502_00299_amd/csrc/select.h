@@ -96,7 +96,7 @@ __device__ __forceinline__ Selected select_chunks(Scores scores, int P, int c, i
       }
     }
   };
-  // f(chunk index, rank) for every own chunk with pred(index, key), rank = how many such chunks lie before it
+  // f(chunk index, rank) for every own chunk with pred(index, key), rank = how many such chunks lie before it; -> how many there are
   auto ranked = [&](auto pred, auto f) __attribute__((always_inline)) {
     int base = 0;
     for (int i0 = 0; i0 < C; i0 += KR * T) {
@@ -139,6 +139,7 @@ __device__ __forceinline__ Selected select_chunks(Scores scores, int P, int c, i
       base += s_total;
       if (i0 + KR * T < C) __syncthreads();
     }
+    return base;
   };
 
   for (int i = tid; i < kTopkBins; i += T) s_hist[i] = 0;
