@@ -7,6 +7,7 @@ namespace ckv {
 constexpr int kPagedBatch = 128;        // sequences per launch: their tables travel as kernel arguments
 constexpr int kPagedMaxTokens = 1 << 24;
 constexpr int kPagedMaxGroup = 256;     // query heads per kv-head
+constexpr int64_t kPagedStreamBytes = 128 << 20;   // what a call writes is streamed from here on: half of the memory-side cache
 
 // A pool of pages, strides in bytes.  Slots are addressed by blocks of 16: a page is a whole number of them, so a block
 // never crosses pages, whatever the page size is.
@@ -103,6 +104,7 @@ struct PagedCompactArgs {
   int64_t imp_pitch;
   int32_t layer0, reuse, batch0, batch_total, n_kv_heads, window, chunk, elem_bytes, sel_cap, slot_pitch, whole_chunks;
   int32_t entries;                                // selection entries of a workgroup
+  int32_t stream;                                 // 1: streaming stores
 };
 
 struct PagedDecodeArgs {
@@ -165,6 +167,7 @@ struct PagedEvictArgs {
   int32_t *lists;                       // [layer][batch_total][Hkv][1 + 2 * pitch]: number of moves, slots that move, free slots
   int32_t pitch;
   int32_t apart;                        // 1: the moves are a launch of their own
+  int32_t stream;                       // 1: with streaming stores
   int32_t batch0, batch_total, n_kv_heads, slot_pitch, recent;
   int32_t row_bytes;
   int32_t budget[kPagedBatch], max_tokens[kPagedBatch];

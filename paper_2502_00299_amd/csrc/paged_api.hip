@@ -113,12 +113,14 @@ int check_evict(const chunkkv_pages *p, int32_t n_layers, const int32_t *budget)
     if (budget[b] < 0) return CHUNKKV_ERR_SHAPE;
   return CHUNKKV_OK;
 }
-int list_pitch(const chunkkv_pages *p, const int32_t *budget) {   // most slots that a head can move
+// Most slots that a head of sequence b can move, and that any head can.
+int most_moves(const chunkkv_pages *p, const int32_t *budget, int b) {
+  const int over = p->max_tokens[b] - budget[b], m = over < budget[b] ? over : budget[b];
+  return m > 0 ? m : 0;
+}
+int list_pitch(const chunkkv_pages *p, const int32_t *budget) {
   int most = 0;
-  for (int b = 0; b < p->batch; ++b) {
-    const int over = p->max_tokens[b] - budget[b], m = over < budget[b] ? over : budget[b];
-    most = m > most ? m : most;
-  }
+  for (int b = 0; b < p->batch; ++b) most = most_moves(p, budget, b) > most ? most_moves(p, budget, b) : most;
   return most;
 }
 
@@ -149,6 +151,9 @@ int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *page
     if (misaligned(k[l]) || misaligned(v[l]) || misaligned(k_pages[l]) || misaligned(v_pages[l])) return CHUNKKV_ERR_SHAPE;
   }
   hipStream_t s = (hipStream_t)stream;
+  int64_t kept = 0;
+  for (int b = 0; b < prob->batch; ++b) kept += prob->n_keep[b] + prob->window;
+  const int64_t written = 2 * kept * n_layers * prob->n_kv_heads * prob->head_dim * elem_bytes(prob->dtype);
   for (int l0 = 0; l0 < n_layers; l0 += kMaxLayersPerLaunch) {
     const int nl = n_layers - l0 < kMaxLayersPerLaunch ? n_layers - l0 : kMaxLayersPerLaunch;
     for (int b0 = 0; b0 < prob->batch; b0 += kMaxBatchPerLaunch) {
@@ -175,6 +180,7 @@ int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *page
       a.layer0 = l0; a.reuse = reuse; a.batch0 = b0; a.batch_total = prob->batch; a.n_kv_heads = prob->n_kv_heads;
       a.window = prob->window; a.chunk = prob->chunk; a.elem_bytes = elem_bytes(prob->dtype); a.slot_pitch = pages->slot_pitch;
       a.whole_chunks = (prob->flags & CHUNKKV_FLAG_WHOLE_CHUNKS) ? 1 : 0;
+      a.stream = written > kPagedStreamBytes;
       Timed t(kCompact, s);
       if ((rc = launch_paged_compact(prob->head_dim * elem_bytes(prob->dtype), a, nl, nb, s))) return rc;
     }
@@ -316,6 +322,9 @@ int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int3
   if (!workspace || workspace_bytes < chunkkv_paged_evict_workspace_bytes(pages, n_layers, budget) || misaligned(workspace)) return CHUNKKV_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   const int pitch = list_pitch(pages, budget);
+  int64_t movable = 0;   // slots, at most
+  for (int b = 0; b < pages->batch; ++b) movable += most_moves(pages, budget, b);
+  const int64_t written = 2 * movable * n_layers * pages->n_kv_heads * pages->head_dim * elem_bytes(pages->dtype);
   for (int l0 = 0; l0 < n_layers; l0 += kMaxLayersPerLaunch) {
     const int nl = n_layers - l0 < kMaxLayersPerLaunch ? n_layers - l0 : kMaxLayersPerLaunch;
     const int64_t heads0 = (int64_t)l0 * pages->batch * pages->n_kv_heads;
@@ -331,6 +340,7 @@ int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int3
       a.lists = (int32_t *)workspace + heads0 * (2 * (int64_t)pitch + 1);
       a.pitch = pitch; a.batch0 = b0; a.batch_total = pages->batch; a.n_kv_heads = pages->n_kv_heads; a.slot_pitch = pages->slot_pitch;
       a.recent = recent; a.row_bytes = pages->head_dim * elem_bytes(pages->dtype);
+      a.stream = written > kPagedStreamBytes;
       int most = 0;
       for (int i = 0; i < nb; ++i) {
         const int n = pages->max_tokens[b0 + i];

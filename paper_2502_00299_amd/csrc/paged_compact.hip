@@ -4,16 +4,18 @@
 // extra entries of up to `chunk` rows.  The lengths of the entries before them give its first slot.  Rows are taken 128 at
 // a time: one thread per row finds source token and slot, writes position and weight, and leaves both addresses in LDS;
 // then all threads copy K and V rows as 16-byte segments.
-// Bound by HBM over a stack (every row read and written once), by latency over a layer.
+// Bound by HBM over a stack (every row read and written once), by latency over a layer.  The full cache is read with streaming
+// loads: nobody needs it again.  Stores are streaming where what is written is more than half of the memory-side cache; below, the
+// next decoding step finds the pages there.  32 layers of 32768 tokens at 20 %: 316 us with both (5.5 TB/s), plain stores 340.
 // Grid: x = group of entries, y = (sequence, kv-head), z = layer.
 #include "paged.h"
 
 namespace ckv {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-constexpr int kPagedRows = 128;
+constexpr int kPagedRows = 128, kAhead = 5;
 
-template <int NSEG>   // 16-byte segments per row
+template <int NSEG, bool STREAM>   // 16-byte segments per row; streaming stores
 __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int bl = blockIdx.y / a.n_kv_heads, h = blockIdx.y % a.n_kv_heads, b = a.batch0 + bl, layer = blockIdx.z;
@@ -93,20 +95,23 @@ __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArg
     }
     __syncthreads();
     const int total = 2 * n * NSEG;
-    for (int u0 = threadIdx.x; u0 < total; u0 += 4 * kThreads) {
-      u32x4 x[4];
-      char *to[4];
+    for (int u0 = threadIdx.x; u0 < total; u0 += kAhead * kThreads) {
+      u32x4 x[kAhead];
+      char *to[kAhead];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kAhead; ++j) {
         const int u = u0 + j * kThreads < total ? u0 + j * kThreads : u0;   // lanes without a segment read one of theirs again
         const bool is_v = u >= n * NSEG;
         const int uu = is_v ? u - n * NSEG : u, row = uu / NSEG, seg = uu % NSEG;
-        x[j] = *(const u32x4 *)((is_v ? vin : kin) + s_from[row] + seg * 16);
+        x[j] = __builtin_nontemporal_load((const u32x4 *)((is_v ? vin : kin) + s_from[row] + seg * 16));
         to[j] = s_to[row] >= 0 && u0 + j * kThreads < total ? (is_v ? vout : kout) + s_to[row] + seg * 16 : nullptr;
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (to[j] != nullptr) *(u32x4 *)to[j] = x[j];
+      for (int j = 0; j < kAhead; ++j)
+        if (to[j] != nullptr) {
+          if constexpr (STREAM) __builtin_nontemporal_store(x[j], (u32x4 *)to[j]);
+          else *(u32x4 *)to[j] = x[j];
+        }
     }
     __syncthreads();
   }
@@ -122,9 +127,10 @@ int launch_paged_compact(int row_bytes, const PagedCompactArgs &args, int n_laye
     most = e > most ? e : most;
   }
   const dim3 grid((most + a.entries - 1) / a.entries, batch * a.n_kv_heads, n_layers);
-  if (row_bytes == 128) hipLaunchKernelGGL(paged_compact_kernel<8>, grid, dim3(kThreads), 0, s, a);
-  else if (row_bytes == 256) hipLaunchKernelGGL(paged_compact_kernel<16>, grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL(paged_compact_kernel<32>, grid, dim3(kThreads), 0, s, a);
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, a); };
+  if (row_bytes == 128) a.stream ? go(paged_compact_kernel<8, true>) : go(paged_compact_kernel<8, false>);
+  else if (row_bytes == 256) a.stream ? go(paged_compact_kernel<16, true>) : go(paged_compact_kernel<16, false>);
+  else a.stream ? go(paged_compact_kernel<32, true>) : go(paged_compact_kernel<32, false>);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 

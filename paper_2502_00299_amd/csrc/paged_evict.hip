@@ -141,10 +141,11 @@ __global__ __launch_bounds__(T) void paged_evict_kernel(PagedEvictArgs a) {
 }
 
 // The moves of a head, kMovesPerGroup a workgroup: one thread per move looks up both places and takes position and weight
-// along, then all copy rows as 16-byte segments, four of K or V in flight per thread.
+// along, then all copy rows as 16-byte segments, four of K or V in flight per thread.  Streaming loads and, where the moves may be
+// more than half of the memory-side cache, streaming stores, as in the compaction: half of 53385 slots in 8 layers 79 us, plain 86.
 // Grid: x = group of moves, y = (sequence, kv-head), z = layer.
 constexpr int kMovesPerGroup = 64;
-template <int NSEG>   // 16-byte segments per row
+template <int NSEG, bool STREAM>   // 16-byte segments per row; streaming stores
 __global__ __launch_bounds__(kThreads) void paged_move_kernel(PagedEvictArgs a) {
   const int bl = blockIdx.y / a.n_kv_heads, h = blockIdx.y % a.n_kv_heads, b = a.batch0 + bl, layer = blockIdx.z;
   const int64_t head = ((int64_t)layer * a.batch_total + b) * a.n_kv_heads + h;
@@ -175,13 +176,16 @@ __global__ __launch_bounds__(kThreads) void paged_move_kernel(PagedEvictArgs a) 
       to[j] = nullptr;
       if (u < total && s_from[row] >= 0) {
         char *pool = u >= half ? vp : kp;
-        x[j] = *(const u32x4 *)(pool + s_from[row] + seg * 16);
+        x[j] = __builtin_nontemporal_load((const u32x4 *)(pool + s_from[row] + seg * 16));   // nobody reads this slot again
         to[j] = pool + s_to[row] + seg * 16;
       }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (to[j] != nullptr) *(u32x4 *)to[j] = x[j];
+      if (to[j] != nullptr) {
+        if constexpr (STREAM) __builtin_nontemporal_store(x[j], (u32x4 *)to[j]);
+        else *(u32x4 *)to[j] = x[j];
+      }
   }
 }
 
@@ -202,9 +206,10 @@ int launch_paged_evict(const PagedEvictArgs &args, int n_layers, int batch, int 
 
 int launch_paged_move(const PagedEvictArgs &a, int n_layers, int batch, hipStream_t s) {
   const dim3 grid((a.pitch + kMovesPerGroup - 1) / kMovesPerGroup, batch * a.n_kv_heads, n_layers);
-  if (a.row_bytes == 128) hipLaunchKernelGGL(paged_move_kernel<8>, grid, dim3(kThreads), 0, s, a);
-  else if (a.row_bytes == 256) hipLaunchKernelGGL(paged_move_kernel<16>, grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL(paged_move_kernel<32>, grid, dim3(kThreads), 0, s, a);
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, a); };
+  if (a.row_bytes == 128) a.stream ? go(paged_move_kernel<8, true>) : go(paged_move_kernel<8, false>);
+  else if (a.row_bytes == 256) a.stream ? go(paged_move_kernel<16, true>) : go(paged_move_kernel<16, false>);
+  else a.stream ? go(paged_move_kernel<32, true>) : go(paged_move_kernel<32, false>);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 
