@@ -280,7 +280,7 @@ int chunkkv_decode_attention_static(const chunkkv_problem *prob, int32_t compact
  * [n_pages][page_tokens][Hkv][d] fit.  Rows are 16-byte aligned.  The tokens of a (sequence, kv-head) are in SLOTS
  * 0 .. kv_len-1: slot s is row s % page_tokens of page page_table[b][s / page_tokens].  Slots carry no order: attention
  * does not need one, and the position of a slot's token is in token_pos.  Device arrays:
- *   page_table    int32 [B][table_pitch], shared by all heads and layers; entries of pages without slots are not read.
+ *   page_table    int32 [B][table_pitch], shared by all heads and layers; entries of pages without slots are not used.
  *                 An entry outside [0, n_pages) is a page that is not there: nothing is stored in it, its slots are
  *                 left out of the attention and are not moved; no call reads or writes outside the pools for it
  *   kv_len        int32 [B][Hkv], clamped to [0, max_tokens_b]
@@ -344,7 +344,7 @@ int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *page
  *   kv_len       read: tokens before;  kv_len_out  written: tokens after; may be kv_len itself
  *   token_pos, token_weight   NULL, or written for the new slots (the position; 0)
  * A token past max_tokens_b is not stored and not counted; its query is computed all the same.
- * One launch per 128 sequences, two where kv_len_out is kv_len and a sequence has more than one new token.              */
+ * One launch per 64 sequences, two where kv_len_out is kv_len and a sequence has more than one new token.              */
 int chunkkv_paged_append(const chunkkv_pages *pages, const int32_t *n_new, const void *q, int64_t q_stride_tok,
                          const void *k, int64_t k_stride_tok, const void *v, int64_t v_stride_tok,
                          const int32_t *positions, const void *q_norm, const void *k_norm, float eps,

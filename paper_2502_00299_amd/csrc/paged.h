@@ -4,7 +4,8 @@
 
 namespace ckv {
 
-constexpr int kPagedBatch = 128;        // sequences per launch: their tables travel as kernel arguments
+// Sequences per launch: their tables travel as kernel arguments, which cost the host 0.25 us per KB and launch.
+constexpr int kPagedBatch = 64;
 constexpr int kPagedMaxTokens = 1 << 24;
 constexpr int kPagedMaxGroup = 256;     // query heads per kv-head
 constexpr int64_t kPagedStreamBytes = 128 << 20;   // what a call writes is streamed from here on: half of the memory-side cache
@@ -22,12 +23,13 @@ struct PageGeom {
 __device__ __forceinline__ uint32_t page_of_block(const PageGeom &g, uint32_t blk) {
   return g.blocks == 1 ? blk : __umulhi(blk, g.magic);
 }
-// Byte offset in a pool of the first row of block `blk` of kv-head h, or -1 where the page is not there.
-__device__ __forceinline__ int64_t block_offset(const PageGeom &g, const int32_t *row, int h, uint32_t blk) {
-  const uint32_t p = page_of_block(g, blk);
-  const int32_t page = row[p];
-  const int64_t at = (int64_t)page * g.page + (int64_t)h * g.head + (int64_t)((blk - p * g.blocks) * 16) * g.tok;
+// Byte offset in a pool of the first row of block `blk` of kv-head h, whose page's table entry is `page`; -1 where that is not there.
+__device__ __forceinline__ int64_t block_offset(const PageGeom &g, int32_t page, int h, uint32_t blk) {
+  const int64_t at = (int64_t)page * g.page + (int64_t)h * g.head + (int64_t)((blk - page_of_block(g, blk) * g.blocks) * 16) * g.tok;
   return page >= 0 && page < g.n_pages ? at : -1;
+}
+__device__ __forceinline__ int64_t block_offset(const PageGeom &g, const int32_t *row, int h, uint32_t blk) {
+  return block_offset(g, row[page_of_block(g, blk)], h, blk);
 }
 // The same for one slot.
 __device__ __forceinline__ int64_t slot_offset(const PageGeom &g, const int32_t *row, int h, int slot) {
@@ -36,7 +38,7 @@ __device__ __forceinline__ int64_t slot_offset(const PageGeom &g, const int32_t 
 }
 
 // Sequence of entry x of a grid that counts the entries (ranges, tokens) of all sequences of a launch; first[i]: number of
-// the first entry of sequence i, INT32_MAX past the last one.  Two levels, so that at most 22 scalars are compared.
+// the first entry of sequence i, INT32_MAX past the last one.  Two levels, so that at most 18 scalars are compared.
 #define CKV_PAGED_SEQUENCE(ARGS, x, nb) paged_sequence<offsetof(ARGS, first)>(x, nb)
 template <size_t FIRST>
 __device__ __forceinline__ int paged_sequence(int x, int nb) {
@@ -136,6 +138,32 @@ __device__ __forceinline__ int paged_length(const PagedDecodeArgs &a, int bl, in
   if (a.kv_len == nullptr) return most;
   const int n = a.kv_len[(int64_t)(a.batch0 + bl) * a.n_kv_heads + h];
   return n < 0 ? 0 : (n > most ? most : n);
+}
+// One key range of a head: rows r0 .. r0 + len - 1 (len <= 0: none), and this lane's table entry, that of the range's block `lane`.
+// The entry is read together with the length, for the range as it is where the head is as long as it can be; only a head whose
+// ranges turn out shorter reads it again.
+struct PagedRange {
+  int r0, len;
+  int32_t page;
+};
+__device__ __forceinline__ PagedRange paged_range(const PagedDecodeArgs &a, int bl, int h, int split, int splits, int lane) {
+  const int most = CKV_ARG(PagedDecodeArgs, max_tokens, bl), full = paged_range_rows(most, splits);
+  const int32_t *row = a.geom.table + (int64_t)(a.batch0 + bl) * a.geom.pitch;
+  auto entry = [&](int first_row, int rows) __attribute__((always_inline)) {
+    return 16 * lane < rows && first_row + 16 * lane < most ? row[page_of_block(a.geom, (uint32_t)(first_row / 16 + lane))] : -1;
+  };
+  PagedRange r;
+  r.page = entry(split * full, full);
+  int n = most;
+  if (a.kv_len != nullptr) {
+    n = a.kv_len[(int64_t)(a.batch0 + bl) * a.n_kv_heads + h];
+    n = n < 0 ? 0 : (n > most ? most : n);
+  }
+  const int rps = paged_range_rows(n, splits);
+  r.r0 = split * rps;
+  r.len = r.r0 + rps < n ? rps : n - r.r0;
+  if (rps != full) r.page = entry(r.r0, rps);
+  return r;
 }
 // Number of key ranges that the launch has for a sequence.
 __device__ __forceinline__ int paged_splits(int bl) {

@@ -58,8 +58,8 @@ int range_count(int tokens, int rows) { return tokens > rows ? ceil_div(tokens, 
 // results, and with one and a half workgroups per CU half of the CUs wait.  us of a call, so and otherwise (bf16, 8 kv-heads of 4
 // heads): 13171 slots, 256 workgroups of 416 rows 15.8, 824 of 128 22.0; 30000, 240 of 1024 25.4, 320 of 768 30.2, 472 of 512 25.8;
 // 60000, 472 of 1024 43.9, 944 of 512 46.6; fp32, 20000 slots of 8 heads, 216 of 768 30.3, 320 of 512 37.0.
-// Without weights to add up, heads of up to kPagedDirect slots are one range and nothing has to be joined: sixteen
-// sequences of 500 slots 10.9, in ranges of 128 13.9; 300 slots 8.3 and 10.8.
+// Without weights to add up, heads of up to kPagedDirect slots of 16-bit rows are one range and nothing has to be joined: sixteen
+// sequences of 500 slots 10.9, in ranges of 128 13.9; 300 slots 8.3 and 10.8; but fp32, 300 slots 13.7 and 11.7.
 constexpr int kPagedDirect = 512;
 int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
   const int g = p->n_q_heads / p->n_kv_heads, G = paged_decode_heads(p->dtype, g);
@@ -70,7 +70,7 @@ int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
     rows += p->max_tokens[b];
     most = p->max_tokens[b] > most ? p->max_tokens[b] : most;
   }
-  if (!weights && most <= kPagedDirect) return kPagedDirect;
+  if (!weights && most <= kPagedDirect && p->dtype != CHUNKKV_F32) return kPagedDirect;
   const int64_t round = 256, rounds = (rows * per_range + round * kPagedMaxRange - 1) / (round * kPagedMaxRange);
   int lo = kPagedMinRange / 32, hi = kPagedMaxRange / 32;
   while (lo < hi) {

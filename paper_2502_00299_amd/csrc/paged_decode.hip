@@ -24,10 +24,6 @@ __global__ __launch_bounds__(NW * 64) void paged_f32_kernel(PagedDecodeArgs a) {
   const int h = blockIdx.y, j0 = blockIdx.z * G;
   const int bl = CKV_PAGED_SEQUENCE(PagedDecodeArgs, (int)blockIdx.x, a.batch), b = a.batch0 + bl;
   const int split = blockIdx.x - CKV_ARG(PagedDecodeArgs, first, bl), splits = paged_splits(bl);
-  const int n = paged_length(a, bl, h), rps = paged_range_rows(n, splits);
-  const int r0 = split * rps, r1 = r0 + rps < n ? r0 + rps : n;
-  if (r0 >= n && split > 0) return;   // the join knows how many ranges hold rows
-
   __shared__ int64_t s_block[kPagedMaxRange / 16];
   f32x4 q[G];
 #pragma unroll
@@ -35,9 +31,11 @@ __global__ __launch_bounds__(NW * 64) void paged_f32_kernel(PagedDecodeArgs a) {
     q[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (j0 + j < a.group) q[j] = *(const f32x4 *)((const float *)a.q + ((int64_t)b * a.n_q_heads + (int64_t)h * a.group + j0 + j) * HD + seg * 4);
   }
-  static_assert(kPagedMaxRange / 16 <= 64, "a block per lane of the first wavefront");
-  if ((int)threadIdx.x < kPagedMaxRange / 16 && r0 + 16 * (int)threadIdx.x < r1)
-    s_block[threadIdx.x] = block_offset(a.geom, a.geom.table + (int64_t)b * a.geom.pitch, h, (uint32_t)(r0 / 16 + threadIdx.x));
+  static_assert(kPagedMaxRange / 16 == 64, "a block per lane");
+  const PagedRange range = paged_range(a, bl, h, split, splits, lane);
+  const int r0 = range.r0, r1 = r0 + range.len;
+  if (range.len <= 0 && split > 0) return;   // the join knows how many ranges hold rows
+  if (wave == 0 && 16 * lane < range.len) s_block[lane] = block_offset(a.geom, range.page, h, (uint32_t)(r0 / 16 + lane));
   __syncthreads();
 
   const char *kbase = (const char *)a.k + seg * 16, *vbase = (const char *)a.v + seg * 16;
@@ -50,6 +48,8 @@ __global__ __launch_bounds__(NW * 64) void paged_f32_kernel(PagedDecodeArgs a) {
     o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const float c1 = a.scale_log2e;
+  const bool keeps = W != 0 && seg < G && j0 + seg < a.group;
+  float *scores = keeps ? head_scores(a, bl, h * a.group + j0 + seg) : nullptr;
   f32x4 kn[U], vn[U];
   auto load = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
@@ -84,10 +84,11 @@ __global__ __launch_bounds__(NW * 64) void paged_f32_kernel(PagedDecodeArgs a) {
         d = row_sum<LPR>(d);
         s[u][j] = there ? d * c1 : kMasked;
       }
-      if constexpr (W != 0) {
+      if constexpr (W != 0) {   // lane j of a row keeps the score of head j
+        float mine = s[u][0];
 #pragma unroll
-        for (int j = 0; j < G; ++j)
-          if (seg == j && row < r1 && j0 + j < a.group) head_scores(a, bl, h * a.group + j0 + j)[row] = s[u][j];
+        for (int j = 1; j < G; ++j) mine = seg == j ? s[u][j] : mine;
+        if (keeps && row < r1) scores[row] = mine;
       }
     }
 #pragma unroll

@@ -94,10 +94,6 @@ __global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs
   const int g = a.group;
   const int bl = CKV_PAGED_SEQUENCE(PagedDecodeArgs, (int)blockIdx.x, a.batch), b = a.batch0 + bl;
   const int split = blockIdx.x - CKV_ARG(PagedDecodeArgs, first, bl), splits = paged_splits(bl);
-  const int nrow = paged_length(a, bl, h), rps = paged_range_rows(nrow, splits), r0 = split * rps;
-  const int len = r0 + rps < nrow ? rps : nrow - r0;   // rows of this range
-  if (len <= 0 && split > 0) return;                   // the join knows how many ranges hold rows
-
   // query operand: column n holds head n % G (heads the kv-head does not have read as zero); before the lookups, whose wait
   // is theirs too
   const int head = n % G, part = n / G;
@@ -110,11 +106,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs
   }
   // block `lane` of the range: its place in the pools, and the bytes from its first row to the end of its last one that
   // holds a token (0: no such row, or no page)
+  const PagedRange range = paged_range(a, bl, h, split, splits, lane);
+  const int r0 = range.r0, len = range.len;
+  if (len <= 0 && split > 0) return;                   // the join knows how many ranges hold rows
   int64_t block_at = 0;
   uint32_t block_span = 0;
   const uint32_t tok = (uint32_t)a.geom.tok;
   if (16 * lane < len) {
-    const int64_t at = block_offset(a.geom, a.geom.table + (int64_t)b * a.geom.pitch, h, (uint32_t)(r0 / 16 + lane));
+    const int64_t at = block_offset(a.geom, range.page, h, (uint32_t)(r0 / 16 + lane));
     const int rows = len - 16 * lane < 16 ? len - 16 * lane : 16;
     if (at >= 0) {
       block_at = at;
