@@ -334,7 +334,7 @@ int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *page
  *   `interleaved` (y_2i, y_2i+1), becomes (y_i cos a_i - y_j sin a_i, y_j cos a_i + y_i sin a_i); elements from r on stay.
  *   Product and reduction to a revolution are in double: 3 * 2^-25 of a revolution at a position of 2^31, 2^-34 at 2^20.
  * Values, and with neither norm nor rotation keys and queries too, are copied bit by bit.
- *   n_new        HOST int32 [batch], each >= 0
+ *   n_new        HOST int32 [batch], each >= 0 (all 0: only kv_len_out is written, arrays of tokens may be NULL)
  *   q, k, v      device rows [T][heads][d] with a token stride in elements, heads contiguous: rows of a fused projection
  *                fit.  q may be NULL (then q_out and q_norm too): keys and values only
  *   positions    device int32 [T]

@@ -494,6 +494,15 @@ def _pools(where: str, dev: int, name: str, ts: Sequence, kind, elements: int):
     return array("Q", map(_data_ptr, ts))
 
 
+def _scratch(where: str, dev: int, t: Optional[torch.Tensor]):
+    """Address and bytes of a workspace of any type."""
+    if t is None:
+        return None, 0
+    if t.get_device() != dev or not t.is_contiguous():
+        _refuse(where, dev, "workspace", t, t.dtype, 0)
+    return t.data_ptr(), t.nbytes
+
+
 def _at(table) -> Optional[int]:
     return None if table is None else table.buffer_info()[0]
 
@@ -533,7 +542,9 @@ def chunkkv_paged_compact(prob: Problem, pages: Pages, reuse: int, k: Sequence, 
         ("page_table", page_table, _I32, pages.batch * pages.table_pitch), ("kv_len", kv_len, _I32, n * heads), ("token_pos", token_pos, _I32, slots),
         ("token_weight", token_weight, _F32, slots))
     given = None if token_importance is None else _pools(where, dev, "token_importance", token_importance, _F32, heads * prob.score_cap * prob.chunk)
-    ks, vs = _pools(where, dev, "k", k, kind, 0), _pools(where, dev, "v", v, kind, 0)
+    reach = (max(base + (int(rows) - 1) * prob.kv_stride_tok for base, rows in zip(prob.kv_base, prob.seqlen))
+             + (prob.n_kv_heads - 1) * prob.kv_stride_head + prob.head_dim)
+    ks, vs = _pools(where, dev, "k", k, kind, reach), _pools(where, dev, "v", v, kind, reach)
     kp, vp = _pools(where, dev, "k_pages", k_pages, kind, room), _pools(where, dev, "v_pages", v_pages, kind, room)
     _check(load_library().chunkkv_paged_compact(prob._c(), cp, n, reuse, _at(ks), _at(vs), chunks, lens, count, _at(given), table, _at(kp), _at(vp), length,
                                                 pos, weight, _stream(stream)), where)
@@ -575,7 +586,7 @@ def chunkkv_paged_decode_attention(pages: Pages, page_table, kv_len, q, k_pages,
         ("out", out, _F32, rows * pages.head_dim), ("lse", lse, _F32, rows), ("token_weight", token_weight, _F32, heads * pages.slot_pitch))
     _check(load_library().chunkkv_paged_decode_attention(
         cp, table, length, qp, _pool(where, dev, "k_pages", k_pages, kind, room), _pool(where, dev, "v_pages", v_pages, kind, room), op, lp, weight,
-        _ptr(workspace), _bytes(workspace), _stream(stream)), where)
+        *_scratch(where, dev, workspace), _stream(stream)), where)
 
 
 def _budgets(where: str, pages: Pages, budget: Sequence[int]):
@@ -599,8 +610,8 @@ def chunkkv_paged_evict(pages: Pages, budget: Sequence[int], recent: int, page_t
     table, length, pos, weight = _arrays(where, dev, ("page_table", page_table, _I32, pages.batch * pages.table_pitch), ("kv_len", kv_len, _I32, heads),
                                          ("token_pos", token_pos, _I32, slots), ("token_weight", token_weight, _F32, slots))
     kp, vp = _pools(where, dev, "k_pages", k_pages, kind, room), _pools(where, dev, "v_pages", v_pages, kind, room)
-    _check(load_library().chunkkv_paged_evict(cp, n, _budgets(where, pages, budget), recent, table, _at(kp), _at(vp), length, pos, weight, _ptr(workspace),
-                                              _bytes(workspace), _stream(stream)), where)
+    _check(load_library().chunkkv_paged_evict(cp, n, _budgets(where, pages, budget), recent, table, _at(kp), _at(vp), length, pos, weight,
+                                              *_scratch(where, dev, workspace), _stream(stream)), where)
 
 
 def chunkkv_timing_begin(max_records: int = 4096) -> None:

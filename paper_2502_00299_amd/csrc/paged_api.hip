@@ -1,4 +1,5 @@
 // Host side of the calls over pages: argument checks, workspace plans and launches.
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -196,15 +197,7 @@ int chunkkv_paged_append(const chunkkv_pages *pages, const int32_t *n_new, const
                          int32_t *kv_len_out, int32_t *token_pos, float *token_weight, void *stream) {
   int rc = check_pages(pages);
   if (rc) return rc;
-  if (!n_new || !k || !v || !positions || !page_table || !k_pages || !v_pages || !kv_len || !kv_len_out) return CHUNKKV_ERR_NULL;
-  if ((q != nullptr) != (q_out != nullptr) || (q_norm && !q) || (rotary_dim > 0 && !inv_freq)) return CHUNKKV_ERR_NULL;
-  if (rotary_dim < 0 || rotary_dim > pages->head_dim || (inv_freq && rotary_dim == 0) || !fine_scale(eps)) return CHUNKKV_ERR_SHAPE;
-  if (rotary_dim % 16 != 0) return CHUNKKV_ERR_UNSUPPORTED;
-  const int esz = elem_bytes(pages->dtype), d = pages->head_dim;
-  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_norm) || misaligned(k_norm) || misaligned(q_out) || misaligned(k_pages) || misaligned(v_pages))
-    return CHUNKKV_ERR_SHAPE;
-  if ((q && q_stride_tok < (int64_t)pages->n_q_heads * d) || k_stride_tok < (int64_t)pages->n_kv_heads * d || v_stride_tok < (int64_t)pages->n_kv_heads * d) return CHUNKKV_ERR_SHAPE;
-  if ((q && (q_stride_tok * esz) % 16) || (k_stride_tok * esz) % 16 || (v_stride_tok * esz) % 16) return CHUNKKV_ERR_SHAPE;
+  if (!n_new || !page_table || !k_pages || !v_pages || !kv_len || !kv_len_out || (rotary_dim > 0 && !inv_freq)) return CHUNKKV_ERR_NULL;
   int64_t total = 0;
   bool none = false, many = false;
   for (int b = 0; b < pages->batch; ++b) {
@@ -213,6 +206,16 @@ int chunkkv_paged_append(const chunkkv_pages *pages, const int32_t *n_new, const
     none |= n_new[b] == 0;
     many |= n_new[b] > 1;
   }
+  if (total > 0) {   // arrays of no tokens may be anything
+    if (!k || !v || !positions || (q != nullptr) != (q_out != nullptr) || (q_norm && !q)) return CHUNKKV_ERR_NULL;
+  }
+  if (rotary_dim < 0 || rotary_dim > pages->head_dim || (inv_freq && rotary_dim == 0) || !fine_scale(eps)) return CHUNKKV_ERR_SHAPE;
+  if (rotary_dim % 16 != 0) return CHUNKKV_ERR_UNSUPPORTED;
+  const int esz = elem_bytes(pages->dtype), d = pages->head_dim;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(q_norm) || misaligned(k_norm) || misaligned(q_out) || misaligned(k_pages) || misaligned(v_pages))
+    return CHUNKKV_ERR_SHAPE;
+  if ((total > 0) && ((q && q_stride_tok < (int64_t)pages->n_q_heads * d) || k_stride_tok < (int64_t)pages->n_kv_heads * d || v_stride_tok < (int64_t)pages->n_kv_heads * d)) return CHUNKKV_ERR_SHAPE;
+  if ((q && (q_stride_tok * esz) % 16) || (k_stride_tok * esz) % 16 || (v_stride_tok * esz) % 16) return CHUNKKV_ERR_SHAPE;
   if (total > kPagedMaxTokens) return CHUNKKV_ERR_UNSUPPORTED;
   // Who writes the lengths: the append kernel where every sequence has a token in it and nobody reads a length that it
   // has written (one token each), or they go to another array; otherwise a kernel of their own.
@@ -282,7 +285,8 @@ int chunkkv_paged_decode_attention(const chunkkv_pages *pages, const int32_t *pa
     a.scores = (float *)((char *)workspace + pl.off_scores);
     a.batch0 = b0; a.batch = nb; a.n_q_heads = pages->n_q_heads; a.n_kv_heads = pages->n_kv_heads;
     a.group = pages->n_q_heads / pages->n_kv_heads; a.slot_pitch = pages->slot_pitch;
-    a.scale_log2e = scale * 1.4426950408889634f;
+    // a scale that vanishes in fp32 gives all slots the same weight; kept above zero, which minus infinity cannot be multiplied by
+    a.scale_log2e = scale * 1.4426950408889634f > FLT_MIN ? scale * 1.4426950408889634f : FLT_MIN;
     const int r = range_rows(pages, b0, nb, token_weight != nullptr);
     for (int i = 0; i < kPagedBatch + 16; ++i) a.first[i] = INT32_MAX;
     int ranges = 0, rows = 0;

@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[t][i] = (t == 0 ? span0 : span1) != 0 && key0 + 16 * t + 4 * q + i < len ? sc[t][i] : -3.0e38f;
+        for (int i = 0; i < 4; ++i) sc[t][i] = (t == 0 ? span0 : span1) != 0 && key0 + 16 * t + 4 * q + i < len ? sc[t][i] : -__builtin_inff();   // times any scale
     }
     if constexpr (W != 0) {
       __builtin_amdgcn_sched_barrier(0);

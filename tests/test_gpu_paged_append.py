@@ -191,3 +191,16 @@ def test_refused_by_the_binding(lib):
                 dict(vp=vp.half()), dict(length=n[:, :1].contiguous()), dict(token_pos=cache.pos[0, :, :1].contiguous().to(DEV)), dict(token_pos=cache.pos[0])):
         with pytest.raises((ValueError, ckv.ChunkKVError)):
             call(cache, **{**good, **bad})
+
+
+def test_no_new_tokens(lib):
+    """A step in which no sequence has a token: lengths are carried over, nothing else is touched."""
+    gen = torch.Generator().manual_seed(3)
+    cache = H.Cache(gen, F16, 4, 2, 64, 16, [40, 9], [10, 9])
+    none = torch.zeros((0, 8, 64), dtype=torch.float16)
+    kp, vp, n, after = cache.pool(cache.k)[0], cache.pool(cache.v)[0], cache.len[0].to(DEV), torch.full((2, 2), -3, dtype=torch.int32, device=DEV)
+    tp = cache.pos[0].to(DEV)
+    call(cache, [0, 0], none, torch.zeros(0, dtype=torch.int32), None, None, None, False, kp, vp, n, after, tp, None)
+    assert torch.equal(after, n) and H.same_bits(cache.back([kp])[0], cache.k[0]) and H.same_bits(tp.cpu(), cache.pos[0])
+    call(cache, [0, 0], none, torch.zeros(0, dtype=torch.int32), None, None, None, False, kp, vp, n, n, None, None)
+    assert torch.equal(after, n)

@@ -117,6 +117,16 @@ def test_pages_that_are_not_there(lib, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("scale", [1e-45, 1e-30])
+def test_missing_pages_at_vanishing_scales(lib, dtype, scale):
+    """Whole steps without a slot that is there, where a scaled mask could vanish too."""
+    gen = torch.Generator().manual_seed(14)
+    cache = H.Cache(gen, dtype, 4, 1, 64, 16, [900], [900], scale=scale)
+    cache.table[0, 2:40] = -1
+    check(cache, torch.randn((1, 4, 64), generator=gen).to(H.KIND[dtype]), [[900]])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("scale", [0.0, 3.0, 1e-30])
 def test_scales_and_far_logits(lib, dtype, scale):
     """Logits of some hundred nats: one slot has all the weight; vanishing ones: all have the same."""
@@ -155,3 +165,19 @@ def test_same_bits_again_and_without_lse(lib, dtype):
     for x, y in zip(a, b):
         assert H.same_bits(x, y)
     assert H.same_bits(run(cache, q, None, None, lse=False)[0], run(cache, q, None, None)[0])
+
+
+def test_refused_by_the_binding(lib):
+    gen = torch.Generator().manual_seed(1)
+    cache = H.Cache(gen, BF16, 4, 2, 64, 16, [40], [40])
+    q, table, n = torch.randn((1, 4, 64), generator=gen).bfloat16().to(DEV), cache.table.to(DEV), cache.len[0].to(DEV)
+    kp, out = cache.pool(cache.k)[0], torch.zeros((1, 4, 64), device=DEV)
+    ws = torch.empty(ckv.chunkkv_paged_decode_workspace_bytes(cache.pages, True), dtype=torch.uint8, device=DEV)
+    good = dict(table=table, n=n, q=q, k=kp, v=kp, out=out, lse=None, w=cache.weight[0].to(DEV), ws=ws)
+    call = lambda x: ckv.chunkkv_paged_decode_attention(cache.pages, x["table"], x["n"], x["q"], x["k"], x["v"], x["out"], x["lse"], x["w"], x["ws"])  # noqa: E731
+    call(good)
+    for bad in (dict(table=table[:, :-1]), dict(table=table.long()), dict(n=n[:, :1].contiguous()), dict(q=q.half()), dict(q=q.transpose(1, 2)), dict(k=kp[1:].clone()),
+                dict(v=kp.cpu()), dict(out=out.double()), dict(out=out[0, :2]), dict(lse=torch.zeros(3, device=DEV)), dict(w=cache.weight[0]), dict(ws=ws.cpu()), dict(ws=None),
+                dict(ws=ws[:-256])):
+        with pytest.raises((ValueError, ckv.ChunkKVError)):
+            call({**good, **bad})

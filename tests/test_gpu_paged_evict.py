@@ -199,3 +199,27 @@ def test_malformed_selections_store_nothing(lib):
         got, kept = cache.back(kp), cache.k.clone()
         kept[0, used] = got[0, used]
         assert H.same_bits(got, kept) and (n == 80).all() and H.same_bits(pos.cpu()[..., 80:], cache.pos[..., 80:])
+
+
+def test_refused_by_the_binding(lib):
+    gen = torch.Generator().manual_seed(1)
+    cache = H.Cache(gen, BF16, 2, 1, 64, 16, [80], [80])
+    kp, vp, n, pos, w = cache.pool(cache.k), cache.pool(cache.v), cache.len.to(DEV), cache.pos.to(DEV), cache.weight.to(DEV)
+    ws = torch.empty(ckv.chunkkv_paged_evict_workspace_bytes(cache.pages, 1, [70]), dtype=torch.uint8, device=DEV)
+    good = dict(budget=[70], recent=3, table=cache.table.to(DEV), k=kp, v=vp, n=n, pos=pos, w=w, ws=ws)
+    call = lambda x: ckv.chunkkv_paged_evict(cache.pages, x["budget"], x["recent"], x["table"], x["k"], x["v"], x["n"], x["pos"], x["w"], x["ws"])  # noqa: E731
+    for bad in (dict(budget=[70, 1]), dict(recent=71), dict(recent=-1), dict(k=[kp[0][:-1].clone()]), dict(v=[]), dict(v=[vp[0].float()]), dict(n=n.cpu()), dict(pos=pos[..., :-1].contiguous()),
+                dict(w=w.double()), dict(ws=ws.cpu()), dict(ws=None), dict(ws=ws[:-1])):
+        with pytest.raises((ValueError, ckv.ChunkKVError)):
+            call({**good, **bad})
+    call(good)
+    prob = ckv.Problem(2, 1, 64, 16, 8, BF16, [200], [64], [0], 200 * 64, 64)
+    sel = [torch.zeros(prob.sel_cap, dtype=torch.int32, device=DEV) for _ in range(2)] + [torch.zeros(1, dtype=torch.int32, device=DEV)]
+    full = torch.zeros(200 * 64, dtype=torch.bfloat16, device=DEV)
+    fill = lambda x: ckv.chunkkv_paged_compact(prob, cache.pages, 1, x["k"], x["v"], *x["sel"], x["imp"], good["table"], x["kp"], vp, x["n"], pos, None)  # noqa: E731
+    good = {**good, "k": [full], "v": [full], "sel": sel, "imp": None, "kp": kp}
+    fill(good)
+    for bad in (dict(k=[full[:-1].clone()]), dict(v=[full.cpu()]), dict(v=[full, full]), dict(k=[full.half()]), dict(sel=[sel[0], sel[1][1:], sel[2]]), dict(kp=[kp[0][1:].clone()]),
+                dict(imp=[]), dict(imp=[torch.zeros(100, device=DEV)]), dict(n=n.long())):
+        with pytest.raises((ValueError, ckv.ChunkKVError)):
+            fill({**good, **bad})
