@@ -120,11 +120,13 @@ struct PagedDecodeArgs {
   int32_t batch0, batch, n_q_heads, n_kv_heads, group, slot_pitch;
   float scale_log2e;
   int32_t direct;                       // 1: every head is one range, the range kernel writes the outputs
+  int32_t alone;                        // 1: and adds up the weights: no launch follows (16-bit rows)
   int32_t first[kPagedBatch + 16];      // number of the first key range of every sequence
   int32_t first_row[kPagedBatch];       // rows of the sequences before, each rounded up to 32
   int32_t max_tokens[kPagedBatch];
 };
 constexpr int kPagedMinRange = 128, kPagedMaxRange = 1024;   // rows of a key range
+constexpr int kPagedAlone = 960;                             // of a head that one workgroup of eight wavefronts takes
 // Rows of every range of a head with n slots that `splits` ranges share.  From the length that the device knows, so that
 // all ranges have work when max_tokens is far above it.
 __host__ __device__ inline int paged_range_rows(int n, int splits) {

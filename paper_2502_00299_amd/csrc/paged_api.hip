@@ -62,6 +62,14 @@ int range_count(int tokens, int rows) { return tokens > rows ? ceil_div(tokens, 
 // Without weights to add up, heads of up to kPagedDirect slots of 16-bit rows are one range and nothing has to be joined: sixteen
 // sequences of 500 slots 10.9, in ranges of 128 13.9; 300 slots 8.3 and 10.8; but fp32, 300 slots 13.7 and 11.7.
 constexpr int kPagedDirect = 512;
+// With weights, heads of up to kPagedAloneFew slots (kPagedAlone where they fill half of the CUs, and no more than there are) are one
+// workgroup that needs no launch behind it, see paged_decode_mfma.hip.
+constexpr int kPagedAloneFew = 512, kPagedAloneHeads = 128, kCUs = 256;
+bool paged_alone(const chunkkv_pages *p, int nb, int most, bool weights) {
+  const int64_t heads = (int64_t)nb * p->n_kv_heads;
+  return weights && p->dtype != CHUNKKV_F32 && p->n_q_heads / p->n_kv_heads <= 8 && heads <= kCUs &&
+         most <= (heads >= kPagedAloneHeads ? kPagedAlone : kPagedAloneFew);
+}
 int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
   const int g = p->n_q_heads / p->n_kv_heads, G = paged_decode_heads(p->dtype, g);
   const int64_t per_range = (int64_t)p->n_kv_heads * ((g + G - 1) / G);   // workgroups
@@ -71,8 +79,9 @@ int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
     rows += p->max_tokens[b];
     most = p->max_tokens[b] > most ? p->max_tokens[b] : most;
   }
+  if (paged_alone(p, nb, most, weights)) return kPagedAlone;
   if (!weights && most <= kPagedDirect && p->dtype != CHUNKKV_F32) return kPagedDirect;
-  const int64_t round = 256, rounds = (rows * per_range + round * kPagedMaxRange - 1) / (round * kPagedMaxRange);
+  const int64_t round = kCUs, rounds = (rows * per_range + round * kPagedMaxRange - 1) / (round * kPagedMaxRange);
   int lo = kPagedMinRange / 32, hi = kPagedMaxRange / 32;
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
@@ -299,6 +308,9 @@ int chunkkv_paged_decode_attention(const chunkkv_pages *pages, const int32_t *pa
       if (c > 1) a.direct = 0;
     }
     a.first[nb] = ranges;
+    int most = 1;
+    for (int i = 0; i < nb; ++i) most = a.max_tokens[i] > most ? a.max_tokens[i] : most;
+    a.alone = paged_alone(pages, nb, most, token_weight != nullptr);
     Timed t(kDecode, s);
     if ((rc = launch_paged_decode(pages->dtype, pages->head_dim, a, s))) return rc;
   }

@@ -312,7 +312,7 @@ int launch_decode_hd(int dtype, const PagedDecodeArgs &a, hipStream_t s) {
   int rc;
   if (dtype != CHUNKKV_F32) rc = launch_paged_mfma(dtype, HD, a, s);
   else rc = G == 1 ? launch_f32<HD, 1>(a, s) : (G == 2 ? launch_f32<HD, 2>(a, s) : launch_f32<HD, 4>(a, s));
-  if (rc) return rc;
+  if (rc || a.alone) return rc;
   const int joins = a.direct ? 0 : a.batch * a.n_q_heads;
   if (a.weight != nullptr) hipLaunchKernelGGL((paged_finish_kernel<HD, 1>), dim3(joins + ranges * a.n_kv_heads), dim3(kThreads), 0, s, a, joins);
   else if (joins > 0) hipLaunchKernelGGL((paged_finish_kernel<HD, 0>), dim3(joins), dim3(kThreads), 0, s, a, joins);

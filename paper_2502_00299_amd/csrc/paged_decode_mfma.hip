@@ -8,9 +8,14 @@
 // i of its range (a range has at most 64), one load of 64 table entries; a step then takes two blocks' addresses out
 // of those registers by readlane, and each block has a buffer descriptor of its own, which covers exactly the rows that hold
 // tokens: slots past the last one, and blocks whose page is not there, read as zeros without touching memory.
-// Weights: W = 1 keeps the scaled logits (fp32, log2 units) for the kernel that adds up what every slot received.  They go
+// Weights: kStored keeps the scaled logits (fp32, log2 units) for the launch that adds up what every slot received.  They go
 // out by buffer stores whose idle columns lie out of range, so every step has two and the waits can count them together with
 // the loads (both leave the counter in the order they were issued).
+// kAdded keeps them in LDS: a head that is one range of eight wavefronts knows its log-sum-exps in the end and adds its own
+// weights, and nothing follows.
+// us in a graph, with and without a launch behind: 8 heads of 256 slots 7.7 / 9.5, of 512 9.2 / 9.6, of 800 11.9 / 9.8; 128 heads of 512
+// 12.0 / 13.5, of 960 16.9 / 18.3; 256 of 960 23.6 / 29.0; d = 64, 8 of 512 7.2 / 8.6, 256 of 960 15.0 / 19.1.  Eight wavefronts for ranges that
+// are joined are slower, with as many rows in flight: 13171 slots 16.2, four 15.2.
 // Grid: x = key range of any sequence, y = (batch of G query heads, kv-head).
 #include "decode_mfma.h"
 #include "paged.h"
@@ -70,10 +75,12 @@ __device__ __forceinline__ void join_parts(f32x4 (&acc)[NSET][NMT]) {
     }
 }
 
-// DT: bf16 or fp16, HD: head dim, G: 4 or 8 query heads per workgroup, NST: K/V slot pairs of a wavefront
-template <int DT, int HD, int G, int NST, int W>
-__global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs a) {
-  constexpr int NW = kThreads / 64;
+// What becomes of the scores: nothing, to the workspace for the launch behind, added up as weights here (one range per head).
+enum Scores { kDropped, kStored, kAdded };
+
+// DT: bf16 or fp16, HD: head dim, G: 4 or 8 query heads per workgroup, NST: K/V slot pairs of a wavefront, NW: wavefronts
+template <int DT, int HD, int G, int NST, int NW, int W>
+__global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(PagedDecodeArgs a) {
   constexpr int ROWB = HD * 2, SEGS = ROWB / 16;   // bytes and 16-byte segments of a row
   constexpr int RPL = 1024 / ROWB;                 // rows that one 1 KB load fills
   constexpr int NLB = 16 / RPL, NLD = 2 * NLB;     // loads of a block, of a slot
@@ -81,7 +88,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs
   constexpr int NKS = HD / 32, NMT = HD / 16;      // products of a 16-key score tile, 16-dim output tiles
   constexpr int NSET = G == 4 ? 1 : 2;             // products per output tile
   constexpr bool BF = DT == CHUNKKV_BF16;
-  extern __shared__ __align__(16) char smem[];
+  constexpr int RING = NW * NST * 2 * SLOT;
+  static_assert(RING >= NW * G * (HD + 2) * 4 + G * 4, "the states of the wavefronts take the ring's place");
+  __shared__ __align__(16) char smem[RING + (W == kAdded ? G * kPagedAlone * 4 : 0)];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -166,20 +175,25 @@ __global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs
   static_assert(SEGS == 16 || SEGS == 8, "rows 16 apart share the swizzle");
 
   // where this lane's scores go: slots 4 q .. of head n of the workgroup's; out of range for the columns past the heads
-  const uint32_t spitch = W != 0 ? ((uint32_t)CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31u) & ~31u : 0u;
+  const uint32_t spitch = W == kStored ? ((uint32_t)CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31u) & ~31u : 0u;
   const int sheads = g - j0 < G ? g - j0 : G;
-  const __amdgpu_buffer_rsrc_t srs = __builtin_amdgcn_make_buffer_rsrc(W != 0 ? (void *)head_scores(a, bl, h * g + j0) : nullptr, 0, (int)((uint32_t)sheads * spitch * 4u), 0x00020000);
+  const __amdgpu_buffer_rsrc_t srs = __builtin_amdgcn_make_buffer_rsrc(W == kStored ? (void *)head_scores(a, bl, h * g + j0) : nullptr, 0, (int)((uint32_t)sheads * spitch * 4u), 0x00020000);
   const bool scored = n < sheads;
   const uint32_t soff = ((uint32_t)n * spitch + (uint32_t)(r0 + 4 * q)) * 4u;
+  float *lscores = (float *)(smem + RING);   // [G][kPagedAlone]
   auto keep = [&](int key, const f32x4 &x) __attribute__((always_inline)) {
+    if constexpr (W == kAdded) {
+      if (scored) *(f32x4 *)(lscores + n * kPagedAlone + key + 4 * q) = x;
+      return;
+    }
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), srs, scored ? (int)(soff + (uint32_t)key * 4u) : -1, 0, 0);
   };
   // Accesses behind the slot that is waited for: loads of the other slots and, once every slot has been refilled, the two
   // stores of each of NST steps.
-  constexpr int kLoads = (2 * NST - 1) * NLD, kBehind = kLoads + (W != 0 ? 2 * NST : 0);
+  constexpr int kLoads = (2 * NST - 1) * NLD, kBehind = kLoads + (W == kStored ? 2 * NST : 0);
   static_assert(kBehind < 64, "vmcnt");
   auto wait = [&](int s) __attribute__((always_inline)) {
-    if (W != 0 && s < NST) __builtin_amdgcn_s_waitcnt(vm_imm(kLoads));
+    if (W == kStored && s < NST) __builtin_amdgcn_s_waitcnt(vm_imm(kLoads));
     else __builtin_amdgcn_s_waitcnt(vm_imm(kBehind));
   };
 
@@ -228,7 +242,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) sc[t][i] = (t == 0 ? span0 : span1) != 0 && key0 + 16 * t + 4 * q + i < len ? sc[t][i] : -__builtin_inff();   // times any scale
     }
-    if constexpr (W != 0) {
+    if constexpr (W != kDropped) {
       __builtin_amdgcn_sched_barrier(0);
       keep(key0, sc[0] * c1);
       keep(key0 + 16, sc[1] * c1);
@@ -285,14 +299,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs
   // ---- merge the wavefronts through LDS, in wavefront order; the loads of the empty steps still write zeros into the slots
   __builtin_amdgcn_s_waitcnt(vm_imm(0));
   __syncthreads();
-  float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G;   // [NW][G], [NW][G], [NW][G][HD]
+  float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G, *s_lse = s_o + NW * G * HD;   // [NW][G], [NW][G], [NW][G][HD], [G]
   if (n < G) {
     if (q == 0) { s_m[wave * G + n] = m; s_l[wave * G + n] = l; }
 #pragma unroll
     for (int mt = 0; mt < NMT; ++mt) *(f32x4 *)(s_o + (wave * G + n) * HD + 16 * mt + 4 * q) = acc[0][mt];
   }
   __syncthreads();
-  for (int t = tid; t < G * HD; t += kThreads) {
+  for (int t = tid; t < G * HD; t += NW * 64) {
     const int j = t / HD, e = t % HD;
     if (j0 + j >= g) break;
     float M = s_m[j];
@@ -306,20 +320,32 @@ __global__ __launch_bounds__(kThreads, 2) void paged_mfma_kernel(PagedDecodeArgs
       o += s_o[(w * G + j) * HD + e] * f;
     }
     store_range<HD>(a, b, h * g + j0 + j, e, M, L, o);
+    if (W == kAdded && e == 0) s_lse[j] = L > 0.f ? M + __builtin_log2f(L) : 3.0e38f;   // no slot is there: no weight
+  }
+  if constexpr (W == kAdded) {   // heads in order
+    __syncthreads();
+    float *weight = a.weight + ((int64_t)b * a.n_kv_heads + h) * a.slot_pitch;
+    for (int r = tid; r < len; r += NW * 64) {
+      float sum = 0.f;
+      for (int j = 0; j < g; ++j) sum += __builtin_amdgcn_exp2f(lscores[j * kPagedAlone + r] - s_lse[j]);
+      weight[r] += sum;
+    }
   }
 }
 
-template <int DT, int HD, int G, int W>
-int launch_cfg(const PagedDecodeArgs &a, hipStream_t s) {
-  constexpr int NST = HD == 128 ? 1 : 2, kLds = 4 * NST * 2 * kStepKeys * HD * 2;
-  static_assert(kLds >= 4 * G * (HD + 2) * 4 && kLds <= 64 * 1024, "two workgroups on a CU, and no more than a launch may ask for as it is");
-  hipLaunchKernelGGL((paged_mfma_kernel<DT, HD, G, NST, W>), dim3(a.first[a.batch], a.n_kv_heads * ((a.group + G - 1) / G)), dim3(kThreads), kLds, s, a);
+template <int DT, int HD, int G>
+int launch_g(const PagedDecodeArgs &a, hipStream_t s) {
+  constexpr int NST = HD == 128 ? 1 : 2;
+  const dim3 grid(a.first[a.batch], a.n_kv_heads * ((a.group + G - 1) / G));
+  auto go = [&](auto kern, int waves) { hipLaunchKernelGGL(kern, grid, dim3(waves * 64), 0, s, a); };
+  if (a.alone) go(paged_mfma_kernel<DT, HD, G, NST, 8, kAdded>, 8);
+  else if (a.weight != nullptr) go(paged_mfma_kernel<DT, HD, G, NST, 4, kStored>, 4);
+  else go(paged_mfma_kernel<DT, HD, G, NST, 4, kDropped>, 4);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 template <int DT, int HD>
 int launch_hd(const PagedDecodeArgs &a, hipStream_t s) {
-  if (paged_decode_heads(DT, a.group) == 4) return a.weight != nullptr ? launch_cfg<DT, HD, 4, 1>(a, s) : launch_cfg<DT, HD, 4, 0>(a, s);
-  return a.weight != nullptr ? launch_cfg<DT, HD, 8, 1>(a, s) : launch_cfg<DT, HD, 8, 0>(a, s);
+  return paged_decode_heads(DT, a.group) == 4 ? launch_g<DT, HD, 4>(a, s) : launch_g<DT, HD, 8>(a, s);
 }
 int launch_paged_mfma(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s) {
   if (dtype == CHUNKKV_BF16) return head_dim == 128 ? launch_hd<CHUNKKV_BF16, 128>(a, s) : launch_hd<CHUNKKV_BF16, 64>(a, s);

@@ -84,6 +84,21 @@ def test_key_ranges(lib, dtype, hq, hkv, d, page, room):
     assert (d0[0] == 0).all() and (d0[1] == float("-inf")).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 1, 64), (3, 1, 128), (40, 8, 64)])
+def test_around_one_workgroup_per_head(lib, dtype, hq, hkv, d):
+    """512 slots of few heads, 960 of 128 heads and more: the last that one workgroup takes, the first that it does not, and heads short of
+    that many; 256 heads and more."""
+    gen = torch.Generator().manual_seed(d + hq)
+    for batch, top in ((1, 512), (1, 513), (3, 500), (128 // hkv, 960), (128 // hkv, 961), (256 // hkv, 40), (264 // hkv, 40)):
+        if batch > 32 and d * hq > 700:
+            continue
+        room = [top if i % 5 == 0 else (i * 37) % top for i in range(batch)]
+        cache = H.Cache(gen, dtype, hq, hkv, d, 16, room, room)
+        cache.table[0, 3:5] = -1
+        check(cache, torch.randn((batch, hq, d), generator=gen).to(H.KIND[dtype]), cache.len[0].tolist())
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_many_sequences(lib, dtype):
     """More than a launch's tables hold, most of them short, some empty."""
