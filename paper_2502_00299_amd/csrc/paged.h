@@ -189,13 +189,15 @@ __device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int
   }
 }
 
+constexpr int kEvictLdsKeys = 32768;    // slots of a head whose keys are ranked in LDS
 struct PagedEvictArgs {
   PageGeom geom;
   void *k_pages[kMaxLayersPerLaunch], *v_pages[kMaxLayersPerLaunch];
   int32_t *kv_len, *token_pos;          // [layer][batch_total][Hkv]..., from the launch's first layer on
   float *token_weight;
-  int32_t *lists;                       // [layer][batch_total][Hkv][1 + 2 * pitch]: number of moves, slots that move, free slots
-  int32_t pitch;
+  int32_t *lists;                       // [layer][batch_total][Hkv][1 + 2 * pitch]: number of moves, free slots, as many that move into them
+  uint32_t *keys;                       // [layer][batch_total][Hkv][key_pitch]: keys of heads that are too long for LDS
+  int32_t pitch, key_pitch;
   int32_t apart;                        // 1: the moves are a launch of their own
   int32_t stream;                       // 1: with streaming stores
   int32_t batch0, batch_total, n_kv_heads, slot_pitch, recent;

@@ -134,6 +134,24 @@ int list_pitch(const chunkkv_pages *p, const int32_t *budget) {
   return most;
 }
 
+// Keys per head that the workspace has room for: of the sequences that are too long for LDS and can be over their budget.
+int key_pitch(const chunkkv_pages *p, const int32_t *budget) {
+  int most = 0;
+  for (int b = 0; b < p->batch; ++b)
+    if (p->max_tokens[b] > budget[b] && p->max_tokens[b] > most) most = p->max_tokens[b];
+  return most > kEvictLdsKeys ? most : 0;
+}
+struct EvictPlan {
+  size_t off_keys, total;
+};
+EvictPlan evict_plan(const chunkkv_pages *p, int32_t n_layers, const int32_t *budget) {
+  const size_t heads = (size_t)n_layers * p->batch * p->n_kv_heads;
+  EvictPlan pl;
+  pl.off_keys = align256(heads * (2 * (size_t)list_pitch(p, budget) + 1) * sizeof(int32_t));
+  pl.total = pl.off_keys + align256(heads * (size_t)key_pitch(p, budget) * sizeof(uint32_t));
+  return pl;
+}
+
 }  // namespace
 }  // namespace ckv
 
@@ -319,7 +337,7 @@ int chunkkv_paged_decode_attention(const chunkkv_pages *pages, const int32_t *pa
 
 size_t chunkkv_paged_evict_workspace_bytes(const chunkkv_pages *pages, int32_t n_layers, const int32_t *budget) {
   if (check_evict(pages, n_layers, budget)) return 0;
-  return align256((size_t)n_layers * pages->batch * pages->n_kv_heads * (2 * (size_t)list_pitch(pages, budget) + 1) * sizeof(int32_t));
+  return evict_plan(pages, n_layers, budget).total;
 }
 
 int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int32_t *budget, int32_t recent,
@@ -335,7 +353,8 @@ int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int3
     if (!k_pages[l] || !v_pages[l]) return CHUNKKV_ERR_NULL;
     if (misaligned(k_pages[l]) || misaligned(v_pages[l])) return CHUNKKV_ERR_SHAPE;
   }
-  if (!workspace || workspace_bytes < chunkkv_paged_evict_workspace_bytes(pages, n_layers, budget) || misaligned(workspace)) return CHUNKKV_ERR_WORKSPACE;
+  const EvictPlan pl = evict_plan(pages, n_layers, budget);
+  if (!workspace || workspace_bytes < pl.total || misaligned(workspace)) return CHUNKKV_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   const int pitch = list_pitch(pages, budget);
   int64_t movable = 0;   // slots, at most
@@ -354,6 +373,8 @@ int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int3
       a.token_pos = token_pos + heads0 * pages->slot_pitch;
       a.token_weight = token_weight + heads0 * pages->slot_pitch;
       a.lists = (int32_t *)workspace + heads0 * (2 * (int64_t)pitch + 1);
+      a.key_pitch = key_pitch(pages, budget);
+      a.keys = (uint32_t *)((char *)workspace + pl.off_keys) + heads0 * a.key_pitch;
       a.pitch = pitch; a.batch0 = b0; a.batch_total = pages->batch; a.n_kv_heads = pages->n_kv_heads; a.slot_pitch = pages->slot_pitch;
       a.recent = recent; a.row_bytes = pages->head_dim * elem_bytes(pages->dtype);
       a.stream = written > kPagedStreamBytes;

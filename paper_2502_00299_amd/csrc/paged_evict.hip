@@ -6,8 +6,11 @@
 // written and the moves have no order; only slots that move cost bytes of K and V.
 // Up to kFewMoves slots move in the selecting workgroup, more of them in a launch of their own, which has workgroups for 64
 // moves each and is bound by HBM.
-// The selection is bound by latency.  Weights and positions of all slots that there is room for are read together with the
-// length, before it is known how many count, and ranked out of LDS, up to 16384 of them (64 KB); more are read again in every step.
+// The selection is bound by latency for few slots (849 of 8 heads 8.5 us with its one move) and by the instructions of one workgroup's
+// passes over a head for many (see kInLds and the launcher).  Up to 16384 slots a thread has its own in registers, read together
+// with the length, before it is known how many count; up to 32768 their keys are in LDS, beyond in the workspace.
+// One pass of ranks gives both lists: slots on the wrong side of the budget, in ascending order, are the free ones, then the
+// ones that move, as many.
 #include "paged.h"
 #include "select.h"
 
@@ -16,17 +19,6 @@ namespace ckv {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kFewMoves = 64;
-
-// Slots as they are ranked: by weight, protected ones above all of them.
-struct EvictKeys {
-  const float *weight;
-  const int32_t *pos;
-  int64_t since;   // positions above it are protected
-  __device__ __forceinline__ uint32_t operator[](int i) const {
-    const uint32_t w = order_key(weight[i]);
-    return (int64_t)pos[i] > since ? 0xFFFFFFFFu : w;
-  }
-};
 
 // Moves [i0, i0 + n) of a head's lists, one after the other for the threads of a workgroup.
 __device__ __forceinline__ void move_slots(const PagedEvictArgs &a, int layer, int b, int h, int64_t head, const int32_t *source, const int32_t *target, int n) {
@@ -50,29 +42,50 @@ __device__ __forceinline__ void move_slots(const PagedEvictArgs &a, int layer, i
   }
 }
 
-// T threads, KR slots each; REG: all of them stay in registers and LDS
-template <int T, int KR, bool REG>
+// Where a workgroup's keys are while it selects: KR of every thread in registers and LDS, all in LDS, in the workspace.
+enum Keys { kInRegisters, kInLds, kInMemory };
+
+// Largest over the T threads of a workgroup; s_red has room for one value per wavefront.
+template <int T, typename V>
+__device__ __forceinline__ V block_max(V x, V *s_red) {
+  for (int o = 32; o > 0; o >>= 1) {
+    const V y = __shfl_xor(x, o);
+    x = y > x ? y : x;
+  }
+  if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = x;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < T / 64; ++i) x = s_red[i] > x ? s_red[i] : x;
+  return x;
+}
+
+// T threads, KR slots each in a round
+template <int T, int KR, int KEYS>
 __global__ __launch_bounds__(T) void paged_evict_kernel(PagedEvictArgs a) {
+  constexpr bool REG = KEYS == kInRegisters;
   const int bl = blockIdx.x / a.n_kv_heads, h = blockIdx.x % a.n_kv_heads, b = a.batch0 + bl, layer = blockIdx.y;
   const int64_t head = ((int64_t)layer * a.batch_total + b) * a.n_kv_heads + h;
   const int m = CKV_ARG(PagedEvictArgs, budget, bl), most = CKV_ARG(PagedEvictArgs, max_tokens, bl), tid = threadIdx.x;
   const int32_t *pos = a.token_pos + head * a.slot_pitch;
   const float *weight = a.token_weight + head * a.slot_pitch;
-  int32_t *moves = a.lists + head * (2 * (int64_t)a.pitch + 1), *source = moves + 1, *target = source + a.pitch;
+  int32_t *moves = a.lists + head * (2 * (int64_t)a.pitch + 1), *list = moves + 1;
 
-  __shared__ int s_newest[T / 64], s_list[2][kFewMoves];
+  __shared__ int s_newest[T / 64], s_list[2 * kFewMoves];
   __shared__ uint32_t s_top[T / 64];
-  __shared__ uint32_t s_key[REG ? T * KR : 1];
-  float w[REG ? KR : 1];
-  int32_t p[REG ? KR : 1];
-  if constexpr (REG) {   // room for `most` slots there is, however many hold a token
+  __shared__ uint32_t s_key[REG ? T * KR : (KEYS == kInLds ? kEvictLdsKeys : 1)];
+  uint32_t *key = KEYS == kInMemory ? a.keys + head * a.key_pitch : s_key;
+  float w[KR];
+  int32_t p[KR];
+  // the round of slots from i0 on; there is room for `most` of them, however many hold a token
+  auto read = [&](int i0, int end) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < KR; ++j) {
-      const bool in = j * T + tid < most;
-      w[j] = in ? weight[j * T + tid] : 0.f;
-      p[j] = in ? pos[j * T + tid] : 0;
+      const bool in = i0 + j * T + tid < end;
+      w[j] = in ? weight[i0 + j * T + tid] : 0.f;
+      p[j] = in ? pos[i0 + j * T + tid] : INT32_MIN;
     }
-  }
+  };
+  if constexpr (REG) read(0, most);   // beside the length
   int n = a.kv_len[head];
   n = n > most ? most : n;
   if (n <= m) {
@@ -80,60 +93,48 @@ __global__ __launch_bounds__(T) void paged_evict_kernel(PagedEvictArgs a) {
     return;
   }
   int newest = INT32_MIN;
-  if constexpr (REG) {
+  for (int i0 = 0; i0 < (REG ? 1 : n); i0 += T * KR) {
+    if constexpr (!REG) read(i0, n);
 #pragma unroll
-    for (int j = 0; j < KR; ++j) newest = j * T + tid < n && p[j] > newest ? p[j] : newest;
-  } else {
-    for (int i = tid; i < n; i += T) newest = pos[i] > newest ? pos[i] : newest;
+    for (int j = 0; j < KR; ++j) newest = i0 + j * T + tid < n && p[j] > newest ? p[j] : newest;
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    const int y = __shfl_xor(newest, o);
-    newest = y > newest ? y : newest;
-  }
-  if ((tid & 63) == 0) s_newest[tid >> 6] = newest;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < T / 64; ++i) newest = s_newest[i] > newest ? s_newest[i] : newest;
-  const int64_t since = (int64_t)newest - a.recent;
-  if constexpr (REG) {   // read again by the same thread, or behind a barrier
-    // Protected slots right above the largest weight: the selection's digits are then spread over the weights alone.
-    uint32_t top = 0, own[KR];
+  newest = block_max<T>(newest, s_newest);
+  // positions from `since` on are protected; with recent = 0 none
+  const int64_t since64 = (int64_t)newest - a.recent + 1;
+  const int32_t since = since64 < INT32_MIN ? INT32_MIN : (int32_t)since64;
+  const bool protects = a.recent > 0;
+  // Slots as they are ranked: by weight, protected ones right above the largest, so that the selection's digits are spread over
+  // the weights alone.
+  uint32_t top = 0;
+  for (int i0 = 0; i0 < (REG ? 1 : n); i0 += T * KR) {
+    if constexpr (!REG) read(i0, n);
 #pragma unroll
     for (int j = 0; j < KR; ++j) {
-      own[j] = j * T + tid < n && (int64_t)p[j] <= since ? order_key(w[j]) : 0u;
-      top = own[j] > top ? own[j] : top;
+      const int i = i0 + j * T + tid;
+      const uint32_t own = i < n && !(protects && p[j] >= since) ? order_key(w[j]) : 0u;
+      top = own > top ? own : top;
+      if (REG || i < n) key[i] = own;   // read again by the same thread, or behind a barrier
     }
-    for (int o = 32; o > 0; o >>= 1) {
-      const uint32_t y = __shfl_xor(top, o);
-      top = y > top ? y : top;
-    }
-    if ((tid & 63) == 0) s_top[tid >> 6] = top;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < T / 64; ++i) top = s_top[i] > top ? s_top[i] : top;
-    const uint32_t above = top + (top != 0xFFFFFFFFu ? 1u : 0u);   // there is room for one more above infinity's key
-#pragma unroll
-    for (int j = 0; j < KR; ++j) s_key[j * T + tid] = own[j] != 0 ? own[j] : above;
   }
+  top = block_max<T>(top, s_top);
+  top += top != 0xFFFFFFFFu ? 1u : 0u;   // there is room for one more above infinity's key
+  for (int i = tid; i < n; i += T)
+    if (key[i] == 0) key[i] = top;
   const bool few = !a.apart;
   int count = 0;   // slots that move
   if (m > 0) {
+    // Slots on the wrong side of the budget, in ascending order: the free ones, then as many that move into them.
     auto lists = [&](auto ranked, auto selected) __attribute__((always_inline)) {
-      count = ranked([&](int i, uint32_t k) { return i >= m && i < n && selected(i, k); }, [&](int i, int rank) {
-        if (few) s_list[0][rank] = i;
-        else source[rank] = i;
-      });
-      __syncthreads();
-      ranked([&](int i, uint32_t k) { return i < m && !selected(i, k); }, [&](int i, int rank) {
-        if (few) s_list[1][rank] = i;
-        else target[rank] = i;
-      });
+      count = ranked([&](int i, uint32_t k) { return i < n && (i < m) != selected(i, k); }, [&](int i, int rank) {
+        if (few) s_list[rank] = i;
+        else list[rank] = i;
+      }) / 2;
     };
-    if constexpr (REG) select_chunks<T, KR, REG>((const uint32_t *)s_key, n, 1, m, false, 0, lists);
-    else select_chunks<T, KR, REG>(EvictKeys{weight, pos, since}, n, 1, m, false, 0, lists);
+    __syncthreads();
+    select_chunks<T, KR, REG>((const uint32_t *)key, n, 1, m, false, 0, lists);
   }
   __syncthreads();
-  if (few) move_slots(a, layer, b, h, head, s_list[0], s_list[1], count);
+  if (few) move_slots(a, layer, b, h, head, s_list + count, s_list, count);
   if (tid == 0) {
     a.kv_len[head] = m;
     if (!few) *moves = count;
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(kThreads) void paged_move_kernel(PagedEvictArgs a) 
   if (n <= 0) return;
   __shared__ int64_t s_from[kMovesPerGroup], s_to[kMovesPerGroup];
   if ((int)threadIdx.x < n) {
-    const int from = moves[1 + i0 + threadIdx.x], to = moves[1 + a.pitch + i0 + threadIdx.x];
+    const int to = moves[1 + i0 + threadIdx.x], from = moves[1 + all + i0 + threadIdx.x];
     const int32_t *table = a.geom.table + (int64_t)b * a.geom.pitch;
     const int64_t f = slot_offset(a.geom, table, h, from), t = slot_offset(a.geom, table, h, to);
     s_from[threadIdx.x] = t >= 0 ? f : -1;
@@ -195,12 +196,16 @@ int launch_paged_evict(const PagedEvictArgs &args, int n_layers, int batch, int 
   PagedEvictArgs a = args;
   a.apart = paged_moves_apart(a);
   const dim3 grid(batch * a.n_kv_heads, n_layers);
-  if (max_tokens <= 256) hipLaunchKernelGGL((paged_evict_kernel<256, 1, true>), grid, dim3(256), 0, s, a);
-  else if (max_tokens <= 1024) hipLaunchKernelGGL((paged_evict_kernel<256, 4, true>), grid, dim3(256), 0, s, a);
-  else if (max_tokens <= 4096) hipLaunchKernelGGL((paged_evict_kernel<1024, 4, true>), grid, dim3(1024), 0, s, a);
-  else if (max_tokens <= 8192) hipLaunchKernelGGL((paged_evict_kernel<1024, 8, true>), grid, dim3(1024), 0, s, a);
-  else if (max_tokens <= 16384) hipLaunchKernelGGL((paged_evict_kernel<1024, 16, true>), grid, dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((paged_evict_kernel<1024, 16, false>), grid, dim3(1024), 0, s, a);
+  auto go = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, grid, dim3(threads), 0, s, a); };
+  if (max_tokens <= 256) go(paged_evict_kernel<256, 1, kInRegisters>, 256);
+  else if (max_tokens <= 512) go(paged_evict_kernel<256, 2, kInRegisters>, 256);
+  else if (max_tokens <= 1024) go(paged_evict_kernel<256, 4, kInRegisters>, 256);
+  else if (max_tokens <= 2048) go(paged_evict_kernel<512, 4, kInRegisters>, 512);
+  else if (max_tokens <= 4096) go(paged_evict_kernel<1024, 4, kInRegisters>, 1024);
+  else if (max_tokens <= 8192) go(paged_evict_kernel<1024, 8, kInRegisters>, 1024);
+  else if (max_tokens <= 16384) go(paged_evict_kernel<1024, 16, kInRegisters>, 1024);
+  else if (max_tokens <= kEvictLdsKeys) go(paged_evict_kernel<1024, 16, kInLds>, 1024);
+  else go(paged_evict_kernel<1024, 16, kInMemory>, 1024);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 
