@@ -120,7 +120,7 @@ struct PagedDecodeArgs {
   int32_t batch0, batch, n_q_heads, n_kv_heads, group, slot_pitch;
   float scale_log2e;
   int32_t direct;                       // 1: every head is one range, the range kernel writes the outputs
-  int32_t alone;                        // 1: and adds up the weights: no launch follows (16-bit rows)
+  int32_t alone;                        // 1: and adds up the weights: no launch follows
   int32_t first[kPagedBatch + 16];      // number of the first key range of every sequence
   int32_t first_row[kPagedBatch];       // rows of the sequences before, each rounded up to 32
   int32_t max_tokens[kPagedBatch];
@@ -189,6 +189,18 @@ __device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int
   }
 }
 
+// What becomes of the scores: nothing, to the workspace for the launch behind, added up as weights by a workgroup that has a whole head.
+enum Scores { kDropped, kStored, kAdded };
+// token_weight[s] += sum_i 2^(x_i(s) - lse_i), heads in order; x: [heads][kPagedAlone] in LDS.
+__device__ __forceinline__ void add_weights(const PagedDecodeArgs &a, int b, int h, int len, const float *x, const float *lse, int threads) {
+  float *weight = a.weight + ((int64_t)b * a.n_kv_heads + h) * a.slot_pitch;
+  for (int r = threadIdx.x; r < len; r += threads) {
+    float sum = 0.f;
+    for (int j = 0; j < a.group; ++j) sum += __builtin_amdgcn_exp2f(x[j * kPagedAlone + r] - lse[j]);
+    weight[r] += sum;
+  }
+}
+
 constexpr int kEvictLdsKeys = 32768;    // slots of a head whose keys are ranked in LDS
 struct PagedEvictArgs {
   PageGeom geom;
@@ -210,6 +222,7 @@ int launch_paged_len(const PagedLenArgs &a, hipStream_t s);
 int launch_paged_compact(int row_bytes, const PagedCompactArgs &a, int n_layers, int batch, hipStream_t s);
 int launch_paged_decode(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s);
 int launch_paged_mfma(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s);   // 16-bit rows
+int launch_paged_f32(int head_dim, const PagedDecodeArgs &a, hipStream_t s);
 int paged_decode_heads(int dtype, int group);   // query heads of a kv-head that a workgroup serves
 int launch_paged_evict(const PagedEvictArgs &a, int n_layers, int batch, int max_tokens, hipStream_t s);
 bool paged_moves_apart(const PagedEvictArgs &a);   // are there moves enough for a launch of their own

@@ -59,15 +59,15 @@ int range_count(int tokens, int rows) { return tokens > rows ? ceil_div(tokens, 
 // results, and with one and a half workgroups per CU half of the CUs wait.  us of a call, so and otherwise (bf16, 8 kv-heads of 4
 // heads): 13171 slots, 256 workgroups of 416 rows 15.8, 824 of 128 22.0; 30000, 240 of 1024 25.4, 320 of 768 30.2, 472 of 512 25.8;
 // 60000, 472 of 1024 43.9, 944 of 512 46.6; fp32, 20000 slots of 8 heads, 216 of 768 30.3, 320 of 512 37.0.
-// Without weights to add up, heads of up to kPagedDirect slots of 16-bit rows are one range and nothing has to be joined: sixteen
-// sequences of 500 slots 10.9, in ranges of 128 13.9; 300 slots 8.3 and 10.8; but fp32, 300 slots 13.7 and 11.7.
+// Without weights to add up, heads of up to kPagedDirect slots are one range and nothing has to be joined: sixteen
+// sequences of 500 slots 10.9, in ranges of 128 13.9; 300 slots 8.3 and 10.8.
 constexpr int kPagedDirect = 512;
 // With weights, heads of up to kPagedAloneFew slots (kPagedAlone where they fill half of the CUs, and no more than there are) are one
 // workgroup that needs no launch behind it, see paged_decode_mfma.hip.
 constexpr int kPagedAloneFew = 512, kPagedAloneHeads = 128, kCUs = 256;
 bool paged_alone(const chunkkv_pages *p, int nb, int most, bool weights) {
   const int64_t heads = (int64_t)nb * p->n_kv_heads;
-  return weights && p->dtype != CHUNKKV_F32 && p->n_q_heads / p->n_kv_heads <= 8 && heads <= kCUs &&
+  return weights && p->n_q_heads / p->n_kv_heads <= 8 && heads <= kCUs &&
          most <= (heads >= kPagedAloneHeads ? kPagedAlone : kPagedAloneFew);
 }
 int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
@@ -80,7 +80,7 @@ int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
     most = p->max_tokens[b] > most ? p->max_tokens[b] : most;
   }
   if (paged_alone(p, nb, most, weights)) return kPagedAlone;
-  if (!weights && most <= kPagedDirect && p->dtype != CHUNKKV_F32) return kPagedDirect;
+  if (!weights && most <= kPagedDirect) return kPagedDirect;
   const int64_t round = kCUs, rounds = (rows * per_range + round * kPagedMaxRange - 1) / (round * kPagedMaxRange);
   int lo = kPagedMinRange / 32, hi = kPagedMaxRange / 32;
   while (lo < hi) {

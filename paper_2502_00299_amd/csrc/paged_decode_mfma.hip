@@ -75,9 +75,6 @@ __device__ __forceinline__ void join_parts(f32x4 (&acc)[NSET][NMT]) {
     }
 }
 
-// What becomes of the scores: nothing, to the workspace for the launch behind, added up as weights here (one range per head).
-enum Scores { kDropped, kStored, kAdded };
-
 // DT: bf16 or fp16, HD: head dim, G: 4 or 8 query heads per workgroup, NST: K/V slot pairs of a wavefront, NW: wavefronts
 template <int DT, int HD, int G, int NST, int NW, int W>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(PagedDecodeArgs a) {
@@ -322,14 +319,9 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
     store_range<HD>(a, b, h * g + j0 + j, e, M, L, o);
     if (W == kAdded && e == 0) s_lse[j] = L > 0.f ? M + __builtin_log2f(L) : 3.0e38f;   // no slot is there: no weight
   }
-  if constexpr (W == kAdded) {   // heads in order
+  if constexpr (W == kAdded) {
     __syncthreads();
-    float *weight = a.weight + ((int64_t)b * a.n_kv_heads + h) * a.slot_pitch;
-    for (int r = tid; r < len; r += NW * 64) {
-      float sum = 0.f;
-      for (int j = 0; j < g; ++j) sum += __builtin_amdgcn_exp2f(lscores[j * kPagedAlone + r] - s_lse[j]);
-      weight[r] += sum;
-    }
+    add_weights(a, b, h, len, lscores, s_lse, NW * 64);
   }
 }
 
@@ -344,12 +336,12 @@ int launch_g(const PagedDecodeArgs &a, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 template <int DT, int HD>
-int launch_hd(const PagedDecodeArgs &a, hipStream_t s) {
+int launch_16(const PagedDecodeArgs &a, hipStream_t s) {
   return paged_decode_heads(DT, a.group) == 4 ? launch_g<DT, HD, 4>(a, s) : launch_g<DT, HD, 8>(a, s);
 }
 int launch_paged_mfma(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s) {
-  if (dtype == CHUNKKV_BF16) return head_dim == 128 ? launch_hd<CHUNKKV_BF16, 128>(a, s) : launch_hd<CHUNKKV_BF16, 64>(a, s);
-  return head_dim == 128 ? launch_hd<CHUNKKV_F16, 128>(a, s) : launch_hd<CHUNKKV_F16, 64>(a, s);
+  if (dtype == CHUNKKV_BF16) return head_dim == 128 ? launch_16<CHUNKKV_BF16, 128>(a, s) : launch_16<CHUNKKV_BF16, 64>(a, s);
+  return head_dim == 128 ? launch_16<CHUNKKV_F16, 128>(a, s) : launch_16<CHUNKKV_F16, 64>(a, s);
 }
 
 }  // namespace ckv
