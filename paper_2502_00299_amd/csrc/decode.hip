@@ -35,21 +35,6 @@ constexpr int kDecodeUnroll = 4;        // row loads of K (and of V) in flight p
 constexpr float kDecodeNegBig = -1.0e30f;
 
 template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x) {
-  return x + __builtin_amdgcn_update_dpp(0.f, x, CTRL, 0xf, 0xf, false);
-}
-// Sum over the LPR lanes that share a row; every lane of the group ends with the same bits.
-template <int LPR>
-__device__ __forceinline__ float row_sum(float x) {
-  x = dpp_add<0xB1>(x);                          // quad_perm [1,0,3,2]
-  x = dpp_add<0x4E>(x);                          // quad_perm [2,3,0,1]
-  if constexpr (LPR >= 8) x = dpp_add<0x141>(x);   // row_half_mirror: the other quad of 8 lanes
-  if constexpr (LPR >= 16) x = dpp_add<0x140>(x);  // row_mirror: the other half of 16 lanes
-  if constexpr (LPR >= 32) x += __shfl_xor(x, 16);
-  return x;
-}
-
-template <int CTRL>
 __device__ __forceinline__ float dpp_get(float x) {
   return __builtin_amdgcn_update_dpp(0.f, x, CTRL, 0xf, 0xf, false);
 }

@@ -164,6 +164,21 @@ __device__ __forceinline__ T kernarg_at(size_t offset, int i) {
 }
 #define CKV_ARG(STRUCT, FIELD, I) kernarg_at<std::remove_cv_t<std::remove_extent_t<decltype(STRUCT::FIELD)>>>(offsetof(STRUCT, FIELD), (I))
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_amdgcn_update_dpp(0.f, x, CTRL, 0xf, 0xf, false);
+}
+// Sum over the LPR lanes that share a row; every lane of the group ends with the same bits.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float x) {
+  x = dpp_add<0xB1>(x);                            // quad_perm [1,0,3,2]
+  x = dpp_add<0x4E>(x);                            // quad_perm [2,3,0,1]
+  if constexpr (LPR >= 8) x = dpp_add<0x141>(x);   // row_half_mirror: the other quad of 8 lanes
+  if constexpr (LPR >= 16) x = dpp_add<0x140>(x);  // row_mirror: the other half of 16 lanes
+  if constexpr (LPR >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
+
 // Single-pass scoring: periods (160 keys) one workgroup walks, for a sequence of n_periods periods.  A function
 // of the sequence alone (at most 32 ranges per sequence and kv-head, at least 4 periods each), so the key ranges,
 // and with them every rounding of a score, do not depend on how many layers or sequences share a launch.

@@ -53,21 +53,6 @@ __device__ __forceinline__ int paged_sequence(int x, int nb) {
   return b;
 }
 
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x) {
-  return x + __builtin_amdgcn_update_dpp(0.f, x, CTRL, 0xf, 0xf, false);
-}
-// Sum over the LPR lanes that share a row; every lane of the group ends with the same bits.
-template <int LPR>
-__device__ __forceinline__ float row_sum(float x) {
-  x = dpp_add<0xB1>(x);                            // quad_perm [1,0,3,2]
-  x = dpp_add<0x4E>(x);                            // quad_perm [2,3,0,1]
-  if constexpr (LPR >= 8) x = dpp_add<0x141>(x);   // row_half_mirror: the other quad of 8 lanes
-  if constexpr (LPR >= 16) x = dpp_add<0x140>(x);  // row_mirror: the other half of 16 lanes
-  if constexpr (LPR >= 32) x += __shfl_xor(x, 16);
-  return x;
-}
-
 struct PagedAppendArgs {
   PageGeom geom;
   const void *q, *k, *v;
@@ -120,13 +105,14 @@ struct PagedDecodeArgs {
   int32_t batch0, batch, n_q_heads, n_kv_heads, group, slot_pitch;
   float scale_log2e;
   int32_t direct;                       // 1: every head is one range, the range kernel writes the outputs
-  int32_t alone;                        // 1: and adds up the weights: no launch follows
+  int32_t alone;                        // its wavefronts if it adds up the weights as well, and no launch follows; 0
   int32_t first[kPagedBatch + 16];      // number of the first key range of every sequence
   int32_t first_row[kPagedBatch];       // rows of the sequences before, each rounded up to 32
   int32_t max_tokens[kPagedBatch];
 };
 constexpr int kPagedMinRange = 128, kPagedMaxRange = 1024;   // rows of a key range
-constexpr int kPagedAlone = 960;                             // of a head that one workgroup of eight wavefronts takes
+// Rows of a head that a workgroup of so many wavefronts takes as a whole, its scores beside the ring in LDS.
+__host__ __device__ constexpr int alone_rows(int waves) { return waves == 8 ? 960 : 512; }
 // Rows of every range of a head with n slots that `splits` ranges share.  From the length that the device knows, so that
 // all ranges have work when max_tokens is far above it.
 __host__ __device__ inline int paged_range_rows(int n, int splits) {
@@ -191,12 +177,13 @@ __device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int
 
 // What becomes of the scores: nothing, to the workspace for the launch behind, added up as weights by a workgroup that has a whole head.
 enum Scores { kDropped, kStored, kAdded };
-// token_weight[s] += sum_i 2^(x_i(s) - lse_i), heads in order; x: [heads][kPagedAlone] in LDS.
-__device__ __forceinline__ void add_weights(const PagedDecodeArgs &a, int b, int h, int len, const float *x, const float *lse, int threads) {
+// token_weight[s] += sum_i 2^(x_i(s) - lse_i), heads in order; x: [heads][alone_rows] in LDS.
+template <int NW>
+__device__ __forceinline__ void add_weights(const PagedDecodeArgs &a, int b, int h, int len, const float *x, const float *lse) {
   float *weight = a.weight + ((int64_t)b * a.n_kv_heads + h) * a.slot_pitch;
-  for (int r = threadIdx.x; r < len; r += threads) {
+  for (int r = threadIdx.x; r < len; r += NW * 64) {
     float sum = 0.f;
-    for (int j = 0; j < a.group; ++j) sum += __builtin_amdgcn_exp2f(x[j * kPagedAlone + r] - lse[j]);
+    for (int j = 0; j < a.group; ++j) sum += __builtin_amdgcn_exp2f(x[j * alone_rows(NW) + r] - lse[j]);
     weight[r] += sum;
   }
 }

@@ -59,16 +59,20 @@ int range_count(int tokens, int rows) { return tokens > rows ? ceil_div(tokens, 
 // results, and with one and a half workgroups per CU half of the CUs wait.  us of a call, so and otherwise (bf16, 8 kv-heads of 4
 // heads): 13171 slots, 256 workgroups of 416 rows 15.8, 824 of 128 22.0; 30000, 240 of 1024 25.4, 320 of 768 30.2, 472 of 512 25.8;
 // 60000, 472 of 1024 43.9, 944 of 512 46.6; fp32, 20000 slots of 8 heads, 216 of 768 30.3, 320 of 512 37.0.
-// Without weights to add up, heads of up to kPagedDirect slots are one range and nothing has to be joined: sixteen
-// sequences of 500 slots 10.9, in ranges of 128 13.9; 300 slots 8.3 and 10.8.
-constexpr int kPagedDirect = 512;
-// With weights, heads of up to kPagedAloneFew slots (kPagedAlone where they fill half of the CUs, and no more than there are) are one
-// workgroup that needs no launch behind it, see paged_decode_mfma.hip.
-constexpr int kPagedAloneFew = 512, kPagedAloneHeads = 128, kCUs = 256;
-bool paged_alone(const chunkkv_pages *p, int nb, int most, bool weights) {
+// Without weights to add up, heads whose K rows take up to 128 KB are one range and nothing has to be joined: us in a graph, so and in
+// ranges of 128, 8 heads of 300 slots 7.3 / 8.4, of 512 8.1 / 8.5, d = 64 6.5 / 7.5, fp32 of 200 9.6 / 9.8, of 300 10.9 / 9.9.
+constexpr int kPagedShortBytes = 128 << 10;
+int short_rows(const chunkkv_pages *p) { return kPagedShortBytes / (p->head_dim * elem_bytes(p->dtype)); }
+// With weights, heads as short (where they fill half of the CUs, longer ones too) are one workgroup that needs no launch behind it.
+// Four wavefronts, of which two workgroups fit a CU, or eight for the longer heads, where they are few.  us in a graph, ranges and a launch
+// behind / eight / four: 8 heads of 128 slots 9.5 / 6.8 / 6.3, of 256 9.5 / 7.7 / 7.3, of 300 9.7 / 8.4 / 8.9, of 512 9.6 / 9.2 / 9.6, of 800 9.8 / 11.6 / -;
+// 64 of 300 10.5 / 9.2 / 9.1, of 512 11.2 / 11.3 / 10.6; 128 of 900 18.0 / 16.9 / -; 256 of 300 14.8 / 11.2 / 10.9, of 960 28.8 / 23.8 / -; 512 of 40
+// 12.6 / 13.3 / 8.2, of 500 30.7 / 28.3 / 24.4, of 900 49.2 / 45.4 / -; fp32, 8 of 200 11.2 / 10.5 / 10.9, of 300 11.3 / 11.6 / 12.7, 512 of 500 51.6 / 47.3 / 44.2.
+constexpr int kPagedAloneHeads = 128, kPagedFourHeads = 64, kPagedFourRows = 256, kCUs = 256;
+int paged_alone(const chunkkv_pages *p, int nb, int most, bool weights) {   // -> wavefronts, 0: no
   const int64_t heads = (int64_t)nb * p->n_kv_heads;
-  return weights && p->n_q_heads / p->n_kv_heads <= 8 && heads <= kCUs &&
-         most <= (heads >= kPagedAloneHeads ? kPagedAlone : kPagedAloneFew);
+  if (!weights || p->n_q_heads / p->n_kv_heads > 8 || most > alone_rows(8) || (heads < kPagedAloneHeads && most > short_rows(p))) return 0;
+  return most <= kPagedFourRows || (heads >= kPagedFourHeads && most <= alone_rows(4)) ? 4 : 8;
 }
 int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
   const int g = p->n_q_heads / p->n_kv_heads, G = paged_decode_heads(p->dtype, g);
@@ -79,8 +83,7 @@ int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
     rows += p->max_tokens[b];
     most = p->max_tokens[b] > most ? p->max_tokens[b] : most;
   }
-  if (paged_alone(p, nb, most, weights)) return kPagedAlone;
-  if (!weights && most <= kPagedDirect) return kPagedDirect;
+  if (paged_alone(p, nb, most, weights) || (!weights && most <= short_rows(p))) return kPagedMaxRange;
   const int64_t round = kCUs, rounds = (rows * per_range + round * kPagedMaxRange - 1) / (round * kPagedMaxRange);
   int lo = kPagedMinRange / 32, hi = kPagedMaxRange / 32;
   while (lo < hi) {

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
   constexpr int NKS = HD / 16, NH = HD / 64;               // 64-byte pieces of a key, 64-dim pieces of the output
   constexpr int RING = NW * NST * 2 * SLOT, AH = 8;        // AH: most heads of a workgroup that adds up weights
   static_assert(RING >= NW * G * (HD + 2) * 4 + G * 4, "the states of the wavefronts take the ring's place");
-  __shared__ __align__(16) char smem[RING + (W == kAdded ? AH * kPagedAlone * 4 : 0)];
+  __shared__ __align__(16) char smem[RING + (W == kAdded ? AH * alone_rows(NW) * 4 : 0)];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
   const __amdgpu_buffer_rsrc_t srs = __builtin_amdgcn_make_buffer_rsrc(W == kStored ? (void *)head_scores(a, bl, h * g + j0) : nullptr, 0, (int)((uint32_t)heads * spitch * 4u), 0x00020000);
   const bool scored = n < heads;
   const uint32_t soff = ((uint32_t)n * spitch + (uint32_t)(r0 + 4 * q)) * 4u;
-  float *lscores = (float *)(smem + RING);   // [AH][kPagedAlone]
+  float *lscores = (float *)(smem + RING);   // [AH][alone_rows(NW)]
   // Accesses behind the slot that is waited for: loads of the other slots and, once every slot has been refilled, the store of
   // each of NST steps.
   constexpr int kLoads = (2 * NST - 1) * NLD, kBehind = kLoads + (W == kStored ? NST : 0);
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
       __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sc * c1), srs, scored ? (int)(soff + (uint32_t)key0 * 4u) : -1, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     } else if constexpr (W == kAdded) {
-      if (scored) *(f32x4 *)(lscores + n * kPagedAlone + key0 + 4 * q) = sc * c1;
+      if (scored) *(f32x4 *)(lscores + n * alone_rows(NW) + key0 + 4 * q) = sc * c1;
     }
     float p[4];
     auto weights = [&]() __attribute__((always_inline)) {
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
   }
   if constexpr (W == kAdded) {
     __syncthreads();
-    add_weights(a, b, h, len, lscores, s_lse, NW * 64);
+    add_weights<NW>(a, b, h, len, lscores, s_lse);
   }
 }
 
@@ -237,7 +237,8 @@ int launch_hd(const PagedDecodeArgs &a, hipStream_t s) {
   constexpr int NST = HD == 128 ? 1 : 2;
   const dim3 grid(a.first[a.batch], a.n_kv_heads * ((a.group + 15) / 16));
   auto go = [&](auto kern, int waves) { hipLaunchKernelGGL(kern, grid, dim3(waves * 64), 0, s, a); };
-  if (a.alone) go(paged_f32_kernel<HD, NST, 8, kAdded>, 8);
+  if (a.alone == 8) go(paged_f32_kernel<HD, NST, 8, kAdded>, 8);
+  else if (a.alone == 4) go(paged_f32_kernel<HD, NST, 4, kAdded>, 4);
   else if (a.weight != nullptr) go(paged_f32_kernel<HD, NST, 4, kStored>, 4);
   else go(paged_f32_kernel<HD, NST, 4, kDropped>, 4);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;

@@ -11,11 +11,9 @@
 // Weights: kStored keeps the scaled logits (fp32, log2 units) for the launch that adds up what every slot received.  They go
 // out by buffer stores whose idle columns lie out of range, so every step has two and the waits can count them together with
 // the loads (both leave the counter in the order they were issued).
-// kAdded keeps them in LDS: a head that is one range of eight wavefronts knows its log-sum-exps in the end and adds its own
-// weights, and nothing follows.
-// us in a graph, with and without a launch behind: 8 heads of 256 slots 7.7 / 9.5, of 512 9.2 / 9.6, of 800 11.9 / 9.8; 128 heads of 512
-// 12.0 / 13.5, of 960 16.9 / 18.3; 256 of 960 23.6 / 29.0; d = 64, 8 of 512 7.2 / 8.6, 256 of 960 15.0 / 19.1.  Eight wavefronts for ranges that
-// are joined are slower, with as many rows in flight: 13171 slots 16.2, four 15.2.
+// kAdded keeps them in LDS: a head that is one range knows its log-sum-exps in the end and adds its own weights, and nothing
+// follows.  It has four wavefronts or eight (paged_alone says when); eight for ranges that are joined are slower, with as many rows in
+// flight: 13171 slots 16.2 us, four 15.2.
 // Grid: x = key range of any sequence, y = (batch of G query heads, kv-head).
 #include "decode_mfma.h"
 #include "paged.h"
@@ -87,7 +85,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   constexpr bool BF = DT == CHUNKKV_BF16;
   constexpr int RING = NW * NST * 2 * SLOT;
   static_assert(RING >= NW * G * (HD + 2) * 4 + G * 4, "the states of the wavefronts take the ring's place");
-  __shared__ __align__(16) char smem[RING + (W == kAdded ? G * kPagedAlone * 4 : 0)];
+  __shared__ __align__(16) char smem[RING + (W == kAdded ? G * alone_rows(NW) * 4 : 0)];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -177,10 +175,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   const __amdgpu_buffer_rsrc_t srs = __builtin_amdgcn_make_buffer_rsrc(W == kStored ? (void *)head_scores(a, bl, h * g + j0) : nullptr, 0, (int)((uint32_t)sheads * spitch * 4u), 0x00020000);
   const bool scored = n < sheads;
   const uint32_t soff = ((uint32_t)n * spitch + (uint32_t)(r0 + 4 * q)) * 4u;
-  float *lscores = (float *)(smem + RING);   // [G][kPagedAlone]
+  float *lscores = (float *)(smem + RING);   // [G][alone_rows(NW)]
   auto keep = [&](int key, const f32x4 &x) __attribute__((always_inline)) {
     if constexpr (W == kAdded) {
-      if (scored) *(f32x4 *)(lscores + n * kPagedAlone + key + 4 * q) = x;
+      if (scored) *(f32x4 *)(lscores + n * alone_rows(NW) + key + 4 * q) = x;
       return;
     }
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), srs, scored ? (int)(soff + (uint32_t)key * 4u) : -1, 0, 0);
@@ -321,7 +319,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   }
   if constexpr (W == kAdded) {
     __syncthreads();
-    add_weights(a, b, h, len, lscores, s_lse, NW * 64);
+    add_weights<NW>(a, b, h, len, lscores, s_lse);
   }
 }
 
@@ -330,7 +328,8 @@ int launch_g(const PagedDecodeArgs &a, hipStream_t s) {
   constexpr int NST = HD == 128 ? 1 : 2;
   const dim3 grid(a.first[a.batch], a.n_kv_heads * ((a.group + G - 1) / G));
   auto go = [&](auto kern, int waves) { hipLaunchKernelGGL(kern, grid, dim3(waves * 64), 0, s, a); };
-  if (a.alone) go(paged_mfma_kernel<DT, HD, G, NST, 8, kAdded>, 8);
+  if (a.alone == 8) go(paged_mfma_kernel<DT, HD, G, NST, 8, kAdded>, 8);
+  else if (a.alone == 4) go(paged_mfma_kernel<DT, HD, G, NST, 4, kAdded>, 4);
   else if (a.weight != nullptr) go(paged_mfma_kernel<DT, HD, G, NST, 4, kStored>, 4);
   else go(paged_mfma_kernel<DT, HD, G, NST, 4, kDropped>, 4);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;

@@ -84,13 +84,13 @@ def test_key_ranges(lib, dtype, hq, hkv, d, page, room):
     assert (d0[0] == 0).all() and (d0[1] == float("-inf")).all()
 
 
-@pytest.mark.parametrize("dtype", [BF16, F16])
-@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 1, 64), (3, 1, 128), (40, 8, 64)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (8, 1, 64), (3, 1, 128), (40, 8, 64), (17, 1, 64), (72, 8, 64)])
 def test_around_one_workgroup_per_head(lib, dtype, hq, hkv, d):
-    """512 slots of few heads, 960 of 128 heads and more: the last that one workgroup takes, the first that it does not, and heads short of
-    that many; 256 heads and more."""
+    """Lengths and numbers of heads at which one workgroup takes a head, of four wavefronts and of eight, or ranges do."""
     gen = torch.Generator().manual_seed(d + hq)
-    for batch, top in ((1, 512), (1, 513), (3, 500), (128 // hkv, 960), (128 // hkv, 961), (256 // hkv, 40), (264 // hkv, 40)):
+    for batch, top in ((1, 256), (1, 257), (1, 512), (1, 513), (3, 500), (1, 960), (1, 961), (1, 1025), (64 // hkv, 512), (64 // hkv, 513), (128 // hkv, 960), (128 // hkv, 961),
+                       (256 // hkv, 40), (264 // hkv, 40)):
         if batch > 32 and d * hq > 700:
             continue
         room = [top if i % 5 == 0 else (i * 37) % top for i in range(batch)]
