@@ -454,7 +454,7 @@ def chunkkv_decode_attention_static(prob: Problem, compacted: bool, kv_len, q, k
 # and 0.1 us a pool of a list.
 _KINDS = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}
 _I32, _F32 = torch.int32, torch.float32
-_get_device, _data_ptr, _nbytes = torch.Tensor.get_device, torch.Tensor.data_ptr, attrgetter("nbytes")
+_get_device, _data_ptr, _is_contiguous, _nbytes = torch.Tensor.get_device, torch.Tensor.data_ptr, torch.Tensor.is_contiguous, attrgetter("nbytes")
 
 
 def _refuse(where: str, dev: int, name: str, t, kind, elements: int):
@@ -488,8 +488,10 @@ def _pool(where: str, dev: int, name: str, t: torch.Tensor, kind, elements: int)
 
 
 def _pools(where: str, dev: int, name: str, ts: Sequence, kind, elements: int):
-    """Addresses of the pools of several layers, as an array whose own address the library reads them from."""
-    if len(ts) <= 4 or ts[0].dtype is not kind or set(map(_get_device, ts)) != {dev} or min(map(_nbytes, ts)) < elements * ts[0].element_size():
+    """Addresses of the pools of several layers, as an array whose own address the library reads them from.  In a long list the
+    first pool's type stands for all; devices, bytes and contiguity are everyone's."""
+    if (len(ts) <= 4 or ts[0].dtype is not kind or set(map(_get_device, ts)) != {dev} or min(map(_nbytes, ts)) < elements * ts[0].element_size()
+            or not all(map(_is_contiguous, ts))):
         return array("Q", [_pool(where, dev, name, t, kind, elements) for t in ts])
     return array("Q", map(_data_ptr, ts))
 

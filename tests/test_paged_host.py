@@ -173,3 +173,19 @@ def test_oracle_attention_and_eviction():
     assert orc.evict(weight, pos, 6, 3, 1) == (3, [(4, 1), (5, 2)])     # the newest in any case
     assert orc.evict([1.0] * 6, pos, 6, 2, 0) == (2, [])                # ties: the lower slots
     assert orc.evict(weight, pos, 6, 0, 0) == (0, [])
+
+
+@pytest.mark.parametrize("layers", [3, 6])
+def test_pools_of_a_stack_are_measured(layers):
+    from paper_2502_00299_amd import binding
+    pools = [torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16) for _ in range(layers)]
+    at = binding._pools("here", -1, "k_pages", pools, torch.bfloat16, 4 * 2 * 16 * 64)
+    assert list(at) == [t.data_ptr() for t in pools]
+    bigger = torch.zeros(9, 4, 16, 64, dtype=torch.bfloat16)
+    views = pools[:-1] + [bigger[1:5, :2]]   # not contiguous, but with as much memory behind it
+    assert binding._pools("here", -1, "k_pages", views, torch.bfloat16, 4 * 2 * 16 * 64)[-1] == bigger[1].data_ptr()
+    for wrong in (pools[0][:3], torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16).expand(4, 2, 16, 64)):
+        with pytest.raises(ValueError, match="k_pages has"):
+            binding._pools("here", -1, "k_pages", pools[:-1] + [wrong], torch.bfloat16, 4 * 2 * 16 * 64)
+    with pytest.raises(ValueError, match="on device"):
+        binding._pools("here", 0, "k_pages", pools, torch.bfloat16, 16)
