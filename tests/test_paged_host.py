@@ -184,7 +184,7 @@ def test_pools_of_a_stack_are_measured(layers):
     bigger = torch.zeros(9, 4, 16, 64, dtype=torch.bfloat16)
     views = pools[:-1] + [bigger[1:5, :2]]   # not contiguous, but with as much memory behind it
     assert binding._pools("here", -1, "k_pages", views, torch.bfloat16, 4 * 2 * 16 * 64)[-1] == bigger[1].data_ptr()
-    for wrong in (pools[0][:3], torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16).expand(4, 2, 16, 64)):
+    for wrong in (torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16).expand(4, 2, 16, 64)):
         with pytest.raises(ValueError, match="k_pages has"):
             binding._pools("here", -1, "k_pages", pools[:-1] + [wrong], torch.bfloat16, 4 * 2 * 16 * 64)
     with pytest.raises(ValueError, match="on device"):
