@@ -110,6 +110,7 @@ struct PagedDecodeArgs {
   int32_t first_row[kPagedBatch];       // rows of the sequences before, each rounded up to 32
   int32_t max_tokens[kPagedBatch];
 };
+constexpr float kPagedLowest = -3.3e38f;                      // reference of a softmax that has seen no slot: below all scores that are worth telling apart
 constexpr int kPagedMinRange = 128, kPagedMaxRange = 1024;   // rows of a key range
 // Rows of a head that a workgroup of so many wavefronts takes as a whole, its scores beside the ring in LDS.
 __host__ __device__ constexpr int alone_rows(int waves) { return waves == 8 ? 960 : 512; }

@@ -7,8 +7,6 @@
 
 namespace ckv {
 
-constexpr float kNegBig = -1.0e30f;
-
 // The launch behind the ranges.
 //
 // Its first `joins` workgroups join a query head each: out = sum_r o_r 2^(m_r - M) / sum_r l_r 2^(m_r - M).  A thread owns four
@@ -27,7 +25,7 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
     const int64_t slot = (int64_t)CKV_ARG(PagedDecodeArgs, first, bl) * a.n_q_heads + hq;
     const float2 *ml = a.part_ml + slot;
     const float *po = a.part_o + slot * HD + col * 4;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, m = kNegBig, lsum = 0.f;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, m = kPagedLowest, lsum = 0.f;
     for (int r0 = grp; r0 < used; r0 += UN * NG) {
       float2 p[UN];
       float4 o4[UN];
@@ -90,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          sx[j][i] = kNegBig;
+          sx[j][i] = kPagedLowest;
           if (j0 + j < a.group && t + i * kThreads < len) sx[j][i] = scores[(int64_t)(j0 + j) * pitch + t + i * kThreads];
         }
     };
@@ -102,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
       old[i] = t + i * kThreads < len ? weight[t + i * kThreads] : 0.f;
     }
     for (int j = wave; j < a.group; j += kThreads / 64) {
-      float m = kNegBig, l = 0.f;
+      float m = kPagedLowest, l = 0.f;
       for (int r = lane; r < used; r += 64) {
         const float2 p = a.part_ml[(int64_t)(first + r) * a.n_q_heads + h * a.group + j];
         const float mm = fmaxf(m, p.x);

@@ -113,7 +113,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
     issue(a.k, koff, s, kslot(s));
     issue(a.v, voff, s, vslot(s));
   }
-  float m = -1.0e30f, l = 0.f;
+  float m = kPagedLowest, l = 0.f;   // m before the scale
   f32x4 acc[NH][4];
 #pragma unroll
   for (int t = 0; t < NH; ++t)
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
     float p[4];
     auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], c1, -m));
+      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f((sc[i] - m) * c1);
     };
     weights();
     float sum = (p[0] + p[1]) + (p[2] + p[3]);
@@ -168,8 +168,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       over = fmaxf(over, __shfl_xor(over, 16));
       over = fmaxf(over, __shfl_xor(over, 32));
-      const float m_new = over >= 16.f ? mx * c1 : m;
-      const float f = __builtin_amdgcn_exp2f(m - m_new);
+      const float m_new = over >= 16.f ? mx : m;
+      const float f = __builtin_amdgcn_exp2f((m - m_new) * c1);
       m = m_new;
       l *= f;
 #pragma unroll
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
   __syncthreads();
   float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G, *s_lse = s_o + NW * G * HD;   // [NW][G], [NW][G], [NW][G][HD], [G]
   if (scored) {
-    if (q == 0) { s_m[wave * G + n] = m; s_l[wave * G + n] = l; }
+    if (q == 0) { s_m[wave * G + n] = m * c1; s_l[wave * G + n] = l; }
 #pragma unroll
     for (int t = 0; t < NH; ++t)
 #pragma unroll

@@ -198,7 +198,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
     issue(a.k, koff, s, kslot(s));
     issue(a.v, voff, s, vslot(s));
   }
-  float m = kNegBig, l = 0.f;
+  float m = kPagedLowest, l = 0.f;   // m before the scale: a difference of scores is exact where it counts, however large they are
   f32x4 acc[NSET][NMT];
 #pragma unroll
   for (int s = 0; s < NSET; ++s)
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
     float p[8];
     auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i / 4][i % 4], c1, -m));
+      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f((sc[i / 4][i % 4] - m) * c1);
     };
     weights();
     float sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
@@ -260,8 +260,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       over = fmaxf(over, __shfl_xor(over, 16));
       over = fmaxf(over, __shfl_xor(over, 32));
-      const float m_new = over >= kOver ? mx * c1 : m;
-      const float f = __builtin_amdgcn_exp2f(m - m_new);
+      const float m_new = over >= kOver ? mx : m;
+      const float f = __builtin_amdgcn_exp2f((m - m_new) * c1);
       m = m_new;
       l *= f;
 #pragma unroll
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   __syncthreads();
   float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G, *s_lse = s_o + NW * G * HD;   // [NW][G], [NW][G], [NW][G][HD], [G]
   if (n < G) {
-    if (q == 0) { s_m[wave * G + n] = m; s_l[wave * G + n] = l; }
+    if (q == 0) { s_m[wave * G + n] = m * c1; s_l[wave * G + n] = l; }
 #pragma unroll
     for (int mt = 0; mt < NMT; ++mt) *(f32x4 *)(s_o + (wave * G + n) * HD + 16 * mt + 4 * q) = acc[0][mt];
   }

@@ -160,6 +160,28 @@ def test_scales_and_far_logits(lib, dtype, scale):
     check(cache, q, cache.len[0].tolist())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("room", [200, 400, 3000])
+@pytest.mark.parametrize("times", [1.0, 1.2109375])   # a scale times it is exact, or is not
+def test_logits_far_below_zero(lib, dtype, room, times):
+    """-2^110 / 8 and more for one slot and twice that for the others: it gets all the weight, whatever the softmax starts from."""
+    gen = torch.Generator().manual_seed(8)
+    cache = H.Cache(gen, dtype, 8, 2, 64, 16, [room], [room])
+    there = torch.isfinite(cache.k[0])
+    there[..., 1:] = False
+    cache.k[0][torch.isfinite(cache.k[0])] = 0
+    cache.k[0][there] = -2.0 ** 51
+    _, page, row = cache.slots(0, 0, room)
+    cache.k[0, page[137], :, row[137], 0] = -2.0 ** 50
+    q = torch.zeros((1, 8, 64), dtype=H.KIND[dtype])
+    q[..., 0] = times * 2.0 ** 60
+    out, lse, weight = run(cache, q, None, torch.zeros_like(cache.weight[0]))
+    want = cache.v[0, page[137], :, row[137]].float()
+    assert torch.equal(out[0], want.repeat_interleave(4, 0))
+    assert float((lse / (-times * 2.0 ** 107) - 1).abs().max()) <= 4 * 2.0 ** -24   # times log2 e, its rounding and back
+    assert float(weight[0, :, 137].min()) == float(weight[0, :, 137].max()) == 4 and float(weight[0].sum()) == 8
+
+
 def test_equal_keys_and_exact_weights(lib):
     """Equal keys: every slot gets g / n, summed over calls."""
     gen = torch.Generator().manual_seed(6)
