@@ -49,29 +49,32 @@ def build(verbose: bool = True) -> str:
     return LIB
 
 
-def build_host_sanitizer_check(out_dir: str) -> str:
-    """Builds tests/host_sanitizer_main.cpp against the library's sources with AddressSanitizer and
+CHECKED = ["api.hip", "paged_api.hip"]   # every argument check and workspace plan
+
+
+def build_host_sanitizer_check(out_dir: str, main: str = "host_sanitizer_main") -> str:
+    """Builds tests/<main>.cpp against the library's sources with AddressSanitizer and
     UndefinedBehaviorSanitizer on the HOST pass only (device code is compiled as usual and never runs in that
-    program): api.hip, which holds every argument check and workspace plan, is recompiled with the sanitizers;
+    program): the sources that hold the argument checks and workspace plans are recompiled with the sanitizers;
     the kernels' objects are the ones build() made.  Returns the path of the executable."""
     os.makedirs(out_dir, exist_ok=True)
     if not all(os.path.exists(os.path.join(OBJ, s.replace(".hip", ".o"))) for s in SOURCES):
         build(verbose=False)
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
            "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer", "-g"]
-    api_o = os.path.join(out_dir, "api_san.o")
-    main_o = os.path.join(out_dir, "host_sanitizer_main.o")
-    exe = os.path.join(out_dir, "host_sanitizer_check")
+    checked = [os.path.join(out_dir, s.replace(".hip", "_san.o")) for s in CHECKED]
+    main_o = os.path.join(out_dir, main + ".o")
+    exe = os.path.join(out_dir, main)
     clangxx = os.path.join(os.path.dirname(os.path.realpath(HIPCC)), "..", "lib", "llvm", "bin", "clang++")
     if not os.path.exists(clangxx):
         clangxx = "/opt/rocm/lib/llvm/bin/clang++"
     steps = [
-        [HIPCC, *FLAGS, *san, "-c", os.path.join(CSRC, "api.hip"), "-o", api_o],
+        *[[HIPCC, *FLAGS, *san, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(CHECKED, checked)],
         [clangxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined",
          "-fno-omit-frame-pointer", "-I", os.path.join(ROOT, "include"), "-c",
-         os.path.join(ROOT, "tests", "host_sanitizer_main.cpp"), "-o", main_o],
-        [clangxx, "-fsanitize=address,undefined", "-o", exe, main_o, api_o,
-         *[os.path.join(OBJ, s.replace(".hip", ".o")) for s in SOURCES if s != "api.hip"],
+         os.path.join(ROOT, "tests", main + ".cpp"), "-o", main_o],
+        [clangxx, "-fsanitize=address,undefined", "-o", exe, main_o, *checked,
+         *[os.path.join(OBJ, s.replace(".hip", ".o")) for s in SOURCES if s not in CHECKED],
          "-L/opt/rocm/lib", "-lamdhip64", "-Wl,-rpath,/opt/rocm/lib"],
     ]
     for cmd in steps:

@@ -1,7 +1,9 @@
 """Calls over caches in pages, without a GPU: argument checks, workspace sizes, the kept struct, the oracle's own pins."""
 import copy
 import ctypes as C
+import os
 import pickle
+import subprocess
 
 import numpy as np
 import pytest
@@ -189,3 +191,13 @@ def test_pools_of_a_stack_are_measured(layers):
             binding._pools("here", -1, "k_pages", pools[:-1] + [wrong], torch.bfloat16, 4 * 2 * 16 * 64)
     with pytest.raises(ValueError, match="on device"):
         binding._pools("here", 0, "k_pages", pools, torch.bfloat16, 16)
+
+
+def test_checks_and_plans_are_clean_under_asan_and_ubsan(tmp_path):
+    from paper_2502_00299_amd import build
+    exe = build.build_host_sanitizer_check(str(tmp_path), "host_sanitizer_pages")
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300, env=env)
+    out = r.stdout + r.stderr
+    assert r.returncode == 0 and "HOST SANITIZER RUN OK" in r.stdout, out[-4000:]
+    assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
