@@ -201,7 +201,7 @@ struct PagedEvictArgs {
   int32_t apart;                        // 1: the moves are a launch of their own
   int32_t stream;                       // 1: with streaming stores
   int32_t batch0, batch_total, n_kv_heads, slot_pitch, recent;
-  int32_t row_bytes;
+  int32_t row_shift;                    // log2 of the 16-byte segments of a row
   int32_t budget[kPagedBatch], max_tokens[kPagedBatch];
 };
 

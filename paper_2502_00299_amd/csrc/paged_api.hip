@@ -379,7 +379,7 @@ int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int3
       a.key_pitch = key_pitch(pages, budget);
       a.keys = (uint32_t *)((char *)workspace + pl.off_keys) + heads0 * a.key_pitch;
       a.pitch = pitch; a.batch0 = b0; a.batch_total = pages->batch; a.n_kv_heads = pages->n_kv_heads; a.slot_pitch = pages->slot_pitch;
-      a.recent = recent; a.row_bytes = pages->head_dim * elem_bytes(pages->dtype);
+      a.recent = recent; a.row_shift = 31 - __builtin_clz(pages->head_dim * elem_bytes(pages->dtype) / 16);
       a.stream = written > kPagedStreamBytes;
       int most = 0;
       for (int i = 0; i < nb; ++i) {

@@ -3,6 +3,7 @@
 // A row (one head of one token) is spread over LPR = d * element size / 16 lanes, 16 bytes each; a wavefront takes 64 / LPR
 // rows at a time, a key row together with its value row, so the slot's address is formed once for both and kv_len[b][h]
 // has one reader per token.  Per row: sum of squares over the lanes (DPP), scale, rotation, one rounding, store.
+// Bound by HBM for prompts (8192 tokens of 32 + 8 + 8 heads, bf16, 38 us, 5.3 TB/s), by latency for single ones (8 tokens 3.6 us from a graph).
 // Angles: position * inv_freq / 2 pi in double, reduced to a part of a revolution there (off by 3 * 2^-25 of one at a
 // position of 2^31, by 2^-34 at 2^20), sine and cosine of that part in fp32.  All rows of a token have the same angles: a
 // wavefront's row groups form a share of them each and exchange them, once for all the rows that it takes.
@@ -210,9 +211,16 @@ int launch_append(const PagedAppendArgs &a, dim3 grid, hipStream_t s) {
 int launch_paged_append(int dtype, int head_dim, const PagedAppendArgs &args, hipStream_t s) {
   PagedAppendArgs a = args;
   const int rows = 64 / (head_dim * elem_bytes(dtype) / 16);
-  const int groups = ((a.q != nullptr ? a.n_q_heads : 0) + a.n_kv_heads + rows - 1) / rows;   // rounds of a token's rows
-  const int parts = (int)((4096 + a.tokens - 1) / a.tokens);
-  a.parts = parts > groups ? groups : parts;
+  const int rounds = ((a.q != nullptr ? a.n_q_heads : 0) + a.n_kv_heads + rows - 1) / rows;   // of a token's rows
+  // Wavefronts that share a token: so many that there are 4096, or that each has five rounds, whichever is more; then the fewest with
+  // as many rounds each.  us by wavefronts, bf16, 10 rounds: 300 tokens 2 6.2, 4 5.5, 10 4.8; 600: 4 6.7, 5 6.3, 8 8.2; 2080: 1 17.2, 2 14.6, 4 16.1;
+  // 8192: 1 39.6, 2 38.4, 4 45.1; 40000: 1 194, 2 184, 4 209; fp32, 20 rounds: 600: 4 10.2, 7 9.7, 8 10.9; 8192: 1 92.9, 3 81.5, 4 78.9, 8 86.5;
+  // fp16 of d = 64, 2 rounds: 8192: 1 15.7, 2 19.2.
+  int parts = (4096 + a.tokens - 1) / a.tokens;
+  if (parts < rounds / 5) parts = rounds / 5;
+  if (parts > rounds) parts = rounds;
+  const int each = (rounds + parts - 1) / parts;
+  a.parts = (rounds + each - 1) / each;
   const dim3 grid((uint32_t)(((int64_t)a.tokens * a.parts + kThreads / 64 - 1) / (kThreads / 64)));
   if (head_dim == 128) {
     if (dtype == CHUNKKV_F32) return launch_append<CHUNKKV_F32, 128>(a, grid, s);

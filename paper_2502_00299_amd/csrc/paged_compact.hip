@@ -6,7 +6,8 @@
 // then all threads copy K and V rows as 16-byte segments.
 // Bound by HBM over a stack (every row read and written once), by latency over a layer.  The full cache is read with streaming
 // loads: nobody needs it again.  Stores are streaming where what is written is more than half of the memory-side cache; below, the
-// next decoding step finds the pages there.  32 layers of 32768 tokens at 20 %: 316 us with both (5.5 TB/s), plain stores 340.
+// next decoding step finds the pages there.  32 layers of 32768 tokens at 20 %: 309 us (5.6 TB/s; at 80 rows per workgroup 316, and
+// with plain stores 340).
 // Grid: x = group of entries, y = (sequence, kv-head), z = layer.
 #include "paged.h"
 
@@ -119,7 +120,9 @@ __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArg
 
 int launch_paged_compact(int row_bytes, const PagedCompactArgs &args, int n_layers, int batch, hipStream_t s) {
   PagedCompactArgs a = args;
-  int n = 80 / a.chunk;
+  // About 40 rows per workgroup.  us for 20 / 40 / 80 / 160, from a graph: a layer of 8192 tokens at 10 % 4.7 / 4.6 / 5.5 / 8.3; 32 layers of it
+  // 47 / 40 / 40 / 43; 32 layers of 32768 at 20 % 334 / 301 / 307 / 333.
+  int n = 40 / a.chunk;
   a.entries = n < 1 ? 1 : (n > kCompactEntries ? kCompactEntries : n);
   int most = 0;
   for (int i = 0; i < batch; ++i) {

@@ -20,14 +20,14 @@
 
 namespace ckv {
 
-// HD: head dim, NST: K/V slot pairs of a wavefront, NW: wavefronts
-template <int HD, int NST, int NW, int W>
+// HD: head dim, NW: wavefronts
+template <int HD, int NW, int W>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(PagedDecodeArgs a) {
   constexpr int G = 16, ROWB = HD * 4, SEGS = ROWB / 16;   // bytes and 16-byte segments of a row
   constexpr int RPL = 1024 / ROWB, NLD = 16 / RPL;         // rows that one 1 KB load fills, loads of a slot
   constexpr int SLOT = 16 * ROWB;
   constexpr int NKS = HD / 16, NH = HD / 64;               // 64-byte pieces of a key, 64-dim pieces of the output
-  constexpr int RING = NW * NST * 2 * SLOT, AH = 8;        // AH: most heads of a workgroup that adds up weights
+  constexpr int RING = NW * 2 * SLOT, AH = 8;        // AH: most heads of a workgroup that adds up weights
   static_assert(RING >= NW * G * (HD + 2) * 4 + G * 4, "the states of the wavefronts take the ring's place");
   __shared__ __align__(16) char smem[RING + (W == kAdded ? AH * alone_rows(NW) * 4 : 0)];
 
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
     koff[j] = (uint32_t)row * tok + (uint32_t)((pos ^ row) * 16);
     voff[j] = (uint32_t)row * tok + (uint32_t)(pos * 16);
   }
-  const uint32_t ring = (uint32_t)(wave * (2 * NST * SLOT));
+  const uint32_t ks_ = (uint32_t)(wave * 2 * SLOT), vs_ = ks_ + SLOT;   // this wavefront's slots
   auto issue = [&](const void *base, const uint32_t *off, int step, uint32_t slot) __attribute__((always_inline)) {
     const int blk = wave + step * NW, at = blk & 63;
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)block_at, at), hi = (uint32_t)__builtin_amdgcn_readlane((int)(block_at >> 32), at);
@@ -86,8 +86,6 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
     for (int j = 0; j < NLD; ++j)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(smem + slot + j * 1024), 16, off[j], 0, 0, 2);
   };
-  auto kslot = [&](int s) { return ring + (uint32_t)((s % NST) * (2 * SLOT)); };
-  auto vslot = [&](int s) { return ring + (uint32_t)((s % NST) * (2 * SLOT) + SLOT); };
   uint32_t kaddr[NKS];
 #pragma unroll
   for (int ks = 0; ks < NKS; ++ks) kaddr[ks] = (uint32_t)(n * ROWB + (((4 * ks + q) ^ n) * 16));
@@ -98,21 +96,17 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
   const bool scored = n < heads;
   const uint32_t soff = ((uint32_t)n * spitch + (uint32_t)(r0 + 4 * q)) * 4u;
   float *lscores = (float *)(smem + RING);   // [AH][alone_rows(NW)]
-  // Accesses behind the slot that is waited for: loads of the other slots and, once every slot has been refilled, the store of
-  // each of NST steps.
-  constexpr int kLoads = (2 * NST - 1) * NLD, kBehind = kLoads + (W == kStored ? NST : 0);
+  // Accesses behind the slot that is waited for: the loads of the other one and, from the second step on, a store.
+  constexpr int kBehind = NLD + (W == kStored ? 1 : 0);
   static_assert(kBehind < 64, "vmcnt");
   auto wait = [&](int s) __attribute__((always_inline)) {
-    if (W == kStored && s < NST) __builtin_amdgcn_s_waitcnt(vm_imm(kLoads));
+    if (W == kStored && s == 0) __builtin_amdgcn_s_waitcnt(vm_imm(NLD));
     else __builtin_amdgcn_s_waitcnt(vm_imm(kBehind));
   };
 
   const float c1 = a.scale_log2e;
-#pragma unroll
-  for (int s = 0; s < NST; ++s) {
-    issue(a.k, koff, s, kslot(s));
-    issue(a.v, voff, s, vslot(s));
-  }
+  issue(a.k, koff, 0, ks_);
+  issue(a.v, voff, 0, vs_);
   float m = kPagedLowest, l = 0.f;   // m before the scale
   f32x4 acc[NH][4];
 #pragma unroll
@@ -122,7 +116,6 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
 
   for (int s = 0; s < nstep; ++s) {
     wait(s);
-    const uint32_t ks_ = kslot(s), vs_ = vslot(s);
     f32x4 kf[NKS], part[NKS];
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) kf[ks] = *(const f32x4 *)(smem + (ks_ + kaddr[ks]));
@@ -139,7 +132,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
     f32x4 sc = part[0];
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0xC07F);   // the fragments are in registers: the K slot is free
-    issue(a.k, koff, s + NST, ks_);
+    issue(a.k, koff, s + 1, ks_);
 
     const int key0 = (wave + s * NW) * 16;
     const int span = __builtin_amdgcn_readlane((int)block_span, wave + s * NW);   // below 64
@@ -193,7 +186,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
     }
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0xC07F);   // the V slot is free
-    issue(a.v, voff, s + NST, vs_);
+    issue(a.v, voff, s + 1, vs_);
   }
 
   l += __shfl_xor(l, 16);
@@ -234,13 +227,12 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
 
 template <int HD>
 int launch_hd(const PagedDecodeArgs &a, hipStream_t s) {
-  constexpr int NST = HD == 128 ? 1 : 2;
   const dim3 grid(a.first[a.batch], a.n_kv_heads * ((a.group + 15) / 16));
   auto go = [&](auto kern, int waves) { hipLaunchKernelGGL(kern, grid, dim3(waves * 64), 0, s, a); };
-  if (a.alone == 8) go(paged_f32_kernel<HD, NST, 8, kAdded>, 8);
-  else if (a.alone == 4) go(paged_f32_kernel<HD, NST, 4, kAdded>, 4);
-  else if (a.weight != nullptr) go(paged_f32_kernel<HD, NST, 4, kStored>, 4);
-  else go(paged_f32_kernel<HD, NST, 4, kDropped>, 4);
+  if (a.alone == 8) go(paged_f32_kernel<HD, 8, kAdded>, 8);
+  else if (a.alone == 4) go(paged_f32_kernel<HD, 4, kAdded>, 4);
+  else if (a.weight != nullptr) go(paged_f32_kernel<HD, 4, kStored>, 4);
+  else go(paged_f32_kernel<HD, 4, kDropped>, 4);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 int launch_paged_f32(int head_dim, const PagedDecodeArgs &a, hipStream_t s) {

@@ -8,6 +8,8 @@
 // i of its range (a range has at most 64), one load of 64 table entries; a step then takes two blocks' addresses out
 // of those registers by readlane, and each block has a buffer descriptor of its own, which covers exactly the rows that hold
 // tokens: slots past the last one, and blocks whose page is not there, read as zeros without touching memory.
+// A wavefront has one slot for K and one for V, each refilled as soon as it is read.  A second pair is slower, as it takes the place
+// of other workgroups: 131072 slots 95.8 us, 89.0 so (d = 64: 47.2, 46.4), 13171 slots 16.1 and 14.7.
 // Weights: kStored keeps the scaled logits (fp32, log2 units) for the launch that adds up what every slot received.  They go
 // out by buffer stores whose idle columns lie out of range, so every step has two and the waits can count them together with
 // the loads (both leave the counter in the order they were issued).
@@ -73,8 +75,8 @@ __device__ __forceinline__ void join_parts(f32x4 (&acc)[NSET][NMT]) {
     }
 }
 
-// DT: bf16 or fp16, HD: head dim, G: 4 or 8 query heads per workgroup, NST: K/V slot pairs of a wavefront, NW: wavefronts
-template <int DT, int HD, int G, int NST, int NW, int W>
+// DT: bf16 or fp16, HD: head dim, G: 4 or 8 query heads per workgroup, NW: wavefronts
+template <int DT, int HD, int G, int NW, int W>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(PagedDecodeArgs a) {
   constexpr int ROWB = HD * 2, SEGS = ROWB / 16;   // bytes and 16-byte segments of a row
   constexpr int RPL = 1024 / ROWB;                 // rows that one 1 KB load fills
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   constexpr int NKS = HD / 32, NMT = HD / 16;      // products of a 16-key score tile, 16-dim output tiles
   constexpr int NSET = G == 4 ? 1 : 2;             // products per output tile
   constexpr bool BF = DT == CHUNKKV_BF16;
-  constexpr int RING = NW * NST * 2 * SLOT;
+  constexpr int RING = NW * 2 * SLOT;
   static_assert(RING >= NW * G * (HD + 2) * 4 + G * 4, "the states of the wavefronts take the ring's place");
   __shared__ __align__(16) char smem[RING + (W == kAdded ? G * alone_rows(NW) * 4 : 0)];
 
@@ -139,7 +141,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
     koff[j] = (uint32_t)row * tok + (uint32_t)((pos ^ kswz(row)) * 16);
     voff[j] = (uint32_t)row * tok + (uint32_t)((pos ^ vswz(row)) * 16);
   }
-  const uint32_t ring = (uint32_t)(wave * (2 * NST * SLOT));
+  const uint32_t ks_ = (uint32_t)(wave * 2 * SLOT), vs_ = ks_ + SLOT;   // this wavefront's slots
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
   // Steps past the last one are issued too, through empty descriptors (their blocks have no rows): the number of loads in
   // flight is known at every wait.
@@ -155,8 +157,6 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(smem + slot + (t * NLB + j) * 1024), 16, off[j], 0, 0, 2);
     }
   };
-  auto kslot = [&](int s) { return ring + (uint32_t)((s % NST) * (2 * SLOT)); };
-  auto vslot = [&](int s) { return ring + (uint32_t)((s % NST) * (2 * SLOT) + SLOT); };
 
   // LDS addresses: K fragment of row 16 t + n, segment 4 ks + q; V piece of keys 16 t + 4 q + (n / 4), dims 16 mt + 4 (n % 4)
   uint32_t kaddr[NKS], vaddr[NMT];
@@ -183,21 +183,17 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
     }
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), srs, scored ? (int)(soff + (uint32_t)key * 4u) : -1, 0, 0);
   };
-  // Accesses behind the slot that is waited for: loads of the other slots and, once every slot has been refilled, the two
-  // stores of each of NST steps.
-  constexpr int kLoads = (2 * NST - 1) * NLD, kBehind = kLoads + (W == kStored ? 2 * NST : 0);
+  // Accesses behind the slot that is waited for: the loads of the other one and, from the second step on, two stores.
+  constexpr int kBehind = NLD + (W == kStored ? 2 : 0);
   static_assert(kBehind < 64, "vmcnt");
   auto wait = [&](int s) __attribute__((always_inline)) {
-    if (W == kStored && s < NST) __builtin_amdgcn_s_waitcnt(vm_imm(kLoads));
+    if (W == kStored && s == 0) __builtin_amdgcn_s_waitcnt(vm_imm(NLD));
     else __builtin_amdgcn_s_waitcnt(vm_imm(kBehind));
   };
 
   const float c1 = a.scale_log2e;
-#pragma unroll
-  for (int s = 0; s < NST; ++s) {
-    issue(a.k, koff, s, kslot(s));
-    issue(a.v, voff, s, vslot(s));
-  }
+  issue(a.k, koff, 0, ks_);
+  issue(a.v, voff, 0, vs_);
   float m = kPagedLowest, l = 0.f;   // m before the scale: a difference of scores is exact where it counts, however large they are
   f32x4 acc[NSET][NMT];
 #pragma unroll
@@ -207,7 +203,6 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
 
   for (int s = 0; s < nstep; ++s) {
     wait(s);
-    const uint32_t ks_ = kslot(s), vs_ = vslot(s);
     u32x4 kf[2][NKS];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -227,7 +222,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
     }
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0xC07F);   // the fragments are in registers: the K slot is free
-    issue(a.k, koff, s + NST, ks_);
+    issue(a.k, koff, s + 1, ks_);
 
     const int key0 = (wave + s * NW) * kStepKeys;
     const int span0 = __builtin_amdgcn_readlane((int)block_span, key0 / 16), span1 = __builtin_amdgcn_readlane((int)block_span, key0 / 16 + 1);   // key0 < 1024
@@ -284,7 +279,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
 #pragma unroll
         for (int st = 0; st < NSET; ++st) acc[st][m4 + i] = mma16<DT>(vf[i], pf[st], acc[st][m4 + i]);
     }
-    issue(a.v, voff, s + NST, vs_);
+    issue(a.v, voff, s + 1, vs_);
   }
 
   // ---- parts of a head -> its output (lanes n < G), lanes of a column -> its sum
@@ -325,13 +320,12 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
 
 template <int DT, int HD, int G>
 int launch_g(const PagedDecodeArgs &a, hipStream_t s) {
-  constexpr int NST = HD == 128 ? 1 : 2;
   const dim3 grid(a.first[a.batch], a.n_kv_heads * ((a.group + G - 1) / G));
   auto go = [&](auto kern, int waves) { hipLaunchKernelGGL(kern, grid, dim3(waves * 64), 0, s, a); };
-  if (a.alone == 8) go(paged_mfma_kernel<DT, HD, G, NST, 8, kAdded>, 8);
-  else if (a.alone == 4) go(paged_mfma_kernel<DT, HD, G, NST, 4, kAdded>, 4);
-  else if (a.weight != nullptr) go(paged_mfma_kernel<DT, HD, G, NST, 4, kStored>, 4);
-  else go(paged_mfma_kernel<DT, HD, G, NST, 4, kDropped>, 4);
+  if (a.alone == 8) go(paged_mfma_kernel<DT, HD, G, 8, kAdded>, 8);
+  else if (a.alone == 4) go(paged_mfma_kernel<DT, HD, G, 4, kAdded>, 4);
+  else if (a.weight != nullptr) go(paged_mfma_kernel<DT, HD, G, 4, kStored>, 4);
+  else go(paged_mfma_kernel<DT, HD, G, 4, kDropped>, 4);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 template <int DT, int HD>

@@ -5,10 +5,11 @@
 // slots that became free there.  Sources lie at or above the budget and destinations below it, so nothing that is read is
 // written and the moves have no order; only slots that move cost bytes of K and V.
 // Up to kFewMoves slots move in the selecting workgroup, more of them in a launch of their own, which has workgroups for 64
-// moves each and is bound by HBM.
-// The selection is bound by latency for few slots (849 of 8 heads 8.5 us with its one move) and by the instructions of one workgroup's
-// passes over a head for many (see kInLds and the launcher).  Up to 16384 slots a thread has its own in registers, read together
-// with the length, before it is known how many count; up to 32768 their keys are in LDS, beyond in the workspace.
+// moves each and is bound by HBM.  us, so and in a launch: 200 moves of 8 heads 14.3 / 16.3, of 256 heads 21.7 / 29.0; 400 moves 17.0 / 16.3 and
+// 31.5 / 34.5 (these and those at the launcher from a graph, with a copy that brings positions and weights back before every call).
+// The selection is bound by latency for few slots (849 of 8 heads 8.3 us with its one move) and by the instructions of one workgroup's
+// passes over a head for many.  Up to 8192 slots a thread has its own in registers, read together with the length, before it is
+// known how many count; up to 32768 their keys are in LDS, beyond in the workspace.
 // One pass of ranks gives both lists: slots on the wrong side of the budget, in ascending order, are the free ones, then the
 // ones that move, as many.
 #include "paged.h"
@@ -18,17 +19,17 @@ namespace ckv {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kFewMoves = 64;
+constexpr int kFewMoves = 256, kMovesPerGroup = 64;
 
-// Moves [i0, i0 + n) of a head's lists, one after the other for the threads of a workgroup.
+// All n moves of a head by one workgroup, a segment of K and of V per thread at a time; looking both places up once per move, behind a
+// barrier, is slower for so few of them (200 moves 17.3 us, 14.6 so).
 __device__ __forceinline__ void move_slots(const PagedEvictArgs &a, int layer, int b, int h, int64_t head, const int32_t *source, const int32_t *target, int n) {
-  const int segs = a.row_bytes / 16;
   char *kp = (char *)CKV_ARG(PagedEvictArgs, k_pages, layer), *vp = (char *)CKV_ARG(PagedEvictArgs, v_pages, layer);
   const int32_t *table = a.geom.table + (int64_t)b * a.geom.pitch;
   int32_t *pos = a.token_pos + head * a.slot_pitch;
   float *weight = a.token_weight + head * a.slot_pitch;
-  for (int u = threadIdx.x; u < n * segs; u += blockDim.x) {
-    const int i = u / segs, seg = u % segs, from = source[i], to = target[i];
+  for (int u = threadIdx.x; u < n << a.row_shift; u += blockDim.x) {
+    const int i = u >> a.row_shift, seg = u & ((1 << a.row_shift) - 1), from = source[i], to = target[i];
     const int64_t f = slot_offset(a.geom, table, h, from), t = slot_offset(a.geom, table, h, to);
     if (f >= 0 && t >= 0) {
       const u32x4 x = *(const u32x4 *)(kp + f + seg * 16), y = *(const u32x4 *)(vp + f + seg * 16);
@@ -145,8 +146,7 @@ __global__ __launch_bounds__(T) void paged_evict_kernel(PagedEvictArgs a) {
 // along, then all copy rows as 16-byte segments, four of K or V in flight per thread.  Streaming loads and, where the moves may be
 // more than half of the memory-side cache, streaming stores, as in the compaction: half of 53385 slots in 8 layers 79 us, plain 86.
 // Grid: x = group of moves, y = (sequence, kv-head), z = layer.
-constexpr int kMovesPerGroup = 64;
-template <int NSEG, bool STREAM>   // 16-byte segments per row; streaming stores
+template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void paged_move_kernel(PagedEvictArgs a) {
   const int bl = blockIdx.y / a.n_kv_heads, h = blockIdx.y % a.n_kv_heads, b = a.batch0 + bl, layer = blockIdx.z;
   const int64_t head = ((int64_t)layer * a.batch_total + b) * a.n_kv_heads + h;
@@ -154,12 +154,13 @@ __global__ __launch_bounds__(kThreads) void paged_move_kernel(PagedEvictArgs a) 
   const int i0 = blockIdx.x * kMovesPerGroup, all = *moves, n = all - i0 < kMovesPerGroup ? all - i0 : kMovesPerGroup;
   if (n <= 0) return;
   __shared__ int64_t s_from[kMovesPerGroup], s_to[kMovesPerGroup];
-  if ((int)threadIdx.x < n) {
-    const int to = moves[1 + i0 + threadIdx.x], from = moves[1 + all + i0 + threadIdx.x];
+  const int tid = threadIdx.x;
+  if (tid < n) {
+    const int to = moves[1 + i0 + tid], from = moves[1 + all + i0 + tid];
     const int32_t *table = a.geom.table + (int64_t)b * a.geom.pitch;
     const int64_t f = slot_offset(a.geom, table, h, from), t = slot_offset(a.geom, table, h, to);
-    s_from[threadIdx.x] = t >= 0 ? f : -1;
-    s_to[threadIdx.x] = t;
+    s_from[tid] = t >= 0 ? f : -1;
+    s_to[tid] = t;
     int32_t *pos = a.token_pos + head * a.slot_pitch;
     float *weight = a.token_weight + head * a.slot_pitch;
     pos[to] = pos[from];
@@ -167,13 +168,13 @@ __global__ __launch_bounds__(kThreads) void paged_move_kernel(PagedEvictArgs a) 
   }
   __syncthreads();
   char *kp = (char *)CKV_ARG(PagedEvictArgs, k_pages, layer), *vp = (char *)CKV_ARG(PagedEvictArgs, v_pages, layer);
-  const int half = n * NSEG, total = 2 * half;
-  for (int u0 = threadIdx.x; u0 < total; u0 += 4 * kThreads) {
+  const int half = n << a.row_shift, total = 2 * half;
+  for (int u0 = tid; u0 < total; u0 += 4 * kThreads) {
     u32x4 x[4];
     char *to[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int u = u0 + j * kThreads, uu = u >= half ? u - half : u, row = uu / NSEG, seg = uu % NSEG;
+      const int u = u0 + j * kThreads, uu = u >= half ? u - half : u, row = uu >> a.row_shift, seg = uu & ((1 << a.row_shift) - 1);
       to[j] = nullptr;
       if (u < total && s_from[row] >= 0) {
         char *pool = u >= half ? vp : kp;
@@ -192,18 +193,21 @@ __global__ __launch_bounds__(kThreads) void paged_move_kernel(PagedEvictArgs a) 
 
 bool paged_moves_apart(const PagedEvictArgs &a) { return a.pitch > kFewMoves; }
 
+// Threads and slots of each: the variant that a head of max_tokens just fits.  us for 8 heads / 512 heads: 500 slots, 512 x 1 7.7 / 15.1,
+// 256 x 2 7.9 / 15.5; 849, 512 x 2 8.2 / 21.0, 256 x 4 8.5 / 21.8, 1024 x 1 9.0 / 22.9; 2000, 512 x 4 9.2 / 22.2, 1024 x 2 9.6 / 23.0; 4000, 1024 x 4
+// 10.4 / 28.3, 1024 x 8 11.7 / 31.0; 8000, 1024 x 8 14.2 / 41.9, in LDS 16.3 / 41.7; 16000, 1024 x 16 21.5 / 73.8, in LDS 21.0 / 66.5; 30000, in LDS
+// 32.8 / 119.6, in the workspace 43.5 / 132.3.
 int launch_paged_evict(const PagedEvictArgs &args, int n_layers, int batch, int max_tokens, hipStream_t s) {
   PagedEvictArgs a = args;
   a.apart = paged_moves_apart(a);
   const dim3 grid(batch * a.n_kv_heads, n_layers);
   auto go = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, grid, dim3(threads), 0, s, a); };
   if (max_tokens <= 256) go(paged_evict_kernel<256, 1, kInRegisters>, 256);
-  else if (max_tokens <= 512) go(paged_evict_kernel<256, 2, kInRegisters>, 256);
-  else if (max_tokens <= 1024) go(paged_evict_kernel<256, 4, kInRegisters>, 256);
+  else if (max_tokens <= 512) go(paged_evict_kernel<512, 1, kInRegisters>, 512);
+  else if (max_tokens <= 1024) go(paged_evict_kernel<512, 2, kInRegisters>, 512);
   else if (max_tokens <= 2048) go(paged_evict_kernel<512, 4, kInRegisters>, 512);
   else if (max_tokens <= 4096) go(paged_evict_kernel<1024, 4, kInRegisters>, 1024);
   else if (max_tokens <= 8192) go(paged_evict_kernel<1024, 8, kInRegisters>, 1024);
-  else if (max_tokens <= 16384) go(paged_evict_kernel<1024, 16, kInRegisters>, 1024);
   else if (max_tokens <= kEvictLdsKeys) go(paged_evict_kernel<1024, 16, kInLds>, 1024);
   else go(paged_evict_kernel<1024, 16, kInMemory>, 1024);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
@@ -211,10 +215,8 @@ int launch_paged_evict(const PagedEvictArgs &args, int n_layers, int batch, int 
 
 int launch_paged_move(const PagedEvictArgs &a, int n_layers, int batch, hipStream_t s) {
   const dim3 grid((a.pitch + kMovesPerGroup - 1) / kMovesPerGroup, batch * a.n_kv_heads, n_layers);
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, a); };
-  if (a.row_bytes == 128) a.stream ? go(paged_move_kernel<8, true>) : go(paged_move_kernel<8, false>);
-  else if (a.row_bytes == 256) a.stream ? go(paged_move_kernel<16, true>) : go(paged_move_kernel<16, false>);
-  else a.stream ? go(paged_move_kernel<32, true>) : go(paged_move_kernel<32, false>);
+  if (a.stream) hipLaunchKernelGGL(paged_move_kernel<true>, grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL(paged_move_kernel<false>, grid, dim3(kThreads), 0, s, a);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 
