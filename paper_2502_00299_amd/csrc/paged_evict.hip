@@ -195,8 +195,8 @@ bool paged_moves_apart(const PagedEvictArgs &a) { return a.pitch > kFewMoves; }
 
 // Threads and slots of each: the variant that a head of max_tokens just fits.  us for 8 heads / 512 heads: 500 slots, 512 x 1 7.7 / 15.1,
 // 256 x 2 7.9 / 15.5; 849, 512 x 2 8.2 / 21.0, 256 x 4 8.5 / 21.8, 1024 x 1 9.0 / 22.9; 2000, 512 x 4 9.2 / 22.2, 1024 x 2 9.6 / 23.0; 4000, 1024 x 4
-// 10.4 / 28.3, 1024 x 8 11.7 / 31.0; 8000, 1024 x 8 14.2 / 41.9, in LDS 16.3 / 41.7; 16000, 1024 x 16 21.5 / 73.8, in LDS 21.0 / 66.5; 30000, in LDS
-// 32.8 / 119.6, in the workspace 43.5 / 132.3.
+// 10.4 / 28.3, 1024 x 8 11.7 / 31.0; 8000, 1024 x 8 14.2 / 41.9, in LDS 16.3 / 41.7; 16000, 1024 x 16 21.5 / 73.8, in LDS 21.0 / 66.5 (where half of the
+// slots leave, the registers are 3 % faster); 30000, in LDS 32.8 / 119.6, in the workspace 43.5 / 132.3.
 int launch_paged_evict(const PagedEvictArgs &args, int n_layers, int batch, int max_tokens, hipStream_t s) {
   PagedEvictArgs a = args;
   a.apart = paged_moves_apart(a);
