@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
           sx[j][i] = kPagedLowest;
-          if (j0 + j < a.group && t + i * kThreads < len) sx[j][i] = scores[(int64_t)(j0 + j) * pitch + t + i * kThreads];
+          if (j0 + j < a.group && t + i * kThreads < len) sx[j][i] = __builtin_nontemporal_load(scores + (int64_t)(j0 + j) * pitch + t + i * kThreads);   // for the last time
         }
     };
     load(0);

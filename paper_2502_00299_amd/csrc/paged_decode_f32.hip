@@ -140,11 +140,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
 #pragma unroll
       for (int i = 0; i < 4; ++i) sc[i] = span != 0 && key0 + 4 * q + i < len ? sc[i] : -__builtin_inff();   // times any scale
     }
-    if constexpr (W == kStored) {
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sc * c1), srs, scored ? (int)(soff + (uint32_t)key0 * 4u) : -1, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-    } else if constexpr (W == kAdded) {
+    if constexpr (W == kAdded) {
       if (scored) *(f32x4 *)(lscores + n * alone_rows(NW) + key0 + 4 * q) = sc * c1;
     }
     float p[4];
@@ -187,6 +183,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0xC07F);   // the V slot is free
     issue(a.v, voff, s + 1, vs_);
+    if constexpr (W == kStored) {   // last, so that no wait for rows is one for a store of the same step
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sc * c1), srs, scored ? (int)(soff + (uint32_t)key0 * 4u) : -1, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
   l += __shfl_xor(l, 16);

@@ -11,8 +11,8 @@
 // A wavefront has one slot for K and one for V, each refilled as soon as it is read.  A second pair is slower, as it takes the place
 // of other workgroups: 131072 slots 95.8 us, 89.0 so (d = 64: 47.2, 46.4), 13171 slots 16.1 and 14.7.
 // Weights: kStored keeps the scaled logits (fp32, log2 units) for the launch that adds up what every slot received.  They go
-// out by buffer stores whose idle columns lie out of range, so every step has two and the waits can count them together with
-// the loads (both leave the counter in the order they were issued).
+// out by a buffer store whose idle columns lie out of range, so every step has one and the waits can count them together with
+// the loads (both leave the counter in the order they were issued).  17 MB of them beside 537 MB of K and V cost 10 us.
 // kAdded keeps them in LDS: a head that is one range knows its log-sum-exps in the end and adds its own weights, and nothing
 // follows.  It has four wavefronts or eight (paged_alone says when); eight for ranges that are joined are slower, with as many rows in
 // flight: 13171 slots 16.2 us, four 15.2.
@@ -169,22 +169,23 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   }
   static_assert(SEGS == 16 || SEGS == 8, "rows 16 apart share the swizzle");
 
-  // where this lane's scores go: slots 4 q .. of head n of the workgroup's; out of range for the columns past the heads
+  // where this lane's scores go: slots 4 q .. of a step's first block from the columns of the first part, of its second block from
+  // those of the second, which hold the same products; out of range for the other columns
   const uint32_t spitch = W == kStored ? ((uint32_t)CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31u) & ~31u : 0u;
   const int sheads = g - j0 < G ? g - j0 : G;
   const __amdgpu_buffer_rsrc_t srs = __builtin_amdgcn_make_buffer_rsrc(W == kStored ? (void *)head_scores(a, bl, h * g + j0) : nullptr, 0, (int)((uint32_t)sheads * spitch * 4u), 0x00020000);
-  const bool scored = n < sheads;
-  const uint32_t soff = ((uint32_t)n * spitch + (uint32_t)(r0 + 4 * q)) * 4u;
+  const bool scored = head < sheads && part < 2;
+  const uint32_t soff = ((uint32_t)head * spitch + (uint32_t)(r0 + 16 * part + 4 * q)) * 4u;
   float *lscores = (float *)(smem + RING);   // [G][alone_rows(NW)]
   auto keep = [&](int key, const f32x4 &x) __attribute__((always_inline)) {
     if constexpr (W == kAdded) {
-      if (scored) *(f32x4 *)(lscores + n * alone_rows(NW) + key + 4 * q) = x;
+      if (scored) *(f32x4 *)(lscores + head * alone_rows(NW) + key + 16 * part + 4 * q) = x;
       return;
     }
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), srs, scored ? (int)(soff + (uint32_t)key * 4u) : -1, 0, 0);
   };
-  // Accesses behind the slot that is waited for: the loads of the other one and, from the second step on, two stores.
-  constexpr int kBehind = NLD + (W == kStored ? 2 : 0);
+  // Accesses behind the slot that is waited for: the loads of the other one and, from the second step on, a store.
+  constexpr int kBehind = NLD + (W == kStored ? 1 : 0);
   static_assert(kBehind < 64, "vmcnt");
   auto wait = [&](int s) __attribute__((always_inline)) {
     if (W == kStored && s == 0) __builtin_amdgcn_s_waitcnt(vm_imm(NLD));
@@ -232,12 +233,6 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
 #pragma unroll
         for (int i = 0; i < 4; ++i) sc[t][i] = (t == 0 ? span0 : span1) != 0 && key0 + 16 * t + 4 * q + i < len ? sc[t][i] : -__builtin_inff();   // times any scale
     }
-    if constexpr (W != kDropped) {
-      __builtin_amdgcn_sched_barrier(0);
-      keep(key0, sc[0] * c1);
-      keep(key0 + 16, sc[1] * c1);
-      __builtin_amdgcn_sched_barrier(0);
-    }
     float p[8];
     auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -280,6 +275,14 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
         for (int st = 0; st < NSET; ++st) acc[st][m4 + i] = mma16<DT>(vf[i], pf[st], acc[st][m4 + i]);
     }
     issue(a.v, voff, s + 1, vs_);
+    if constexpr (W != kDropped) {   // last, so that no wait for rows is one for a store of the same step
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (part == 0 ? sc[0][i] : sc[1][i]) * c1;
+      keep(key0, x);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
   // ---- parts of a head -> its output (lanes n < G), lanes of a column -> its sum
