@@ -366,8 +366,8 @@ int chunkkv_paged_decode_attention(const chunkkv_pages *pages, const int32_t *pa
                                    float *token_weight, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Eviction by accumulated attention weight, in place: of a (layer, sequence, kv-head) with n > budget_b slots the
- * budget_b first ones stay in the order (protected first, weight descending, slot ascending); protected are the tokens
- * of the `recent` newest positions, position > max position - recent.  Kept slots below budget_b stay where they are; the
+ * budget_b first ones stay in the order (protected ones by slot, then the others by weight descending and slot); protected are
+ * the tokens of the `recent` newest positions, position > max position - recent.  Kept slots below budget_b stay where they are; the
  * others move, in ascending order, into the slots below budget_b that became free, in ascending order: rows, positions
  * and weights of a moved slot are copied, everything else stays as it was, and kv_len becomes budget_b.  A head of
  * budget_b slots or fewer is left alone.  Weights must not be NaN; -0 counts as +0.

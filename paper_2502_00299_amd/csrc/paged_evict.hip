@@ -1,6 +1,6 @@
 // Eviction by accumulated attention weight, in place.
 //
-// A workgroup selects for one (layer, sequence, kv-head): the budget_b-th slot in the order (protected, weight, slot) is
+// A workgroup selects for one (layer, sequence, kv-head): the budget_b-th slot in the order (protected by slot, weight, slot) is
 // found as chunks are selected (select.h, chunks of one token).  Kept slots below the budget stay; the others move into the
 // slots that became free there.  Sources lie at or above the budget and destinations below it, so nothing that is read is
 // written and the moves have no order; only slots that move cost bytes of K and V.
