@@ -103,6 +103,7 @@ struct PagedDecodeArgs {
   float *part_o;                        // [range][Hq][d]
   float *scores;                        // scaled logits in log2 units: first_row * Hq numbers of the sequences before, then [Hq][rows_b]
   int32_t batch0, batch, n_q_heads, n_kv_heads, group, slot_pitch;
+  int32_t heads;                        // query heads of a kv-head that a workgroup serves: 4, 8 or 16
   float scale_log2e;
   int32_t direct;                       // 1: every head is one range, the range kernel writes the outputs
   int32_t alone;                        // its wavefronts if it adds up the weights as well, and no launch follows; 0
@@ -211,7 +212,6 @@ int launch_paged_compact(int row_bytes, const PagedCompactArgs &a, int n_layers,
 int launch_paged_decode(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s);
 int launch_paged_mfma(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s);   // 16-bit rows
 int launch_paged_f32(int head_dim, const PagedDecodeArgs &a, hipStream_t s);
-int paged_decode_heads(int dtype, int group);   // query heads of a kv-head that a workgroup serves
 int launch_paged_evict(const PagedEvictArgs &a, int n_layers, int batch, int max_tokens, hipStream_t s);
 bool paged_moves_apart(const PagedEvictArgs &a);   // are there moves enough for a launch of their own
 int launch_paged_move(const PagedEvictArgs &a, int n_layers, int batch, hipStream_t s);

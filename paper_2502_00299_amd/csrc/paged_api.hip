@@ -74,8 +74,22 @@ int paged_alone(const chunkkv_pages *p, int nb, int most, bool weights) {   // -
   if (!weights || p->n_q_heads / p->n_kv_heads > 8 || most > alone_rows(8) || (heads < kPagedAloneHeads && most > short_rows(p))) return 0;
   return most <= kPagedFourRows || (heads >= kPagedFourHeads && most <= alone_rows(4)) ? 4 : 8;
 }
+// Query heads of one kv-head that a workgroup serves.  16-bit rows: 4 or 8; 5 to 7 are one padded batch of 8, not two passes over
+// K and V: 5 heads of each of 4 kv-heads 131072 slots 47.5 us, in two passes 85.9, 13171 slots 11.6 and 12.2, 848 slots 8.5 and 8.4.  More than
+// 8: one batch of 16 from 20 MB of K and V on, where reading them again is what costs; below, more workgroups are faster.  us of 16
+// and of 8 at a time: 16 heads of each of 8 kv-heads 60000 slots 46.3 / 84.0, 16 sequences of 3000 40.5 / 67.6, 13171 slots 17.2 / 17.2, 900 slots 10.4 / 9.4; 12 of
+// 4 60000 slots 26.7 / 43.2; 9 of one 60000 slots (31 MB) 15.7 / 17.3, 13171 (7 MB) 11.4 / 11.5; 16 of 2 13171 slots (13 MB) 12.7 / 12.2.  fp32: 16.
+constexpr int64_t kPagedWideBytes = 20 << 20;
+int heads_at_once(const chunkkv_pages *p, int b0, int nb) {
+  const int g = p->n_q_heads / p->n_kv_heads;
+  if (p->dtype == CHUNKKV_F32) return 16;
+  if (g <= 8) return g > 4 ? 8 : 4;
+  int64_t rows = 0;
+  for (int b = b0; b < b0 + nb; ++b) rows += p->max_tokens[b];
+  return 2 * rows * p->n_kv_heads * p->head_dim * elem_bytes(p->dtype) >= kPagedWideBytes ? 16 : 8;
+}
 int range_rows(const chunkkv_pages *p, int b0, int nb, bool weights) {
-  const int g = p->n_q_heads / p->n_kv_heads, G = paged_decode_heads(p->dtype, g);
+  const int g = p->n_q_heads / p->n_kv_heads, G = heads_at_once(p, b0, nb);
   const int64_t per_range = (int64_t)p->n_kv_heads * ((g + G - 1) / G);   // workgroups
   int64_t rows = 0;
   int most = 1;
@@ -314,7 +328,7 @@ int chunkkv_paged_decode_attention(const chunkkv_pages *pages, const int32_t *pa
     a.part_o = (float *)((char *)workspace + pl.off_o);
     a.scores = (float *)((char *)workspace + pl.off_scores);
     a.batch0 = b0; a.batch = nb; a.n_q_heads = pages->n_q_heads; a.n_kv_heads = pages->n_kv_heads;
-    a.group = pages->n_q_heads / pages->n_kv_heads; a.slot_pitch = pages->slot_pitch;
+    a.group = pages->n_q_heads / pages->n_kv_heads; a.slot_pitch = pages->slot_pitch; a.heads = heads_at_once(pages, b0, nb);
     // a scale that vanishes in fp32 gives all slots the same weight; kept above zero, which minus infinity cannot be multiplied by
     a.scale_log2e = scale * 1.4426950408889634f > FLT_MIN ? scale * 1.4426950408889634f : FLT_MIN;
     const int r = range_rows(pages, b0, nb, token_weight != nullptr);

@@ -131,13 +131,6 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
   }
 }
 
-// Query heads of one kv-head that a workgroup serves.  16-bit rows: 4 or 8; 5 to 7 are one padded batch of 8, not two passes over
-// K and V: 5 heads of each of 4 kv-heads 131072 slots 47.5 us, in two passes 85.9, 13171 slots 11.6 and 12.2, 848 slots 8.5 and 8.4.  fp32: 16.
-int paged_decode_heads(int dtype, int group) {
-  if (dtype == CHUNKKV_F32) return 16;
-  return group > 4 ? 8 : 4;
-}
-
 template <int HD>
 int launch_finish(const PagedDecodeArgs &a, hipStream_t s) {
   const int joins = a.direct ? 0 : a.batch * a.n_q_heads, ranges = a.first[a.batch];

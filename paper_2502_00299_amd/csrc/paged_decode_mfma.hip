@@ -3,6 +3,7 @@
 // Bound by HBM bandwidth for long caches: every K and V row is read once.  Layout of the two contractions, weights as
 // sums of 16-bit parts and the lazy reference of the online softmax are those of decode_mfma.hip, which says why; what
 // differs is where rows come from and what else is kept.
+// (16 heads fill the columns: each part is a product of its own, three for bf16 and four for fp16.)
 //
 // Rows: a step of 32 slots is two blocks of 16, and a block never crosses pages.  Lane i of every wavefront looks up block
 // i of its range (a range has at most 64), one load of 64 table entries; a step then takes two blocks' addresses out
@@ -35,7 +36,8 @@ __device__ __forceinline__ void weight_parts(const float (&p)[8], int part, u32x
         const float p1 = p0 - __uint_as_float(__float_as_uint(p0) & 0xFFFF0000u);
         const float p2 = p1 - __uint_as_float(__float_as_uint(p1) & 0xFFFF0000u);
         if constexpr (G == 4) x[e][0] = part == 0 ? p0 : (part == 1 ? p1 : p2);
-        else { x[e][0] = part == 0 ? p0 : p1; x[e][1] = p2; }
+        else if constexpr (G == 8) { x[e][0] = part == 0 ? p0 : p1; x[e][1] = p2; }
+        else { x[e][0] = p0; x[e][1] = p1; x[e][2] = p2; }
       }
 #pragma unroll
       for (int st = 0; st < NSET; ++st)   // upper halves: the truncation
@@ -51,7 +53,8 @@ __device__ __forceinline__ void weight_parts(const float (&p)[8], int part, u32x
       const fp16x2 h3 = __builtin_amdgcn_cvt_pkrtz(a3, b3);
       const uint32_t w0 = __builtin_bit_cast(uint32_t, h0), w1 = __builtin_bit_cast(uint32_t, h1), w2 = __builtin_bit_cast(uint32_t, h2), w3 = __builtin_bit_cast(uint32_t, h3);
       if constexpr (G == 4) pf[0][i2] = part < 2 ? (part == 0 ? w0 : w1) : (part == 2 ? w2 : w3);
-      else { pf[0][i2] = part == 0 ? w0 : w1; pf[1][i2] = part == 0 ? w2 : w3; }
+      else if constexpr (G == 8) { pf[0][i2] = part == 0 ? w0 : w1; pf[1][i2] = part == 0 ? w2 : w3; }
+      else { pf[0][i2] = w0; pf[1][i2] = w1; pf[2][i2] = w2; pf[3][i2] = w3; }
     }
   }
 }
@@ -68,6 +71,10 @@ __device__ __forceinline__ void join_parts(f32x4 (&acc)[NSET][NMT]) {
       if constexpr (G == 4) {
         const float rest = BF ? row_shl<8>(x) : row_shl<8>(x) * kS2 + row_shl<12>(x) * kS3;
         acc[0][mt][i] = x * kS0 + (row_shl<4>(x) * kS1 + rest);
+      } else if constexpr (G == 16) {
+        float rest = acc[2][mt][i] * kS2;
+        if constexpr (!BF) rest += acc[3][mt][i] * kS3;
+        acc[0][mt][i] = x * kS0 + (acc[1][mt][i] * kS1 + rest);
       } else {
         const float y = acc[1][mt][i], rest = BF ? y : y * kS2 + row_shl<8>(y) * kS3;
         acc[0][mt][i] = x * kS0 + (row_shl<8>(x) * kS1 + rest);
@@ -75,7 +82,7 @@ __device__ __forceinline__ void join_parts(f32x4 (&acc)[NSET][NMT]) {
     }
 }
 
-// DT: bf16 or fp16, HD: head dim, G: 4 or 8 query heads per workgroup, NW: wavefronts
+// DT: bf16 or fp16, HD: head dim, G: 4, 8 or 16 query heads per workgroup, NW: wavefronts
 template <int DT, int HD, int G, int NW, int W>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(PagedDecodeArgs a) {
   constexpr int ROWB = HD * 2, SEGS = ROWB / 16;   // bytes and 16-byte segments of a row
@@ -83,8 +90,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   constexpr int NLB = 16 / RPL, NLD = 2 * NLB;     // loads of a block, of a slot
   constexpr int SLOT = kStepKeys * ROWB;
   constexpr int NKS = HD / 32, NMT = HD / 16;      // products of a 16-key score tile, 16-dim output tiles
-  constexpr int NSET = G == 4 ? 1 : 2;             // products per output tile
   constexpr bool BF = DT == CHUNKKV_BF16;
+  constexpr int NSET = G == 4 ? 1 : (G == 8 ? 2 : (BF ? 3 : 4));   // products per output tile
   constexpr int RING = NW * 2 * SLOT;
   static_assert(RING >= NW * G * (HD + 2) * 4 + G * 4, "the states of the wavefronts take the ring's place");
   __shared__ __align__(16) char smem[RING + (W == kAdded ? G * alone_rows(NW) * 4 : 0)];
@@ -170,7 +177,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   static_assert(SEGS == 16 || SEGS == 8, "rows 16 apart share the swizzle");
 
   // where this lane's scores go: slots 4 q .. of a step's first block from the columns of the first part, of its second block from
-  // those of the second, which hold the same products; out of range for the other columns
+  // those of the second, which hold the same products (16 heads have no second: two stores); out of range for the other columns
   const uint32_t spitch = W == kStored ? ((uint32_t)CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31u) & ~31u : 0u;
   const int sheads = g - j0 < G ? g - j0 : G;
   const __amdgpu_buffer_rsrc_t srs = __builtin_amdgcn_make_buffer_rsrc(W == kStored ? (void *)head_scores(a, bl, h * g + j0) : nullptr, 0, (int)((uint32_t)sheads * spitch * 4u), 0x00020000);
@@ -184,8 +191,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
     }
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), srs, scored ? (int)(soff + (uint32_t)key * 4u) : -1, 0, 0);
   };
-  // Accesses behind the slot that is waited for: the loads of the other one and, from the second step on, a store.
-  constexpr int kBehind = NLD + (W == kStored ? 1 : 0);
+  // Accesses behind the slot that is waited for: the loads of the other one and, from the second step on, the stores of a step.
+  constexpr int kStores = G == 16 ? 2 : 1, kBehind = NLD + (W == kStored ? kStores : 0);
   static_assert(kBehind < 64, "vmcnt");
   auto wait = [&](int s) __attribute__((always_inline)) {
     if (W == kStored && s == 0) __builtin_amdgcn_s_waitcnt(vm_imm(NLD));
@@ -281,6 +288,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = (part == 0 ? sc[0][i] : sc[1][i]) * c1;
       keep(key0, x);
+      if constexpr (G == 16) keep(key0 + 16, sc[1] * c1);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -325,15 +333,18 @@ template <int DT, int HD, int G>
 int launch_g(const PagedDecodeArgs &a, hipStream_t s) {
   const dim3 grid(a.first[a.batch], a.n_kv_heads * ((a.group + G - 1) / G));
   auto go = [&](auto kern, int waves) { hipLaunchKernelGGL(kern, grid, dim3(waves * 64), 0, s, a); };
-  if (a.alone == 8) go(paged_mfma_kernel<DT, HD, G, 8, kAdded>, 8);
-  else if (a.alone == 4) go(paged_mfma_kernel<DT, HD, G, 4, kAdded>, 4);
-  else if (a.weight != nullptr) go(paged_mfma_kernel<DT, HD, G, 4, kStored>, 4);
+  if constexpr (G <= 8) {   // no more heads than that are alone
+    if (a.alone == 8) go(paged_mfma_kernel<DT, HD, G, 8, kAdded>, 8);
+    if (a.alone == 4) go(paged_mfma_kernel<DT, HD, G, 4, kAdded>, 4);
+    if (a.alone) return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
+  }
+  if (a.weight != nullptr) go(paged_mfma_kernel<DT, HD, G, 4, kStored>, 4);
   else go(paged_mfma_kernel<DT, HD, G, 4, kDropped>, 4);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
 template <int DT, int HD>
 int launch_16(const PagedDecodeArgs &a, hipStream_t s) {
-  return paged_decode_heads(DT, a.group) == 4 ? launch_g<DT, HD, 4>(a, s) : launch_g<DT, HD, 8>(a, s);
+  return a.heads == 4 ? launch_g<DT, HD, 4>(a, s) : (a.heads == 8 ? launch_g<DT, HD, 8>(a, s) : launch_g<DT, HD, 16>(a, s));
 }
 int launch_paged_mfma(int dtype, int head_dim, const PagedDecodeArgs &a, hipStream_t s) {
   if (dtype == CHUNKKV_BF16) return head_dim == 128 ? launch_16<CHUNKKV_BF16, 128>(a, s) : launch_16<CHUNKKV_BF16, 64>(a, s);

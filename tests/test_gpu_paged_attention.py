@@ -99,6 +99,17 @@ def test_around_one_workgroup_per_head(lib, dtype, hq, hkv, d):
         check(cache, torch.randn((batch, hq, d), generator=gen).to(H.KIND[dtype]), cache.len[0].tolist())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("hq,hkv,d,room", [(16, 1, 128, [45000, 300]), (12, 1, 64, [79000, 1, 4000]), (40, 2, 128, [20600, 0, 33]), (9, 1, 64, [90000])])
+@pytest.mark.parametrize("weights", [False, True])
+def test_sixteen_heads_at_once(lib, dtype, hq, hkv, d, room, weights):
+    """More than eight heads of a kv-head over 20 MB of K and V: one pass over them, in batches of 16."""
+    gen = torch.Generator().manual_seed(hq + d)
+    cache = H.Cache(gen, dtype, hq, hkv, d, 256, room, [max(0, n - 5) for n in room])
+    cache.table[0, 7] = -1
+    check(cache, torch.randn((len(room), hq, d), generator=gen).to(H.KIND[dtype]), cache.len[0].tolist(), with_weights=weights)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_many_sequences(lib, dtype):
     """More than a launch's tables hold, most of them short, some empty."""
