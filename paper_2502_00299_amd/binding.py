@@ -118,8 +118,13 @@ class Problem(_KeepsStruct):
         if kept is None or kept[0] != now:
             cp = self.as_c()
             plain = tuple(tuple(map(int, x)) if isinstance(x, tuple) else float(x) if isinstance(x, float) else int(x) for x in now)
-            kept = self._kept = (plain, cp, C.byref(cp))
+            kept = self._kept = (plain, cp, C.byref(cp), self._kv_elements())
         return kept[2]
+
+    def _kv_elements(self) -> int:
+        """Elements from the start of a cache to the end of its last row."""
+        return (max(int(base) + (int(rows) - 1) * int(self.kv_stride_tok) for base, rows in zip(self.kv_base, self.seqlen))
+                + (int(self.n_kv_heads) - 1) * int(self.kv_stride_head) + int(self.head_dim))
 
     def __getstate__(self):
         return self.__dict__.copy()   # the kept struct is neither copied nor pickled
@@ -294,10 +299,10 @@ def _bytes(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.nbytes
 
 
-def _stream(stream):
+def _stream(stream, dev: Optional[int] = None):
     if stream is None:
         # the handle itself: building a torch.cuda.Stream object around it takes 2.7 us
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev is None else dev)
     return stream.cuda_stream
 
 
@@ -454,6 +459,8 @@ def chunkkv_decode_attention_static(prob: Problem, compacted: bool, kv_len, q, k
 # and 0.1 us a pool of a list.
 _KINDS = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}
 _I32, _F32 = torch.int32, torch.float32
+# torch.cuda.current_device() without its look at whether the runtime has been started (0.5 us): a call's tensors have done that
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _get_device, _data_ptr, _is_contiguous, _nbytes = torch.Tensor.get_device, torch.Tensor.data_ptr, torch.Tensor.is_contiguous, attrgetter("nbytes")
 
 
@@ -534,7 +541,7 @@ def _ints(xs: Sequence[int]):
 
 def chunkkv_paged_compact(prob: Problem, pages: Pages, reuse: int, k: Sequence, v: Sequence, sel_chunk, sel_len, sel_count, token_importance,
                           page_table, k_pages: Sequence, v_pages: Sequence, kv_len, token_pos, token_weight, stream=None) -> None:
-    where, n, dev = "chunkkv_paged_compact", len(k), torch.cuda.current_device()
+    where, n, dev = "chunkkv_paged_compact", len(k), _device()
     heads, groups, cp = pages.batch * pages.n_kv_heads, -(-n // max(1, reuse)), pages._c()
     if not len(v) == len(k_pages) == len(v_pages) == n or (token_importance is not None and len(token_importance) != groups):
         raise ValueError(f"{where}: lists of {n}, {len(v)}, {len(k_pages)} and {len(v_pages)} layers")
@@ -544,18 +551,18 @@ def chunkkv_paged_compact(prob: Problem, pages: Pages, reuse: int, k: Sequence, 
         ("page_table", page_table, _I32, pages.batch * pages.table_pitch), ("kv_len", kv_len, _I32, n * heads), ("token_pos", token_pos, _I32, slots),
         ("token_weight", token_weight, _F32, slots))
     given = None if token_importance is None else _pools(where, dev, "token_importance", token_importance, _F32, heads * prob.score_cap * prob.chunk)
-    reach = (max(base + (int(rows) - 1) * prob.kv_stride_tok for base, rows in zip(prob.kv_base, prob.seqlen))
-             + (prob.n_kv_heads - 1) * prob.kv_stride_head + prob.head_dim)
+    full = prob._c()
+    reach = prob._kept[3]   # of the struct just returned
     ks, vs = _pools(where, dev, "k", k, kind, reach), _pools(where, dev, "v", v, kind, reach)
     kp, vp = _pools(where, dev, "k_pages", k_pages, kind, room), _pools(where, dev, "v_pages", v_pages, kind, room)
-    _check(load_library().chunkkv_paged_compact(prob._c(), cp, n, reuse, _at(ks), _at(vs), chunks, lens, count, _at(given), table, _at(kp), _at(vp), length,
-                                                pos, weight, _stream(stream)), where)
+    _check(load_library().chunkkv_paged_compact(full, cp, n, reuse, _at(ks), _at(vs), chunks, lens, count, _at(given), table, _at(kp), _at(vp), length,
+                                                pos, weight, _stream(stream, dev)), where)
 
 
 def chunkkv_paged_append(pages: Pages, n_new: Sequence[int], q, k, v, positions, q_norm, k_norm, eps: float, inv_freq, interleaved: bool, q_out,
                          page_table, k_pages, v_pages, kv_len, kv_len_out, token_pos, token_weight, stream=None) -> None:
     """q, k, v: [tokens][heads][head_dim], views of a fused projection among them; rotary_dim is twice inv_freq's length."""
-    where, dev, kind = "chunkkv_paged_append", torch.cuda.current_device(), _KINDS.get(pages.dtype)
+    where, dev, kind = "chunkkv_paged_append", _device(), _KINDS.get(pages.dtype)
     batch, hkv, d, cp = pages.batch, pages.n_kv_heads, pages.head_dim, pages._c()
     numbers, new = _ints(n_new)
     if len(numbers) != batch:
@@ -572,7 +579,7 @@ def chunkkv_paged_append(pages: Pages, n_new: Sequence[int], q, k, v, positions,
     _check(load_library().chunkkv_paged_append(
         cp, new, None if q is None else q.data_ptr(), q_tok, k.data_ptr(), k_tok, v.data_ptr(), v_tok, at, qn, kn, eps, freq,
         0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, out, table, _pool(where, dev, "k_pages", k_pages, kind, room),
-        _pool(where, dev, "v_pages", v_pages, kind, room), length, after, pos, weight, _stream(stream)), where)
+        _pool(where, dev, "v_pages", v_pages, kind, room), length, after, pos, weight, _stream(stream, dev)), where)
 
 
 def chunkkv_paged_decode_workspace_bytes(pages: Pages, with_weights: bool = False) -> int:
@@ -580,7 +587,7 @@ def chunkkv_paged_decode_workspace_bytes(pages: Pages, with_weights: bool = Fals
 
 
 def chunkkv_paged_decode_attention(pages: Pages, page_table, kv_len, q, k_pages, v_pages, out, lse, token_weight, workspace, stream=None) -> None:
-    where, dev, kind = "chunkkv_paged_decode_attention", torch.cuda.current_device(), _KINDS.get(pages.dtype)
+    where, dev, kind = "chunkkv_paged_decode_attention", _device(), _KINDS.get(pages.dtype)
     cp, batch = pages._c(), pages.batch
     rows, heads, room = batch * pages.n_q_heads, batch * pages.n_kv_heads, pages._pool_elements()
     table, length, qp, op, lp, weight = _arrays(
@@ -588,7 +595,7 @@ def chunkkv_paged_decode_attention(pages: Pages, page_table, kv_len, q, k_pages,
         ("out", out, _F32, rows * pages.head_dim), ("lse", lse, _F32, rows), ("token_weight", token_weight, _F32, heads * pages.slot_pitch))
     _check(load_library().chunkkv_paged_decode_attention(
         cp, table, length, qp, _pool(where, dev, "k_pages", k_pages, kind, room), _pool(where, dev, "v_pages", v_pages, kind, room), op, lp, weight,
-        *_scratch(where, dev, workspace), _stream(stream)), where)
+        *_scratch(where, dev, workspace), _stream(stream, dev)), where)
 
 
 def _budgets(where: str, pages: Pages, budget: Sequence[int]):
@@ -604,7 +611,7 @@ def chunkkv_paged_evict_workspace_bytes(pages: Pages, n_layers: int, budget: Seq
 
 def chunkkv_paged_evict(pages: Pages, budget: Sequence[int], recent: int, page_table, k_pages: Sequence, v_pages: Sequence, kv_len, token_pos,
                         token_weight, workspace, stream=None) -> None:
-    where, n, dev, kind = "chunkkv_paged_evict", len(k_pages), torch.cuda.current_device(), _KINDS.get(pages.dtype)
+    where, n, dev, kind = "chunkkv_paged_evict", len(k_pages), _device(), _KINDS.get(pages.dtype)
     if len(v_pages) != n:
         raise ValueError(f"{where}: lists of {n} and {len(v_pages)} layers")
     cp, heads = pages._c(), n * pages.batch * pages.n_kv_heads
@@ -613,7 +620,7 @@ def chunkkv_paged_evict(pages: Pages, budget: Sequence[int], recent: int, page_t
                                          ("token_pos", token_pos, _I32, slots), ("token_weight", token_weight, _F32, slots))
     kp, vp = _pools(where, dev, "k_pages", k_pages, kind, room), _pools(where, dev, "v_pages", v_pages, kind, room)
     _check(load_library().chunkkv_paged_evict(cp, n, _budgets(where, pages, budget), recent, table, _at(kp), _at(vp), length, pos, weight,
-                                              *_scratch(where, dev, workspace), _stream(stream)), where)
+                                              *_scratch(where, dev, workspace), _stream(stream, dev)), where)
 
 
 def chunkkv_timing_begin(max_records: int = 4096) -> None:
