@@ -99,7 +99,7 @@ struct PagedDecodeArgs {
   const void *q, *k, *v;
   float *out, *lse, *weight;
   const int32_t *kv_len;
-  float2 *part_ml;                      // (max in log2 units, sum) of every range and query head: [range][Hq]
+  float2 *part_ml;                      // (reference before the scale, sum) of every range and query head: [range][Hq]
   float *part_o;                        // [range][Hq][d]
   float *scores;                        // scaled logits in log2 units: first_row * Hq numbers of the sequences before, then [Hq][rows_b]
   int32_t batch0, batch, n_q_heads, n_kv_heads, group, slot_pitch;
@@ -111,7 +111,9 @@ struct PagedDecodeArgs {
   int32_t first_row[kPagedBatch];       // rows of the sequences before, each rounded up to 32
   int32_t max_tokens[kPagedBatch];
 };
-constexpr float kPagedLowest = -3.3e38f;                      // reference of a softmax that has seen no slot: below all scores that are worth telling apart
+// Reference of a softmax that has seen no slot: below all scores that are worth telling apart.  References are kept and compared before
+// the scale, everywhere: scaled, this one is minus infinity from a scale of 0.715 on, and the factor between two that are is no number.
+constexpr float kPagedLowest = -3.3e38f;
 constexpr int kPagedMinRange = 128, kPagedMaxRange = 1024;   // rows of a key range
 // Rows of a head that a workgroup of so many wavefronts takes as a whole, its scores beside the ring in LDS.
 __host__ __device__ constexpr int alone_rows(int waves) { return waves == 8 ? 960 : 512; }
@@ -163,7 +165,7 @@ __device__ __forceinline__ float *head_scores(const PagedDecodeArgs &a, int bl, 
   const int64_t rows = (CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31) & ~31;
   return a.scores + (int64_t)CKV_ARG(PagedDecodeArgs, first_row, bl) * a.n_q_heads + (int64_t)hq * rows;
 }
-// Element e of the state (M, L, o) that this workgroup's key range leaves of query head hq of sequence b.
+// Element e of the state (M, L, o) that this workgroup's key range leaves of query head hq of sequence b; M before the scale.
 template <int HD>
 __device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int hq, int e, float M, float L, float o) {
   const int64_t slot = (int64_t)blockIdx.x * a.n_q_heads + hq;
@@ -171,7 +173,7 @@ __device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int
   if (a.direct) {
     const int64_t head = (int64_t)b * a.n_q_heads + hq;
     a.out[head * HD + e] = L > 0.f ? o / L : 0.f;
-    if (a.lse != nullptr && e == 0) a.lse[head] = L > 0.f ? (M + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+    if (a.lse != nullptr && e == 0) a.lse[head] = L > 0.f ? (M * a.scale_log2e + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
   } else {
     a.part_o[slot * HD + e] = o;
   }

@@ -9,7 +9,7 @@ namespace ckv {
 
 // The launch behind the ranges.
 //
-// Its first `joins` workgroups join a query head each: out = sum_r o_r 2^(m_r - M) / sum_r l_r 2^(m_r - M).  A thread owns four
+// Its first `joins` workgroups join a query head each: out = sum_r o_r f_r / sum_r l_r f_r, f_r = 2^(c (m_r - M)), c the scale in log2 units.  A thread owns four
 // columns and every so many-th range, four of them in flight; the groups of ranges are folded through LDS in order.
 // With weights (W = 1) the others add token_weight[s] += sum_i 2^(x_i(s) - lse_i) to the slots of one key range of one kv-head,
 // heads in order: the scores of the first four heads are on their way while the log-sum-exps are formed from all ranges' pairs.
@@ -19,6 +19,7 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
   __shared__ float s_acc[NG][HD + 2];
   __shared__ float s_lse[W != 0 ? kPagedMaxGroup : 1];
   const int t = threadIdx.x;
+  const float c1 = a.scale_log2e;
   if (W == 0 || (int)blockIdx.x < joins) {
     const int bl = blockIdx.x / a.n_q_heads, hq = blockIdx.x % a.n_q_heads, col = t % TPR, grp = t / TPR;
     const int n = paged_length(a, bl, hq / a.group), rps = paged_range_rows(n, paged_splits(bl)), used = n > 0 ? (n + rps - 1) / rps : 1;
@@ -38,13 +39,13 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
       float mm = m;
 #pragma unroll
       for (int u = 0; u < UN; ++u) mm = fmaxf(mm, p[u].x);
-      const float f0 = __builtin_amdgcn_exp2f(m - mm);
+      const float f0 = __builtin_amdgcn_exp2f((m - mm) * c1);
       lsum *= f0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] *= f0;
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
-        const float f = r0 + u * NG < used ? __builtin_amdgcn_exp2f(p[u].x - mm) : 0.f;
+        const float f = r0 + u * NG < used ? __builtin_amdgcn_exp2f((p[u].x - mm) * c1) : 0.f;
         lsum += p[u].y * f;
         acc[0] += o4[u].x * f; acc[1] += o4[u].y * f; acc[2] += o4[u].z * f; acc[3] += o4[u].w * f;
       }
@@ -61,13 +62,13 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
       float v = 0.f, L = 0.f;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const float f = __builtin_amdgcn_exp2f(s_acc[g][HD + 1] - M);
+        const float f = __builtin_amdgcn_exp2f((s_acc[g][HD + 1] - M) * c1);
         v += s_acc[g][t] * f;
         L += s_acc[g][HD] * f;
       }
       const int64_t head = (int64_t)(a.batch0 + bl) * a.n_q_heads + hq;
       a.out[head * HD + t] = L > 0.f ? v / L : 0.f;
-      if (a.lse != nullptr && t == 0) a.lse[head] = L > 0.f ? (M + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+      if (a.lse != nullptr && t == 0) a.lse[head] = L > 0.f ? (M * c1 + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
     }
     return;
   }
@@ -104,14 +105,14 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
       for (int r = lane; r < used; r += 64) {
         const float2 p = a.part_ml[(int64_t)(first + r) * a.n_q_heads + h * a.group + j];
         const float mm = fmaxf(m, p.x);
-        l = l * __builtin_amdgcn_exp2f(m - mm) + p.y * __builtin_amdgcn_exp2f(p.x - mm);
+        l = l * __builtin_amdgcn_exp2f((m - mm) * c1) + p.y * __builtin_amdgcn_exp2f((p.x - mm) * c1);
         m = mm;
       }
       float M = m;
       for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-      l *= __builtin_amdgcn_exp2f(m - M);
+      l *= __builtin_amdgcn_exp2f((m - M) * c1);
       for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
-      if (lane == 0) s_lse[j] = l > 0.f ? M + __builtin_log2f(l) : 3.0e38f;   // no slot is there: no weight
+      if (lane == 0) s_lse[j] = l > 0.f ? M * c1 + __builtin_log2f(l) : 3.0e38f;   // no slot is there: no weight
     }
     __syncthreads();
     for (int j0 = 0;;) {

@@ -302,7 +302,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   __syncthreads();
   float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G, *s_lse = s_o + NW * G * HD;   // [NW][G], [NW][G], [NW][G][HD], [G]
   if (n < G) {
-    if (q == 0) { s_m[wave * G + n] = m * c1; s_l[wave * G + n] = l; }
+    if (q == 0) { s_m[wave * G + n] = m; s_l[wave * G + n] = l; }
 #pragma unroll
     for (int mt = 0; mt < NMT; ++mt) *(f32x4 *)(s_o + (wave * G + n) * HD + 16 * mt + 4 * q) = acc[0][mt];
   }
@@ -316,12 +316,12 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
     float L = 0.f, o = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s_m[w * G + j] - M);
+      const float f = __builtin_amdgcn_exp2f((s_m[w * G + j] - M) * c1);
       L += s_l[w * G + j] * f;
       o += s_o[(w * G + j) * HD + e] * f;
     }
     store_range<HD>(a, b, h * g + j0 + j, e, M, L, o);
-    if (W == kAdded && e == 0) s_lse[j] = L > 0.f ? M + __builtin_log2f(L) : 3.0e38f;   // no slot is there: no weight
+    if (W == kAdded && e == 0) s_lse[j] = L > 0.f ? M * c1 + __builtin_log2f(L) : 3.0e38f;   // no slot is there: no weight
   }
   if constexpr (W == kAdded) {
     __syncthreads();
