@@ -101,7 +101,7 @@ struct PagedDecodeArgs {
   const int32_t *kv_len;
   float2 *part_ml;                      // (reference before the scale, sum) of every range and query head: [range][Hq]
   float *part_o;                        // [range][Hq][d]
-  float *scores;                        // scaled logits in log2 units: first_row * Hq numbers of the sequences before, then [Hq][rows_b]
+  float *scores;                        // products q . k, before the scale: first_row * Hq numbers of the sequences before, then [Hq][rows_b]
   int32_t batch0, batch, n_q_heads, n_kv_heads, group, slot_pitch;
   int32_t heads;                        // query heads of a kv-head that a workgroup serves: 4, 8 or 16
   float scale_log2e;
@@ -181,13 +181,20 @@ __device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int
 
 // What becomes of the scores: nothing, to the workspace for the launch behind, added up as weights by a workgroup that has a whole head.
 enum Scores { kDropped, kStored, kAdded };
-// token_weight[s] += sum_i 2^(x_i(s) - lse_i), heads in order; x: [heads][alone_rows] in LDS.
+// A head's softmax weights are 2^(c (x - M)) / L, x before the scale: M and 1 / L are kept apart, as their sum in log2 units loses log2 L
+// beside an M of 2^24.
+struct HeadNorm {
+  float ref, inv;                       // M, 1 / L; 0 if no slot is there
+};
+// (the reciprocal instruction is off by a step of fp32 at most; a division costs 0.16 us of 13.75 with 16 heads of 13171 slots)
+__device__ __forceinline__ HeadNorm head_norm(float M, float L) { return {M, L > 0.f ? __builtin_amdgcn_rcpf(L) : 0.f}; }
+// token_weight[s] += sum_i 2^(c (x_i(s) - M_i)) / L_i, heads in order; x: [heads][alone_rows] in LDS.
 template <int NW>
-__device__ __forceinline__ void add_weights(const PagedDecodeArgs &a, int b, int h, int len, const float *x, const float *lse) {
+__device__ __forceinline__ void add_weights(const PagedDecodeArgs &a, int b, int h, int len, const float *x, const HeadNorm *norm) {
   float *weight = a.weight + ((int64_t)b * a.n_kv_heads + h) * a.slot_pitch;
   for (int r = threadIdx.x; r < len; r += NW * 64) {
     float sum = 0.f;
-    for (int j = 0; j < a.group; ++j) sum += __builtin_amdgcn_exp2f(x[j * alone_rows(NW) + r] - lse[j]);
+    for (int j = 0; j < a.group; ++j) sum += __builtin_amdgcn_exp2f((x[j * alone_rows(NW) + r] - norm[j].ref) * a.scale_log2e) * norm[j].inv;
     weight[r] += sum;
   }
 }

@@ -11,13 +11,13 @@ namespace ckv {
 //
 // Its first `joins` workgroups join a query head each: out = sum_r o_r f_r / sum_r l_r f_r, f_r = 2^(c (m_r - M)), c the scale in log2 units.  A thread owns four
 // columns and every so many-th range, four of them in flight; the groups of ranges are folded through LDS in order.
-// With weights (W = 1) the others add token_weight[s] += sum_i 2^(x_i(s) - lse_i) to the slots of one key range of one kv-head,
-// heads in order: the scores of the first four heads are on their way while the log-sum-exps are formed from all ranges' pairs.
+// With weights (W = 1) the others add token_weight[s] += sum_i 2^(c (x_i(s) - M_i)) / L_i to the slots of one key range of one kv-head,
+// heads in order: the scores of the first four heads are on their way while M_i and 1 / L_i are formed from all ranges' pairs.
 template <int HD, int W>
 __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs a, int joins) {
   constexpr int TPR = HD / 4, NG = kThreads / TPR, UN = 4;
   __shared__ float s_acc[NG][HD + 2];
-  __shared__ float s_lse[W != 0 ? kPagedMaxGroup : 1];
+  __shared__ HeadNorm s_norm[W != 0 ? kPagedMaxGroup : 1];
   const int t = threadIdx.x;
   const float c1 = a.scale_log2e;
   if (W == 0 || (int)blockIdx.x < joins) {
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          sx[j][i] = kPagedLowest;
+          sx[j][i] = -__builtin_inff();
           if (j0 + j < a.group && t + i * kThreads < len) sx[j][i] = __builtin_nontemporal_load(scores + (int64_t)(j0 + j) * pitch + t + i * kThreads);   // for the last time
         }
     };
@@ -112,15 +112,15 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
       for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
       l *= __builtin_amdgcn_exp2f((m - M) * c1);
       for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
-      if (lane == 0) s_lse[j] = l > 0.f ? M * c1 + __builtin_log2f(l) : 3.0e38f;   // no slot is there: no weight
+      if (lane == 0) s_norm[j] = head_norm(M, l);
     }
     __syncthreads();
     for (int j0 = 0;;) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float lse = j0 + j < a.group ? s_lse[j0 + j] : 3.0e38f;
+        const HeadNorm norm = j0 + j < a.group ? s_norm[j0 + j] : HeadNorm{0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < NR; ++i) sum[i] += __builtin_amdgcn_exp2f(sx[j][i] - lse);
+        for (int i = 0; i < NR; ++i) sum[i] += __builtin_amdgcn_exp2f((sx[j][i] - norm.ref) * c1) * norm.inv;
       }
       j0 += 4;
       if (j0 >= a.group) break;

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
   constexpr int SLOT = 16 * ROWB;
   constexpr int NKS = HD / 16, NH = HD / 64;               // 64-byte pieces of a key, 64-dim pieces of the output
   constexpr int RING = NW * 2 * SLOT, AH = 8;        // AH: most heads of a workgroup that adds up weights
-  static_assert(RING >= NW * G * (HD + 2) * 4 + G * 4, "the states of the wavefronts take the ring's place");
+  static_assert(RING >= NW * G * (HD + 2) * 4 + G * 8, "the states of the wavefronts take the ring's place");
   __shared__ __align__(16) char smem[RING + (W == kAdded ? AH * alone_rows(NW) * 4 : 0)];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
       for (int i = 0; i < 4; ++i) sc[i] = span != 0 && key0 + 4 * q + i < len ? sc[i] : -__builtin_inff();   // times any scale
     }
     if constexpr (W == kAdded) {
-      if (scored) *(f32x4 *)(lscores + n * alone_rows(NW) + key0 + 4 * q) = sc * c1;
+      if (scored) *(f32x4 *)(lscores + n * alone_rows(NW) + key0 + 4 * q) = sc;
     }
     float p[4];
     auto weights = [&]() __attribute__((always_inline)) {
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
     issue(a.v, voff, s + 1, vs_);
     if constexpr (W == kStored) {   // last, so that no wait for rows is one for a store of the same step
       __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sc * c1), srs, scored ? (int)(soff + (uint32_t)key0 * 4u) : -1, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sc), srs, scored ? (int)(soff + (uint32_t)key0 * 4u) : -1, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -195,7 +195,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
   // ---- merge the wavefronts through LDS, in wavefront order; the loads of the empty steps still write zeros into the slots
   __builtin_amdgcn_s_waitcnt(vm_imm(0));
   __syncthreads();
-  float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G, *s_lse = s_o + NW * G * HD;   // [NW][G], [NW][G], [NW][G][HD], [G]
+  float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G;   // [NW][G], [NW][G], [NW][G][HD]
+  HeadNorm *s_norm = (HeadNorm *)(s_o + NW * G * HD);                              // [G]
   if (scored) {
     if (q == 0) { s_m[wave * G + n] = m; s_l[wave * G + n] = l; }
 #pragma unroll
@@ -218,11 +219,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_f32_kernel(Pag
       o += s_o[(w * G + j) * HD + e] * f;
     }
     store_range<HD>(a, b, h * g + j0 + j, e, M, L, o);
-    if (W == kAdded && e == 0) s_lse[j] = L > 0.f ? M * c1 + __builtin_log2f(L) : 3.0e38f;   // no slot is there: no weight
+    if (W == kAdded && e == 0) s_norm[j] = head_norm(M, L);
   }
   if constexpr (W == kAdded) {
     __syncthreads();
-    add_weights<NW>(a, b, h, len, lscores, s_lse);
+    add_weights<NW>(a, b, h, len, lscores, s_norm);
   }
 }
 

@@ -11,7 +11,7 @@
 // tokens: slots past the last one, and blocks whose page is not there, read as zeros without touching memory.
 // A wavefront has one slot for K and one for V, each refilled as soon as it is read.  A second pair is slower, as it takes the place
 // of other workgroups: 131072 slots 95.8 us, 89.0 so (d = 64: 47.2, 46.4), 13171 slots 16.1 and 14.7.
-// Weights: kStored keeps the scaled logits (fp32, log2 units) for the launch that adds up what every slot received.  They go
+// Weights: kStored keeps the scores (fp32, before the scale) for the launch that adds up what every slot received.  They go
 // out by a buffer store whose idle columns lie out of range, so every step has one and the waits can count them together with
 // the loads (both leave the counter in the order they were issued).  17 MB of them beside 537 MB of K and V cost 10 us.
 // kAdded keeps them in LDS: a head that is one range knows its log-sum-exps in the end and adds its own weights, and nothing
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   constexpr bool BF = DT == CHUNKKV_BF16;
   constexpr int NSET = G == 4 ? 1 : (G == 8 ? 2 : (BF ? 3 : 4));   // products per output tile
   constexpr int RING = NW * 2 * SLOT;
-  static_assert(RING >= NW * G * (HD + 2) * 4 + G * 4, "the states of the wavefronts take the ring's place");
+  static_assert(RING >= NW * G * (HD + 2) * 4 + G * 8, "the states of the wavefronts take the ring's place");
   __shared__ __align__(16) char smem[RING + (W == kAdded ? G * alone_rows(NW) * 4 : 0)];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -286,9 +286,9 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
       __builtin_amdgcn_sched_barrier(0);
       f32x4 x;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = (part == 0 ? sc[0][i] : sc[1][i]) * c1;
+      for (int i = 0; i < 4; ++i) x[i] = part == 0 ? sc[0][i] : sc[1][i];
       keep(key0, x);
-      if constexpr (G == 16) keep(key0 + 16, sc[1] * c1);
+      if constexpr (G == 16) keep(key0 + 16, sc[1]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -300,7 +300,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
   // ---- merge the wavefronts through LDS, in wavefront order; the loads of the empty steps still write zeros into the slots
   __builtin_amdgcn_s_waitcnt(vm_imm(0));
   __syncthreads();
-  float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G, *s_lse = s_o + NW * G * HD;   // [NW][G], [NW][G], [NW][G][HD], [G]
+  float *s_m = (float *)smem, *s_l = s_m + NW * G, *s_o = s_l + NW * G;   // [NW][G], [NW][G], [NW][G][HD]
+  HeadNorm *s_norm = (HeadNorm *)(s_o + NW * G * HD);                              // [G]
   if (n < G) {
     if (q == 0) { s_m[wave * G + n] = m; s_l[wave * G + n] = l; }
 #pragma unroll
@@ -321,11 +322,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void paged_mfma_kernel(Pa
       o += s_o[(w * G + j) * HD + e] * f;
     }
     store_range<HD>(a, b, h * g + j0 + j, e, M, L, o);
-    if (W == kAdded && e == 0) s_lse[j] = L > 0.f ? M * c1 + __builtin_log2f(L) : 3.0e38f;   // no slot is there: no weight
+    if (W == kAdded && e == 0) s_norm[j] = head_norm(M, L);
   }
   if constexpr (W == kAdded) {
     __syncthreads();
-    add_weights<NW>(a, b, h, len, lscores, s_lse);
+    add_weights<NW>(a, b, h, len, lscores, s_norm);
   }
 }
 

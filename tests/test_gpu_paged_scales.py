@@ -4,7 +4,7 @@ import torch
 
 import paper_2502_00299_amd as ckv
 from tests import paged_helpers as H
-from tests.test_gpu_paged_attention import check
+from tests.test_gpu_paged_attention import PAIR, check, run
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = ckv.F32, ckv.BF16, ckv.F16
@@ -55,3 +55,48 @@ def test_sixteen_heads_with_missing_ranges(lib, dtype, weights):
     cache = H.Cache(gen, dtype, 16, 1, 128, 256, [45000], [45000], scale=1.0)
     cache.table[0, 8:16] = -1
     check(cache, queries(gen, cache), cache.len[0].tolist(), weights)
+
+
+def far(gen, dtype, room, d, sign, far_k, far_q, every=1, scale=0.0):
+    """A cache whose scores are sign * far_k * far_q in every so many-th slot and twice as far below zero, or half as far above, in the others."""
+    cache = H.Cache(gen, dtype, 8, 2, d, 16, [room], [room], scale=scale)
+    there = torch.isfinite(cache.k[0])
+    cache.k[0][there] = 0
+    _, page, row = cache.slots(0, 0, room)
+    first = torch.full((room,), sign * far_k * (0.5 if sign > 0 else 2.0))
+    first[::every] = sign * far_k
+    cache.k[0, page, :, row, 0] = first[:, None].to(H.KIND[dtype])
+    q = torch.zeros((1, 8, d), dtype=H.KIND[dtype])
+    q[..., 0] = far_q
+    return cache, q
+
+
+def equal_shares(cache, q, every):
+    """Every so many-th slot of a head gets the same part of every query head, the others nothing."""
+    room = int(cache.len[0, 0, 0])
+    n = -(-room // every)
+    out, lse, weight = run(cache, q, None, torch.zeros_like(cache.weight[0]))
+    # the reciprocal of n, off by a step of fp32 (two roundings), once per query head and added up: its sums of two and four are
+    # exact, that of three and the one with what was there are rounded; the reference is the scores' own, so that their exponentials are 1
+    want = torch.zeros(room)
+    want[::every] = 4.0 / n
+    assert float((weight[0, :, :room] - want).abs().max()) <= 5 * 2.0 ** -24 * 4.0 / n
+    for h in range(2):
+        _, v = cache.rows(cache.v, 0, h, room)
+        v = v[::every]
+        assert float((out[0, 4 * h:4 * h + 4].double() - v.mean(0)).abs().max()) <= PAIR * float(v.abs().max())
+    return lse
+
+
+@pytest.mark.parametrize("every", [1, 3])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("room", [200, 500, 900, 3000])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_equal_keys_far_from_zero(lib, dtype, room, sign, every):
+    """Logits of 2^24 and of 2^57: what a slot receives is not lost beside them."""
+    far_k, far_q = (2.0 ** 13, 2.0 ** 14) if dtype == F16 else (2.0 ** 30, 2.0 ** 30)
+    gen = torch.Generator().manual_seed(room)
+    cache, q = far(gen, dtype, room, 64, sign, far_k, far_q, every)
+    lse = equal_shares(cache, q, every)
+    logit = sign * far_k * far_q / 8
+    assert float((lse.double() - logit).abs().max()) <= 4 * 2.0 ** -24 * abs(logit) + 10
