@@ -1,5 +1,7 @@
 // Caches in pages: what the kernels of paged_*.hip and their entry points share.
 #pragma once
+#include <float.h>
+
 #include "internal.h"
 
 namespace ckv {
@@ -104,16 +106,16 @@ struct PagedDecodeArgs {
   float *scores;                        // products q . k, before the scale: first_row * Hq numbers of the sequences before, then [Hq][rows_b]
   int32_t batch0, batch, n_q_heads, n_kv_heads, group, slot_pitch;
   int32_t heads;                        // query heads of a kv-head that a workgroup serves: 4, 8 or 16
-  float scale_log2e;
+  float scale, scale_log2e;             // between FLT_MIN and what is finite in both units
   int32_t direct;                       // 1: every head is one range, the range kernel writes the outputs
   int32_t alone;                        // its wavefronts if it adds up the weights as well, and no launch follows; 0
   int32_t first[kPagedBatch + 16];      // number of the first key range of every sequence
   int32_t first_row[kPagedBatch];       // rows of the sequences before, each rounded up to 32
   int32_t max_tokens[kPagedBatch];
 };
-// Reference of a softmax that has seen no slot: below all scores that are worth telling apart.  References are kept and compared before
+// Reference of a softmax that has seen no slot: below all scores, which are finite.  References are kept and compared before
 // the scale, everywhere: scaled, this one is minus infinity from a scale of 0.715 on, and the factor between two that are is no number.
-constexpr float kPagedLowest = -3.3e38f;
+constexpr float kPagedLowest = -FLT_MAX;
 constexpr int kPagedMinRange = 128, kPagedMaxRange = 1024;   // rows of a key range
 // Rows of a head that a workgroup of so many wavefronts takes as a whole, its scores beside the ring in LDS.
 __host__ __device__ constexpr int alone_rows(int waves) { return waves == 8 ? 960 : 512; }
@@ -165,6 +167,10 @@ __device__ __forceinline__ float *head_scores(const PagedDecodeArgs &a, int bl, 
   const int64_t rows = (CKV_ARG(PagedDecodeArgs, max_tokens, bl) + 31) & ~31;
   return a.scores + (int64_t)CKV_ARG(PagedDecodeArgs, first_row, bl) * a.n_q_heads + (int64_t)hq * rows;
 }
+// Natural log of sum_s exp(scale x(s)), M before the scale: rounded once at its own size, and finite where the logits are.
+__device__ __forceinline__ float log_sum_exp(const PagedDecodeArgs &a, float M, float L) {
+  return L > 0.f ? __builtin_fmaf(M, a.scale, __builtin_log2f(L) * 0.6931471805599453f) : -__builtin_inff();
+}
 // Element e of the state (M, L, o) that this workgroup's key range leaves of query head hq of sequence b; M before the scale.
 template <int HD>
 __device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int hq, int e, float M, float L, float o) {
@@ -173,7 +179,7 @@ __device__ __forceinline__ void store_range(const PagedDecodeArgs &a, int b, int
   if (a.direct) {
     const int64_t head = (int64_t)b * a.n_q_heads + hq;
     a.out[head * HD + e] = L > 0.f ? o / L : 0.f;
-    if (a.lse != nullptr && e == 0) a.lse[head] = L > 0.f ? (M * a.scale_log2e + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+    if (a.lse != nullptr && e == 0) a.lse[head] = log_sum_exp(a, M, L);
   } else {
     a.part_o[slot * HD + e] = o;
   }

@@ -1,5 +1,4 @@
 // Host side of the calls over pages: argument checks, workspace plans and launches.
-#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -329,8 +328,10 @@ int chunkkv_paged_decode_attention(const chunkkv_pages *pages, const int32_t *pa
     a.scores = (float *)((char *)workspace + pl.off_scores);
     a.batch0 = b0; a.batch = nb; a.n_q_heads = pages->n_q_heads; a.n_kv_heads = pages->n_kv_heads;
     a.group = pages->n_q_heads / pages->n_kv_heads; a.slot_pitch = pages->slot_pitch; a.heads = heads_at_once(pages, b0, nb);
-    // a scale that vanishes in fp32 gives all slots the same weight; kept above zero, which minus infinity cannot be multiplied by
-    a.scale_log2e = scale * 1.4426950408889634f > FLT_MIN ? scale * 1.4426950408889634f : FLT_MIN;
+    // A scale that vanishes in fp32 gives all slots the same weight; kept above zero, which minus infinity cannot be multiplied by.  One
+    // that is finite and not so times log2 e tells apart what any as large does: the largest scores have all the weight.
+    a.scale = scale > FLT_MIN ? scale : FLT_MIN;
+    a.scale_log2e = a.scale < FLT_MAX / 1.4426952f ? a.scale * 1.4426950408889634f : FLT_MAX;
     const int r = range_rows(pages, b0, nb, token_weight != nullptr);
     for (int i = 0; i < kPagedBatch + 16; ++i) a.first[i] = INT32_MAX;
     int ranges = 0, rows = 0;

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void paged_finish_kernel(PagedDecodeArgs 
       }
       const int64_t head = (int64_t)(a.batch0 + bl) * a.n_q_heads + hq;
       a.out[head * HD + t] = L > 0.f ? v / L : 0.f;
-      if (a.lse != nullptr && t == 0) a.lse[head] = L > 0.f ? (M * c1 + __builtin_log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+      if (a.lse != nullptr && t == 0) a.lse[head] = log_sum_exp(a, M, L);
     }
     return;
   }

@@ -4,7 +4,7 @@ import torch
 
 import paper_2502_00299_amd as ckv
 from tests import paged_helpers as H
-from tests.test_gpu_paged_attention import PAIR, check, run
+from tests.test_gpu_paged_attention import LOGIT, PAIR, check, run
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = ckv.F32, ckv.BF16, ckv.F16
@@ -100,3 +100,43 @@ def test_equal_keys_far_from_zero(lib, dtype, room, sign, every):
     lse = equal_shares(cache, q, every)
     logit = sign * far_k * far_q / 8
     assert float((lse.double() - logit).abs().max()) <= 4 * 2.0 ** -24 * abs(logit) + 10
+
+
+@pytest.mark.parametrize("every", [1, 3])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("room", [200, 900, 3000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_logits_at_the_ends_of_fp32(lib, dtype, room, sign, every):
+    """Logits of up to 255 / 128 * 2^127 in magnitude, finite as they are and not in units of log2 e."""
+    far_k = 1.9921875 * 2.0 ** 63 * (1.0 if sign > 0 or every == 1 else 0.5)
+    gen = torch.Generator().manual_seed(room)
+    cache, q = far(gen, dtype, room, 128, sign, far_k, 2.0 ** 64, every, scale=1.0)
+    lse = equal_shares(cache, q, every)
+    logit = sign * far_k * 2.0 ** 64
+    assert bool(torch.isfinite(lse).all()) and float((lse.double() - logit).abs().max()) <= 4 * 2.0 ** -24 * abs(logit)
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("room", [200, 900, 3000])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_scales_at_the_end_of_fp32(lib, dtype, room, weights):
+    """A scale that is finite as it is and not in units of log2 e: the largest score has all the weight; missing pages and equal scores beside it."""
+    scale = float(torch.tensor(3.0e38))
+    gen = torch.Generator().manual_seed(room)
+    cache = H.Cache(gen, dtype, 8, 2, 64, 16, [room, 70], [room, 70], scale=scale)
+    cache.k[0][torch.isfinite(cache.k[0])] = 0
+    _, page, row = cache.slots(0, 0, room)
+    cache.k[0, page[137], :, row[137], 0] = 1.0
+    cache.table[0, 4:6] = -1
+    q = torch.zeros((2, 8, 64), dtype=H.KIND[dtype])
+    q[..., 0] = 1.0
+    out, lse, weight = run(cache, q, None, torch.zeros_like(cache.weight[0]) if weights else None)
+    assert torch.equal(out[0], cache.v[0, page[137], :, row[137]].float().repeat_interleave(4, 0))
+    assert float((lse[0].double() / scale - 1).abs().max()) <= 4 * 2.0 ** -24
+    for h in range(2):   # all logits of the second sequence are zero
+        _, v = cache.rows(cache.v, 1, h, 70)
+        assert float((out[1, 4 * h:4 * h + 4].double() - v.mean(0)).abs().max()) <= PAIR * float(v.abs().max())
+    assert float((lse[1] - torch.log(torch.tensor(70.0))).abs().max()) <= LOGIT
+    if weights:
+        assert float(weight[0, :, 137].min()) == float(weight[0, :, 137].max()) == 4 and float(weight[0].sum()) == 8
+        assert float((weight[1, :, :70] - 4 / 70).abs().max()) <= 5 * 2.0 ** -24 * 4 / 70
