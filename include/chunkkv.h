@@ -312,14 +312,16 @@ typedef struct {
  * rows named by the selection of group l / reuse, in ascending order, then the window rows, go to slots 0, 1, ...
  *   prob         geometry of the full caches, window, chunk, n_keep, flags; its out_* fields are not used
  *   k, v         HOST arrays of n_layers full caches;  k_pages, v_pages   HOST arrays of n_layers pools
- *   sel_*        as in chunkkv_compress_stack, ceil(n_layers / reuse) groups (chunkkv_chunk_topk writes one)
+ *   sel_*        as in chunkkv_compress_stack, ceil(n_layers / reuse) groups (chunkkv_chunk_topk writes one).  Any number of
+ *                chunks may be cut: a head's count is clamped to [0, min(sel_cap, n_keep_b)], as an entry keeps a token at least
  *   token_importance  NULL, or a HOST array of ceil(n_layers / reuse) device arrays as chunkkv_score writes them
  *                ([B][Hkv][score_cap*chunk]): the weight a prefix token starts with.  Without it weights start at 0;
  *                window tokens always do
  *   kv_len       written: the rows stored, n_keep_b + w (whole-chunk mode: as many as the selection keeps)
  *   token_pos    NULL, or written: the token's index in the full cache;  token_weight  NULL, or written
  * prob and pages have to agree on batch, heads, head_dim and dtype, and n_keep_b + w <= max_tokens_b
- * (CHUNKKV_ERR_SHAPE).  A malformed selection entry stores nothing; slots it should have filled stay as they are.      */
+ * (CHUNKKV_ERR_SHAPE).  A malformed selection entry stores nothing; slots it should have filled stay as they are.  The window
+ * and kv_len are written whatever the entries are.                                                                      */
 int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *pages, int32_t n_layers, int32_t reuse,
                           const void *const *k, const void *const *v, const int32_t *sel_chunk, const int32_t *sel_len,
                           const int32_t *sel_count, const float *const *token_importance, const int32_t *page_table,
