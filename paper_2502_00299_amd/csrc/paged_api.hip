@@ -222,7 +222,8 @@ int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *page
       a.kv_stride_head = prob->kv_stride_head; a.kv_stride_tok = prob->kv_stride_tok;
       a.imp_pitch = (int64_t)prob->score_cap * prob->chunk;
       a.layer0 = l0; a.reuse = reuse; a.batch0 = b0; a.batch_total = prob->batch; a.n_kv_heads = prob->n_kv_heads;
-      a.window = prob->window; a.chunk = prob->chunk; a.elem_bytes = elem_bytes(prob->dtype); a.slot_pitch = pages->slot_pitch;
+      // rows that span less than 2 GiB are fewer than 2^24: larger chunks are one, and sums with their size would pass 32 bits
+      a.window = prob->window; a.chunk = prob->chunk < kPagedMaxTokens ? prob->chunk : kPagedMaxTokens; a.elem_bytes = elem_bytes(prob->dtype); a.slot_pitch = pages->slot_pitch;
       a.whole_chunks = (prob->flags & CHUNKKV_FLAG_WHOLE_CHUNKS) ? 1 : 0;
       a.stream = written > kPagedStreamBytes;
       Timed t(kCompact, s);

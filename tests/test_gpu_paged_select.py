@@ -86,3 +86,21 @@ def test_counts_out_of_bounds(lib, cap, count, whole):
     want_k[place], want_v[place] = k.view(200, 64)[tokens], v.view(200, 64)[tokens]
     want_pos[0, 0, 0, s] = torch.tensor(tokens, dtype=torch.int32)
     assert H.same_bits(cache.back(kp), want_k) and H.same_bits(cache.back(vp), want_v) and H.same_bits(pos.cpu(), want_pos)
+
+
+@pytest.mark.parametrize("c", [2 ** 24 + 1, 2 ** 31 - 20, 2 ** 31 - 1])
+def test_chunks_longer_than_any_prefix(lib, c):
+    """One chunk holds the whole prefix, whatever its size is said to be."""
+    gen = torch.Generator().manual_seed(5)
+    k, v = (torch.randn(200 * 64, generator=gen).bfloat16() for _ in range(2))
+    prob = ckv.Problem(2, 1, 64, 16, c, BF16, [200], [64], [0], 200 * 64, 64)
+    sel = [torch.tensor(x, dtype=torch.int32, device=DEV) for x in ([0, -1], [64, -1], [1])]
+    cache = H.Cache(gen, BF16, 2, 1, 64, 16, [80], [0])
+    kp, vp, n, pos = cache.pool(cache.k), cache.pool(cache.v), cache.len.to(DEV), cache.pos.to(DEV)
+    ckv.chunkkv_paged_compact(prob, cache.pages, 1, [k.to(DEV)], [v.to(DEV)], *sel, None, cache.table.to(DEV), kp, vp, n, pos, None)
+    tokens, s = list(range(64)) + list(range(184, 200)), torch.arange(80)
+    want_k, want_v = cache.k.clone(), cache.v.clone()
+    place = (0, cache.table[0].long()[s // 16], 0, s % 16)
+    want_k[place], want_v[place] = k.view(200, 64)[tokens], v.view(200, 64)[tokens]
+    assert int(n) == 80 and pos[0, 0, 0, :80].tolist() == tokens
+    assert H.same_bits(cache.back(kp), want_k) and H.same_bits(cache.back(vp), want_v)
