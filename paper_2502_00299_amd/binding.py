@@ -11,7 +11,6 @@ import ctypes as C
 import os
 from array import array
 from dataclasses import dataclass
-from operator import attrgetter
 from typing import Optional, Sequence
 
 import torch
@@ -461,7 +460,8 @@ _KINDS = {F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16}
 _I32, _F32 = torch.int32, torch.float32
 # torch.cuda.current_device() without its look at whether the runtime has been started (0.5 us): a call's tensors have done that
 _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-_get_device, _data_ptr, _is_contiguous, _nbytes = torch.Tensor.get_device, torch.Tensor.data_ptr, torch.Tensor.is_contiguous, attrgetter("nbytes")
+_get_device, _data_ptr, _is_contiguous = torch.Tensor.get_device, torch.Tensor.data_ptr, torch.Tensor.is_contiguous
+_dtype, _nbytes = torch.Tensor.dtype.__get__, torch.Tensor.nbytes.__get__
 
 
 def _refuse(where: str, dev: int, name: str, t, kind, elements: int):
@@ -494,13 +494,29 @@ def _pool(where: str, dev: int, name: str, t: torch.Tensor, kind, elements: int)
     return t.data_ptr()
 
 
+def _alike(dev: int, ts: Sequence, kind, elements: int) -> bool:
+    """Are all of the type and on the device, contiguous and large enough; for a long list, at 0.03 us a tensor and property."""
+    n = len(ts)
+    return ([*map(_dtype, ts)].count(kind) == n and [*map(_get_device, ts)].count(dev) == n and min(map(_nbytes, ts)) >= elements * ts[0].element_size()
+            and all(map(_is_contiguous, ts)))
+
+
 def _pools(where: str, dev: int, name: str, ts: Sequence, kind, elements: int):
-    """Addresses of the pools of several layers, as an array whose own address the library reads them from.  In a long list the
-    first pool's type stands for all; devices, bytes and contiguity are everyone's."""
-    if (len(ts) <= 4 or ts[0].dtype is not kind or set(map(_get_device, ts)) != {dev} or min(map(_nbytes, ts)) < elements * ts[0].element_size()
-            or not all(map(_is_contiguous, ts))):
+    """Addresses of the pools of several layers, as an array whose own address the library reads them from."""
+    if len(ts) <= 4 or not _alike(dev, ts, kind, elements):
         return array("Q", [_pool(where, dev, name, t, kind, elements) for t in ts])
-    return array("Q", map(_data_ptr, ts))
+    return array("Q", [*map(_data_ptr, ts)])
+
+
+def _pool_pairs(where: str, dev: int, names: Sequence[str], a: Sequence, b: Sequence, kind, elements: int):
+    """The same for two lists of as many pools, looked through as one; -> the array and where either's addresses begin."""
+    ts = [*a, *b]
+    if len(ts) <= 4 or not _alike(dev, ts, kind, elements):
+        at = array("Q", [_pool(where, dev, name, t, kind, elements) for name, xs in zip(names, (a, b)) for t in xs])
+    else:
+        at = array("Q", [*map(_data_ptr, ts)])
+    first = at.buffer_info()[0]
+    return at, first, first + 8 * len(a)
 
 
 def _scratch(where: str, dev: int, t: Optional[torch.Tensor]):
@@ -553,10 +569,10 @@ def chunkkv_paged_compact(prob: Problem, pages: Pages, reuse: int, k: Sequence, 
     given = None if token_importance is None else _pools(where, dev, "token_importance", token_importance, _F32, heads * prob.score_cap * prob.chunk)
     full = prob._c()
     reach = prob._kept[3]   # of the struct just returned
-    ks, vs = _pools(where, dev, "k", k, kind, reach), _pools(where, dev, "v", v, kind, reach)
-    kp, vp = _pools(where, dev, "k_pages", k_pages, kind, room), _pools(where, dev, "v_pages", v_pages, kind, room)
-    _check(load_library().chunkkv_paged_compact(full, cp, n, reuse, _at(ks), _at(vs), chunks, lens, count, _at(given), table, _at(kp), _at(vp), length,
-                                                pos, weight, _stream(stream, dev)), where)
+    caches, ks, vs = _pool_pairs(where, dev, ("k", "v"), k, v, kind, reach)   # caches, pools: hold the addresses until the call returns
+    pools, kp, vp = _pool_pairs(where, dev, ("k_pages", "v_pages"), k_pages, v_pages, kind, room)
+    _check(load_library().chunkkv_paged_compact(full, cp, n, reuse, ks, vs, chunks, lens, count, _at(given), table, kp, vp, length, pos, weight,
+                                                _stream(stream, dev)), where)
 
 
 def chunkkv_paged_append(pages: Pages, n_new: Sequence[int], q, k, v, positions, q_norm, k_norm, eps: float, inv_freq, interleaved: bool, q_out,
@@ -618,8 +634,8 @@ def chunkkv_paged_evict(pages: Pages, budget: Sequence[int], recent: int, page_t
     room, slots = pages._pool_elements(), heads * pages.slot_pitch
     table, length, pos, weight = _arrays(where, dev, ("page_table", page_table, _I32, pages.batch * pages.table_pitch), ("kv_len", kv_len, _I32, heads),
                                          ("token_pos", token_pos, _I32, slots), ("token_weight", token_weight, _F32, slots))
-    kp, vp = _pools(where, dev, "k_pages", k_pages, kind, room), _pools(where, dev, "v_pages", v_pages, kind, room)
-    _check(load_library().chunkkv_paged_evict(cp, n, _budgets(where, pages, budget), recent, table, _at(kp), _at(vp), length, pos, weight,
+    pools, kp, vp = _pool_pairs(where, dev, ("k_pages", "v_pages"), k_pages, v_pages, kind, room)   # pools: holds the addresses until the call returns
+    _check(load_library().chunkkv_paged_evict(cp, n, _budgets(where, pages, budget), recent, table, kp, vp, length, pos, weight,
                                               *_scratch(where, dev, workspace), _stream(stream, dev)), where)
 
 

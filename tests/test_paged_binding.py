@@ -1,0 +1,39 @@
+"""Checks of the binding of the calls over pages that need no GPU."""
+import pytest
+import torch
+
+from paper_2502_00299_amd import binding
+
+ROOM = 4 * 2 * 16 * 64
+
+
+def pools(layers, kind=torch.bfloat16):
+    return [torch.zeros(4, 2, 16, 64, dtype=kind) for _ in range(layers)]
+
+
+@pytest.mark.parametrize("layers", [1, 4, 5, 32])
+@pytest.mark.parametrize("kind", [torch.float16, torch.float32, torch.int16])
+@pytest.mark.parametrize("place", [0, -1])
+def test_every_pool_of_a_stack_has_the_type(layers, kind, place):
+    """A pool of another type is refused wherever it is in the list, also where it has as many bytes or more."""
+    ts = pools(layers)
+    assert list(binding._pools("here", -1, "k_pages", ts, torch.bfloat16, ROOM)) == [t.data_ptr() for t in ts]
+    ts[place] = torch.zeros(4, 2, 16, 64, dtype=kind)
+    with pytest.raises(ValueError, match="k_pages is torch"):
+        binding._pools("here", -1, "k_pages", ts, torch.bfloat16, ROOM)
+
+
+@pytest.mark.parametrize("layers", [1, 2, 3, 32])
+@pytest.mark.parametrize("kind", [torch.float16, torch.float32])
+def test_two_lists_of_pools(layers, kind):
+    ks, vs = pools(layers), pools(layers)
+    at, k, v = binding._pool_pairs("here", -1, ("k_pages", "v_pages"), ks, vs, torch.bfloat16, ROOM)
+    assert list(at) == [t.data_ptr() for t in ks + vs] and (k, v) == (at.buffer_info()[0], at.buffer_info()[0] + 8 * layers)
+    for name, ts in (("k_pages", ks), ("v_pages", vs)):
+        for wrong, why in ((torch.zeros(4, 2, 16, 64, dtype=kind), "is torch"), (torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16), "has")):
+            good, ts[-1] = ts[-1], wrong
+            with pytest.raises(ValueError, match=f"{name} {why}"):
+                binding._pool_pairs("here", -1, ("k_pages", "v_pages"), ks, vs, torch.bfloat16, ROOM)
+            ts[-1] = good
+    with pytest.raises(ValueError, match="k_pages is on device"):
+        binding._pool_pairs("here", 0, ("k_pages", "v_pages"), ks, vs, torch.bfloat16, ROOM)
