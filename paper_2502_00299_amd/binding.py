@@ -485,7 +485,10 @@ def _arrays(where: str, dev: int, *arrays):
     return out
 
 
-def _pool(where: str, dev: int, name: str, t: torch.Tensor, kind, elements: int) -> int:
+def _pool(where: str, dev: int, name: str, t: Optional[torch.Tensor], kind, elements: int) -> int:
+    """Address of a pool, 0 without one: what has to be there is the library's to say."""
+    if t is None:
+        return 0
     if t.dtype is not kind or t.get_device() != dev or t.numel() < elements or not t.is_contiguous():
         # a view of something larger: what counts is the memory behind its first element
         room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
@@ -497,8 +500,11 @@ def _pool(where: str, dev: int, name: str, t: torch.Tensor, kind, elements: int)
 def _alike(dev: int, ts: Sequence, kind, elements: int) -> bool:
     """Are all of the type and on the device, contiguous and large enough; for a long list, at 0.03 us a tensor and property."""
     n = len(ts)
-    return ([*map(_dtype, ts)].count(kind) == n and [*map(_get_device, ts)].count(dev) == n and min(map(_nbytes, ts)) >= elements * ts[0].element_size()
-            and all(map(_is_contiguous, ts)))
+    try:
+        return ([*map(_dtype, ts)].count(kind) == n and [*map(_get_device, ts)].count(dev) == n and min(map(_nbytes, ts)) >= elements * ts[0].element_size()
+                and all(map(_is_contiguous, ts)))
+    except TypeError:   # one is None
+        return False
 
 
 def _pools(where: str, dev: int, name: str, ts: Sequence, kind, elements: int):
@@ -532,14 +538,16 @@ def _at(table) -> Optional[int]:
     return None if table is None else table.buffer_info()[0]
 
 
-def _new_rows(where: str, dev: int, name: str, t: torch.Tensor, kind, tokens: int, heads: int, dim: int) -> int:
-    """Token stride of [tokens][heads][dim] rows."""
+def _new_rows(where: str, dev: int, name: str, t: Optional[torch.Tensor], kind, tokens: int, heads: int, dim: int):
+    """Address and token stride of [tokens][heads][dim] rows."""
+    if t is None:
+        return None, 0
     if t.dtype is not kind or t.get_device() != dev:
         _refuse(where, dev, name, t, kind, 0)
     strides = t.stride()
     if t.shape != (tokens, heads, dim) or (tokens and (strides[2] != 1 or (heads > 1 and strides[1] != dim))):
         raise ValueError(f"{where}: {name} is {tuple(t.shape)} with strides {strides}, not [{tokens}][{heads}][{dim}] with contiguous heads")
-    return strides[0] if tokens > 1 else max(strides[0], heads * dim)
+    return t.data_ptr(), strides[0] if tokens > 1 else max(strides[0], heads * dim)
 
 
 _last_ints = ((), None)   # the host array of the last call's numbers, found again by the numbers
@@ -577,15 +585,16 @@ def chunkkv_paged_compact(prob: Problem, pages: Pages, reuse: int, k: Sequence, 
 
 def chunkkv_paged_append(pages: Pages, n_new: Sequence[int], q, k, v, positions, q_norm, k_norm, eps: float, inv_freq, interleaved: bool, q_out,
                          page_table, k_pages, v_pages, kv_len, kv_len_out, token_pos, token_weight, stream=None) -> None:
-    """q, k, v: [tokens][heads][head_dim], views of a fused projection among them; rotary_dim is twice inv_freq's length."""
+    """q, k, v: [tokens][heads][head_dim], views of a fused projection among them, None without tokens; rotary_dim is twice inv_freq's length."""
     where, dev, kind = "chunkkv_paged_append", _device(), _KINDS.get(pages.dtype)
     batch, hkv, d, cp = pages.batch, pages.n_kv_heads, pages.head_dim, pages._c()
     numbers, new = _ints(n_new)
     if len(numbers) != batch:
         raise ValueError(f"{where}: n_new has {len(numbers)} entries for {batch} sequences")
     tokens, heads = max(0, sum(numbers)), batch * hkv
-    q_tok = 0 if q is None else _new_rows(where, dev, "q", q, kind, tokens, pages.n_q_heads, d)
-    k_tok, v_tok = _new_rows(where, dev, "k", k, kind, tokens, hkv, d), _new_rows(where, dev, "v", v, kind, tokens, hkv, d)
+    qp, q_tok = _new_rows(where, dev, "q", q, kind, tokens, pages.n_q_heads, d)
+    kp, k_tok = _new_rows(where, dev, "k", k, kind, tokens, hkv, d)
+    vp, v_tok = _new_rows(where, dev, "v", v, kind, tokens, hkv, d)
     at, qn, kn, out, table, length, after, freq, pos, weight = _arrays(
         where, dev, ("positions", positions, _I32, tokens), ("q_norm", q_norm, kind, d), ("k_norm", k_norm, kind, d),
         ("q_out", q_out, kind, tokens * pages.n_q_heads * d), ("page_table", page_table, _I32, batch * pages.table_pitch), ("kv_len", kv_len, _I32, heads),
@@ -593,7 +602,7 @@ def chunkkv_paged_append(pages: Pages, n_new: Sequence[int], q, k, v, positions,
         ("token_weight", token_weight, _F32, heads * pages.slot_pitch))
     room = pages._pool_elements()
     _check(load_library().chunkkv_paged_append(
-        cp, new, None if q is None else q.data_ptr(), q_tok, k.data_ptr(), k_tok, v.data_ptr(), v_tok, at, qn, kn, eps, freq,
+        cp, new, qp, q_tok, kp, k_tok, vp, v_tok, at, qn, kn, eps, freq,
         0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, out, table, _pool(where, dev, "k_pages", k_pages, kind, room),
         _pool(where, dev, "v_pages", v_pages, kind, room), length, after, pos, weight, _stream(stream, dev)), where)
 
