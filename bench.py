@@ -39,16 +39,20 @@ def algorithmic_bytes(wl, n_keep, n_layers, reuse):
             "stack": leaders * k_read + n_layers * gather}
 
 
+# The sources of the kernels whose traffic profiles/hbm_traffic.json holds (scoring, selection, gather) and of what launches them.  A kernel
+# of another call can change without them: decoding, the quality metrics, caches in pages.
+TRAFFIC_SOURCES = ("api.hip", "compact.hip", "internal.h", "score_bf16.hip", "score_f16.hip", "score_f32.hip", "score_impl.h", "score_misc.hip", "score_plan.h",
+                   "score_single.h", "score_single_bf16.hip", "score_single_f16.hip", "select.h", "topk.hip")
+
+
 def csrc_hash():
-    """sha256 over the library's sources (file names and contents, sorted): what profiles/hbm_traffic.json is tied to."""
+    """sha256 over these sources (names and contents): what profiles/hbm_traffic.json is tied to."""
     import hashlib
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2502_00299_amd", "csrc")
-    for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".h")):
-            h.update(name.encode())
-            h.update(open(os.path.join(d, name), "rb").read())
-    h.update(open(os.path.join(ROOT, "include", "chunkkv.h"), "rb").read())
+    for name in TRAFFIC_SOURCES:
+        h.update(name.encode())
+        h.update(open(os.path.join(d, name), "rb").read())
     return h.hexdigest()
 
 
