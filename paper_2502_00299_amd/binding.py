@@ -117,13 +117,14 @@ class Problem(_KeepsStruct):
         if kept is None or kept[0] != now:
             cp = self.as_c()
             plain = tuple(tuple(map(int, x)) if isinstance(x, tuple) else float(x) if isinstance(x, float) else int(x) for x in now)
-            kept = self._kept = (plain, cp, C.byref(cp), self._kv_elements())
+            kept = self._kept = (plain, cp, C.byref(cp), self._kv_elements(cp))
         return kept[2]
 
-    def _kv_elements(self) -> int:
-        """Elements from the start of a cache to the end of its last row."""
-        return (max(int(base) + (int(rows) - 1) * int(self.kv_stride_tok) for base, rows in zip(self.kv_base, self.seqlen))
-                + (int(self.n_kv_heads) - 1) * int(self.kv_stride_head) + int(self.head_dim))
+    @staticmethod
+    def _kv_elements(cp) -> int:
+        """Elements from the start of a cache to the end of its last row, by the struct: a list that is too short goes on with zeros there."""
+        return (max((cp.kv_base[b] + (cp.seqlen[b] - 1) * cp.kv_stride_tok for b in range(cp.batch)), default=0)
+                + (cp.n_kv_heads - 1) * cp.kv_stride_head + cp.head_dim)
 
     def __getstate__(self):
         return self.__dict__.copy()   # the kept struct is neither copied nor pickled

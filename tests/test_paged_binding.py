@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import paper_2502_00299_amd as ckv
 from paper_2502_00299_amd import binding
 
 ROOM = 4 * 2 * 16 * 64
@@ -37,3 +38,19 @@ def test_two_lists_of_pools(layers, kind):
             ts[-1] = good
     with pytest.raises(ValueError, match="k_pages is on device"):
         binding._pool_pairs("here", 0, ("k_pages", "v_pages"), ks, vs, torch.bfloat16, ROOM)
+
+
+def test_problems_without_sequences_are_the_library_s_to_refuse():
+    p = ckv.Problem(4, 2, 64, 16, 8, ckv.BF16, [], [], [], 64, 64, out_base=[], sel_cap=1, score_cap=1)
+    assert ckv.chunkkv_workspace_bytes(p, 1, 1) == 0 and ckv.chunkkv_decode_workspace_bytes(p, False) == 0
+
+
+def test_reach_of_full_caches():
+    """What has to be behind a cache's first element: by every sequence that the library sees, one past a short list of bases too."""
+    d, hkv = 64, 2
+    prob = ckv.Problem(4, hkv, d, 16, 8, ckv.BF16, [100, 40], [8, 8], [0, 100 * hkv * d], d, hkv * d)
+    prob._c()
+    assert prob._kept[3] == 140 * hkv * d
+    prob.seqlen, prob.kv_base = [100, 4000], [0]
+    prob._c()
+    assert prob._kept[1].kv_base[1] == 0 and prob._kept[3] == 4000 * hkv * d
