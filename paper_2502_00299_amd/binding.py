@@ -213,8 +213,18 @@ class Pages(_KeepsStruct):
         most = (C.c_int32 * B)(*[int(x) for x in self.max_tokens])
         cp = _CPages(B, self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype, self.softmax_scale, self.page_tokens, self.n_pages,
                      self.table_pitch, self.slot_pitch, self.stride_page, self.stride_head, self.stride_tok, most)
+        # a number that does not fit its type would be another one for the library than for the checks of sizes
+        for name, kind in _CPages._fields_[:-1]:
+            if kind is not C.c_float and getattr(cp, name) != getattr(self, name, B):
+                raise ValueError(f"chunkkv_pages.{name}: {getattr(self, name)} does not fit")
+        _fits("chunkkv_pages.max_tokens", most, self.max_tokens)
         cp._keep = most
         return cp
+
+
+def _fits(what: str, host, numbers: Sequence[int]):
+    if list(host) != [int(x) for x in numbers]:
+        raise ValueError(f"{what}: {list(numbers)} does not fit")
 
 
 _lib = None
@@ -560,24 +570,26 @@ def _ints(xs: Sequence[int]):
     last = _last_ints
     if last[0] != key:
         key = tuple(map(int, key))
-        last = _last_ints = (key, (C.c_int32 * len(key))(*key))
+        host = (C.c_int32 * len(key))(*key)
+        _fits("host array", host, key)
+        last = _last_ints = (key, host)
     return last
 
 
 def chunkkv_paged_compact(prob: Problem, pages: Pages, reuse: int, k: Sequence, v: Sequence, sel_chunk, sel_len, sel_count, token_importance,
                           page_table, k_pages: Sequence, v_pages: Sequence, kv_len, token_pos, token_weight, stream=None) -> None:
     where, n, dev = "chunkkv_paged_compact", len(k), _device()
-    heads, groups, cp = pages.batch * pages.n_kv_heads, -(-n // max(1, reuse)), pages._c()
+    reuse = min(reuse, n)   # of all layers, at most
+    heads, groups, cp, full = pages.batch * pages.n_kv_heads, -(-n // max(1, reuse)), pages._c(), prob._c()
+    _, seen, _, reach = prob._kept   # of the struct just returned: sizes are the library's
     if not len(v) == len(k_pages) == len(v_pages) == n or (token_importance is not None and len(token_importance) != groups):
         raise ValueError(f"{where}: lists of {n}, {len(v)}, {len(k_pages)} and {len(v_pages)} layers")
-    sel, slots, kind, room = groups * heads * prob.sel_cap, n * heads * pages.slot_pitch, _KINDS.get(pages.dtype), pages._pool_elements()
+    sel, slots, kind, room = groups * heads * seen.sel_cap, n * heads * pages.slot_pitch, _KINDS.get(pages.dtype), pages._pool_elements()
     chunks, lens, count, table, length, pos, weight = _arrays(
         where, dev, ("sel_chunk", sel_chunk, _I32, sel), ("sel_len", sel_len, _I32, sel), ("sel_count", sel_count, _I32, groups * heads),
         ("page_table", page_table, _I32, pages.batch * pages.table_pitch), ("kv_len", kv_len, _I32, n * heads), ("token_pos", token_pos, _I32, slots),
         ("token_weight", token_weight, _F32, slots))
-    given = None if token_importance is None else _pools(where, dev, "token_importance", token_importance, _F32, heads * prob.score_cap * prob.chunk)
-    full = prob._c()
-    reach = prob._kept[3]   # of the struct just returned
+    given = None if token_importance is None else _pools(where, dev, "token_importance", token_importance, _F32, heads * seen.score_cap * seen.chunk)
     caches, ks, vs = _pool_pairs(where, dev, ("k", "v"), k, v, kind, reach)   # caches, pools: hold the addresses until the call returns
     pools, kp, vp = _pool_pairs(where, dev, ("k_pages", "v_pages"), k_pages, v_pages, kind, room)
     _check(load_library().chunkkv_paged_compact(full, cp, n, reuse, ks, vs, chunks, lens, count, _at(given), table, kp, vp, length, pos, weight,

@@ -54,3 +54,29 @@ def test_reach_of_full_caches():
     prob.seqlen, prob.kv_base = [100, 4000], [0]
     prob._c()
     assert prob._kept[1].kv_base[1] == 0 and prob._kept[3] == 4000 * hkv * d
+
+
+GOOD = dict(n_q_heads=32, n_kv_heads=8, head_dim=128, dtype=ckv.BF16, page_tokens=16, n_pages=100, max_tokens=[848, 17])
+
+
+@pytest.mark.parametrize("name", ["n_q_heads", "n_kv_heads", "page_tokens", "n_pages", "table_pitch", "slot_pitch", "max_tokens"])
+@pytest.mark.parametrize("off", [1 << 32, -(1 << 32)])
+def test_numbers_that_do_not_fit(name, off):
+    """Sizes of which the library would see the lower 32 bits alone, fewer than none for the checks."""
+    p = ckv.Pages(**GOOD)
+    assert ckv.chunkkv_paged_decode_workspace_bytes(p, True) > 0
+    setattr(p, name, [848, 17 + off] if name == "max_tokens" else getattr(p, name) + off)
+    with pytest.raises(ValueError, match="does not fit"):
+        ckv.chunkkv_paged_decode_workspace_bytes(p, True)
+
+
+def test_strides_that_do_not_fit():
+    with pytest.raises(ValueError, match="does not fit"):
+        ckv.chunkkv_paged_decode_workspace_bytes(ckv.Pages(**GOOD, stride_tok=128, stride_head=2048, stride_page=(1 << 64) + 16384), True)
+
+
+def test_host_numbers_that_do_not_fit():
+    for numbers in ([(1 << 32) + 3, 1], [1 - (1 << 32), 2]):
+        with pytest.raises(ValueError, match="does not fit"):
+            binding._ints(numbers)
+    assert list(binding._ints([3, 2 ** 31 - 1])[1]) == [3, 2 ** 31 - 1]
