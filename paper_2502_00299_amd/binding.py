@@ -558,7 +558,7 @@ def _new_rows(where: str, dev: int, name: str, t: Optional[torch.Tensor], kind, 
     strides = t.stride()
     if t.shape != (tokens, heads, dim) or (tokens and (strides[2] != 1 or (heads > 1 and strides[1] != dim))):
         raise ValueError(f"{where}: {name} is {tuple(t.shape)} with strides {strides}, not [{tokens}][{heads}][{dim}] with contiguous heads")
-    return t.data_ptr(), strides[0] if tokens > 1 else max(strides[0], heads * dim)
+    return t.data_ptr(), strides[0] if tokens > 1 else heads * dim   # that of a single row can be anything
 
 
 _last_ints = ((), None)   # the host array of the last call's numbers, found again by the numbers

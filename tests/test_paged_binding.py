@@ -80,3 +80,14 @@ def test_host_numbers_that_do_not_fit():
         with pytest.raises(ValueError, match="does not fit"):
             binding._ints(numbers)
     assert list(binding._ints([3, 2 ** 31 - 1])[1]) == [3, 2 ** 31 - 1]
+
+
+@pytest.mark.parametrize("tokens", [0, 1])
+@pytest.mark.parametrize("pitch", [0, 1, 385, 4096])
+def test_rows_without_a_next_one(tokens, pitch):
+    """The stride of an axis of one token is not looked at: rows of 384 elements, 385 apart in something longer."""
+    x = torch.zeros(9000, dtype=torch.bfloat16).as_strided((tokens, 3, 128), (pitch, 128, 1))
+    at, stride = binding._new_rows("here", -1, "k", x, torch.bfloat16, tokens, 3, 128)
+    assert stride == 384 and at == x.data_ptr()
+    y = torch.zeros(9000, dtype=torch.bfloat16).as_strided((2, 3, 128), (400, 128, 1))
+    assert binding._new_rows("here", -1, "k", y, torch.bfloat16, 2, 3, 128) == (y.data_ptr(), 400)
