@@ -115,7 +115,8 @@ int chunkkv_chunk_topk(const chunkkv_problem *prob, const float *chunk_scores, i
 
 /* Algorithm 1, compression + concatenation: K'[h] = rows of K[h] named by the selection, in order,
  * followed by the window rows [P, L); same for V.  Pure copies, bit-exact.  The selection must obey
- * the descriptor rules above and keep exactly n_keep_b tokens (not checked on the device).         */
+ * the descriptor rules above, keep exactly n_keep_b tokens and have ceil(n_keep_b / c) + 1 entries at
+ * most, as many as there are where one chunk is cut (not checked on the device).                   */
 int chunkkv_compact(const chunkkv_problem *prob, const void *k, const void *v, const int32_t *sel_chunk,
                     const int32_t *sel_len, const int32_t *sel_count, void *k_out, void *v_out,
                     void *stream);
@@ -299,7 +300,7 @@ int chunkkv_decode_attention_static(const chunkkv_problem *prob, int32_t compact
 typedef struct {
   int32_t batch, n_q_heads, n_kv_heads, head_dim;
   int32_t dtype;                /* chunkkv_dtype: of queries, new tokens and pages                             */
-  float softmax_scale;          /* 0 selects 1/sqrt(head_dim)                                                  */
+  float softmax_scale;          /* 0 selects 1/sqrt(head_dim); below 2^-126 taken as that                      */
   int32_t page_tokens;          /* slots of a page                                                             */
   int32_t n_pages;              /* pages of a pool, >= 1                                                       */
   int32_t table_pitch;          /* entries of a row of page_table, >= max_b ceil(max_tokens_b / page_tokens)   */
@@ -334,7 +335,8 @@ int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *page
  *   y = x * 1/sqrt(mean(x^2) + eps) * norm                                   (norm NULL: y = x)
  *   with r = rotary_dim and a_i = positions[t] * inv_freq[i], 0 <= i < r/2, the pair (y_i, y_{i+r/2}), or with
  *   `interleaved` (y_2i, y_2i+1), becomes (y_i cos a_i - y_j sin a_i, y_j cos a_i + y_i sin a_i); elements from r on stay.
- *   Product and reduction to a revolution are in double: 3 * 2^-25 of a revolution at a position of 2^31, 2^-34 at 2^20.
+ *   Product and reduction to a revolution are in double: 3 * 2^-25 of a revolution at a position of 2^31, 2^-34 at 2^20.  The
+ *   part of a revolution that is left is rounded to fp32, 2^-26 of one at most, and its sine and cosine are fp32.
  * Values, and with neither norm nor rotation keys and queries too, are copied bit by bit.
  *   n_new        HOST int32 [batch], each >= 0 (all 0: only kv_len_out is written, arrays of tokens may be NULL)
  *   q, k, v      device rows [T][heads][d] with a token stride in elements, heads contiguous: rows of a fused projection
@@ -343,10 +345,13 @@ int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *page
  *   q_norm, k_norm   device [d] in the storage type, or NULL
  *   inv_freq     device float [rotary_dim / 2], or NULL with rotary_dim 0; rotary_dim a multiple of 16, <= head_dim
  *   q_out        device [T][Hq][d];  must not alias an input
- *   kv_len       read: tokens before;  kv_len_out  written: tokens after; may be kv_len itself
+ *   kv_len       read: tokens before;  kv_len_out  written: tokens after; may be kv_len itself (a sequence without a new token
+ *                then keeps the number that is there, clamped or not)
  *   token_pos, token_weight   NULL, or written for the new slots (the position; 0)
  * A token past max_tokens_b is not stored and not counted; its query is computed all the same.
- * One launch per 64 sequences, two where kv_len_out is kv_len and a sequence has more than one new token.              */
+ * One launch per 64 sequences, with the lengths, as long as nobody reads a length that it has written and each is some token's to
+ * write.  Two where kv_len_out is kv_len and any sequence of the call has more than one new token, and where kv_len_out is another
+ * array and any sequence has none.                                                                                      */
 int chunkkv_paged_append(const chunkkv_pages *pages, const int32_t *n_new, const void *q, int64_t q_stride_tok,
                          const void *k, int64_t k_stride_tok, const void *v, int64_t v_stride_tok,
                          const int32_t *positions, const void *q_norm, const void *k_norm, float eps,
@@ -360,7 +365,7 @@ int chunkkv_paged_append(const chunkkv_pages *pages, const int32_t *n_new, const
  *   token_weight  NULL, or += for every slot the sum over the g heads of its softmax weight, in fp32, in a fixed order
  *   workspace     chunkkv_paged_decode_workspace_bytes(pages, token_weight != NULL) bytes (0 = invalid), contents scratch
  * Precision as chunkkv_decode_attention: products and sums in fp32, softmax weights exact to fp32 (fp16: to 2^-72 of
- * the largest).  Slots that hold no token may hold any bits; a NaN or an infinity in a slot that does gives undefined
+ * the largest), also those that token_weight receives, and beside logits of any finite size; lse is rounded at its own size.  Slots that hold no token may hold any bits; a NaN or an infinity in a slot that does gives undefined
  * outputs of its kv-head's query heads.  The same call on the same inputs gives the same bits.                           */
 size_t chunkkv_paged_decode_workspace_bytes(const chunkkv_pages *pages, int32_t with_weights);
 int chunkkv_paged_decode_attention(const chunkkv_pages *pages, const int32_t *page_table, const int32_t *kv_len,

@@ -5,7 +5,8 @@
 // has one reader per token.  Per row: sum of squares over the lanes (DPP), scale, rotation, one rounding, store.
 // Bound by HBM for prompts (8192 tokens of 32 + 8 + 8 heads, bf16, 38 us, 5.3 TB/s), by latency for single ones (8 tokens 3.6 us from a graph).
 // Angles: position * inv_freq / 2 pi in double, reduced to a part of a revolution there (off by 3 * 2^-25 of one at a
-// position of 2^31, by 2^-34 at 2^20), sine and cosine of that part in fp32.  All rows of a token have the same angles: a
+// position of 2^31, by 2^-34 at 2^20).  That part is rounded to fp32, by 2^-26 of a revolution at most, which is 1.6 * 2^-24 of the
+// rotated pair and less than the roundings of sine, cosine and products beside it; sine and cosine in fp32.  All rows of a token have the same angles: a
 // wavefront's row groups form a share of them each and exchange them, once for all the rows that it takes.
 // The two halves of a pair lie in lanes LPR/2 apart where the whole head turns (one or two DPP moves), further in where a
 // part of it does, in one lane where neighbours are pairs.
