@@ -335,8 +335,8 @@ int chunkkv_paged_compact(const chunkkv_problem *prob, const chunkkv_pages *page
  *   y = x * 1/sqrt(mean(x^2) + eps) * norm                                   (norm NULL: y = x)
  *   with r = rotary_dim and a_i = positions[t] * inv_freq[i], 0 <= i < r/2, the pair (y_i, y_{i+r/2}), or with
  *   `interleaved` (y_2i, y_2i+1), becomes (y_i cos a_i - y_j sin a_i, y_j cos a_i + y_i sin a_i); elements from r on stay.
- *   Product and reduction to a revolution are in double: 3 * 2^-25 of a revolution at a position of 2^31, 2^-34 at 2^20.  The
- *   part of a revolution that is left is rounded to fp32, 2^-26 of one at most, and its sine and cosine are fp32.
+ *   Product and reduction to a revolution are in double: 3 * 2^-25 of a revolution at a position of 2^31, 2^-34 at 2^20.  Sine
+ *   and cosine of it are fp32, off by 1.6 * 2^-24 at most beside that.
  * Values, and with neither norm nor rotation keys and queries too, are copied bit by bit.
  *   n_new        HOST int32 [batch], each >= 0 (all 0: only kv_len_out is written, arrays of tokens may be NULL)
  *   q, k, v      device rows [T][heads][d] with a token stride in elements, heads contiguous: rows of a fused projection

@@ -5,9 +5,10 @@
 // has one reader per token.  Per row: sum of squares over the lanes (DPP), scale, rotation, one rounding, store.
 // Bound by HBM for prompts (8192 tokens of 32 + 8 + 8 heads, bf16, 38 us, 5.3 TB/s), by latency for single ones (8 tokens 3.6 us from a graph).
 // Angles: position * inv_freq / 2 pi in double, reduced to a part of a revolution there (off by 3 * 2^-25 of one at a
-// position of 2^31, by 2^-34 at 2^20).  That part is rounded to fp32, by 2^-26 of a revolution at most, which is 1.6 * 2^-24 of the
-// rotated pair and less than the roundings of sine, cosine and products beside it; sine and cosine in fp32.  All rows of a token have the same angles: a
-// wavefront's row groups form a share of them each and exchange them, once for all the rows that it takes.
+// position of 2^31, by 2^-34 at 2^20).  Sine and cosine in fp32 of that part rounded to fp32, which takes up to 2^-26 of a
+// revolution or 1.6 * 2^-24 in radians from it, and the first-order step back over what was taken (0.03 us of a single token's
+// 3.0).  All rows of a token have the same angles: a wavefront's row groups form a share of them each and exchange them, once
+// for all the rows that it takes.
 // The two halves of a pair lie in lanes LPR/2 apart where the whole head turns (one or two DPP moves), further in where a
 // part of it does, in one lane where neighbours are pairs.
 #include "paged.h"
@@ -96,7 +97,11 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedAppendArgs 
       const int f = TURN == kNeighbours ? x0 / 2 + k : (x0 < half ? x0 + k : x0 - half + k);
       double rev = turns ? (double)position * (double)a.inv_freq[f] * 0.15915494309189535 : 0.0;
       rev -= __builtin_rint(rev);
-      sincospif(2.f * (float)rev, &s_own[i], &c_own[i]);
+      const float part = (float)rev, rest = (float)(rev - (double)part) * 6.2831853f;   // in radians
+      float s, c;
+      sincospif(2.f * part, &s, &c);
+      s_own[i] = __builtin_fmaf(c, rest, s);
+      c_own[i] = __builtin_fmaf(-s, rest, c);
     }
 #pragma unroll
     for (int k = 0; k < NA; ++k) {
