@@ -388,6 +388,97 @@ int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int3
                         const int32_t *page_table, void *const *k_pages, void *const *v_pages, int32_t *kv_len,
                         int32_t *token_pos, float *token_weight, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- A cache that many queries read -----------------------------------------------------------------------------
+ * A compressed document (Algorithm 1's K', V') is made once and read by many: the tokens of a question attend to all of it, and a
+ * batch of sequences goes on behind it.  The calls below rotate the keys and window queries it is made from, and attend to it with
+ * any number of queries.  Conventions, errors and streams as above; all of the calls can be captured into a graph, the host arrays are
+ * then those of the capture.  A workspace may be shared by calls that run one after the other.                                    */
+
+/* Frequencies of a rotation by position for a context `factor` times as long as the one that was trained, on the host:
+ *   f_i = base^(-2 i / rotary_dim),  r_i = trained_tokens * f_i / (2 pi)  turns within the trained context,
+ *   inv_freq[i] = f_i * s_i + f_i / factor * (1 - s_i),  s_i = 0 up to `slow` turns, 1 from `fast` turns on, linear between
+ * (NTK-by-parts, arXiv 2309.00071 Section 3.2; `slow` = `fast` is a step, factor 1 leaves base^(-2 i / rotary_dim), and trained_tokens 0 divides
+ * all frequencies, which is position interpolation).  In double, rounded once.  base > 1, factor >= 1, 0 <= slow <= fast, rotary_dim even.
+ *   inv_freq   HOST float [rotary_dim / 2]; a copy of it on the device is what chunkkv_rotate and chunkkv_paged_append take          */
+int chunkkv_rotary_frequencies(int32_t rotary_dim, double base, double factor, double slow, double fast, double trained_tokens, float *inv_freq);
+
+/* Rows of heads, in and out: row (sequence b, token t, head h) starts at element b*stride_seq + t*stride_tok + h*stride_head, its
+ * head_dim elements are contiguous, rows are 16-byte aligned.  Rows of a fused projection and those of a cache both fit, in different
+ * orders too.  In place (out == in) the strides have to be the same.                                                              */
+typedef struct {
+  const void *in;
+  void *out;
+  int32_t n_heads;
+  int64_t in_stride_seq, in_stride_head, in_stride_tok;
+  int64_t out_stride_seq, out_stride_head, out_stride_tok;
+} chunkkv_rows;
+
+/* Queries and keys of a prompt, or of a step, rotated by position: in fp32, rounded to the storage type once,
+ *   with r = rotary_dim and a_i = positions[b][t] * inv_freq[i], 0 <= i < r/2, the pair (x_i, x_{i+r/2}), or with `interleaved`
+ *   (x_2i, x_2i+1), becomes magnitude * (x_i cos a_i - x_j sin a_i, x_j cos a_i + x_i sin a_i); elements from r on are copied.
+ * Sine and cosine as in chunkkv_paged_append, which rotates tokens on their way into pages.  Keys that are in a cache move from position p
+ * to p' by a rotation by p' - p; one by -p is the inverse and, but for the magnitude's place, the gradient.
+ *   dtype, head_dim    storage type; 64 or 128
+ *   q, k               either may be NULL
+ *   positions          device int32 [n_seq][n_tokens], of any sign
+ *   inv_freq           device float [rotary_dim / 2]; rotary_dim a multiple of 16, 16 to head_dim
+ *   magnitude          > 0 and finite, or 0, which selects 1: what cosine and sine are multiplied by (a long context's scale of attention)
+ * Up to 2^24 tokens and 65536 heads of a kind.  n_seq or n_tokens of 0: nothing is done.  One launch.                                  */
+int chunkkv_rotate(int32_t dtype, int32_t head_dim, int32_t n_seq, int32_t n_tokens, const chunkkv_rows *q, const chunkkv_rows *k,
+                   const int32_t *positions, const float *inv_freq, int32_t rotary_dim, int32_t interleaved, float magnitude, void *stream);
+
+/* Attention of any number of queries to states of another length, without an order between them: a question's tokens over a
+ * compressed cache, a decoder's over an encoder's states.  Query head i of every token of sequence b attends to all states of kv-head
+ * i / g (g = Hq / Hkv):  out = sum_s softmax_s(scale * q . k_s) v_s.
+ * Token t of query head h of sequence b starts at element q_base[b] + t*q_stride_tok + h*q_stride_head, its output at out_base[b] +
+ * t*out_stride_tok + h*out_stride_head, state s of kv-head h of K and V at kv_base[b] + s*kv_stride_tok + h*kv_stride_head; rows have
+ * head_dim contiguous elements and are 16-byte aligned.
+ * Limits: head_dim 64 or 128; up to 1023 kv-heads and 256 query heads per kv-head; up to 2^24 states of a sequence, up to 4 MB apart;
+ * 2^30 tokens, and as many query rows (tokens times g) of a sequence.                                                             */
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim;
+  int32_t dtype;                /* chunkkv_dtype: of queries, states and outputs                               */
+  float softmax_scale;          /* 0 selects 1/sqrt(head_dim); below 2^-126 taken as that                      */
+  const int32_t *q_len;         /* host[batch]   query tokens, >= 0                                            */
+  const int32_t *seqlen;        /* host[batch]   states, >= 0                                                  */
+  const int64_t *q_base, *kv_base, *out_base;   /* host[batch]   element offsets                               */
+  int64_t q_stride_head, q_stride_tok, kv_stride_head, kv_stride_tok, out_stride_head, out_stride_tok;
+  int32_t mask_pitch;           /* bytes of a row of kv_mask, >= max_b seqlen_b where there is one             */
+} chunkkv_cross;
+
+/*   kv_len     device int32 [B][Hkv] or NULL: states that there are, clamped to [0, seqlen_b] (heads of a whole-chunk cache differ)
+ *   kv_mask    device bytes [B][mask_pitch] or NULL: 0 takes a state out, for all heads.  K and V of a state that is taken out, by
+ *              the mask or by kv_len, may hold any bits
+ *   out        device, in the storage type; 0 where no state is left
+ *   lse        NULL or device float [sum of q_len][Hq], tokens of sequence 0 first: natural log of the softmax denominator (-inf where no
+ *              state is left).  With it, parts of an attention can be joined: over a cache here, among the tokens themselves elsewhere
+ *   workspace  chunkkv_cross_workspace_bytes(cross) bytes (0 = invalid), contents scratch
+ * Products and sums in fp32.  Softmax weights of 16-bit types are rounded to that type once, to nearest, and normalised by the sum of
+ * the rounded ones (fp16: those below 2^-24 of the largest lose bits, down to 2^-34); outputs are rounded once more, lse not at all below
+ * fp32.  The same call on the same inputs gives the same bits.  A NaN or an infinity in a state that counts gives undefined outputs of
+ * its kv-head's query heads.  One or two launches per 32 sequences.                                                                  */
+size_t chunkkv_cross_workspace_bytes(const chunkkv_cross *cross);
+int chunkkv_cross_attention(const chunkkv_cross *cross, const int32_t *kv_len, const uint8_t *kv_mask, const void *q, const void *k,
+                            const void *v, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* chunkkv_paged_decode_attention for sequences that share a prefix: sequence b attends to all slots of its prefix and to those of
+ * its own, and a prefix is read once for all sequences that share it.  Sequences are ordered by prefix: the first n_sharing[0] share prefix 0.
+ *   prefix       geometry of the prefixes: batch is their number, max_tokens their slots; pages of the same pools, so heads, head_dim,
+ *                dtype, softmax_scale, page_tokens, n_pages and strides are those of `pages` (CHUNKKV_ERR_SHAPE).  slot_pitch is not used
+ *   pages        geometry of the sequences' own slots
+ *   n_sharing    HOST int32 [prefixes], each >= 0; their sum is pages->batch
+ *   prefix_table device int32 [prefixes][prefix->table_pitch];  prefix_len  device int32 [prefixes][Hkv], or NULL: max_tokens
+ *   page_table   device int32 [B][pages->table_pitch];          kv_len      device int32 [B][Hkv], or NULL: max_tokens
+ *   q            device [B][Hq][d], 16-byte aligned;  out  device [B][Hq][d] in the storage type;  lse  NULL or device float [B][Hq]
+ *   workspace    chunkkv_shared_decode_workspace_bytes(prefix, pages, n_sharing) bytes (0 = invalid), contents scratch
+ * No slot in either: out = 0, lse = -inf.  Pages that are not there, rows without a token and precision of weights and outputs as in
+ * chunkkv_paged_decode_attention and chunkkv_cross_attention.  Two launches up to 64 sequences and 16 prefixes.                   */
+size_t chunkkv_shared_decode_workspace_bytes(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing);
+int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing,
+                                    const int32_t *prefix_table, const int32_t *prefix_len, const int32_t *page_table, const int32_t *kv_len,
+                                    const void *q, const void *k_pages, const void *v_pages, void *out, float *lse, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
 /* Scoring has two implementations with the same results (to rounding; both keep logits, exponentials and sums in
  * fp32): a single pass over K (bf16 and fp16 caches of head_dim 128, 65 to 256 window rows per kv-head, chunk
  * sizes 5, 10 and 20; not used when token_importance is requested) and a general two-pass one.
@@ -402,7 +493,7 @@ int chunkkv_paged_evict(const chunkkv_pages *pages, int32_t n_layers, const int3
  *   2 score pass 1 (importance, chunk sums) or the single-pass row reduction
  *   3 chunk sums for c larger than a key tile   4 chunk selection, and that of slots to keep   5 compaction, or selection
  *     and compaction where one kernel does both (short launches; then none under 4), the storing of new tokens and the
- *     moving of kept slots in pages   6 decode attention
+ *     moving of kept slots in pages, rotation   6 decode attention, cross attention, attention behind shared prefixes
  * total_ms and launches are host arrays of CHUNKKV_TIMING_KINDS entries.  Process-wide and not thread-safe:
  * one measurement at a time, no compression calls from other threads meanwhile.  It changes no result.   */
 #define CHUNKKV_TIMING_KINDS 7

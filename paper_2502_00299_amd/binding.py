@@ -26,6 +26,8 @@ SYMBOLS = ("chunkkv_status_string", "chunkkv_workspace_bytes", "chunkkv_score", 
            "chunkkv_decode_attention_static", "chunkkv_quality_workspace_bytes", "chunkkv_quality_metrics",
            "chunkkv_paged_compact", "chunkkv_paged_append", "chunkkv_paged_decode_workspace_bytes", "chunkkv_paged_decode_attention",
            "chunkkv_paged_evict_workspace_bytes", "chunkkv_paged_evict",
+           "chunkkv_rotary_frequencies", "chunkkv_rotate", "chunkkv_cross_workspace_bytes", "chunkkv_cross_attention",
+           "chunkkv_shared_decode_workspace_bytes", "chunkkv_shared_decode_attention",
            "chunkkv_timing_begin",
            "chunkkv_timing_end")
 TIMING_KINDS = ("score_stats", "stats_merge", "score_colsum", "chunk_sums", "chunk_topk", "compact", "decode")
@@ -222,6 +224,100 @@ class Pages(_KeepsStruct):
         return cp
 
 
+class _CCross(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32), ("softmax_scale", C.c_float),
+        ("q_len", C.POINTER(C.c_int32)), ("seqlen", C.POINTER(C.c_int32)), ("q_base", C.POINTER(C.c_int64)), ("kv_base", C.POINTER(C.c_int64)),
+        ("out_base", C.POINTER(C.c_int64)), ("q_stride_head", C.c_int64), ("q_stride_tok", C.c_int64), ("kv_stride_head", C.c_int64), ("kv_stride_tok", C.c_int64),
+        ("out_stride_head", C.c_int64), ("out_stride_tok", C.c_int64), ("mask_pitch", C.c_int32),
+    ]
+
+
+class _CRows(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n_heads", C.c_int32), ("in_stride_seq", C.c_int64), ("in_stride_head", C.c_int64), ("in_stride_tok", C.c_int64),
+                ("out_stride_seq", C.c_int64), ("out_stride_head", C.c_int64), ("out_stride_tok", C.c_int64)]
+
+
+@dataclass
+class Cross(_KeepsStruct):
+    """Python mirror of chunkkv_cross (see include/chunkkv.h for the meaning of every field).  Without bases queries and outputs are packed
+    [sum of q_len][n_q_heads][head_dim]; without a pitch a row of kv_mask is as wide as the longest sequence has states."""
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    dtype: int
+    q_len: Sequence[int]
+    seqlen: Sequence[int]
+    kv_base: Sequence[int]
+    kv_stride_head: int
+    kv_stride_tok: int
+    q_base: Optional[Sequence[int]] = None
+    q_stride_head: int = 0
+    q_stride_tok: int = 0
+    out_base: Optional[Sequence[int]] = None
+    out_stride_head: int = 0
+    out_stride_tok: int = 0
+    mask_pitch: int = 0
+    softmax_scale: float = 0.0
+
+    def __post_init__(self):
+        row, base, at = self.n_q_heads * self.head_dim, [], 0
+        for n in self.q_len:
+            base.append(at)
+            at += int(n) * row
+        if self.q_base is None:
+            self.q_base, self.q_stride_head, self.q_stride_tok = base, self.head_dim, row
+        if self.out_base is None:
+            self.out_base, self.out_stride_head, self.out_stride_tok = list(base), self.head_dim, row
+        if self.mask_pitch == 0:
+            self.mask_pitch = max([0] + [int(n) for n in self.seqlen])
+
+    @property
+    def batch(self) -> int:
+        return len(self.q_len)
+
+    # As the struct of a Problem: kept with the numbers it holds, which are compared on every call.
+    def _c(self):
+        now = (self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype, self.q_stride_head, self.q_stride_tok, self.kv_stride_head, self.kv_stride_tok,
+               self.out_stride_head, self.out_stride_tok, self.mask_pitch, self.softmax_scale, tuple(self.q_len), tuple(self.seqlen), tuple(self.q_base),
+               tuple(self.kv_base), tuple(self.out_base))
+        kept = getattr(self, "_kept", None)
+        if kept is None or kept[0] != now:
+            cp = self.as_c()
+            plain = tuple(tuple(map(int, x)) if isinstance(x, tuple) else float(x) if isinstance(x, float) else int(x) for x in now)
+            kept = self._kept = (plain, cp, C.byref(cp), self._reaches(cp))
+        return kept[2]
+
+    @staticmethod
+    def _reaches(cp):
+        """Elements from the start to the end of the last row of q, of K and V, of out; tokens; bytes of a mask."""
+        def reach(lens, base, heads, head, tok):
+            return max((base[b] + (lens[b] - 1) * tok + (heads - 1) * head + cp.head_dim for b in range(cp.batch) if lens[b] > 0), default=0)
+        return (reach(cp.q_len, cp.q_base, cp.n_q_heads, cp.q_stride_head, cp.q_stride_tok), reach(cp.seqlen, cp.kv_base, cp.n_kv_heads, cp.kv_stride_head, cp.kv_stride_tok),
+                reach(cp.q_len, cp.out_base, cp.n_q_heads, cp.out_stride_head, cp.out_stride_tok), sum(max(0, cp.q_len[b]) for b in range(cp.batch)), cp.batch * cp.mask_pitch)
+
+    def __getstate__(self):
+        return self.__dict__.copy()
+
+    def as_c(self):
+        B = self.batch
+        host = {}
+        for name, kind in (("q_len", C.c_int32), ("seqlen", C.c_int32), ("q_base", C.c_int64), ("kv_base", C.c_int64), ("out_base", C.c_int64)):
+            numbers = getattr(self, name)
+            if len(numbers) != B:
+                raise ValueError(f"chunkkv_cross.{name}: {len(numbers)} entries for {B} sequences")
+            host[name] = (kind * B)(*[int(x) for x in numbers])
+            _fits(f"chunkkv_cross.{name}", host[name], numbers)
+        cp = _CCross(B, self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype, self.softmax_scale, host["q_len"], host["seqlen"], host["q_base"], host["kv_base"],
+                     host["out_base"], self.q_stride_head, self.q_stride_tok, self.kv_stride_head, self.kv_stride_tok, self.out_stride_head, self.out_stride_tok,
+                     self.mask_pitch)
+        for name, kind in _CCross._fields_:
+            if kind in (C.c_int32, C.c_int64) and getattr(cp, name) != getattr(self, name, B):
+                raise ValueError(f"chunkkv_cross.{name}: {getattr(self, name)} does not fit")
+        cp._keep = host
+        return cp
+
+
 def _fits(what: str, host, numbers: Sequence[int]):
     if list(host) != [int(x) for x in numbers]:
         raise ValueError(f"{what}: {list(numbers)} does not fit")
@@ -295,6 +391,18 @@ def load_library(path: Optional[str] = None):
     lib.chunkkv_paged_evict_workspace_bytes.argtypes = [C.POINTER(_CPages), C.c_int32, i32p]
     lib.chunkkv_paged_evict.restype = C.c_int
     lib.chunkkv_paged_evict.argtypes = [C.POINTER(_CPages), C.c_int32, i32p, C.c_int32, i32p, vp, vp, i32p, i32p, f32p, vp, C.c_size_t, vp]
+    lib.chunkkv_rotary_frequencies.restype = C.c_int
+    lib.chunkkv_rotary_frequencies.argtypes = [C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, vp]
+    lib.chunkkv_rotate.restype = C.c_int
+    lib.chunkkv_rotate.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, i32p, f32p, C.c_int32, C.c_int32, C.c_float, vp]
+    lib.chunkkv_cross_workspace_bytes.restype = C.c_size_t
+    lib.chunkkv_cross_workspace_bytes.argtypes = [C.POINTER(_CCross)]
+    lib.chunkkv_cross_attention.restype = C.c_int
+    lib.chunkkv_cross_attention.argtypes = [C.POINTER(_CCross), i32p, vp, vp, vp, vp, vp, f32p, vp, C.c_size_t, vp]
+    lib.chunkkv_shared_decode_workspace_bytes.restype = C.c_size_t
+    lib.chunkkv_shared_decode_workspace_bytes.argtypes = [C.POINTER(_CPages), C.POINTER(_CPages), i32p]
+    lib.chunkkv_shared_decode_attention.restype = C.c_int
+    lib.chunkkv_shared_decode_attention.argtypes = [C.POINTER(_CPages), C.POINTER(_CPages), i32p, i32p, i32p, i32p, i32p, vp, vp, vp, vp, f32p, vp, C.c_size_t, vp]
     lib.chunkkv_decode_attention_static.restype = C.c_int
     lib.chunkkv_decode_attention_static.argtypes = [C.POINTER(_CProblem), C.c_int32, i32p, vp, vp, vp, f32p, f32p, vp]
     _lib = lib
@@ -659,6 +767,107 @@ def chunkkv_paged_evict(pages: Pages, budget: Sequence[int], recent: int, page_t
     pools, kp, vp = _pool_pairs(where, dev, ("k_pages", "v_pages"), k_pages, v_pages, kind, room)   # pools: holds the addresses until the call returns
     _check(load_library().chunkkv_paged_evict(cp, n, _budgets(where, pages, budget), recent, table, kp, vp, length, pos, weight,
                                               *_scratch(where, dev, workspace), _stream(stream, dev)), where)
+
+
+# ---- a cache that many queries read ----
+def chunkkv_rotary_frequencies(rotary_dim: int, base: float, factor: float = 1.0, slow: float = 1.0, fast: float = 32.0, trained_tokens: float = 0.0) -> torch.Tensor:
+    """-> [rotary_dim / 2] floats on the host."""
+    out = torch.empty(max(0, rotary_dim // 2), dtype=torch.float32)
+    _check(load_library().chunkkv_rotary_frequencies(rotary_dim, base, factor, slow, fast, trained_tokens, out.data_ptr()), "chunkkv_rotary_frequencies")
+    return out
+
+
+_DTYPES = {kind: code for code, kind in _KINDS.items()}
+
+
+def _four(where: str, name: str, t: torch.Tensor):
+    """Shape and strides of rows as [seqs][tokens][heads][dim]."""
+    if t.dim() not in (3, 4):
+        raise ValueError(f"{where}: {name} is {tuple(t.shape)}, not [tokens][heads][dim] or [seqs][tokens][heads][dim]")
+    shape, strides = t.shape, t.stride()
+    return (shape, strides) if len(shape) == 4 else ((1, *shape), (0, *strides))
+
+
+def _rows(where: str, dev: int, name: str, x: torch.Tensor, y: Optional[torch.Tensor]):
+    """Struct of rows x and y, and their [seqs][tokens][dim], type."""
+    if y is None or x.shape != y.shape or x.dtype is not y.dtype or x.get_device() != dev or y.get_device() != dev:
+        raise ValueError(f"{where}: {name} is {x.dtype} {tuple(x.shape)} on device {x.get_device()}, its output "
+                         + ("missing" if y is None else f"{y.dtype} {tuple(y.shape)} on device {y.get_device()}") + f"; the call runs on {dev}")
+    (n, t, h, d), (xs, xt, xh, xe) = _four(where, name, x)
+    _, (ys, yt, yh, ye) = _four(where, name, y)
+    if x.numel() and (xe != 1 or ye != 1):
+        raise ValueError(f"{where}: {name} has rows that are not contiguous")
+    # the stride of an axis of one entry can be anything
+    xs, ys = (xs, ys) if n > 1 else (0, 0)
+    xt, yt = (xt, yt) if t > 1 else (0, 0)
+    xh, yh = (xh, yh) if h > 1 else (0, 0)
+    return _CRows(x.data_ptr(), y.data_ptr(), h, xs, xh, xt, ys, yh, yt), (n, t, d), x.dtype
+
+
+def chunkkv_rotate(q, k, positions, inv_freq, interleaved: bool, magnitude: float, q_out, k_out, stream=None) -> None:
+    """q, k and their outputs: [tokens][heads][head_dim] or [seqs][tokens][heads][head_dim], views of any strides, either None; an output may be the input
+    itself.  rotary_dim is twice inv_freq's length."""
+    where, dev = "chunkkv_rotate", _device()
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError(f"{where}: rows without an output, or an output without rows")
+    a = b = None
+    shape, kind = None, None
+    if q is not None:
+        a, shape, kind = _rows(where, dev, "q", q, q_out)
+    if k is not None:
+        b, other, kind_k = _rows(where, dev, "k", k, k_out)
+        if a is not None and (other != shape or kind_k is not kind):
+            raise ValueError(f"{where}: q is {kind} {tuple(q.shape)}, k {kind_k} {tuple(k.shape)}")
+        shape, kind = other, kind_k
+    if shape is None or kind not in _DTYPES:
+        raise ValueError(f"{where}: " + ("neither q nor k" if shape is None else f"{kind} rows"))
+    at, freq = _arrays(where, dev, ("positions", positions, _I32, shape[0] * shape[1]), ("inv_freq", inv_freq, _F32, 0))
+    _check(load_library().chunkkv_rotate(_DTYPES[kind], shape[2], shape[0], shape[1], a and C.byref(a), b and C.byref(b), at, freq,
+                                         0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, magnitude, _stream(stream, dev)), where)
+
+
+def chunkkv_cross_workspace_bytes(cross: Cross) -> int:
+    return int(load_library().chunkkv_cross_workspace_bytes(cross._c()))
+
+
+def chunkkv_cross_attention(cross: Cross, kv_len, kv_mask, q, k, v, out, lse, workspace, stream=None) -> None:
+    """q, k, v, out: tensors whose first element the offsets of `cross` count from; kv_mask: [batch][mask_pitch] of torch.bool or torch.uint8."""
+    where, dev, kind = "chunkkv_cross_attention", _device(), _KINDS.get(cross.dtype)
+    cp = cross._c()
+    q_room, kv_room, out_room, tokens, mask_bytes = cross._kept[3]
+    length, norm = _arrays(where, dev, ("kv_len", kv_len, _I32, cross.batch * cross.n_kv_heads), ("lse", lse, _F32, tokens * cross.n_q_heads))
+    mask = None
+    if kv_mask is not None:
+        mask, = _arrays(where, dev, ("kv_mask", kv_mask, kv_mask.dtype if kv_mask.dtype in (torch.bool, torch.uint8) else torch.bool, mask_bytes))
+    _check(load_library().chunkkv_cross_attention(
+        cp, length, mask, _pool(where, dev, "q", q, kind, q_room), _pool(where, dev, "k", k, kind, kv_room), _pool(where, dev, "v", v, kind, kv_room),
+        _pool(where, dev, "out", out, kind, out_room), norm, *_scratch(where, dev, workspace), _stream(stream, dev)), where)
+
+
+def _sharing(where: str, prefix: Pages, pages: Pages, n_sharing: Sequence[int]):
+    numbers, host = _ints(n_sharing)
+    if len(numbers) != prefix.batch:
+        raise ValueError(f"{where}: n_sharing has {len(numbers)} entries for {prefix.batch} prefixes")
+    return host
+
+
+def chunkkv_shared_decode_workspace_bytes(prefix: Pages, pages: Pages, n_sharing: Sequence[int]) -> int:
+    where = "chunkkv_shared_decode_workspace_bytes"
+    return int(load_library().chunkkv_shared_decode_workspace_bytes(prefix._c(), pages._c(), _sharing(where, prefix, pages, n_sharing)))
+
+
+def chunkkv_shared_decode_attention(prefix: Pages, pages: Pages, n_sharing: Sequence[int], prefix_table, prefix_len, page_table, kv_len, q, k_pages, v_pages, out, lse,
+                                    workspace, stream=None) -> None:
+    where, dev, kind = "chunkkv_shared_decode_attention", _device(), _KINDS.get(pages.dtype)
+    whole, cp, batch, hkv = prefix._c(), pages._c(), pages.batch, pages.n_kv_heads
+    rows, room = batch * pages.n_q_heads, pages._pool_elements()
+    ptable, plength, table, length, qp, op, lp = _arrays(
+        where, dev, ("prefix_table", prefix_table, _I32, prefix.batch * prefix.table_pitch), ("prefix_len", prefix_len, _I32, prefix.batch * hkv),
+        ("page_table", page_table, _I32, batch * pages.table_pitch), ("kv_len", kv_len, _I32, batch * hkv), ("q", q, kind, rows * pages.head_dim),
+        ("out", out, kind, rows * pages.head_dim), ("lse", lse, _F32, rows))
+    _check(load_library().chunkkv_shared_decode_attention(
+        whole, cp, _sharing(where, prefix, pages, n_sharing), ptable, plength, table, length, qp, _pool(where, dev, "k_pages", k_pages, kind, room),
+        _pool(where, dev, "v_pages", v_pages, kind, room), op, lp, *_scratch(where, dev, workspace), _stream(stream, dev)), where)
 
 
 def chunkkv_timing_begin(max_records: int = 4096) -> None:

@@ -13,7 +13,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libchunkkv.so")
 SOURCES = ["api.hip", "compact.hip", "decode.hip", "decode_mfma.hip", "quality.hip", "topk.hip", "score_misc.hip", "score_bf16.hip", "score_f32.hip", "score_f16.hip",
            "score_single_bf16.hip", "score_single_f16.hip", "paged_api.hip", "paged_append.hip", "paged_compact.hip", "paged_decode.hip", "paged_decode_f32.hip", "paged_decode_mfma.hip",
-           "paged_evict.hip"]
+           "paged_evict.hip", "rows_api.hip", "rows_bf16.hip", "rows_f16.hip", "rows_f32.hip", "rows_join.hip", "rotate.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed-fp32 instructions are kept out of the generated code on purpose
@@ -49,7 +49,7 @@ def build(verbose: bool = True) -> str:
     return LIB
 
 
-CHECKED = ["api.hip", "paged_api.hip"]   # every argument check and workspace plan
+CHECKED = ["api.hip", "paged_api.hip", "rows_api.hip"]   # every argument check and workspace plan
 
 
 def build_host_sanitizer_check(out_dir: str, main: str = "host_sanitizer_main") -> str:

@@ -221,6 +221,10 @@ struct PagedEvictArgs {
   int32_t budget[kPagedBatch], max_tokens[kPagedBatch];
 };
 
+// ---- host side, shared by the entry points
+bool fine_scale(float x);
+int check_pages(const chunkkv_pages *p);
+PageGeom geometry(const chunkkv_pages *p, const int32_t *table);
 int launch_paged_append(int dtype, int head_dim, const PagedAppendArgs &a, hipStream_t s);
 int launch_paged_len(const PagedLenArgs &a, hipStream_t s);
 int launch_paged_compact(int row_bytes, const PagedCompactArgs &a, int n_layers, int batch, hipStream_t s);

@@ -5,9 +5,6 @@
 #include "paged.h"
 
 namespace ckv {
-namespace {
-
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Finite and not below zero, by its bits: the build lets the compiler assume that nothing is NaN.
 bool fine_scale(float x) {
@@ -47,6 +44,10 @@ PageGeom geometry(const chunkkv_pages *p, const int32_t *table) {
   g.magic = (uint32_t)((((uint64_t)1 << 32) + g.blocks - 1) / g.blocks);
   return g;
 }
+
+namespace {
+
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // ---- attention: key ranges and workspace -------------------------------------------------------------------------
 struct PagedPlan {

@@ -12,62 +12,9 @@
 // The two halves of a pair lie in lanes LPR/2 apart where the whole head turns (one or two DPP moves), further in where a
 // part of it does, in one lane where neighbours are pairs.
 #include "paged.h"
+#include "rotary.h"
 
 namespace ckv {
-
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-template <int DT, int EPL>
-__device__ __forceinline__ void widen(const u32x4 &r, float (&f)[EPL]) {
-  if constexpr (DT == CHUNKKV_F32) {
-    const f32x4 x = __builtin_bit_cast(f32x4, r);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = x[i];
-  } else if constexpr (DT == CHUNKKV_BF16) {
-    const bf16x8 x = __builtin_bit_cast(bf16x8, r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)x[i];
-  } else {
-    const f16x8 x = __builtin_bit_cast(f16x8, r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)x[i];
-  }
-}
-template <int DT, int EPL>
-__device__ __forceinline__ u32x4 narrow(const float (&f)[EPL]) {   // to nearest, ties to even
-  if constexpr (DT == CHUNKKV_F32) {
-    return __builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]});
-  } else if constexpr (DT == CHUNKKV_BF16) {
-    bf16x8 x;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (__bf16)f[i];
-    return __builtin_bit_cast(u32x4, x);
-  } else {
-    f16x8 x;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (_Float16)f[i];
-    return __builtin_bit_cast(u32x4, x);
-  }
-}
-
-// Value of the lane LPR / 2 further on in its row.
-template <int LPR>
-__device__ __forceinline__ float other_half(float x) {
-  if constexpr (LPR == 8) {
-    const float y = __builtin_amdgcn_update_dpp(0.f, x, 0x141, 0xf, 0xf, false);   // row_half_mirror: 7 - i
-    return __builtin_amdgcn_update_dpp(0.f, y, 0x1B, 0xf, 0xf, false);             // quad_perm [3,2,1,0]
-  } else if constexpr (LPR == 16) {
-    return __builtin_amdgcn_update_dpp(0.f, x, 0x128, 0xf, 0xf, false);            // row_ror:8
-  } else {
-    return __shfl_xor(x, 16);
-  }
-}
-
-// How rows turn: not at all, whole heads by halves, the front of a head by halves, neighbours.
-enum Turn { kNone, kWhole, kFront, kNeighbours };
 
 template <int DT, int HD, int TURN>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedAppendArgs a) {

@@ -1,0 +1,402 @@
+// Host side of the calls for caches that many queries read: argument checks, workspace plans and launches.
+#include <math.h>
+#include <string.h>
+
+#include "rows.h"
+
+namespace ckv {
+namespace {
+
+constexpr int64_t kMostElements = (int64_t)1 << 56;   // strides and bases: what no memory has
+constexpr int kMaxQueryRows = 1 << 30;   // of a sequence (or prefix) and kv-head
+constexpr int kJoinPrefixes = kSharedSegments - kJoinSegments;   // prefixes of a launch: the others of its segments are sequences
+constexpr int kRotateMaxHeads = 1 << 16;
+
+// ---- key ranges ---------------------------------------------------------------------------------------------------
+// Segments of a call, as the plan sees them.
+struct Shape {
+  int rows, most;
+};
+
+int ranges_of(int most, int range) { return most > range ? (most + range - 1) / range : 1; }
+
+// Keys of a range, for all segments of a call: what makes the last workgroup end first, by an estimate in units of keys.  A CU holds
+// `per_cu` workgroups; one costs its keys, kStart for its start and end, and, where ranges are joined, writing and reading its rows.
+constexpr int kStart = 96, kJoin = 64, kLeastRange = 64, kCUs = 256;
+template <typename F>
+int plan_range(int n, F &&shape, int n_kv_heads, int per_cu) {
+  int most = kLeastRange, rows = 1;
+  int64_t keys = 0;                      // of all row tiles
+  for (int i = 0; i < n; ++i) {
+    const Shape x = shape(i);
+    if (x.rows == 0) continue;
+    most = x.most > most ? x.most : most;
+    const int r = x.rows < kRowsWide ? x.rows : kRowsWide;
+    rows = r > rows ? r : rows;
+    keys += (int64_t)rows_tiles(x.rows) * x.most;
+  }
+  const int whole = (most + kRowsTile - 1) / kRowsTile * kRowsTile;
+  auto items = [&](int range) {
+    int64_t w = 0;
+    for (int i = 0; i < n; ++i) {
+      const Shape x = shape(i);
+      if (x.rows > 0) w += (int64_t)rows_tiles(x.rows) * ranges_of(x.most, range);
+    }
+    return w * n_kv_heads;
+  };
+  const int64_t slots = (int64_t)kCUs * per_cu;
+  auto cost = [&](int range, int64_t workgroups) {
+    return (workgroups + slots - 1) / slots * (range + kStart + (range < whole ? 2 * rows : 0)) + (range < whole ? kJoin : 0);
+  };
+  int best = whole;
+  int64_t count = items(whole), least = cost(whole, count);
+  for (int rounds = 1; rounds <= 4 && count <= rounds * slots; ++rounds) {
+    // a short range whose workgroups are so many rounds: from what all keys together allow up, by as much as there are too many
+    int64_t range = (keys * n_kv_heads / (rounds * slots) + kRowsTile) / kRowsTile * kRowsTile, w;
+    if (range < kLeastRange) range = kLeastRange;
+    while (range < whole && (w = items((int)range)) > rounds * slots)
+      range = ((range * w + rounds * slots - 1) / (rounds * slots) + kRowsTile) / kRowsTile * kRowsTile;
+    if (range >= whole) continue;
+    const int64_t x = cost((int)range, w);
+    if (x < least) {
+      best = (int)range;
+      least = x;
+    }
+  }
+  return best;
+}
+
+int per_cu(int dtype, int head_dim) { return dtype == CHUNKKV_F32 && head_dim == 128 ? 1 : 2; }
+
+void set_scale(float given, int head_dim, float *scale, float *scale_log2e) {   // as chunkkv_paged_decode_attention has them
+  const float x = given > 0.f ? given : 1.0f / sqrtf((float)head_dim);
+  *scale = x > FLT_MIN ? x : FLT_MIN;
+  *scale_log2e = *scale < FLT_MAX / 1.4426952f ? *scale * 1.4426950408889634f : FLT_MAX;
+}
+
+size_t partial_bytes(int64_t rows, int head_dim, size_t *off_o) {
+  *off_o = align256((size_t)rows * sizeof(float4));
+  return *off_o + align256((size_t)rows * head_dim * sizeof(float));
+}
+
+// ---- cross attention ------------------------------------------------------------------------------------------------
+int check_cross(const chunkkv_cross *c) {
+  if (!c || !c->q_len || !c->seqlen || !c->q_base || !c->kv_base || !c->out_base) return CHUNKKV_ERR_NULL;
+  if (c->batch < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_q_heads % c->n_kv_heads != 0 || !fine_scale(c->softmax_scale) || c->mask_pitch < 0) return CHUNKKV_ERR_SHAPE;
+  if (c->dtype != CHUNKKV_F32 && c->dtype != CHUNKKV_BF16 && c->dtype != CHUNKKV_F16) return CHUNKKV_ERR_UNSUPPORTED;
+  if (c->head_dim != 64 && c->head_dim != 128) return CHUNKKV_ERR_UNSUPPORTED;
+  const int g = c->n_q_heads / c->n_kv_heads, esz = elem_bytes(c->dtype);
+  if (g > kPagedMaxGroup || c->n_kv_heads > 1023) return CHUNKKV_ERR_UNSUPPORTED;
+  if (c->kv_stride_tok < c->head_dim || c->kv_stride_head < 0 || c->q_stride_head < 0 || c->q_stride_tok < 0 || c->out_stride_head < 0 || c->out_stride_tok < 0) return CHUNKKV_ERR_SHAPE;
+  if (c->kv_stride_tok > (1 << 22) / esz) return CHUNKKV_ERR_UNSUPPORTED;   // 16 rows are reached by 32-bit offsets
+  const int64_t strides[] = {c->kv_stride_tok, c->kv_stride_head, c->q_stride_tok, c->q_stride_head, c->out_stride_tok, c->out_stride_head};
+  for (int64_t x : strides) {
+    if (x > kMostElements) return CHUNKKV_ERR_UNSUPPORTED;
+    if ((x * esz) % 16) return CHUNKKV_ERR_SHAPE;
+  }
+  int64_t tokens = 0;
+  for (int b = 0; b < c->batch; ++b) {
+    if (c->q_len[b] < 0 || c->seqlen[b] < 0 || c->q_base[b] < 0 || c->kv_base[b] < 0 || c->out_base[b] < 0) return CHUNKKV_ERR_SHAPE;
+    if (c->q_base[b] > kMostElements || c->kv_base[b] > kMostElements || c->out_base[b] > kMostElements) return CHUNKKV_ERR_UNSUPPORTED;
+    if ((c->q_base[b] * esz) % 16 || (c->kv_base[b] * esz) % 16 || (c->out_base[b] * esz) % 16) return CHUNKKV_ERR_SHAPE;
+    if (c->seqlen[b] > kPagedMaxTokens || (int64_t)c->q_len[b] * g > kMaxQueryRows) return CHUNKKV_ERR_UNSUPPORTED;
+    tokens += c->q_len[b];
+  }
+  return tokens > kMaxQueryRows ? CHUNKKV_ERR_UNSUPPORTED : CHUNKKV_OK;
+}
+
+struct CrossPlan {
+  int range;
+  int64_t partials;
+  size_t off_o, total;
+};
+Shape cross_shape(const chunkkv_cross *c, int b) { return {c->q_len[b] * (c->n_q_heads / c->n_kv_heads), c->seqlen[b]}; }
+// The launches of a call follow one another on the stream and share the workspace.
+int cross_plan(const chunkkv_cross *c, CrossPlan *pl) {
+  pl->range = plan_range(c->batch, [&](int b) { return cross_shape(c, b); }, c->n_kv_heads, per_cu(c->dtype, c->head_dim));
+  pl->partials = 0;
+  for (int b0 = 0; b0 < c->batch; b0 += kCrossSegments) {
+    int64_t rows = 0, items = 0;
+    for (int b = b0; b < c->batch && b < b0 + kCrossSegments; ++b) {
+      const Shape x = cross_shape(c, b);
+      const int splits = ranges_of(x.most, pl->range);
+      if (splits > 1) rows += (int64_t)splits * c->n_kv_heads * x.rows;
+      items += (int64_t)splits * c->n_kv_heads * rows_tiles(x.rows);
+    }
+    if (rows > INT32_MAX || items > INT32_MAX) return CHUNKKV_ERR_UNSUPPORTED;
+    pl->partials = rows > pl->partials ? rows : pl->partials;
+  }
+  pl->total = partial_bytes(pl->partials, c->head_dim, &pl->off_o);
+  return CHUNKKV_OK;
+}
+
+// ---- attention behind shared prefixes -------------------------------------------------------------------------------
+int check_shared(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *n_sharing) {
+  int rc = check_pages(w);
+  if (rc) return rc;
+  if ((rc = check_pages(p))) return rc;
+  if (!n_sharing) return CHUNKKV_ERR_NULL;
+  if (w->n_q_heads != p->n_q_heads || w->n_kv_heads != p->n_kv_heads || w->head_dim != p->head_dim || w->dtype != p->dtype || w->page_tokens != p->page_tokens ||
+      w->n_pages != p->n_pages || w->table_pitch < 1 || w->stride_page != p->stride_page || w->stride_head != p->stride_head || w->stride_tok != p->stride_tok ||
+      w->softmax_scale != p->softmax_scale)
+    return CHUNKKV_ERR_SHAPE;
+  int64_t total = 0;
+  for (int i = 0; i < w->batch; ++i) {
+    if (n_sharing[i] < 0) return CHUNKKV_ERR_SHAPE;
+    total += n_sharing[i];
+  }
+  if (total != p->batch) return CHUNKKV_ERR_SHAPE;
+  return (int64_t)p->batch * (p->n_q_heads / p->n_kv_heads) > kMaxQueryRows ? CHUNKKV_ERR_UNSUPPORTED : CHUNKKV_OK;
+}
+
+struct SharedPlan {
+  int range;
+  int64_t partials, prefix_partials;
+  size_t off_o, total;
+};
+// Segment i: prefix i, or sequence i - prefixes; one without keys has no rows.
+Shape shared_shape(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *n_sharing, int i) {
+  const int g = p->n_q_heads / p->n_kv_heads;
+  if (i < w->batch) return {w->max_tokens[i] > 0 ? n_sharing[i] * g : 0, w->max_tokens[i]};
+  return {p->max_tokens[i - w->batch] > 0 ? g : 0, p->max_tokens[i - w->batch]};
+}
+int shared_splits(const Shape &x, int range) { return x.rows > 0 ? ranges_of(x.most, range) : 0; }
+int shared_plan(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *n_sharing, SharedPlan *pl) {
+  const int n = w->batch + p->batch;
+  pl->range = plan_range(n, [&](int i) { return shared_shape(w, p, n_sharing, i); }, p->n_kv_heads, per_cu(p->dtype, p->head_dim));
+  pl->partials = 0;
+  int64_t items = 0;
+  for (int i = 0; i < n; ++i) {
+    const Shape x = shared_shape(w, p, n_sharing, i);
+    pl->partials += (int64_t)shared_splits(x, pl->range) * p->n_kv_heads * x.rows;
+    items += (int64_t)shared_splits(x, pl->range) * p->n_kv_heads * rows_tiles(x.rows);
+    if (i == w->batch - 1) pl->prefix_partials = pl->partials;
+  }
+  if (pl->partials > INT32_MAX || items > INT32_MAX) return CHUNKKV_ERR_UNSUPPORTED;
+  pl->total = partial_bytes(pl->partials, p->head_dim, &pl->off_o);
+  return CHUNKKV_OK;
+}
+
+}  // namespace
+}  // namespace ckv
+
+using namespace ckv;
+
+extern "C" {
+
+size_t chunkkv_cross_workspace_bytes(const chunkkv_cross *cross) {
+  CrossPlan pl;
+  if (check_cross(cross) || cross_plan(cross, &pl)) return 0;
+  return pl.total > 256 ? pl.total : 256;   // 0 is an invalid problem
+}
+
+int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const uint8_t *kv_mask, const void *q, const void *k, const void *v,
+                            void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = check_cross(c);
+  if (rc) return rc;
+  CrossPlan pl;
+  if ((rc = cross_plan(c, &pl))) return rc;
+  int64_t tokens = 0;
+  int longest = 0;
+  for (int b = 0; b < c->batch; ++b) {
+    tokens += c->q_len[b];
+    longest = c->seqlen[b] > longest ? c->seqlen[b] : longest;
+  }
+  if (tokens > 0 && (!q || !out || (longest > 0 && (!k || !v)))) return CHUNKKV_ERR_NULL;   // arrays of no tokens may be anything
+  if (kv_mask && c->mask_pitch < longest) return CHUNKKV_ERR_SHAPE;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out)) return CHUNKKV_ERR_SHAPE;
+  if (pl.partials > 0 && (!workspace || workspace_bytes < pl.total || misaligned(workspace))) return CHUNKKV_ERR_WORKSPACE;
+  if (tokens == 0) return CHUNKKV_OK;
+  hipStream_t s = (hipStream_t)stream;
+  const int esz = elem_bytes(c->dtype), g = c->n_q_heads / c->n_kv_heads;
+  int token0 = 0;
+  for (int b0 = 0; b0 < c->batch; b0 += kCrossSegments) {
+    const int nb = c->batch - b0 < kCrossSegments ? c->batch - b0 : kCrossSegments;
+    CrossArgs a;
+    JoinArgs j;
+    memset(&a, 0, sizeof(a));
+    memset(&j, 0, sizeof(j));
+    auto &r = a.r;
+    r.geom.head = c->kv_stride_head * esz; r.geom.tok = c->kv_stride_tok * esz;
+    r.kv_len = kv_len; r.mask = kv_mask; r.mask_pitch = c->mask_pitch;
+    r.q = q; r.k = k; r.v = v; r.out = out; r.lse = lse;
+    r.part_ml = (float4 *)workspace; r.part_o = (float *)((char *)workspace + pl.off_o);
+    r.q_tok = c->q_stride_tok * esz; r.q_head = c->q_stride_head * esz; r.out_tok = c->out_stride_tok * esz; r.out_head = c->out_stride_head * esz;
+    r.n_kv_heads = c->n_kv_heads; r.group = g; r.segments = nb; r.seq0 = b0;
+    set_scale(c->softmax_scale, c->head_dim, &r.scale, &r.scale_log2e);
+    for (int i = 0; i <= kCrossSegments; ++i) r.first[i] = INT32_MAX;
+    j.part_ml = r.part_ml; j.part_o = r.part_o; j.out = out; j.lse = lse; j.out_tok = r.out_tok; j.out_head = r.out_head;
+    j.n_kv_heads = c->n_kv_heads; j.group = g; j.scale = r.scale; j.scale_log2e = r.scale_log2e;
+    for (int i = 0; i <= kJoinSegments; ++i) j.first[i] = INT32_MAX;
+    int items = 0, parts = 0;
+    for (int i = 0; i < nb; ++i) {
+      const int b = b0 + i;
+      const Shape x = cross_shape(c, b);
+      const int splits = ranges_of(x.most, pl.range);
+      r.first[i] = items; r.rows[i] = x.rows; r.most[i] = x.most; r.row0[i] = token0;
+      a.q_base[i] = c->q_base[b] * esz; a.kv_base[i] = c->kv_base[b] * esz; a.out_base[i] = c->out_base[b] * esz;
+      r.part[i] = -1;
+      if (splits > 1 && x.rows > 0) {
+        r.part[i] = parts;
+        const int n = j.segments++;
+        j.first[n] = j.tokens; j.part[n] = parts; j.splits[n] = splits; j.rows[n] = x.rows; j.out_base[n] = a.out_base[i];
+        j.lse_base[n] = (int64_t)token0 * c->n_q_heads;
+        j.tokens += c->q_len[b];
+        parts += splits * c->n_kv_heads * x.rows;
+      }
+      items += splits * c->n_kv_heads * rows_tiles(x.rows);
+      token0 += c->q_len[b];
+    }
+    r.first[nb] = items;
+    if (items == 0) continue;
+    Timed t(kDecode, s);
+    rc = c->dtype == CHUNKKV_BF16 ? launch_cross_bf16(c->head_dim, a, s) : (c->dtype == CHUNKKV_F16 ? launch_cross_f16(c->head_dim, a, s) : launch_cross_f32(c->head_dim, a, s));
+    if (rc) return rc;
+    if (j.segments > 0 && (rc = launch_join(c->dtype, c->head_dim, j, s))) return rc;
+  }
+  return CHUNKKV_OK;
+}
+
+size_t chunkkv_shared_decode_workspace_bytes(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing) {
+  SharedPlan pl;
+  if (check_shared(prefix, pages, n_sharing) || shared_plan(prefix, pages, n_sharing, &pl)) return 0;
+  return pl.total > 256 ? pl.total : 256;
+}
+
+int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing, const int32_t *prefix_table,
+                                    const int32_t *prefix_len, const int32_t *page_table, const int32_t *kv_len, const void *q, const void *k_pages,
+                                    const void *v_pages, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = check_shared(prefix, pages, n_sharing);
+  if (rc) return rc;
+  if (!prefix_table || !page_table || !q || !k_pages || !v_pages || !out) return CHUNKKV_ERR_NULL;
+  if (misaligned(q) || misaligned(k_pages) || misaligned(v_pages) || misaligned(out)) return CHUNKKV_ERR_SHAPE;
+  SharedPlan pl;
+  if ((rc = shared_plan(prefix, pages, n_sharing, &pl))) return rc;
+  if (pl.partials > 0 && (!workspace || workspace_bytes < pl.total || misaligned(workspace))) return CHUNKKV_ERR_WORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  const int d = pages->head_dim, esz = elem_bytes(pages->dtype), g = pages->n_q_heads / pages->n_kv_heads, hkv = pages->n_kv_heads;
+  float4 *part_ml = (float4 *)workspace;
+  float *part_o = (float *)((char *)workspace + pl.off_o);
+  float scale, scale_log2e;
+  set_scale(pages->softmax_scale, d, &scale, &scale_log2e);
+  // Partial rows: those of the prefixes, then those of the sequences.  A launch has up to kJoinPrefixes prefixes and kJoinSegments sequences.
+  int parts[2] = {0, (int)pl.prefix_partials}, before = 0;   // before: sequences of the prefixes before
+  for (int i0 = 0, b0 = 0; i0 < prefix->batch || b0 < pages->batch; i0 += kJoinPrefixes, b0 += kJoinSegments) {
+    const int np = i0 >= prefix->batch ? 0 : (prefix->batch - i0 < kJoinPrefixes ? prefix->batch - i0 : kJoinPrefixes);
+    const int nb = b0 >= pages->batch ? 0 : (pages->batch - b0 < kJoinSegments ? pages->batch - b0 : kJoinSegments);
+    SharedArgs a;
+    memset(&a, 0, sizeof(a));
+    auto &r = a.r;
+    r.geom = geometry(pages, page_table);
+    r.prefix_table = prefix_table; r.prefix_pitch = prefix->table_pitch;
+    r.kv_len = kv_len; r.prefix_len = prefix_len;
+    r.q = q; r.k = k_pages; r.v = v_pages; r.out = out; r.lse = lse;
+    r.part_ml = part_ml; r.part_o = part_o;
+    r.q_tok = r.out_tok = (int64_t)pages->n_q_heads * d * esz; r.q_head = r.out_head = (int64_t)d * esz;
+    r.n_kv_heads = hkv; r.group = g; r.segments = np + nb; r.prefixes = np; r.prefix0 = i0; r.seq0 = b0;
+    r.scale = scale; r.scale_log2e = scale_log2e;
+    for (int i = 0; i <= kSharedSegments; ++i) r.first[i] = INT32_MAX;
+    int items = 0;
+    for (int i = 0; i < np + nb; ++i) {
+      const bool own = i >= np;
+      const Shape x = shared_shape(prefix, pages, n_sharing, own ? prefix->batch + b0 + i - np : i0 + i);
+      const int splits = shared_splits(x, pl.range);
+      r.first[i] = items; r.rows[i] = x.rows; r.most[i] = x.most; r.part[i] = parts[own];
+      r.row0[i] = own ? b0 + i - np : before;
+      if (!own) before += n_sharing[i0 + i];
+      items += splits * hkv * rows_tiles(x.rows);
+      parts[own] += splits * hkv * x.rows;
+    }
+    r.first[np + nb] = items;
+    if (items == 0) continue;
+    Timed t(kDecode, s);
+    rc = pages->dtype == CHUNKKV_BF16 ? launch_shared_bf16(d, a, s) : (pages->dtype == CHUNKKV_F16 ? launch_shared_f16(d, a, s) : launch_shared_f32(d, a, s));
+    if (rc) return rc;
+  }
+  // every sequence's own ranges and those of its prefix, in the order in which their rows were numbered
+  int i = 0, nth = 0, prefix_part = 0, own_part = (int)pl.prefix_partials;
+  for (int b0 = 0; b0 < pages->batch; b0 += kJoinSegments) {
+    const int nb = pages->batch - b0 < kJoinSegments ? pages->batch - b0 : kJoinSegments;
+    JoinArgs j;
+    memset(&j, 0, sizeof(j));
+    j.part_ml = part_ml; j.part_o = part_o; j.out = out; j.lse = lse; j.out_tok = (int64_t)pages->n_q_heads * d * esz; j.out_head = (int64_t)d * esz;
+    j.n_kv_heads = hkv; j.group = g; j.scale = scale; j.scale_log2e = scale_log2e; j.segments = j.tokens = nb;
+    for (int n = 0; n <= kJoinSegments; ++n) j.first[n] = n < nb ? n : INT32_MAX;
+    for (int n = 0; n < nb; ++n, ++nth) {
+      for (; nth == n_sharing[i]; ++i, nth = 0) {
+        const Shape x = shared_shape(prefix, pages, n_sharing, i);
+        prefix_part += shared_splits(x, pl.range) * hkv * x.rows;
+      }
+      const Shape whole = shared_shape(prefix, pages, n_sharing, i), own = shared_shape(prefix, pages, n_sharing, prefix->batch + b0 + n);
+      j.part[n] = own_part; j.splits[n] = shared_splits(own, pl.range); j.rows[n] = own.rows;
+      j.prefix_part[n] = prefix_part; j.prefix_splits[n] = shared_splits(whole, pl.range); j.prefix_rows[n] = whole.rows; j.prefix_row0[n] = nth * g;
+      j.out_base[n] = (b0 + n) * j.out_tok; j.lse_base[n] = (int64_t)(b0 + n) * pages->n_q_heads;
+      own_part += j.splits[n] * hkv * own.rows;
+    }
+    Timed t(kDecode, s);
+    if ((rc = launch_join(pages->dtype, d, j, s))) return rc;
+  }
+  return CHUNKKV_OK;
+}
+
+// ---- rotation ---------------------------------------------------------------------------------------------------------
+int chunkkv_rotary_frequencies(int32_t rotary_dim, double base, double factor, double slow, double fast, double trained_tokens, float *inv_freq) {
+  if (!inv_freq) return CHUNKKV_ERR_NULL;
+  // (a NaN fails none of the opposite comparisons in this build: looked at by its bits)
+  const double given[] = {base, factor, slow, fast, trained_tokens};
+  for (double x : given) {
+    uint64_t u;
+    memcpy(&u, &x, sizeof(u));
+    if ((u & 0x7FF0000000000000ull) == 0x7FF0000000000000ull) return CHUNKKV_ERR_SHAPE;
+  }
+  if (rotary_dim < 2 || rotary_dim % 2 != 0 || base <= 1.0 || factor < 1.0 || slow < 0.0 || fast < slow || trained_tokens < 0.0) return CHUNKKV_ERR_SHAPE;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    const double f = pow(base, -2.0 * i / rotary_dim), turns = trained_tokens * f / 6.283185307179586;
+    const double stay = turns >= fast ? 1.0 : (turns <= slow ? 0.0 : (turns - slow) / (fast - slow));
+    inv_freq[i] = (float)(f * stay + f / factor * (1.0 - stay));
+  }
+  return CHUNKKV_OK;
+}
+
+int chunkkv_rotate(int32_t dtype, int32_t head_dim, int32_t n_seq, int32_t n_tokens, const chunkkv_rows *q, const chunkkv_rows *k, const int32_t *positions,
+                   const float *inv_freq, int32_t rotary_dim, int32_t interleaved, float magnitude, void *stream) {
+  if (dtype != CHUNKKV_F32 && dtype != CHUNKKV_BF16 && dtype != CHUNKKV_F16) return CHUNKKV_ERR_UNSUPPORTED;
+  if (head_dim != 64 && head_dim != 128) return CHUNKKV_ERR_UNSUPPORTED;
+  if (n_seq < 0 || n_tokens < 0 || rotary_dim < 1 || rotary_dim > head_dim || !fine_scale(magnitude)) return CHUNKKV_ERR_SHAPE;
+  if (rotary_dim % 16 != 0) return CHUNKKV_ERR_UNSUPPORTED;
+  const int esz = elem_bytes(dtype);
+  RotateArgs a;
+  memset(&a, 0, sizeof(a));
+  a.tokens = (int64_t)n_seq * n_tokens;
+  const chunkkv_rows *given[2] = {q, k};
+  RotateRows *rows[2] = {&a.q, &a.k};
+  int64_t heads = 0;
+  for (int i = 0; i < 2; ++i) {
+    const chunkkv_rows *x = given[i];
+    if (!x) continue;
+    if (x->n_heads < 1) return CHUNKKV_ERR_SHAPE;
+    if (x->n_heads > kRotateMaxHeads) return CHUNKKV_ERR_UNSUPPORTED;
+    if (a.tokens > 0 && (!x->in || !x->out)) return CHUNKKV_ERR_NULL;
+    if (misaligned(x->in) || misaligned(x->out)) return CHUNKKV_ERR_SHAPE;
+    const int64_t in[3] = {x->in_stride_seq, x->in_stride_head, x->in_stride_tok}, out[3] = {x->out_stride_seq, x->out_stride_head, x->out_stride_tok};
+    for (int e = 0; e < 3; ++e) {
+      if (in[e] > kMostElements || out[e] > kMostElements) return CHUNKKV_ERR_UNSUPPORTED;
+      if (in[e] < 0 || out[e] < 0 || (in[e] * esz) % 16 || (out[e] * esz) % 16) return CHUNKKV_ERR_SHAPE;
+      // in place, a row has to be where it was
+      const int n = e == 0 ? n_seq : (e == 1 ? x->n_heads : n_tokens);
+      if (x->in == x->out && n > 1 && in[e] != out[e]) return CHUNKKV_ERR_SHAPE;
+    }
+    *rows[i] = {x->in, x->out, in[0] * esz, in[1] * esz, in[2] * esz, out[0] * esz, out[1] * esz, out[2] * esz, x->n_heads, x->in == x->out};
+    heads += x->n_heads;
+  }
+  if (heads == 0 || (a.tokens > 0 && !positions) || !inv_freq) return CHUNKKV_ERR_NULL;
+  if (a.tokens > kPagedMaxTokens) return CHUNKKV_ERR_UNSUPPORTED;
+  if (a.tokens == 0) return CHUNKKV_OK;
+  a.positions = positions; a.inv_freq = inv_freq; a.n_tokens = n_tokens; a.rotary = rotary_dim;
+  a.magnitude = magnitude == 0.f ? 1.f : magnitude;
+  hipStream_t s = (hipStream_t)stream;
+  Timed t(kCompact, s);
+  return launch_rotate(dtype, head_dim, interleaved != 0, a, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,13 @@
+// Attention of many query rows over the same keys (rows_attention.h), f16.
+#include "rows_attention.h"
+
+namespace ckv {
+
+int launch_cross_f16(int head_dim, const CrossArgs &a, hipStream_t s) {
+  return head_dim == 128 ? launch_rows_cross<CHUNKKV_F16, 128>(a, s) : launch_rows_cross<CHUNKKV_F16, 64>(a, s);
+}
+int launch_shared_f16(int head_dim, const SharedArgs &a, hipStream_t s) {
+  return head_dim == 128 ? launch_rows<CHUNKKV_F16, 128, true, false>(a, s) : launch_rows<CHUNKKV_F16, 64, true, false>(a, s);
+}
+
+}  // namespace ckv

@@ -1,0 +1,207 @@
+"""Calls for a cache that many queries read, without a GPU: argument checks, workspace sizes, the kept struct, frequencies."""
+import copy
+import ctypes as C
+import math
+import os
+import pickle
+import subprocess
+
+import pytest
+import torch
+
+import paper_2502_00299_amd as ckv
+from paper_2502_00299_amd import binding
+
+FAKE = C.c_void_p(0x1000)   # never dereferenced: every call below fails a check before a launch
+ODD = C.c_void_p(0x1008)
+OK, NULL, SHAPE, UNSUPPORTED, WORKSPACE = range(5)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return ckv.load_library()
+
+
+# ---- cross attention ----
+def good(**kw):
+    d = dict(n_q_heads=32, n_kv_heads=8, head_dim=128, dtype=ckv.BF16, q_len=[3, 700], seqlen=[9000, 17], kv_base=[0, 9000 * 1024], kv_stride_head=128, kv_stride_tok=1024)
+    d.update(kw)
+    return ckv.Cross(**d)
+
+
+def cross(lib, p, n=None, mask=None, q=FAKE, k=FAKE, v=FAKE, out=FAKE, lse=None, ws=FAKE, size=1 << 40):
+    return lib.chunkkv_cross_attention(C.byref(p.as_c()), n, mask, q, k, v, out, lse, ws, size, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_q_heads=30), SHAPE), (dict(n_kv_heads=0), SHAPE), (dict(n_q_heads=0), SHAPE), (dict(q_len=[-1, 3]), SHAPE), (dict(seqlen=[5, -1]), SHAPE), (dict(softmax_scale=-1.0), SHAPE),
+    (dict(softmax_scale=float("nan")), SHAPE), (dict(softmax_scale=float("inf")), SHAPE), (dict(kv_stride_tok=120), SHAPE), (dict(kv_stride_tok=1028), SHAPE), (dict(kv_stride_head=-128), SHAPE),
+    (dict(kv_stride_head=132), SHAPE), (dict(kv_base=[-8, 0]), SHAPE), (dict(kv_base=[4, 0]), SHAPE), (dict(q_base=[0, 4], q_stride_head=128, q_stride_tok=4096), SHAPE),
+    (dict(q_base=[0, 0], q_stride_head=132, q_stride_tok=4096), SHAPE), (dict(q_base=[0, 0], q_stride_head=128, q_stride_tok=-4096), SHAPE),
+    (dict(out_base=[0, 8], out_stride_head=128, out_stride_tok=4100), SHAPE), (dict(out_base=[-8, 8], out_stride_head=128, out_stride_tok=4096), SHAPE),
+    (dict(out_base=[0, 8], out_stride_head=-128, out_stride_tok=4096), SHAPE), (dict(mask_pitch=-1), SHAPE),
+    (dict(head_dim=96, kv_stride_head=96), UNSUPPORTED), (dict(dtype=3), UNSUPPORTED), (dict(n_q_heads=257, n_kv_heads=1), UNSUPPORTED), (dict(n_q_heads=4096, n_kv_heads=4096), UNSUPPORTED),
+    (dict(seqlen=[(1 << 24) + 1, 3]), UNSUPPORTED), (dict(kv_stride_tok=(1 << 21) + 8), UNSUPPORTED), (dict(q_len=[1 << 29, 1]), UNSUPPORTED),
+    (dict(q_len=[(1 << 30) // 4, (1 << 30) // 4 + 1, (1 << 30) // 4, (1 << 30) // 4], seqlen=[1] * 4, kv_base=[0] * 4), UNSUPPORTED),
+    (dict(dtype=ckv.F32, kv_stride_tok=1 << 20, seqlen=[5, 5]), OK), (dict(dtype=ckv.F32, kv_stride_tok=(1 << 20) + 4, seqlen=[5, 5]), UNSUPPORTED),
+])
+def test_cross_problems_that_are_refused(lib, kw, status):
+    p = good(**kw)
+    assert (ckv.chunkkv_cross_workspace_bytes(p) > 0) == (status == OK)
+    if status != OK:
+        assert cross(lib, p) == status
+
+
+def test_cross_pointers_and_workspace(lib):
+    p = good()
+    need = ckv.chunkkv_cross_workspace_bytes(p)
+    assert need > 256
+    for kw, status in [(dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(out=None), NULL), (dict(q=ODD), SHAPE), (dict(k=ODD), SHAPE), (dict(v=ODD), SHAPE),
+                       (dict(out=ODD), SHAPE), (dict(ws=None), WORKSPACE), (dict(ws=ODD), WORKSPACE), (dict(size=need - 1), WORKSPACE)]:
+        assert cross(lib, p, **kw) == status, kw
+    assert cross(lib, good(mask_pitch=8999), mask=FAKE) == SHAPE
+    assert lib.chunkkv_cross_attention(None, None, None, FAKE, FAKE, FAKE, FAKE, None, FAKE, 0, None) == NULL
+    for name in ("q_len", "seqlen", "q_base", "kv_base", "out_base"):
+        c = p.as_c()
+        setattr(c, name, None)
+        assert lib.chunkkv_cross_attention(C.byref(c), None, None, FAKE, FAKE, FAKE, FAKE, None, FAKE, 0, None) == NULL
+    # nothing to do: no pointer is asked for
+    assert cross(lib, good(q_len=[0, 0]), q=None, k=None, v=None, out=None, ws=None, size=0) == OK
+    # more partial rows than 32 bits count
+    assert ckv.chunkkv_cross_workspace_bytes(good(n_q_heads=1, n_kv_heads=1, q_len=[1 << 30], seqlen=[1 << 24], kv_base=[0], kv_stride_tok=128)) >= 256
+
+
+def test_cross_numbers_that_do_not_fit():
+    for name in ("n_q_heads", "kv_stride_head", "mask_pitch", "q_len", "kv_base"):
+        p = good()
+        off = 1 << (64 if name in ("kv_stride_head", "kv_base") else 32)
+        now = getattr(p, name)
+        setattr(p, name, [now[0] + off, now[1]] if isinstance(now, list) else now + off)
+        with pytest.raises((ValueError, OverflowError)):
+            ckv.chunkkv_cross_workspace_bytes(p)
+    for name in ("seqlen", "q_base", "kv_base", "out_base"):
+        p = good()
+        setattr(p, name, getattr(p, name)[:1])
+        with pytest.raises(ValueError, match="entries for 2 sequences"):
+            ckv.chunkkv_cross_workspace_bytes(p)
+
+
+def test_cross_struct_follows_its_fields():
+    p = good()
+    first = ckv.chunkkv_cross_workspace_bytes(p)
+    p.seqlen[0] = 128
+    p.q_len = [1, 1]
+    assert ckv.chunkkv_cross_workspace_bytes(p) < first
+    for other in (copy.deepcopy(p), pickle.loads(pickle.dumps(p))):
+        assert other == p and ckv.chunkkv_cross_workspace_bytes(other) == ckv.chunkkv_cross_workspace_bytes(p)
+    p = good(seqlen=[100, 17], kv_base=[0, 100 * 1024], q_len=[2, 0])
+    p._c()
+    assert p._kept[3] == (2 * 4096, 117 * 1024, 2 * 4096, 2, 200)
+
+
+# ---- shared prefixes ----
+def pages(most, **kw):
+    d = dict(n_q_heads=32, n_kv_heads=8, head_dim=128, dtype=ckv.BF16, page_tokens=16, n_pages=1000, max_tokens=most)
+    d.update(kw)
+    return ckv.Pages(**d)
+
+
+def shared(lib, w, p, n=(2, 1), pt=FAKE, table=FAKE, q=FAKE, k=FAKE, v=FAKE, out=FAKE, ws=FAKE, size=1 << 40):
+    n = None if n is None else (C.c_int32 * len(n))(*n)
+    return lib.chunkkv_shared_decode_attention(C.byref(w.as_c()), C.byref(p.as_c()), n, pt, None, table, None, q, k, v, out, None, ws, size, None)
+
+
+@pytest.mark.parametrize("kw", [dict(n_q_heads=64), dict(n_kv_heads=16), dict(head_dim=64), dict(dtype=ckv.F16), dict(page_tokens=32), dict(n_pages=999), dict(softmax_scale=1.0),
+                                dict(stride_tok=1024, stride_head=128, stride_page=16384), dict(stride_tok=128, stride_head=2048, stride_page=32768)])
+def test_prefixes_of_other_pools(lib, kw):
+    w, p = pages([848, 30], **kw), pages([5, 6, 7])
+    assert ckv.chunkkv_shared_decode_workspace_bytes(w, p, [2, 1]) == 0 and shared(lib, w, p) == SHAPE
+    assert shared(lib, p, w, n=(1, 1, 0)) == SHAPE
+
+
+def test_shared_arguments(lib):
+    w, p = pages([848, 30]), pages([5, 6, 7])
+    need = ckv.chunkkv_shared_decode_workspace_bytes(w, p, [2, 1])
+    assert need > 256
+    for kw, status in [(dict(n=None), NULL), (dict(n=(2, 2)), SHAPE), (dict(n=(2, 0)), SHAPE), (dict(n=(4, -1)), SHAPE), (dict(pt=None), NULL), (dict(table=None), NULL), (dict(q=None), NULL),
+                       (dict(k=None), NULL), (dict(v=None), NULL), (dict(out=None), NULL), (dict(q=ODD), SHAPE), (dict(k=ODD), SHAPE), (dict(v=ODD), SHAPE), (dict(out=ODD), SHAPE),
+                       (dict(ws=None), WORKSPACE), (dict(ws=ODD), WORKSPACE), (dict(size=need - 1), WORKSPACE)]:
+        assert shared(lib, w, p, **kw) == status, kw
+    for bad in (dict(page_tokens=24), dict(head_dim=96), dict(n_q_heads=30)):
+        assert shared(lib, pages([848, 30], **bad), p) != OK and shared(lib, w, pages([5, 6, 7], **bad)) != OK
+    with pytest.raises(ValueError, match="n_sharing has 1 entries for 2 prefixes"):
+        ckv.chunkkv_shared_decode_workspace_bytes(w, p, [3])
+    with pytest.raises(ValueError, match="does not fit"):
+        ckv.chunkkv_shared_decode_workspace_bytes(w, p, [2 + (1 << 32), 1 - (1 << 32)])
+
+
+def test_a_prefix_is_counted_once():
+    """Workspace of the partial rows: those of the prefix and of every sequence's own slots, whoever shares."""
+    p = pages([16] * 8)
+    one, eight = (ckv.chunkkv_shared_decode_workspace_bytes(pages([848] * len(n)), p, n) for n in ([8], [1] * 8))
+    assert one <= 2 * eight
+
+
+# ---- rotation ----
+def rows(**kw):
+    d = dict(in_=0x1000, out=0x2000, n_heads=4, in_stride_seq=0, in_stride_head=64, in_stride_tok=256, out_stride_seq=0, out_stride_head=64, out_stride_tok=256)
+    d.update(kw)
+    return binding._CRows(*[d[name] for name, _ in binding._CRows._fields_])
+
+
+def rotate(lib, q=None, k=None, dtype=ckv.BF16, d=64, n=1, t=5, pos=FAKE, freq=FAKE, rotary=64, magnitude=1.0):
+    return lib.chunkkv_rotate(dtype, d, n, t, q and C.byref(q), k and C.byref(k), pos, freq, rotary, 0, magnitude, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED), (dict(d=96), UNSUPPORTED), (dict(n=-1), SHAPE), (dict(t=-1), SHAPE), (dict(rotary=0), SHAPE), (dict(rotary=80), SHAPE),
+    (dict(rotary=24), UNSUPPORTED), (dict(magnitude=-1.0), SHAPE), (dict(magnitude=float("nan")), SHAPE), (dict(magnitude=float("inf")), SHAPE), (dict(pos=None), NULL), (dict(freq=None), NULL),
+    (dict(t=(1 << 24) + 1), UNSUPPORTED), (dict(n=1 << 13, t=1 << 12), UNSUPPORTED), (dict(n=1 << 30, t=1 << 30), UNSUPPORTED),
+])
+def test_rotations_that_are_refused(lib, kw, status):
+    assert rotate(lib, rows(), **kw) == status and rotate(lib, None, rows(), **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(in_=None), NULL), (dict(out=None), NULL), (dict(in_=0x1008), SHAPE), (dict(out=0x1008), SHAPE), (dict(n_heads=0), SHAPE), (dict(n_heads=65537), UNSUPPORTED), (dict(in_stride_tok=-256), SHAPE),
+    (dict(in_stride_head=68), SHAPE), (dict(out_stride_seq=4), SHAPE), (dict(out=0x1000, out_stride_tok=512), SHAPE), (dict(out=0x1000, out_stride_head=128), SHAPE),
+])
+def test_rows_that_are_refused(lib, kw, status):
+    assert rotate(lib, rows(**kw)) == status and rotate(lib, rows(), rows(**kw)) == status
+
+
+def test_rotation_of_nothing(lib):
+    assert rotate(lib) == NULL
+    for kw in (dict(n=0), dict(t=0)):
+        assert rotate(lib, rows(in_=None, out=None), pos=None, **kw) == OK
+
+
+def test_frequencies():
+    r = 128
+    plain = ckv.chunkkv_rotary_frequencies(r, 500000.0)
+    want = 500000.0 ** (-torch.arange(0, r, 2, dtype=torch.float64) / r)
+    assert ((plain.double() - want).abs() <= 2.0 ** -24 * want).all()
+    assert torch.equal(ckv.chunkkv_rotary_frequencies(r, 500000.0, 1.0, 1.0, 32.0, 8192.0), plain)
+    by_parts = ckv.chunkkv_rotary_frequencies(r, 500000.0, 8.0, 1.0, 4.0, 8192.0).double()
+    turns = 8192.0 * want / (2 * math.pi)
+    s = ((turns - 1.0) / 3.0).clamp(0, 1)
+    ref = want * s + want / 8.0 * (1 - s)
+    assert ((by_parts - ref).abs() <= 2.0 ** -23 * ref).all() and (s == 1).any() and (s == 0).any() and ((s > 0) & (s < 1)).any()
+    all_divided = ckv.chunkkv_rotary_frequencies(r, 500000.0, 4.0, trained_tokens=0.0).double()
+    assert ((all_divided - want / 4).abs() <= 2.0 ** -24 * want).all()
+    step = ckv.chunkkv_rotary_frequencies(r, 500000.0, 8.0, 2.0, 2.0, 8192.0).double()
+    assert ((step - torch.where(turns >= 2.0, want, want / 8)).abs() <= 2.0 ** -24 * want).all()
+    for bad in [(0, 1e4), (7, 1e4), (-2, 1e4), (64, 1.0), (64, float("nan")), (64, 1e4, 0.5), (64, 1e4, float("inf")), (64, 1e4, 2.0, -1.0), (64, 1e4, 2.0, 3.0, 2.0), (64, 1e4, 2.0, 1.0, 2.0, -1.0)]:
+        with pytest.raises(ckv.ChunkKVError):
+            ckv.chunkkv_rotary_frequencies(*bad)
+    assert ckv.load_library().chunkkv_rotary_frequencies(64, 1e4, 1.0, 1.0, 1.0, 0.0, None) == NULL
+
+
+def test_argument_checks_and_plans_are_clean_under_asan_and_ubsan(tmp_path):
+    from paper_2502_00299_amd import build
+    exe = build.build_host_sanitizer_check(str(tmp_path), "host_sanitizer_rows")
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300, env=env)
+    out = r.stdout + r.stderr
+    assert r.returncode == 0 and "HOST SANITIZER RUN OK" in r.stdout, out[-4000:]
+    assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
