@@ -454,7 +454,7 @@ typedef struct {
  *              state is left).  With it, parts of an attention can be joined: over a cache here, among the tokens themselves elsewhere
  *   workspace  chunkkv_cross_workspace_bytes(cross) bytes (0 = invalid), contents scratch
  * Products and sums in fp32.  Softmax weights of 16-bit types are rounded to that type once, to nearest, and normalised by the sum of
- * the rounded ones (fp16: those below 2^-24 of the largest lose bits, down to 2^-34); outputs are rounded once more, lse not at all below
+ * the rounded ones (fp16: those below 2^-23 of the largest lose bits, down to 2^-33); outputs are rounded once more, lse not at all below
  * fp32.  The same call on the same inputs gives the same bits.  A NaN or an infinity in a state that counts gives undefined outputs of
  * its kv-head's query heads.  One or two launches per 32 sequences.                                                                  */
 size_t chunkkv_cross_workspace_bytes(const chunkkv_cross *cross);

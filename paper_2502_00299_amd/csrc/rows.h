@@ -12,9 +12,34 @@
 namespace ckv {
 
 constexpr int kRowsTile = 64;            // keys that a workgroup holds at a time
-constexpr int kRowsWide = 128, kRowsNarrow = 64;   // query rows of a workgroup
+constexpr int kRowsNarrow = 32;          // query rows of half a workgroup, where a segment has no more
+constexpr int kRowsWide = 128;           // of a workgroup; or twice as many
+// Narrow tiles of a workgroup: as many as their slots fit into 128 KB of LDS.
+__host__ __device__ constexpr int rows_pairs(int dtype, int head_dim) { return dtype == CHUNKKV_F32 && head_dim == 128 ? 1 : 2; }
 constexpr int kCrossSegments = 32;       // segments of a launch: their table travels as kernel arguments
-constexpr int kSharedSegments = 80;
+constexpr int kSharedSegments = 72;
+
+// A segment of a launch.  Together in 32 bytes: a workgroup reads them with one load.
+struct RowsSegment {
+  int32_t rows;                          // query rows of a kv-head
+  int32_t most;                          // keys, at most
+  int32_t row0;                          // tokens (sequences) before: where its queries are, and of lse
+  int32_t splits;                        // ranges that its keys are cut into
+  int32_t tiles;                         // workgroups that share a range of a kv-head
+  int32_t part;                          // number of its first partial row; -1: its workgroups write the outputs
+  int32_t pad[2];
+};
+
+// x / d for 0 <= x < 2^31 and 0 < d <= 1024: the product is off by 1 at most, and too large then.
+struct Divisor {
+  uint32_t d, magic;                     // ceil(2^32 / d), 2^32 - 1 for 1
+};
+inline Divisor divisor(int d) { return {(uint32_t)d, d == 1 ? 0xFFFFFFFFu : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d)}; }
+__device__ __forceinline__ int divided(int x, const Divisor &by) {
+  if (by.d == 1) return x;
+  const uint32_t q = __umulhi((uint32_t)x, by.magic);
+  return (int)(q * by.d > (uint32_t)x ? q - 1 : q);
+}
 
 template <int N>
 struct RowsArgs {
@@ -29,16 +54,16 @@ struct RowsArgs {
   float4 *part_ml;                       // (reference in log2 units, sum of the weights as multiplied, sum before their rounding, -) of every partial row
   float *part_o;                         // [d] of every partial row
   int64_t q_tok, q_head, out_tok, out_head;        // bytes
-  int32_t n_kv_heads, group, mask_pitch;
+  Divisor heads, group;                  // kv-heads; query heads of one
+  int32_t mask_pitch;
   int32_t segments, prefixes;            // of the launch
   int32_t prefix_pitch;
+  int32_t tile;                          // query rows of a workgroup: kRowsWide, or twice as many; kRowsNarrow where no segment has more
   int32_t prefix0, seq0;                 // number of its first prefix, of its first sequence
   float scale, scale_log2e;              // as PagedDecodeArgs has them
-  int32_t first[N + 1];                  // number of the first workgroup of every segment, INT32_MAX past the last one's end
-  int32_t rows[N];                       // query rows of a kv-head
-  int32_t most[N];                       // keys, at most
-  int32_t row0[N];                       // tokens (sequences) before: where its queries are, and of lse
-  int32_t part[N];                       // number of its first partial row; -1: its workgroups write the outputs
+  static constexpr int kFirst = (N + 15) / 16 * 16 + 1;   // looked through by sixteens
+  int32_t first[kFirst];                 // number of the first workgroup of every segment, INT32_MAX past the last one's end
+  RowsSegment segment[N];
 };
 struct CrossArgs {
   RowsArgs<kCrossSegments> r;
@@ -48,27 +73,28 @@ struct SharedArgs {
   RowsArgs<kSharedSegments> r;
 };
 
-// Rows of a workgroup by those of a segment, and how many workgroups a kv-head has for them.
-__host__ __device__ inline int rows_tile(int rows) { return rows > kRowsNarrow ? kRowsWide : kRowsNarrow; }
-__host__ __device__ inline int rows_tiles(int rows) { return (rows + rows_tile(rows) - 1) / rows_tile(rows); }
 // Keys of each of `splits` ranges of n keys: whole tiles, from the length that the device knows.
 __host__ __device__ inline int rows_range(int n, int splits) { return ((n + splits - 1) / splits + kRowsTile - 1) / kRowsTile * kRowsTile; }
 
 // Joins partial rows: outputs of `tokens` tokens (sequences), each from the ranges of its own segment and, with a prefix, of that.
 constexpr int kJoinSegments = 64;
+struct JoinSegment {
+  int32_t part, splits, rows;            // its partial rows: [split][kv-head][rows]
+  int32_t token0;                        // its first token: where lse is
+  int32_t prefix_part, prefix_splits, prefix_rows, prefix_row0;   // those of its prefix, and its first row in them; splits 0: none
+  int64_t out_base;                      // bytes
+};
 struct JoinArgs {
   const float4 *part_ml;
   const float *part_o;
   void *out;
   float *lse;
   int64_t out_tok, out_head;             // bytes
-  int32_t n_kv_heads, group, segments, tokens;
+  Divisor heads, group;
+  int32_t segments, tokens;
   float scale, scale_log2e;
-  int32_t first[kJoinSegments + 1];      // first token of a segment, from the launch's first one on; INT32_MAX past the last one's end
-  int32_t part[kJoinSegments], splits[kJoinSegments], rows[kJoinSegments];       // its partial rows: [split][Hkv][rows]
-  int32_t prefix_part[kJoinSegments], prefix_splits[kJoinSegments], prefix_rows[kJoinSegments], prefix_row0[kJoinSegments];   // splits 0: none
-  int64_t out_base[kJoinSegments];       // bytes
-  int64_t lse_base[kJoinSegments];       // elements
+  int32_t first[kJoinSegments];          // first token of a segment, from the launch's first one on; INT32_MAX past the last one
+  JoinSegment segment[kJoinSegments];
 };
 
 int launch_cross_bf16(int head_dim, const CrossArgs &a, hipStream_t s);

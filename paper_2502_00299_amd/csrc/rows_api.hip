@@ -9,7 +9,7 @@ namespace {
 
 constexpr int64_t kMostElements = (int64_t)1 << 56;   // strides and bases: what no memory has
 constexpr int kMaxQueryRows = 1 << 30;   // of a sequence (or prefix) and kv-head
-constexpr int kJoinPrefixes = kSharedSegments - kJoinSegments;   // prefixes of a launch: the others of its segments are sequences
+constexpr int kLaunchPrefixes = kSharedSegments - kJoinSegments;   // prefixes of a launch: the others of its segments are sequences
 constexpr int kRotateMaxHeads = 1 << 16;
 
 // ---- key ranges ---------------------------------------------------------------------------------------------------
@@ -17,56 +17,112 @@ constexpr int kRotateMaxHeads = 1 << 16;
 struct Shape {
   int rows, most;
 };
+struct RowsPlan {
+  int tile, pairs;       // rows of a wide workgroup, kRowsNarrow: there is none; narrow tiles of a workgroup
+  int range[2];          // keys of a range of a wide segment, of a narrow one; a multiple of kRowsTile
+};
+int ranges_of(const Shape &x, const RowsPlan &pl) {
+  const int range = pl.range[x.rows <= kRowsNarrow];
+  return x.rows == 0 ? 0 : (x.most > range ? (x.most + range - 1) / range : 1);
+}
+int tiles_of(const Shape &x, const RowsPlan &pl) { return x.rows <= kRowsNarrow ? 1 : (x.rows + pl.tile - 1) / pl.tile; }
+int64_t blocks_of(const Shape &x, const RowsPlan &pl, int n_kv_heads) {
+  const int64_t n = (int64_t)ranges_of(x, pl) * n_kv_heads;
+  return x.rows <= kRowsNarrow ? (n + pl.pairs - 1) / pl.pairs : n * tiles_of(x, pl);
+}
 
-int ranges_of(int most, int range) { return most > range ? (most + range - 1) / range : 1; }
-
-// Keys of a range, for all segments of a call: what makes the last workgroup end first, by an estimate in units of keys.  A CU holds
-// `per_cu` workgroups; one costs its keys, kStart for its start and end, and, where ranges are joined, writing and reading its rows.
-constexpr int kStart = 96, kJoin = 64, kLeastRange = 64, kCUs = 256;
+// Narrow segments alone: ranges that are a workgroup for each CU together, kLeastRange at least; a segment of up to kShortKeys has no launch
+// behind it where it need not.  Fewer and longer ones leave CUs idle, more of them cost more starts and partial rows.
+//
+// Otherwise the ranges and the tile whose last workgroup ends first, by an estimate in microseconds: a workgroup costs kStart, kRow for each of
+// its rows where ranges are joined (written and read again), and its keys, by type and kind.  The launch ends when the longest workgroups have
+// gone through in rounds, when all CUs have done their share, or when all keys have come from memory, whichever is last.
+constexpr int kLeastRange = 128, kShortKeys = 512, kCUs = 256;
+constexpr float kStart = 5.f, kJoin = 3.5f, kRow = 0.05f, kBytes = 5.5e6f;
+constexpr float kKey[2][2][3] = {   // [fp32][d = 128][256 rows, 128, narrow]
+    {{0.020f, 0.012f, 0.008f}, {0.030f, 0.018f, 0.016f}}, {{0.13f, 0.066f, 0.018f}, {0.25f, 0.13f, 0.034f}}};
+int whole_tiles(float keys) { return keys < (float)kPagedMaxTokens ? ((int)keys + kRowsTile - 1) / kRowsTile * kRowsTile : kPagedMaxTokens; }
 template <typename F>
-int plan_range(int n, F &&shape, int n_kv_heads, int per_cu) {
-  int most = kLeastRange, rows = 1;
-  int64_t keys = 0;                      // of all row tiles
+RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bool always_joined) {
+  float keys = 0.f, wide_keys[2] = {0.f, 0.f};   // of all segments; of wide ones times their workgroups, 256 rows and 128
+  int most = 1, rows_most = 0;
   for (int i = 0; i < n; ++i) {
     const Shape x = shape(i);
     if (x.rows == 0) continue;
     most = x.most > most ? x.most : most;
-    const int r = x.rows < kRowsWide ? x.rows : kRowsWide;
-    rows = r > rows ? r : rows;
-    keys += (int64_t)rows_tiles(x.rows) * x.most;
+    rows_most = x.rows > rows_most ? x.rows : rows_most;
+    keys += (float)x.most;
+    if (x.rows > kRowsNarrow)
+      for (int k = 0; k < 2; ++k) wide_keys[k] += (float)x.most * (float)((x.rows + (256 >> k) - 1) / (256 >> k));
   }
-  const int whole = (most + kRowsTile - 1) / kRowsTile * kRowsTile;
-  auto items = [&](int range) {
-    int64_t w = 0;
-    for (int i = 0; i < n; ++i) {
-      const Shape x = shape(i);
-      if (x.rows > 0) w += (int64_t)rows_tiles(x.rows) * ranges_of(x.most, range);
+  const int whole = (most + kRowsTile - 1) / kRowsTile * kRowsTile, pairs = rows_pairs(dtype, head_dim);
+  RowsPlan best = {kRowsNarrow, 1, {whole, whole}};
+  if (rows_most <= kRowsNarrow) {
+    if (!always_joined && most <= kShortKeys) return best;
+    int range = whole_tiles(keys * n_kv_heads / kCUs);
+    for (int again = 0; again < 2; ++again) {   // ends of segments are workgroups too
+      if (range < kLeastRange) range = kLeastRange;
+      int64_t blocks = 0, segments = 0;
+      best.range[1] = range;
+      for (int i = 0; i < n; ++i) {
+        blocks += ranges_of(shape(i), best);
+        segments += shape(i).rows > 0;
+      }
+      blocks *= n_kv_heads;
+      segments *= n_kv_heads;
+      if (blocks <= kCUs || 2 * segments > kCUs) break;
+      range = whole_tiles((float)range * (float)(blocks - segments) / (float)(kCUs - segments));
     }
-    return w * n_kv_heads;
-  };
-  const int64_t slots = (int64_t)kCUs * per_cu;
-  auto cost = [&](int range, int64_t workgroups) {
-    return (workgroups + slots - 1) / slots * (range + kStart + (range < whole ? 2 * rows : 0)) + (range < whole ? kJoin : 0);
-  };
-  int best = whole;
-  int64_t count = items(whole), least = cost(whole, count);
-  for (int rounds = 1; rounds <= 4 && count <= rounds * slots; ++rounds) {
-    // a short range whose workgroups are so many rounds: from what all keys together allow up, by as much as there are too many
-    int64_t range = (keys * n_kv_heads / (rounds * slots) + kRowsTile) / kRowsTile * kRowsTile, w;
-    if (range < kLeastRange) range = kLeastRange;
-    while (range < whole && (w = items((int)range)) > rounds * slots)
-      range = ((range * w + rounds * slots - 1) / (rounds * slots) + kRowsTile) / kRowsTile * kRowsTile;
-    if (range >= whole) continue;
-    const int64_t x = cost((int)range, w);
-    if (x < least) {
-      best = (int)range;
-      least = x;
+    return best;
+  }
+  float least = FLT_MAX;
+  const float memory = 2.f * keys * n_kv_heads * head_dim * elem_bytes(dtype) / kBytes + kStart;
+  const float *rate = kKey[dtype == CHUNKKV_F32][head_dim == 128];
+  for (int k = 0; k < 2; ++k) {
+    const float tile = 1.f / (float)(kRowsWide << (1 - k));
+    // tries ranges of so many keys; -> workgroups
+    auto attempt = [&](int range) {
+      RowsPlan pl = {kRowsWide << (1 - k), pairs, {range, whole_tiles((float)range * rate[k] / rate[2])}};
+      const float per[2] = {1.f / (float)pl.range[0], 1.f / (float)pl.range[1]};
+      float total = 0.f, blocks = 0.f, full = 0.f, longest[2] = {0.f, 0.f};
+      bool joined = always_joined;
+      for (int i = 0; i < n; ++i) {
+        const Shape x = shape(i);
+        if (x.rows == 0) continue;
+        const bool narrow = x.rows <= kRowsNarrow, cut = x.most > pl.range[narrow];
+        const int rows = x.rows < pl.tile ? x.rows : pl.tile;
+        const float count = (cut ? ceilf((float)x.most * per[narrow]) : 1.f) * (narrow ? 1.f / (float)pairs : ceilf((float)x.rows * tile));
+        const float cost = (float)(cut ? pl.range[narrow] : x.most) * rate[narrow ? 2 : k] + kStart + (cut ? (float)rows * kRow : 0.f);
+        total += count * cost;
+        blocks += count;
+        longest[narrow] = cost > longest[narrow] ? cost : longest[narrow];
+        full += !narrow && 2 * x.most > pl.range[0] ? count : 0.f;
+        joined |= cut;
+      }
+      blocks *= (float)n_kv_heads;
+      const float rounds = ceilf(full * (float)n_kv_heads / kCUs), even = total * (float)n_kv_heads / kCUs;
+      float end = rounds * longest[0] + (blocks > rounds * kCUs ? longest[1] : 0.f);   // narrow ones behind the wide
+      end = end > even ? end : even;
+      end = (end > memory ? end : memory) + (joined ? kJoin : 0.f);
+      if (end < least) {
+        least = end;
+        best = pl;
+      }
+      return blocks;
+    };
+    attempt(whole);
+    for (int share : {kCUs / 2, kCUs, 2 * kCUs}) {
+      int range = whole_tiles(wide_keys[k] * n_kv_heads / (float)share);
+      for (int again = 0; again < 2 && range < whole; ++again) {
+        if (range < kLeastRange) range = kLeastRange;
+        const float blocks = attempt(range);
+        if (blocks <= (float)share) break;
+        range = whole_tiles((float)range * blocks / (float)share);   // ends of segments are more workgroups than that
+      }
     }
   }
   return best;
 }
-
-int per_cu(int dtype, int head_dim) { return dtype == CHUNKKV_F32 && head_dim == 128 ? 1 : 2; }
 
 void set_scale(float given, int head_dim, float *scale, float *scale_log2e) {   // as chunkkv_paged_decode_attention has them
   const float x = given > 0.f ? given : 1.0f / sqrtf((float)head_dim);
@@ -106,22 +162,22 @@ int check_cross(const chunkkv_cross *c) {
 }
 
 struct CrossPlan {
-  int range;
+  RowsPlan rows;
   int64_t partials;
   size_t off_o, total;
 };
 Shape cross_shape(const chunkkv_cross *c, int b) { return {c->q_len[b] * (c->n_q_heads / c->n_kv_heads), c->seqlen[b]}; }
 // The launches of a call follow one another on the stream and share the workspace.
 int cross_plan(const chunkkv_cross *c, CrossPlan *pl) {
-  pl->range = plan_range(c->batch, [&](int b) { return cross_shape(c, b); }, c->n_kv_heads, per_cu(c->dtype, c->head_dim));
+  pl->rows = plan_rows(c->batch, [&](int b) { return cross_shape(c, b); }, c->n_kv_heads, c->dtype, c->head_dim, false);
   pl->partials = 0;
   for (int b0 = 0; b0 < c->batch; b0 += kCrossSegments) {
     int64_t rows = 0, items = 0;
     for (int b = b0; b < c->batch && b < b0 + kCrossSegments; ++b) {
       const Shape x = cross_shape(c, b);
-      const int splits = ranges_of(x.most, pl->range);
+      const int splits = ranges_of(x, pl->rows);
       if (splits > 1) rows += (int64_t)splits * c->n_kv_heads * x.rows;
-      items += (int64_t)splits * c->n_kv_heads * rows_tiles(x.rows);
+      items += blocks_of(x, pl->rows, c->n_kv_heads);
     }
     if (rows > INT32_MAX || items > INT32_MAX) return CHUNKKV_ERR_UNSUPPORTED;
     pl->partials = rows > pl->partials ? rows : pl->partials;
@@ -150,7 +206,7 @@ int check_shared(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *
 }
 
 struct SharedPlan {
-  int range;
+  RowsPlan rows;
   int64_t partials, prefix_partials;
   size_t off_o, total;
 };
@@ -160,16 +216,15 @@ Shape shared_shape(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t
   if (i < w->batch) return {w->max_tokens[i] > 0 ? n_sharing[i] * g : 0, w->max_tokens[i]};
   return {p->max_tokens[i - w->batch] > 0 ? g : 0, p->max_tokens[i - w->batch]};
 }
-int shared_splits(const Shape &x, int range) { return x.rows > 0 ? ranges_of(x.most, range) : 0; }
 int shared_plan(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *n_sharing, SharedPlan *pl) {
   const int n = w->batch + p->batch;
-  pl->range = plan_range(n, [&](int i) { return shared_shape(w, p, n_sharing, i); }, p->n_kv_heads, per_cu(p->dtype, p->head_dim));
+  pl->rows = plan_rows(n, [&](int i) { return shared_shape(w, p, n_sharing, i); }, p->n_kv_heads, p->dtype, p->head_dim, true);
   pl->partials = 0;
   int64_t items = 0;
   for (int i = 0; i < n; ++i) {
     const Shape x = shared_shape(w, p, n_sharing, i);
-    pl->partials += (int64_t)shared_splits(x, pl->range) * p->n_kv_heads * x.rows;
-    items += (int64_t)shared_splits(x, pl->range) * p->n_kv_heads * rows_tiles(x.rows);
+    pl->partials += (int64_t)ranges_of(x, pl->rows) * p->n_kv_heads * x.rows;
+    items += blocks_of(x, pl->rows, p->n_kv_heads);
     if (i == w->batch - 1) pl->prefix_partials = pl->partials;
   }
   if (pl->partials > INT32_MAX || items > INT32_MAX) return CHUNKKV_ERR_UNSUPPORTED;
@@ -222,29 +277,30 @@ int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const
     r.q = q; r.k = k; r.v = v; r.out = out; r.lse = lse;
     r.part_ml = (float4 *)workspace; r.part_o = (float *)((char *)workspace + pl.off_o);
     r.q_tok = c->q_stride_tok * esz; r.q_head = c->q_stride_head * esz; r.out_tok = c->out_stride_tok * esz; r.out_head = c->out_stride_head * esz;
-    r.n_kv_heads = c->n_kv_heads; r.group = g; r.segments = nb; r.seq0 = b0;
+    r.heads = divisor(c->n_kv_heads); r.group = divisor(g); r.segments = nb; r.seq0 = b0; r.tile = pl.rows.tile;
     set_scale(c->softmax_scale, c->head_dim, &r.scale, &r.scale_log2e);
-    for (int i = 0; i <= kCrossSegments; ++i) r.first[i] = INT32_MAX;
+    for (int &x : r.first) x = INT32_MAX;
     j.part_ml = r.part_ml; j.part_o = r.part_o; j.out = out; j.lse = lse; j.out_tok = r.out_tok; j.out_head = r.out_head;
-    j.n_kv_heads = c->n_kv_heads; j.group = g; j.scale = r.scale; j.scale_log2e = r.scale_log2e;
-    for (int i = 0; i <= kJoinSegments; ++i) j.first[i] = INT32_MAX;
+    j.heads = divisor(c->n_kv_heads); j.group = divisor(g); j.scale = r.scale; j.scale_log2e = r.scale_log2e;
+    for (int i = 0; i < kJoinSegments; ++i) j.first[i] = INT32_MAX;
     int items = 0, parts = 0;
     for (int i = 0; i < nb; ++i) {
       const int b = b0 + i;
       const Shape x = cross_shape(c, b);
-      const int splits = ranges_of(x.most, pl.range);
-      r.first[i] = items; r.rows[i] = x.rows; r.most[i] = x.most; r.row0[i] = token0;
+      const int splits = ranges_of(x, pl.rows);
+      RowsSegment &seg = r.segment[i];
+      r.first[i] = items;
+      seg.rows = x.rows; seg.most = x.most; seg.row0 = token0; seg.splits = splits; seg.tiles = tiles_of(x, pl.rows); seg.part = -1;
       a.q_base[i] = c->q_base[b] * esz; a.kv_base[i] = c->kv_base[b] * esz; a.out_base[i] = c->out_base[b] * esz;
-      r.part[i] = -1;
       if (splits > 1 && x.rows > 0) {
-        r.part[i] = parts;
+        seg.part = parts;
         const int n = j.segments++;
-        j.first[n] = j.tokens; j.part[n] = parts; j.splits[n] = splits; j.rows[n] = x.rows; j.out_base[n] = a.out_base[i];
-        j.lse_base[n] = (int64_t)token0 * c->n_q_heads;
+        j.first[n] = j.tokens;
+        j.segment[n] = {parts, splits, x.rows, token0, 0, 0, 0, 0, a.out_base[i]};
         j.tokens += c->q_len[b];
         parts += splits * c->n_kv_heads * x.rows;
       }
-      items += splits * c->n_kv_heads * rows_tiles(x.rows);
+      items += (int)blocks_of(x, pl.rows, c->n_kv_heads);
       token0 += c->q_len[b];
     }
     r.first[nb] = items;
@@ -279,10 +335,10 @@ int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_p
   float *part_o = (float *)((char *)workspace + pl.off_o);
   float scale, scale_log2e;
   set_scale(pages->softmax_scale, d, &scale, &scale_log2e);
-  // Partial rows: those of the prefixes, then those of the sequences.  A launch has up to kJoinPrefixes prefixes and kJoinSegments sequences.
+  // Partial rows: those of the prefixes, then those of the sequences.  A launch has up to kLaunchPrefixes prefixes and kJoinSegments sequences.
   int parts[2] = {0, (int)pl.prefix_partials}, before = 0;   // before: sequences of the prefixes before
-  for (int i0 = 0, b0 = 0; i0 < prefix->batch || b0 < pages->batch; i0 += kJoinPrefixes, b0 += kJoinSegments) {
-    const int np = i0 >= prefix->batch ? 0 : (prefix->batch - i0 < kJoinPrefixes ? prefix->batch - i0 : kJoinPrefixes);
+  for (int i0 = 0, b0 = 0; i0 < prefix->batch || b0 < pages->batch; i0 += kLaunchPrefixes, b0 += kJoinSegments) {
+    const int np = i0 >= prefix->batch ? 0 : (prefix->batch - i0 < kLaunchPrefixes ? prefix->batch - i0 : kLaunchPrefixes);
     const int nb = b0 >= pages->batch ? 0 : (pages->batch - b0 < kJoinSegments ? pages->batch - b0 : kJoinSegments);
     SharedArgs a;
     memset(&a, 0, sizeof(a));
@@ -293,18 +349,19 @@ int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_p
     r.q = q; r.k = k_pages; r.v = v_pages; r.out = out; r.lse = lse;
     r.part_ml = part_ml; r.part_o = part_o;
     r.q_tok = r.out_tok = (int64_t)pages->n_q_heads * d * esz; r.q_head = r.out_head = (int64_t)d * esz;
-    r.n_kv_heads = hkv; r.group = g; r.segments = np + nb; r.prefixes = np; r.prefix0 = i0; r.seq0 = b0;
+    r.heads = divisor(hkv); r.group = divisor(g); r.segments = np + nb; r.prefixes = np; r.prefix0 = i0; r.seq0 = b0; r.tile = pl.rows.tile;
     r.scale = scale; r.scale_log2e = scale_log2e;
-    for (int i = 0; i <= kSharedSegments; ++i) r.first[i] = INT32_MAX;
+    for (int &x : r.first) x = INT32_MAX;
     int items = 0;
     for (int i = 0; i < np + nb; ++i) {
       const bool own = i >= np;
       const Shape x = shared_shape(prefix, pages, n_sharing, own ? prefix->batch + b0 + i - np : i0 + i);
-      const int splits = shared_splits(x, pl.range);
-      r.first[i] = items; r.rows[i] = x.rows; r.most[i] = x.most; r.part[i] = parts[own];
-      r.row0[i] = own ? b0 + i - np : before;
+      const int splits = ranges_of(x, pl.rows);
+      RowsSegment &seg = r.segment[i];
+      r.first[i] = items;
+      seg.rows = x.rows; seg.most = x.most; seg.row0 = own ? b0 + i - np : before; seg.splits = splits; seg.tiles = tiles_of(x, pl.rows); seg.part = parts[own];
       if (!own) before += n_sharing[i0 + i];
-      items += splits * hkv * rows_tiles(x.rows);
+      items += (int)blocks_of(x, pl.rows, hkv);
       parts[own] += splits * hkv * x.rows;
     }
     r.first[np + nb] = items;
@@ -320,18 +377,16 @@ int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_p
     JoinArgs j;
     memset(&j, 0, sizeof(j));
     j.part_ml = part_ml; j.part_o = part_o; j.out = out; j.lse = lse; j.out_tok = (int64_t)pages->n_q_heads * d * esz; j.out_head = (int64_t)d * esz;
-    j.n_kv_heads = hkv; j.group = g; j.scale = scale; j.scale_log2e = scale_log2e; j.segments = j.tokens = nb;
-    for (int n = 0; n <= kJoinSegments; ++n) j.first[n] = n < nb ? n : INT32_MAX;
+    j.heads = divisor(hkv); j.group = divisor(g); j.scale = scale; j.scale_log2e = scale_log2e; j.segments = j.tokens = nb;
+    for (int n = 0; n < kJoinSegments; ++n) j.first[n] = n < nb ? n : INT32_MAX;
     for (int n = 0; n < nb; ++n, ++nth) {
       for (; nth == n_sharing[i]; ++i, nth = 0) {
         const Shape x = shared_shape(prefix, pages, n_sharing, i);
-        prefix_part += shared_splits(x, pl.range) * hkv * x.rows;
+        prefix_part += ranges_of(x, pl.rows) * hkv * x.rows;
       }
       const Shape whole = shared_shape(prefix, pages, n_sharing, i), own = shared_shape(prefix, pages, n_sharing, prefix->batch + b0 + n);
-      j.part[n] = own_part; j.splits[n] = shared_splits(own, pl.range); j.rows[n] = own.rows;
-      j.prefix_part[n] = prefix_part; j.prefix_splits[n] = shared_splits(whole, pl.range); j.prefix_rows[n] = whole.rows; j.prefix_row0[n] = nth * g;
-      j.out_base[n] = (b0 + n) * j.out_tok; j.lse_base[n] = (int64_t)(b0 + n) * pages->n_q_heads;
-      own_part += j.splits[n] * hkv * own.rows;
+      j.segment[n] = {own_part, ranges_of(own, pl.rows), own.rows, b0 + n, prefix_part, ranges_of(whole, pl.rows), whole.rows, nth * g, (b0 + n) * j.out_tok};
+      own_part += j.segment[n].splits * hkv * own.rows;
     }
     Timed t(kDecode, s);
     if ((rc = launch_join(pages->dtype, d, j, s))) return rc;

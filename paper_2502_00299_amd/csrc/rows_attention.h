@@ -2,9 +2,11 @@
 //
 //   out_r = sum_s softmax_s(scale * q_r . k_s) v_s
 //
-// A workgroup of four wavefronts has a tile of a segment's query rows (rows.h) and a range of its keys, which it walks in tiles of 64
-// that all its wavefronts share through LDS.  128 rows: every wavefront has 32 of them and all keys.  64 rows, where a segment has no
-// more: two wavefronts have the first 32, each half of a tile's keys, two the others; their states are merged in the end.
+// A workgroup of eight wavefronts has a tile of a segment's query rows (rows.h) and a range of its keys.  Three ways:
+//   256 rows   every wavefront has 32 rows and all keys, which come in tiles of 64 through a ring in LDS that all share;
+//   128 rows   two wavefronts have the same 32 rows, each half of every tile's keys; their states are merged in the end;
+//   32 rows    what a decoding step has: either half of the workgroup has a tile and range of its own, and each of its four wavefronts 32 keys
+//              at a time, every fourth, through LDS slots of its own, without a barrier; four states are merged in the end.
 //
 //   scores   S[key][row] = K Q^T by 32x32 products, keys the M dimension: a lane holds 16 keys of row lane % 32, so a row's
 //            statistics need no exchange but one between the two halves of a wavefront, at the end.
@@ -13,7 +15,7 @@
 //
 // Weights of 16-bit types are rounded to that type once, to nearest: the output has that type, and what the rounding of a weight leaves
 // in it is as much as its own does (2^-8 of the weight's part in bf16).  They are normalised by the sum of the rounded ones, so they add up
-// to one; the log-sum-exp takes the sum before.  fp16 weights are held 2^10 times as large, so that the smallest normal one is 2^-24 of the
+// to one; the log-sum-exp takes the sum before.  fp16 weights are held 2^9 times as large, so that the smallest normal one is 2^-23 of the
 // reference.  Scores, references, sums and outputs are fp32.
 // The reference of the online softmax is lazy: it moves when the weights of a row and tile add up to more than kOver.
 #pragma once
@@ -47,35 +49,49 @@ __device__ __forceinline__ float add2(uint32_t pair, float x) {
   else return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), __builtin_bit_cast(f16x2, 0x3C003C00u), x, false);
 }
 
-// Transposing reads of the V operands of 16 keys: dims 32 i .. of the i-th address, keys 0..3 and, 8 rows on, 4..7 of a lane's half.
-// One assembly block with its own wait, as read_v4.
-template <int OFF, int STEP>
-__device__ __forceinline__ void read_vt(uint32_t a0, uint32_t a1, u32x4 (&v)[2]) {
-  uint64_t x[4];
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-      "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-      : "v"(a0), "v"(a1), "n"(OFF), "n"(OFF + STEP)
-      : "memory");
-#pragma unroll
-  for (int i = 0; i < 2; ++i) v[i] = u32x4{(uint32_t)x[2 * i], (uint32_t)(x[2 * i] >> 32), (uint32_t)x[2 * i + 1], (uint32_t)(x[2 * i + 1] >> 32)};
+// Four numbers as four elements of a row.
+template <int DT>
+__device__ __forceinline__ void store4(char *to, const f32x4 &x) {
+  if constexpr (DT == CHUNKKV_F32) *(f32x4 *)to = x;
+  else *(uint2 *)to = make_uint2(pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3]));
 }
-template <int OFF, int STEP>
-__device__ __forceinline__ void read_vt(uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, u32x4 (&v)[4]) {
+
+// Transposing reads of the V operands of 32 keys: v[ks][i] for keys 16 ks .. and dims 32 i .. at a[i]; keys 0..3 of a lane's half and, 8 rows on,
+// its next four.  One assembly block with its own wait, as read_v4.
+template <int ROW>
+__device__ __forceinline__ void read_vt(const uint32_t (&a)[2], u32x4 (&v)[2][2]) {
   uint64_t x[8];
   asm volatile(
-      "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
-      "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
-      "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
-      "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%10\n\t"
+      "ds_read_b64_tr_b16 %4, %8 offset:%11\n\tds_read_b64_tr_b16 %5, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %9 offset:%11\n\tds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
       "s_waitcnt lgkmcnt(0)"
       : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
-      : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(OFF), "n"(OFF + STEP)
+      : "v"(a[0]), "v"(a[1]), "n"(8 * ROW), "n"(16 * ROW), "n"(24 * ROW)
       : "memory");
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = u32x4{(uint32_t)x[2 * i], (uint32_t)(x[2 * i] >> 32), (uint32_t)x[2 * i + 1], (uint32_t)(x[2 * i + 1] >> 32)};
+  for (int i = 0; i < 4; ++i) v[i / 2][i % 2] = u32x4{(uint32_t)x[2 * i], (uint32_t)(x[2 * i] >> 32), (uint32_t)x[2 * i + 1], (uint32_t)(x[2 * i + 1] >> 32)};
+}
+template <int ROW>
+__device__ __forceinline__ void read_vt(const uint32_t (&a)[4], u32x4 (&v)[2][4]) {
+  uint64_t x[16];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %2, %17\n\tds_read_b64_tr_b16 %3, %17 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %4, %18\n\tds_read_b64_tr_b16 %5, %18 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %6, %19\n\tds_read_b64_tr_b16 %7, %19 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %8, %16 offset:%21\n\tds_read_b64_tr_b16 %9, %16 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %10, %17 offset:%21\n\tds_read_b64_tr_b16 %11, %17 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %12, %18 offset:%21\n\tds_read_b64_tr_b16 %13, %18 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %14, %19 offset:%21\n\tds_read_b64_tr_b16 %15, %19 offset:%22\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(x[8]), "=&v"(x[9]), "=&v"(x[10]),
+        "=&v"(x[11]), "=&v"(x[12]), "=&v"(x[13]), "=&v"(x[14]), "=&v"(x[15])
+      : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(8 * ROW), "n"(16 * ROW), "n"(24 * ROW)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = u32x4{(uint32_t)x[2 * i], (uint32_t)(x[2 * i] >> 32), (uint32_t)x[2 * i + 1], (uint32_t)(x[2 * i + 1] >> 32)};
 }
 
 // Number of the segment of workgroup x.
@@ -92,13 +108,17 @@ __device__ __forceinline__ int rows_segment(int x, int n) {
   for (int i = 1; i < 16; ++i) s += x >= kernarg_at<int32_t>(FIRST, lo + i) ? 1 : 0;
   return s;
 }
-#define CKV_ROWS(FIELD, I) kernarg_at<int32_t>(offsetof(std::remove_cv_t<std::remove_reference_t<decltype(r)>>, FIELD), (I))
+__device__ __forceinline__ RowsSegment rows_segment_at(size_t offset) {
+  auto at = [&](int i) { return kernarg_at<int32_t>(offset, i); };
+  return {at(0), at(1), at(2), at(3), at(4), at(5), {0, 0}};
+}
 
-// What a workgroup works on; the same for all its threads.
+// What a workgroup, or half of one, works on.
 struct RowsWork {
-  int h, rows, row0, split, splits, part;   // row0: first row of the tile
+  int h, rows, row0, split, part;           // row0: first row of the tile
   int r0, len;                              // keys r0 .. r0 + len - 1
   const int32_t *table;                     // pages: of the segment
+  int32_t page;                             // pages: entry of block `lane` of the range
   const char *k, *v;                        // keys in a row: of (segment, kv-head), key r0
   const uint8_t *mask;                      // of key r0, or null
   const char *q;                            // of the segment's first token
@@ -109,23 +129,19 @@ struct RowsWork {
 template <bool PAGED>
 using RowsArgsOf = std::conditional_t<PAGED, SharedArgs, CrossArgs>;
 
+// Item `x` of segment s, `seg`, whose rows are `tile` to a workgroup (or half of one).
 template <bool PAGED, bool MASK>
-__device__ __forceinline__ RowsWork rows_work(const RowsArgsOf<PAGED> &a) {
+__device__ __forceinline__ RowsWork rows_work(const RowsArgsOf<PAGED> &a, const RowsSegment &seg, int s, int x, int tile, int lane) {
   const auto &r = a.r;
   RowsWork w;
-  int x = blockIdx.x;
-  const int s = rows_segment<std::remove_reference_t<decltype(r)>::kSegments>(x, r.segments), first = CKV_ROWS(first, s);
-  const int items = CKV_ROWS(first, s + 1) - first;
-  x -= first;
-  w.rows = CKV_ROWS(rows, s);
-  w.part = CKV_ROWS(part, s);
+  w.rows = seg.rows;
+  w.part = seg.part;
   // kv-heads are the fastest index: workgroups go to the eight XCDs in turn, so those that read the same keys meet in one or two L2s
-  const int tiles = rows_tiles(w.rows), y = x / r.n_kv_heads;
-  w.h = x - y * r.n_kv_heads;
-  w.split = y / tiles;
-  w.row0 = (y - w.split * tiles) * rows_tile(w.rows);
-  w.splits = items / (tiles * r.n_kv_heads);
-  const int most = CKV_ROWS(most, s), tok0 = CKV_ROWS(row0, s);
+  const int y = divided(x, r.heads);
+  w.h = x - y * (int)r.heads.d;
+  w.split = seg.tiles == 1 ? y : y / seg.tiles;
+  w.row0 = (y - w.split * seg.tiles) * tile;
+  const int most = seg.most, tok0 = seg.row0, splits = seg.splits;
   const int32_t *lengths = r.kv_len;
   int64_t seq = r.seq0 + s;
   w.table = nullptr;
@@ -139,20 +155,31 @@ __device__ __forceinline__ RowsWork rows_work(const RowsArgsOf<PAGED> &a) {
       w.table = r.geom.table + seq * r.geom.pitch;
     }
   }
-  int n = most;
+  // The table's entries are read beside the length, for the range as it is where the segment is as long as it can be; only one whose
+  // ranges turn out shorter reads them again.
+  const int full = rows_range(most, splits);
+  auto entry = [&](int first, int end) __attribute__((always_inline)) {
+    const int key = first + 16 * lane;
+    return key < end ? w.table[page_of_block(r.geom, (uint32_t)key >> 4)] : -1;
+  };
+  if constexpr (PAGED) w.page = entry(w.split * full, most < (w.split + 1) * full ? most : (w.split + 1) * full);
+  int n = most, range = full;
   if (lengths != nullptr) {
-    n = lengths[seq * r.n_kv_heads + w.h];
+    n = lengths[seq * (int)r.heads.d + w.h];
     n = n < 0 ? 0 : (n > most ? most : n);
+    range = rows_range(n, splits);
   }
-  const int range = rows_range(n, w.splits);
   w.r0 = w.split * range;
   w.len = n - w.r0 < range ? n - w.r0 : range;
+  if constexpr (PAGED) {
+    if (range != full) w.page = entry(w.r0, w.r0 + w.len);
+  }
   w.q = (const char *)r.q;
   w.out = (char *)r.out;
   w.k = (const char *)r.k;
   w.v = (const char *)r.v;
   w.mask = nullptr;
-  w.lse = r.lse != nullptr ? r.lse + (int64_t)tok0 * r.n_kv_heads * r.group : nullptr;
+  w.lse = r.lse != nullptr ? r.lse + (int64_t)tok0 * (int)(r.heads.d * r.group.d) : nullptr;
   if constexpr (PAGED) {
     w.q += tok0 * r.q_tok;
     w.out += tok0 * r.out_tok;
@@ -167,186 +194,74 @@ __device__ __forceinline__ RowsWork rows_work(const RowsArgsOf<PAGED> &a) {
   return w;
 }
 
-// WK: wavefronts that share the keys of a tile, 1 or 2
-template <int DT, int HD, bool PAGED, bool MASK, bool LSE, int WK>
-__device__ __forceinline__ void rows_body(const RowsArgsOf<PAGED> &a, const RowsWork &w, char *smem) {
-  const auto &r = a.r;
-  constexpr int ESZ = DT == CHUNKKV_F32 ? 4 : 2, ROWB = HD * ESZ, SEGS = ROWB / 16;   // bytes and 16-byte segments of a row
-  constexpr int RPL = 1024 / ROWB, NLD = 16 / RPL;   // rows that one 1 KB load fills; loads of a wavefront's 16 rows
-  constexpr int TILE = kRowsTile * ROWB;
-  constexpr int NKS = DT == CHUNKKV_F32 ? HD / 8 : HD / 16, NDT = HD / 32;             // 16-byte reads of a key by a lane, 32-dim output tiles
-  constexpr int NKB = 2 / WK;                        // 32-key blocks of a tile that a wavefront has
-  constexpr float kOff = DT == CHUNKKV_F16 ? 10.f : 0.f, kOver = DT == CHUNKKV_F16 ? 32768.f : (DT == CHUNKKV_BF16 ? 256.f : 16.f);
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = WK == 2 ? wave & 1 : 0, wr = wave / WK;
-  const int row = w.row0 + 32 * wr + n, g = r.group;
-  const int token = row / g, head = w.h * g + (row - token * g);
-  const bool idle = w.row0 + 32 * wr >= w.rows;      // this wavefront's rows are not there: it loads and waits with the others
+template <int DT, int HD>
+struct RowsShape {
+  static constexpr int kEsz = DT == CHUNKKV_F32 ? 4 : 2, kRow = HD * kEsz, kSegs = kRow / 16;   // bytes and 16-byte segments of a row
+  static constexpr int kRpl = 1024 / kRow;           // rows that one 1 KB load fills
+  static constexpr int kTile = kRowsTile * kRow;     // bytes of a tile of K or V
+  static constexpr int kStages = DT == CHUNKKV_F32 && HD == 128 ? 2 : 4;   // tiles of K and V in the ring
+  static constexpr int kLds = kStages * 2 * kTile;
+  static constexpr int kQ = DT == CHUNKKV_F32 ? HD / 8 : HD / 16, kD = HD / 32;    // 16-byte reads of a key by a lane, 32-dim output tiles
+  static constexpr int kAhead = kQ < 8 ? kQ : 8;     // of which so many are in flight
+  static constexpr int kNarrow = rows_pairs(DT, HD);   // narrow tiles of a workgroup
+  static_assert(kLds >= kNarrow * 4 * 2 * 32 * kRow, "slots of the wavefronts");
+  static_assert(kLds >= 8 * 32 * HD * 4 && 2 * 32 * kRow >= 32 * HD * 4, "states of the wavefronts");
+  // 16-byte segments lie at position segment ^ swizzle(row), so that neither the fragment reads nor the transposing ones meet in a bank
+  static __device__ __forceinline__ int kswz(int i) { return kSegs == 8 ? (i >> 1) & 7 : i & 15; }
+  static __device__ __forceinline__ int vswz(int i) { return DT == CHUNKKV_F32 ? 0 : (kSegs == 16 ? 4 * (i & 3) : 4 * ((i >> 1) & 1)); }
+};
 
-  u32x4 qf[NKS];
-#pragma unroll
-  for (int i = 0; i < NKS; ++i) qf[i] = u32x4{0, 0, 0, 0};
-  if (row < w.rows) {
-    const char *from = w.q + token * r.q_tok + head * r.q_head;
-#pragma unroll
-    for (int i = 0; i < NKS; ++i) qf[i] = *(const u32x4 *)(from + (2 * i + half) * 16);
-  }
-
-  // Loads: this wavefront's rows of a tile are 16 wave ..; lane l of load j lands at row RPL j + l / SEGS, position l % SEGS and
-  // fetches segment position ^ swizzle(row), so that neither the fragment reads nor the transposing ones meet in a bank.
-  const uint32_t tok = (uint32_t)r.geom.tok;
-  auto kswz = [](int i) { return SEGS == 8 ? (i >> 1) & 7 : i & 15; };
-  auto vswz = [](int i) { return DT == CHUNKKV_F32 ? 0 : (SEGS == 16 ? 4 * (i & 3) : 4 * ((i >> 1) & 1)); };
-  uint32_t koff[NLD], voff[NLD];
-#pragma unroll
-  for (int j = 0; j < NLD; ++j) {
-    const int i = RPL * j + lane / SEGS, pos = lane % SEGS;
-    koff[j] = (uint32_t)i * tok + (uint32_t)((pos ^ kswz(i)) * 16);
-    voff[j] = (uint32_t)i * tok + (uint32_t)((pos ^ vswz(i)) * 16);
-  }
-  const int tiles = w.len > 0 ? (w.len + kRowsTile - 1) / kRowsTile : 0;
-  // pages: entry of block `lane` of the current window of 64 blocks, and of the next one
-  int32_t page = -1, page_next = -1;
-  uint64_t present = ~0ull;
-  auto entry = [&](int window) __attribute__((always_inline)) {
-    const int blk = 64 * window + lane;
-    return 16 * blk < w.len ? w.table[page_of_block(r.geom, (uint32_t)(w.r0 / 16 + blk))] : -1;
-  };
-  // Keys of tile t that are there: one bit each.
-  uint8_t byte = 0;                                  // of key `lane` of the tile after the next one
-  auto load_mask = [&](int t) __attribute__((always_inline)) {
-    if constexpr (MASK) {
-      const int key = kRowsTile * t + lane;
-      byte = key < w.len ? w.mask[key] : 0;
-    }
-  };
-  auto alive_of = [&](int t) __attribute__((always_inline)) {
-    const int left = w.len - kRowsTile * t;
-    uint64_t m = left >= 64 ? ~0ull : (left > 0 ? (1ull << left) - 1 : 0ull);
-    if constexpr (MASK) m = __builtin_amdgcn_ballot_w64(byte != 0);
-    if constexpr (PAGED) {
-      const uint32_t four = (uint32_t)(present >> (4 * (t & 15))) & 15u;
-      if (four != 15u)
-        for (int i = 0; i < 4; ++i)
-          if ((four >> i & 1) == 0) m &= ~(0xFFFFull << (16 * i));
-    }
-    return m;
-  };
-  auto next_window = [&](int t) __attribute__((always_inline)) {   // before the first look at tile t
-    if constexpr (PAGED) {
-      if ((t & 15) == 0) {
-        page = page_next;
-        page_next = entry(t / 16 + 1);
-        present = __builtin_amdgcn_ballot_w64(page >= 0 && page < r.geom.n_pages);
-      }
-    }
-  };
-  auto issue = [&](int t, int buf) __attribute__((always_inline)) {
-    const int key0 = kRowsTile * t + 16 * wave, left = w.len - key0, rows = left < 16 ? left : 16;
-    int64_t at = 0;
-    bool there = rows > 0;
-    if constexpr (PAGED) {
-      const int blk = 4 * (t & 15) + wave;
-      at = block_offset(r.geom, __builtin_amdgcn_readlane(page, blk), w.h, (uint32_t)(w.r0 / 16 + key0 / 16));
-      there = there && at >= 0;
-      at = there ? at : 0;
-    } else {
-      at = there ? key0 * r.geom.tok : 0;
-    }
-    const int span = there ? (int)((uint32_t)(rows - 1) * tok) + ROWB : 0;
-    char *to = smem + buf * 2 * TILE + wave * 16 * ROWB;
-    const __amdgpu_buffer_rsrc_t krs = __builtin_amdgcn_make_buffer_rsrc((void *)(w.k + at), 0, span, 0x00020000);
-    const __amdgpu_buffer_rsrc_t vrs = __builtin_amdgcn_make_buffer_rsrc((void *)(w.v + at), 0, span, 0x00020000);
-#pragma unroll
-    for (int j = 0; j < NLD; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(krs, (__attribute__((address_space(3))) void *)(to + j * 1024), 16, koff[j], 0, 0, 0);
-#pragma unroll
-    for (int j = 0; j < NLD; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(vrs, (__attribute__((address_space(3))) void *)(to + TILE + j * 1024), 16, voff[j], 0, 0, 0);
-  };
-
-  // LDS addresses of this lane.  K: key n of a block, segment 2 i + half.  V, 16 bits: keys 4 half + (lane % 16) / 4 of 16, dims 32 i +
-  // 16 (lane / 16 % 2) + 4 (lane % 4) ..; fp32: key 4 half of eight, dims NDT n ..
-  const uint32_t kat = (uint32_t)((32 * wk + n) * ROWB + ((half ^ kswz(n)) * 16));
-  uint32_t vat[NDT];
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
-#pragma unroll
-  for (int i = 0; i < NDT; ++i) {
-    if constexpr (DT == CHUNKKV_F32) {
-      vat[i] = (uint32_t)(TILE + (32 * wk + 4 * half) * ROWB + n * NDT * 4);
-    } else {
-      const int p = lane & 15, key = 4 * half + p / 4, seg = 4 * i + 2 * (lane >> 4 & 1) + (p % 4) / 2;
-      vat[i] = lds0 + (uint32_t)(TILE + (32 * wk + key) * ROWB + ((seg ^ vswz(key)) * 16) + (p & 1) * 8);
-    }
-  }
-
-  const float c1 = r.scale_log2e;
-  float m = kPagedLowest, mc = 0.f, l = 0.f, le = 0.f;
+// A wavefront's 32 query rows and what they have seen: row n = lane % 32 in both halves of the wavefront.
+template <int DT, int HD, bool LSE>
+struct Rows {
+  using S = RowsShape<DT, HD>;
+  // fp16 weights are held 2^kOff times as large.  A reference moves when the 16 or 32 weights of a lane add up to kOver, which they do not
+  // where none is above the reference's own.
+  static constexpr float kOff = DT == CHUNKKV_F16 ? 9.f : 0.f, kOver = DT == CHUNKKV_F16 ? 32768.f : (DT == CHUNKKV_BF16 ? 256.f : 64.f);
+  u32x4 qf[S::kQ];
+  f32x16 acc[S::kD];
+  float m, mc, l, le, c1;
   // Are the references in log2 units below 2^14: their rounding, 2^-24 of them, is then no more than the scores' own, and the difference to
   // them one operation with the scale.
-  bool plain = false;
-  f32x16 acc[NDT];
-#pragma unroll
-  for (int i = 0; i < NDT; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+  bool plain;
 
-  if constexpr (PAGED) page_next = entry(0);
-  next_window(0);
-  load_mask(0);
-  uint64_t alive = tiles > 0 ? alive_of(0) : 0;
-  load_mask(1);
-  if (alive != 0) issue(0, 0);
-  for (int t = 0; t < tiles; ++t) {
-    const uint32_t buf = (uint32_t)(t & 1) * 2 * TILE;
-    __builtin_amdgcn_s_waitcnt(vm_imm(0));
-    if constexpr (MASK) {
-      // values of masked keys are multiplied by weights of zero, whatever bits they are: each wavefront clears those it has loaded
-      const int left = w.len - kRowsTile * t - 16 * wave;
-      const uint32_t dead = ~(uint32_t)(alive >> (16 * wave)) & (left >= 16 ? 0xFFFFu : (left > 0 ? (1u << left) - 1 : 0u));
-      if (dead != 0 && alive != 0) {
+  __device__ __forceinline__ void load(const char *from, int half, float scale_log2e) {
 #pragma unroll
-        for (int j = 0; j < NLD; ++j)
-          if (dead >> (RPL * j + lane / SEGS) & 1) *(u32x4 *)(smem + buf + TILE + wave * 16 * ROWB + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-      }
+    for (int i = 0; i < S::kQ; ++i) qf[i] = *(const u32x4 *)(from + (2 * i + half) * 16);
+    m = kPagedLowest;
+    mc = l = le = 0.f;
+    plain = false;
+    c1 = scale_log2e;
+#pragma unroll
+    for (int i = 0; i < S::kD; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+  }
+  // The rows are there from here on: said behind the first loads of keys, or the compiler waits for those too in front of the loop.
+  __device__ __forceinline__ void settle() {
+#pragma unroll
+    for (int i = 0; i < S::kQ; ++i) asm volatile("" : "+v"(qf[i]));
+  }
+  __device__ __forceinline__ void product(const u32x4 &kf, int i, f32x16 &sc) const {
+    if constexpr (DT == CHUNKKV_F32) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[i][e]), sc, 0, 0, 0);
+    } else {
+      sc = mma32<DT>(kf, qf[i], sc);
     }
-    __syncthreads();
-    const uint64_t now = alive;
-    if (t + 1 < tiles) {
-      next_window(t + 1);
-      alive = alive_of(t + 1);
-      if (alive != 0) issue(t + 1, (t + 1) & 1);
-      load_mask(t + 2);
-    }
-    if (now == 0 || idle) continue;
-
-    f32x16 sc[NKB];
+  }
+  // `bits`: keys of a 32-key block that count
+  static __device__ __forceinline__ void leave_out(f32x16 &sc, uint32_t bits, int half) {
+    bits >>= 4 * half;
 #pragma unroll
-    for (int b = 0; b < NKB; ++b) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NKS; ++i) {
-        const u32x4 kf = *(const u32x4 *)(smem + buf + ((kat ^ (uint32_t)(32 * i)) + (uint32_t)(b * 32 * ROWB)));
-        if constexpr (DT == CHUNKKV_F32) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[i][e]), sc[b], 0, 0, 0);
-        } else {
-          sc[b] = mma32<DT>(kf, qf[i], sc[b]);
-        }
-      }
-    }
-    if (now != ~0ull) {
-#pragma unroll
-      for (int b = 0; b < NKB; ++b) {
-        const uint32_t bits = (uint32_t)(now >> (32 * (b + wk))) >> (4 * half);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sc[b][e] = bits >> (8 * (e / 4) + e % 4) & 1 ? sc[b][e] : -__builtin_inff();
-      }
-    }
-    // weights of the tile and their sums
-    float p[NKB][16], sum, exact;
-    uint32_t pk[NKB][8];
-    auto weights = [&]() __attribute__((always_inline)) {
-      if (plain) {
+    for (int e = 0; e < 16; ++e) sc[e] = bits >> (8 * (e / 4) + e % 4) & 1 ? sc[e] : -__builtin_inff();
+  }
+  // Weights of NKB blocks: p, and for 16-bit types pk, pairs rounded; the sums take them in.
+  template <int NKB, bool SHORT>
+  __device__ __forceinline__ void weigh(const f32x16 (&sc)[NKB], float (&p)[NKB][16], uint32_t (&pk)[NKB][8]) {
+    float sum, exact;
+    auto weights = [&](bool direct) __attribute__((always_inline)) {
+      if (direct) {
 #pragma unroll
         for (int b = 0; b < NKB; ++b)
 #pragma unroll
@@ -373,9 +288,8 @@ __device__ __forceinline__ void rows_body(const RowsArgsOf<PAGED> &a, const Rows
       sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
       exact = (e4[0] + e4[1]) + (e4[2] + e4[3]);
     };
-    weights();
-    if (__builtin_amdgcn_ballot_w64(sum >= kOver) != 0) {
-      // move the references of the rows that outgrew them, in both halves
+    // moves the references of the rows that outgrew them, in both halves; no weight is above 1 then
+    auto move = [&]() __attribute__((always_inline)) {
       float mx = sc[0][0];
 #pragma unroll
       for (int b = 0; b < NKB; ++b)
@@ -383,7 +297,7 @@ __device__ __forceinline__ void rows_body(const RowsArgsOf<PAGED> &a, const Rows
         for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[b][e]);
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       const float over = fmaxf(sum, __shfl_xor(sum, 32));
-      const float m_new = over >= kOver ? mx : m;
+      const float m_new = over >= kOver ? fmaxf(mx, kPagedLowest) : m;
       const float f = __builtin_amdgcn_exp2f((m - m_new) * c1);
       m = m_new;
       mc = m * c1;
@@ -391,134 +305,499 @@ __device__ __forceinline__ void rows_body(const RowsArgsOf<PAGED> &a, const Rows
       l *= f;
       if constexpr (LSE) le *= f;
 #pragma unroll
-      for (int i = 0; i < NDT; ++i) acc[i] *= f;
-      weights();
+      for (int i = 0; i < S::kD; ++i) acc[i] *= f;
+    };
+    if constexpr (SHORT) {   // as few instructions as can be: a short range runs them from cold
+      bool moved = m == kPagedLowest;    // the first keys: from their maximum
+      sum = moved ? kOver : 0.f;
+#pragma nounroll
+      for (;;) {                         // twice at most
+        if (__builtin_amdgcn_ballot_w64(sum >= kOver) != 0) move();
+        weights(false);
+        if (moved || __builtin_amdgcn_ballot_w64(sum >= kOver) == 0) break;
+        moved = true;
+      }
+    } else {
+      weights(plain);
+      if (__builtin_amdgcn_ballot_w64(sum >= kOver) != 0) {
+        move();
+        weights(plain);
+      }
     }
     l += sum;
     if constexpr (LSE) le += exact;
+  }
+  // Values of 32 keys at `at` in LDS, this lane's place among them at vat[].  16 bits: read ahead of their use.
+  struct Values {
+    u32x4 v[2][S::kD];
+  };
+  static __device__ __forceinline__ void read_values(uint32_t at, const uint32_t (&vat)[S::kD], Values &x) {
+    if constexpr (DT != CHUNKKV_F32) {
+      uint32_t from[S::kD];
+#pragma unroll
+      for (int i = 0; i < S::kD; ++i) from[i] = at + vat[i];
+      read_vt<S::kRow>(from, x.v);
+    }
+  }
+  __device__ __forceinline__ void values(const char *smem, uint32_t at, const uint32_t (&vat)[S::kD], const Values &x, const float (&p)[16], const uint32_t (&pk)[8]) {
+    if constexpr (DT == CHUNKKV_F32) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const char *from = smem + at + vat[0] + (8 * (e / 4) + e % 4) * S::kRow;
+        float vf[S::kD];
+        if constexpr (S::kD == 4) {
+          const f32x4 y = *(const f32x4 *)from;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vf[i] = y[i];
+        } else {
+          const f32x2 y = *(const f32x2 *)from;
+          vf[0] = y[0];
+          vf[1] = y[1];
+        }
+#pragma unroll
+        for (int i = 0; i < S::kD; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[i], p[e], acc[i], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const u32x4 pf = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
+#pragma unroll
+        for (int i = 0; i < S::kD; ++i) acc[i] = mma32<DT>(x.v[ks][i], pf, acc[i]);
+      }
+    }
+  }
+  // Halves of a row together; fp16 weights back to their size.
+  __device__ __forceinline__ void close() {
+    l += __shfl_xor(l, 32);
+    if constexpr (LSE) le += __shfl_xor(le, 32);
+    if constexpr (DT == CHUNKKV_F32) le = l;
+    if constexpr (kOff != 0.f) {
+      l *= 0x1p-9f;
+      le *= 0x1p-9f;
+#pragma unroll
+      for (int i = 0; i < S::kD; ++i) acc[i] *= 0x1p-9f;
+    }
+  }
+  // State of wavefront `wave` into LDS: [wavefront][32 rows][HD], 16-byte pieces at piece ^ row; behind them [wavefront][32] of (m, l, le).
+  // Dims of acc[i][e]: 16 bits 32 i + 8 (e / 4) + 4 half + e % 4, fp32 kD (8 (e / 4) + 4 half + e % 4) + i.
+  static __device__ __forceinline__ uint32_t piece(int wave, int row, int dim) {
+    return (uint32_t)((wave * 32 + row) * HD + (((dim / 4) ^ (row & (HD / 4 - 1))) * 4) + dim % 4);
+  }
+  __device__ __forceinline__ void put(float *o, float4 *ml, int wave, int n, int half) const {
+    if (half == 0) ml[wave * 32 + n] = make_float4(m, l, le, 0.f);
+#pragma unroll
+    for (int e = 0; e < 16; e += DT == CHUNKKV_F32 ? 1 : 4) {
+      if constexpr (DT == CHUNKKV_F32 && S::kD == 4) {
+        *(f32x4 *)(o + piece(wave, n, 4 * (2 * (e / 4 * 4) + 4 * half + e % 4))) = f32x4{acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
+      } else if constexpr (DT == CHUNKKV_F32) {
+        *(f32x2 *)(o + piece(wave, n, 2 * (2 * (e / 4 * 4) + 4 * half + e % 4))) = f32x2{acc[0][e], acc[1][e]};
+      } else {
+#pragma unroll
+        for (int i = 0; i < S::kD; ++i) *(f32x4 *)(o + piece(wave, n, 32 * i + 2 * e + 4 * half)) = f32x4{acc[i][e], acc[i][e + 1], acc[i][e + 2], acc[i][e + 3]};
+      }
+    }
+  }
+};
+
+// States of wavefronts in LDS, W of them of the same 32 rows, to outputs or partial rows; eight threads to a row.
+template <int DT, int HD, bool LSE, int W, typename R>
+__device__ __forceinline__ void rows_finish(const R &r, const RowsWork &w, const float *o, const float4 *ml, int rows, int t, int threads) {
+  const int heads = (int)(r.heads.d * r.group.d), first = t % 8 * 4;   // every eighth 16-byte piece of a row
+  for (int i = t / 8; i < rows; i += threads / 8) {
+    const int row = w.row0 + i, wave = i / 32 * W, n = i % 32;
+    float f[W], M = kPagedLowest, l = 0.f, le = 0.f;
+    float4 s[W];
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      s[k] = ml[(wave + k) * 32 + n];
+      M = fmaxf(M, s[k].x);
+    }
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      f[k] = W == 1 ? 1.f : __builtin_amdgcn_exp2f((s[k].x - M) * r.scale_log2e);
+      l += s[k].y * f[k];
+      le += s[k].z * f[k];
+    }
+    f32x4 x[HD / 32];
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j) {
+      x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < W; ++k) x[j] += *(const f32x4 *)(o + Rows<DT, HD, LSE>::piece(wave + k, n, first + 32 * j)) * f[k];
+    }
+    if (w.part < 0) {
+      const int token = divided(row, r.group), head = w.h * (int)r.group.d + (row - token * (int)r.group.d);
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      char *to = w.out + token * r.out_tok + head * r.out_head + first * RowsShape<DT, HD>::kEsz;
+#pragma unroll
+      for (int j = 0; j < HD / 32; ++j) store4<DT>(to + 32 * j * RowsShape<DT, HD>::kEsz, x[j] * inv);
+      if (LSE && w.lse != nullptr && first == 0)
+        w.lse[(int64_t)token * heads + head] = le > 0.f ? __builtin_fmaf(M, r.scale, __builtin_log2f(le) * 0.6931471805599453f) : -__builtin_inff();
+    } else {
+      const int64_t p = w.part + ((int64_t)w.split * (int)r.heads.d + w.h) * w.rows + row;
+      if (first == 0) r.part_ml[p] = make_float4(M, l, le, 0.f);
+#pragma unroll
+      for (int j = 0; j < HD / 32; ++j) *(f32x4 *)(r.part_o + p * HD + first + 32 * j) = x[j];
+    }
+  }
+}
+
+// The keys of a range: which there are, and loads of 16-row blocks of theirs.  They are looked up by windows of 64 blocks, a block to a
+// lane, one window ahead.
+template <int DT, int HD, bool PAGED, bool MASK>
+struct RowsKeys {
+  using S = RowsShape<DT, HD>;
+  const RowsArgsOf<PAGED> &a;
+  const RowsWork &w;
+  int lane;
+  uint32_t tok, live = 0;                // live: keys of this lane's block that count
+  int32_t page = -1, page_next = -1;     // pages: entries of this window and of the next one
+  u32x4 mask_next = {0, 0, 0, 0};        // bytes of the mask
+  __device__ __forceinline__ RowsKeys(const RowsArgsOf<PAGED> &a_, const RowsWork &w_, int lane_) : a(a_), w(w_), lane(lane_), tok((uint32_t)a_.r.geom.tok) {
+    if constexpr (PAGED) page_next = w.page;
+    fetch_mask(0);
+  }
+  __device__ __forceinline__ void fetch_mask(int window) {
+    if constexpr (MASK) {
+      const int key = 16 * (64 * window + lane), left = w.len - key;
+      const uint8_t *from = w.mask + key;
+      mask_next = u32x4{0, 0, 0, 0};
+      if (left >= 16) {
+        __builtin_memcpy(&mask_next, from, 16);
+      } else if (left > 0) {
+#pragma unroll
+        for (int i = 0; i < 15; ++i)
+          if (i < left) mask_next[i / 4] |= (uint32_t)from[i] << (8 * (i % 4));
+      }
+    }
+  }
+  // Before the first look at block 64 `window`.
+  __device__ __forceinline__ void open(int window) {
+    const int blk = 64 * window + lane, left = w.len - 16 * blk;
+    live = left >= 16 ? 0xFFFFu : (left > 0 ? (1u << left) - 1 : 0u);
+    if constexpr (PAGED) {
+      page = page_next;
+      if (page < 0 || page >= a.r.geom.n_pages) live = 0;
+      page_next = left > 1024 ? w.table[page_of_block(a.r.geom, (uint32_t)(w.r0 / 16 + blk + 64))] : -1;
+    }
+    if constexpr (MASK) {
+      uint32_t bits = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {   // a bit for every byte that is not zero
+        uint32_t y = mask_next[i];
+        y |= y >> 4;
+        y |= y >> 2;
+        y |= y >> 1;
+        bits |= (((y & 0x01010101u) * 0x01020408u) >> 24) << (4 * i);
+      }
+      live &= bits;
+      fetch_mask(window + 1);
+    }
+  }
+  // Keys key0 .. key0 + 16 N - 1 that count, one bit each.
+  template <int N>
+  __device__ __forceinline__ uint64_t alive(int key0) const {
+    const int blk = key0 / 16 & 63;
+    uint64_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) bits |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)live, blk + i) << (16 * i);
+    return bits;
+  }
+  // N loads from the block of key key0, a multiple of 16, at this lane's offsets in it; `wanted` false: empty ones, which write zeros.
+  template <int N>
+  __device__ __forceinline__ void load(const char *base, int key0, bool wanted, const uint32_t *off, char *to) const {
+    const int left = w.len - key0, rows = left < 16 ? left : 16;
+    int64_t at = 0;
+    bool there = wanted && rows > 0;
+    if constexpr (PAGED) {
+      at = block_offset(a.r.geom, __builtin_amdgcn_readlane(page, key0 / 16 & 63), w.h, (uint32_t)((w.r0 + key0) / 16));
+      there = there && at >= 0;
+      at = there ? at : 0;
+    } else {
+      at = there ? key0 * a.r.geom.tok : 0;
+    }
+    const int span = there ? (int)((uint32_t)(rows - 1) * tok) + S::kRow : 0;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(base + at), 0, span, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < N; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(to + j * 1024), 16, off[j], 0, 0, 0);
+  }
+};
+
+// This lane's places in a block of 32 keys in LDS.  K: key n, segment 2 i + half is at kat ^ 32 i.  V, 16 bits: keys 4 half + (lane % 16) / 4 of
+// 16, dims 32 i + 16 (lane / 16 % 2) + 4 (lane % 4) ..; fp32: key 4 half of eight, dims kD n ..
+template <int DT, int HD>
+__device__ __forceinline__ void rows_places(int lane, uint32_t lds0, uint32_t &kat, uint32_t (&vat)[HD / 32]) {
+  using S = RowsShape<DT, HD>;
+  const int n = lane & 31, half = lane >> 5;
+  kat = (uint32_t)(n * S::kRow + ((half ^ S::kswz(n)) * 16));
+#pragma unroll
+  for (int i = 0; i < S::kD; ++i) {
+    if constexpr (DT == CHUNKKV_F32) {
+      vat[i] = (uint32_t)(4 * half * S::kRow + n * S::kD * 4);
+    } else {
+      const int p = lane & 15, key = 4 * half + p / 4, seg = 4 * i + 2 * (lane >> 4 & 1) + (p % 4) / 2;
+      vat[i] = lds0 + (uint32_t)(key * S::kRow + ((seg ^ S::vswz(key)) * 16) + (p & 1) * 8);
+    }
+  }
+}
+
+// Query row `row` of a tile; for one that is not there, one that is.
+template <typename R>
+__device__ __forceinline__ const char *rows_query(const R &r, const RowsWork &w, int row) {
+  const int i = row < w.rows ? row : (w.rows > 0 ? w.rows - 1 : 0), token = divided(i, r.group);
+  return w.q + token * r.q_tok + (w.h * (int)r.group.d + (i - token * (int)r.group.d)) * r.q_head;
+}
+
+// A barrier that waits for LDS, not for the loads that are on their way.
+__device__ __forceinline__ void rows_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// 256 rows (WK = 1) or 128 (WK = 2: wavefronts that share rows).
+template <int DT, int HD, bool PAGED, bool MASK, bool LSE, int WK>
+__device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const RowsWork &w, char *smem, int wave, int lane) {
+  using S = RowsShape<DT, HD>;
+  const auto &r = a.r;
+  constexpr int NL = 8 / S::kRpl, NST = S::kStages, NKB = 2 / WK;   // loads of a wavefront's eight rows of a tile; 32-key blocks of a tile that it has
+  const int n = lane & 31, half = lane >> 5, wk = WK == 2 ? wave & 1 : 0, wr = wave / WK;
+  const bool idle = w.row0 + 32 * wr >= w.rows;      // this wavefront's rows are not there: it loads and waits with the others
+  RowsKeys<DT, HD, PAGED, MASK> keys(a, w, lane);
+  uint32_t koff[NL], voff[NL];           // of a lane in this wavefront's rows of a tile, 8 wave ..: half of a block
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    const int i = S::kRpl * j + lane / S::kSegs, pos = lane % S::kSegs, in_block = 8 * (wave & 1) + i;
+    koff[j] = (uint32_t)in_block * keys.tok + (uint32_t)((pos ^ S::kswz(in_block)) * 16);
+    voff[j] = (uint32_t)in_block * keys.tok + (uint32_t)((pos ^ S::vswz(in_block)) * 16);
+  }
+  const int tiles = w.len > 0 ? (w.len + kRowsTile - 1) / kRowsTile : 0;
+  uint64_t alive[NST];                   // keys that count, of the tiles in flight
+  auto issue = [&](int t, int stage) __attribute__((always_inline)) {   // tiles past the last one too: the number of loads in flight is known at every wait
+    if ((t & 15) == 0) keys.open(t / 16);
+    const uint64_t bits = keys.template alive<4>(kRowsTile * t);
+    char *to = smem + stage * 2 * S::kTile + wave * 8 * S::kRow;
+    const int key0 = kRowsTile * t + 16 * (wave / 2);
+    keys.template load<NL>(w.k, key0, bits != 0, koff, to);
+    keys.template load<NL>(w.v, key0, bits != 0, voff, to + S::kTile);
+    return bits;
+  };
+  uint32_t kat, vat[S::kD];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+  rows_places<DT, HD>(lane, lds0, kat, vat);
+  Rows<DT, HD, LSE> x;
+  x.load(rows_query(r, w, w.row0 + 32 * wr + n), half, r.scale_log2e);
+#pragma unroll
+  for (int t = 0; t < NST - 1; ++t) alive[t] = issue(t, t);
+  x.settle();
+  alive[NST - 1] = 0;
+  for (int t = 0; t < tiles; ++t) {
+    const int stage = t % NST;
+    const uint32_t base = (uint32_t)stage * 2 * S::kTile + (uint32_t)(32 * wk * S::kRow);
+    __builtin_amdgcn_s_waitcnt(vm_imm((NST - 2) * 2 * NL));
+    const uint64_t now = alive[0];
+    if constexpr (MASK) {
+      // values of keys that do not count are multiplied by weights of zero, whatever bits they are: each wavefront clears those it has loaded
+      const int left = w.len - kRowsTile * t - 8 * wave;
+      const uint32_t dead = ~(uint32_t)(now >> (8 * wave)) & (left >= 8 ? 0xFFu : (left > 0 ? (1u << left) - 1 : 0u));
+      if (dead != 0 && now != 0) {
+#pragma unroll
+        for (int j = 0; j < NL; ++j)
+          if (dead >> (S::kRpl * j + lane / S::kSegs) & 1) *(u32x4 *)(smem + stage * 2 * S::kTile + S::kTile + wave * 8 * S::kRow + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+      }
+    }
+    rows_barrier();
+#pragma unroll
+    for (int i = 0; i < NST - 2; ++i) alive[i] = alive[i + 1];
+    alive[NST - 2] = issue(t + NST - 1, (t + NST - 1) % NST);
+    if (now == 0 || idle) continue;
+    f32x16 sc[NKB];
+    u32x4 kf[S::kAhead];
+    auto read_k = [&](int j) __attribute__((always_inline)) {   // read j of the tile's, block by block
+      if (j < NKB * S::kQ) kf[j % S::kAhead] = *(const u32x4 *)(smem + base + ((kat ^ (uint32_t)(32 * (j % S::kQ))) + (uint32_t)(j / S::kQ * 32 * S::kRow)));
+    };
+#pragma unroll
+    for (int j = 0; j < S::kAhead; ++j) read_k(j);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int b = 0; b < NKB; ++b) {
-      if constexpr (DT == CHUNKKV_F32) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const char *from = smem + buf + vat[0] + (b * 32 + 8 * (e / 4) + e % 4) * ROWB;
-          float vf[NDT];
-          if constexpr (NDT == 4) {
-            const f32x4 x = *(const f32x4 *)from;
+      for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) vf[i] = x[i];
-          } else {
-            const f32x2 x = *(const f32x2 *)from;
-            vf[0] = x[0];
-            vf[1] = x[1];
-          }
-#pragma unroll
-          for (int i = 0; i < NDT; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[i], p[b][e], acc[i], 0, 0, 0);
-        }
-      } else {
-        auto half_block = [&](auto at) __attribute__((always_inline)) {
-          constexpr int ks = decltype(at)::value;
-          u32x4 vf[NDT];
-          constexpr int OFF = ks * 16 * ROWB;
-          const uint32_t base = buf + (uint32_t)(b * 32 * ROWB);
-          if constexpr (NDT == 4) read_vt<OFF, 8 * ROWB>(base + vat[0], base + vat[1], base + vat[2], base + vat[3], vf);
-          else read_vt<OFF, 8 * ROWB>(base + vat[0], base + vat[1], vf);
-          const u32x4 pf = {pk[b][4 * ks], pk[b][4 * ks + 1], pk[b][4 * ks + 2], pk[b][4 * ks + 3]};
-#pragma unroll
-          for (int i = 0; i < NDT; ++i) acc[i] = mma32<DT>(vf[i], pf, acc[i]);
-        };
-        half_block(std::integral_constant<int, 0>{});
-        half_block(std::integral_constant<int, 1>{});
+      for (int i = 0; i < S::kQ; ++i) {
+        x.product(kf[i % S::kAhead], i, sc[b]);
+        read_k(b * S::kQ + i + S::kAhead);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    typename Rows<DT, HD, LSE>::Values vf;
+    x.read_values(base + (uint32_t)S::kTile, vat, vf);   // while the products run
+    if (now != ~0ull) {
+#pragma unroll
+      for (int b = 0; b < NKB; ++b) x.leave_out(sc[b], (uint32_t)(now >> (32 * (b + wk))), half);
+    }
+    float p[NKB][16];
+    uint32_t pk[NKB][8];
+    x.template weigh<NKB, false>(sc, p, pk);
+#pragma unroll
+    for (int b = 0; b < NKB; ++b) {
+      const uint32_t at = base + (uint32_t)(S::kTile + b * 32 * S::kRow);
+      if (b > 0) x.read_values(at, vat, vf);
+      x.values(smem, at, vat, vf, p[b], pk[b]);
+    }
   }
+  __builtin_amdgcn_s_waitcnt(vm_imm(0));   // the empty loads write into LDS too
+  x.close();
+  __syncthreads();                         // the tiles are read
+  if (!idle) x.put((float *)smem, (float4 *)(smem + S::kLds), wave, n, half);
+  __syncthreads();
+  const int left = w.rows - w.row0, most = 256 / WK;
+  rows_finish<DT, HD, LSE, WK>(r, w, (const float *)smem, (const float4 *)(smem + S::kLds), left < most ? left : most, wave * 64 + lane, 512);
+}
 
-  // ---- halves of a row, then the wavefronts that share rows
-  l += __shfl_xor(l, 32);
-  if constexpr (LSE) le += __shfl_xor(le, 32);
-  if constexpr (DT == CHUNKKV_F32) le = l;
-  if constexpr (kOff != 0.f) {
-    l *= 0x1p-10f;
-    le *= 0x1p-10f;
+// 32 rows, by four wavefronts.
+template <int DT, int HD, bool PAGED, bool MASK, bool LSE>
+__device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const RowsWork &w, char *smem, float4 *ml, int wave, int lane) {
+  using S = RowsShape<DT, HD>;
+  const auto &r = a.r;
+  constexpr int NL = 16 / S::kRpl, SLOT = 32 * S::kRow;   // loads of a block; a slot has two
+  const int n = lane & 31, half = lane >> 5;
+  RowsKeys<DT, HD, PAGED, MASK> keys(a, w, lane);
+  uint32_t koff[NL], voff[NL];
 #pragma unroll
-    for (int i = 0; i < NDT; ++i) acc[i] *= 0x1p-10f;
+  for (int j = 0; j < NL; ++j) {
+    const int i = S::kRpl * j + lane / S::kSegs, pos = lane % S::kSegs;
+    koff[j] = (uint32_t)i * keys.tok + (uint32_t)((pos ^ S::kswz(i)) * 16);
+    voff[j] = (uint32_t)i * keys.tok + (uint32_t)((pos ^ S::vswz(i)) * 16);
   }
-  if constexpr (WK == 2) {
-    __syncthreads();                     // the tiles are read
-    float *state = (float *)smem + wr * (16 * NDT + 3) * 64 + lane;
-    if (wk == 1) {
-      state[0] = m;
-      state[64] = l;
-      state[128] = le;
+  char *kslot = smem + wave * 2 * SLOT, *vslot = kslot + SLOT;
+  auto key_of = [&](int s) { return 32 * (wave + 4 * s); };
+  const int steps_all = w.len > 0 ? (w.len + 31) / 32 : 0, steps = (steps_all - wave + 3) / 4;
+  auto look = [&](int s) __attribute__((always_inline)) {   // keys of step s that count
+    if ((s & 7) == 0) keys.open(s / 8);              // V of step s is issued before the next look
+    return (uint32_t)keys.template alive<2>(key_of(s));
+  };
+  auto issue = [&](const char *base, const uint32_t (&off)[NL], int s, bool wanted, char *to) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < NDT; ++i)
+    for (int t = 0; t < 2; ++t) keys.template load<NL>(base, key_of(s) + 16 * t, wanted, off, to + t * NL * 1024);
+  };
+  uint32_t kat, vat[S::kD];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+  rows_places<DT, HD>(lane, lds0, kat, vat);
+  const uint32_t kbase = (uint32_t)(wave * 2 * SLOT);
+  Rows<DT, HD, LSE> x;
+  x.load(rows_query(r, w, n), half, r.scale_log2e);
+  uint32_t bits = look(0);
+  issue(w.k, koff, 0, bits != 0, kslot);
+  issue(w.v, voff, 0, bits != 0, vslot);
+  x.settle();
+  for (int s = 0; s < steps; ++s) {
+    const uint32_t now = bits;
+    __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL));
+    u32x4 kf[S::kAhead];
+    f32x16 sc[1];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) state[(3 + 16 * i + e) * 64] = acc[i][e];
-    }
-    __syncthreads();
-    if (wk == 1) return;
-    const float m1 = state[0], M = fmaxf(m, m1), f0 = __builtin_amdgcn_exp2f((m - M) * c1), f1 = __builtin_amdgcn_exp2f((m1 - M) * c1);
-    m = M;
-    l = l * f0 + state[64] * f1;
-    le = le * f0 + state[128] * f1;
+    for (int e = 0; e < 16; ++e) sc[0][e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < NDT; ++i)
+    for (int i0 = 0; i0 < S::kQ; i0 += S::kAhead) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][e] = acc[i][e] * f0 + state[(3 + 16 * i + e) * 64] * f1;
-  }
-  if (row >= w.rows) return;
-  // dims of acc[i][e]: 16 bits 32 i + 8 (e / 4) + 4 half + e % 4, fp32 NDT (8 (e / 4) + 4 half + e % 4) + i
-  if (w.part < 0) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    char *to = w.out + token * r.out_tok + head * r.out_head;
-#pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      if constexpr (DT == CHUNKKV_F32) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < NDT; ++i) *(float *)(to + (NDT * (2 * e + 4 * half + j) + i) * 4) = acc[i][e + j] * inv;
-      } else {
-#pragma unroll
-        for (int i = 0; i < NDT; ++i)
-          *(uint2 *)(to + (32 * i + 2 * e + 4 * half) * 2) = make_uint2(pack2<DT>(acc[i][e] * inv, acc[i][e + 1] * inv), pack2<DT>(acc[i][e + 2] * inv, acc[i][e + 3] * inv));
+      for (int i = 0; i < S::kAhead; ++i) kf[i] = *(const u32x4 *)(smem + kbase + (kat ^ (uint32_t)(32 * (i0 + i))));
+      if (i0 + S::kAhead == S::kQ) {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // the fragments are in registers: the K slot is free
+        bits = look(s + 1);
+        issue(w.k, koff, s + 1, bits != 0, kslot);
       }
+#pragma unroll
+      for (int i = 0; i < S::kAhead; ++i) x.product(kf[i], i0 + i, sc[0]);
     }
-    if (LSE && w.lse != nullptr && half == 0)
-      w.lse[(int64_t)token * r.n_kv_heads * g + head] = le > 0.f ? __builtin_fmaf(m, r.scale, __builtin_log2f(le) * 0.6931471805599453f) : -__builtin_inff();
+    if (now != 0) {
+      if (now != ~0u) x.leave_out(sc[0], now, half);
+      float p[1][16];
+      uint32_t pk[1][8];
+      x.template weigh<1, true>(sc, p, pk);
+      __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL));
+      if constexpr (MASK) {
+        const int left = w.len - key_of(s);
+        const uint32_t dead = ~now & (left >= 32 ? ~0u : (1u << left) - 1);
+        if (dead != 0) {
+#pragma unroll
+          for (int j = 0; j < 2 * NL; ++j)
+            if (dead >> (S::kRpl * j + lane / S::kSegs) & 1) *(u32x4 *)(vslot + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+        }
+      }
+      typename Rows<DT, HD, LSE>::Values vf;
+      x.read_values(kbase + SLOT, vat, vf);
+      x.values(smem, kbase + SLOT, vat, vf, p[0], pk[0]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL) & 0xC07F);   // V of this step is there and read
+    issue(w.v, voff, s + 1, bits != 0, vslot);
+  }
+  __builtin_amdgcn_s_waitcnt(vm_imm(0));
+  x.close();
+  __syncthreads();                         // the other wavefronts' slots are read
+  if (n < w.rows) x.put((float *)smem, ml, wave, n, half);
+  __syncthreads();
+  rows_finish<DT, HD, LSE, 4>(r, w, (const float *)smem, ml, w.rows, wave * 64 + lane, 256);
+}
+
+// Segment of this workgroup, and its number in it.
+template <typename R>
+__device__ __forceinline__ RowsSegment rows_find(const R &r, int &s, int &x) {
+  constexpr int N = R::kSegments;
+  s = rows_segment<N>(blockIdx.x, r.segments);
+  x = blockIdx.x - kernarg_at<int32_t>(offsetof(RowsArgs<N>, first), s);
+  return rows_segment_at(offsetof(RowsArgs<N>, segment) + s * sizeof(RowsSegment));
+}
+
+constexpr int kRowsThreads = 512;
+template <int DT, int HD, bool PAGED, bool MASK, bool LSE>
+__global__ __launch_bounds__(kRowsThreads, 2) void rows_kernel(RowsArgsOf<PAGED> a) {
+  using S = RowsShape<DT, HD>;
+  __shared__ __align__(16) char smem[S::kLds + 8 * 32 * sizeof(float4)];
+  const auto &r = a.r;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  int s, x;
+  const RowsSegment seg = rows_find(r, s, x);
+  if (seg.rows <= kRowsNarrow) {
+    const int hf = wave / 4, items = seg.splits * (int)r.heads.d, item = S::kNarrow * x + hf;
+    if (hf >= S::kNarrow) return;
+    const bool none = item >= items;     // an odd number: the other half waits with it, over no keys
+    RowsWork w = rows_work<PAGED, MASK>(a, seg, s, none ? items - 1 : item, kRowsNarrow, lane);
+    if (none) w.len = w.rows = 0;
+    rows_narrow<DT, HD, PAGED, MASK, LSE>(a, w, smem + hf * 4 * 2 * 32 * S::kRow, (float4 *)(smem + S::kLds) + hf * 4 * 32, wave & 3, lane);
   } else {
-    const int64_t at = w.part + ((int64_t)w.split * r.n_kv_heads + w.h) * w.rows + row;
-    if (half == 0) r.part_ml[at] = make_float4(m, l, le, 0.f);
-    float *to = r.part_o + at * HD;
-#pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      if constexpr (DT == CHUNKKV_F32) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < NDT; ++i) to[NDT * (2 * e + 4 * half + j) + i] = acc[i][e + j];
-      } else {
-#pragma unroll
-        for (int i = 0; i < NDT; ++i) *(f32x4 *)(to + 32 * i + 2 * e + 4 * half) = f32x4{acc[i][e], acc[i][e + 1], acc[i][e + 2], acc[i][e + 3]};
-      }
-    }
+    const RowsWork w = rows_work<PAGED, MASK>(a, seg, s, x, r.tile, lane);
+    if (r.tile == 2 * kRowsWide) rows_wide<DT, HD, PAGED, MASK, LSE, 1>(a, w, smem, wave, lane);
+    else rows_wide<DT, HD, PAGED, MASK, LSE, 2>(a, w, smem, wave, lane);
   }
+}
+
+// Where no segment has more than 32 rows: half a workgroup each.  Less code to fetch and no other half to wait for, which is what short
+// ranges consist of.
+template <int DT, int HD, bool PAGED, bool MASK, bool LSE>
+__global__ __launch_bounds__(kThreads, DT == CHUNKKV_F32 && HD == 128 ? 1 : 2) void rows_narrow_kernel(RowsArgsOf<PAGED> a) {
+  using S = RowsShape<DT, HD>;
+  __shared__ __align__(16) char smem[4 * 2 * 32 * S::kRow + 4 * 32 * sizeof(float4)];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  int s, x;
+  const RowsSegment seg = rows_find(a.r, s, x);
+  const RowsWork w = rows_work<PAGED, MASK>(a, seg, s, x, kRowsNarrow, lane);
+  rows_narrow<DT, HD, PAGED, MASK, LSE>(a, w, smem, (float4 *)(smem + 4 * 2 * 32 * S::kRow), wave, lane);
 }
 
 template <int DT, int HD, bool PAGED, bool MASK, bool LSE>
-__global__ __launch_bounds__(kThreads, DT == CHUNKKV_F32 && HD == 128 ? 1 : 2) void rows_kernel(RowsArgsOf<PAGED> a) {
-  __shared__ __align__(16) char smem[4 * kRowsTile * HD * (DT == CHUNKKV_F32 ? 4 : 2)];
-  const RowsWork w = rows_work<PAGED, MASK>(a);
-  if (w.rows > kRowsNarrow) rows_body<DT, HD, PAGED, MASK, LSE, 1>(a, w, smem);
-  else rows_body<DT, HD, PAGED, MASK, LSE, 2>(a, w, smem);
+int launch_rows_of(const RowsArgsOf<PAGED> &a, hipStream_t s) {
+  const dim3 grid((uint32_t)a.r.first[a.r.segments]);
+  if (a.r.tile == kRowsNarrow) hipLaunchKernelGGL((rows_narrow_kernel<DT, HD, PAGED, MASK, LSE>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((rows_kernel<DT, HD, PAGED, MASK, LSE>), grid, dim3(kRowsThreads), 0, s, a);
+  return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
 }
-
 template <int DT, int HD, bool PAGED, bool MASK>
 int launch_rows(const RowsArgsOf<PAGED> &a, hipStream_t s) {
-  const dim3 grid((uint32_t)a.r.first[a.r.segments]);
-  if (a.r.lse != nullptr) hipLaunchKernelGGL((rows_kernel<DT, HD, PAGED, MASK, true>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((rows_kernel<DT, HD, PAGED, MASK, false>), grid, dim3(kThreads), 0, s, a);
-  return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
+  return a.r.lse != nullptr ? launch_rows_of<DT, HD, PAGED, MASK, true>(a, s) : launch_rows_of<DT, HD, PAGED, MASK, false>(a, s);
 }
 template <int DT, int HD>
 int launch_rows_cross(const CrossArgs &a, hipStream_t s) {

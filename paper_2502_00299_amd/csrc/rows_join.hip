@@ -8,29 +8,28 @@
 
 namespace ckv {
 
-#define CKV_JOIN(FIELD, I) kernarg_at<std::remove_extent_t<decltype(JoinArgs::FIELD)>>(offsetof(JoinArgs, FIELD), (I))
-
 template <int DT, int HD, int G>
 __global__ __launch_bounds__(kThreads) void rows_join_kernel(JoinArgs a) {
   constexpr int TPR = HD / 4, RPB = kThreads / (TPR * G), UN = 4;
   __shared__ f32x4 s_acc[G > 1 ? G : 1][TPR];
   __shared__ float s_m[G], s_l[G], s_e[G];
-  const int t = threadIdx.x, col = t % TPR, grp = G > 1 ? t / TPR : 0;
-  const int64_t hq_all = (int64_t)a.n_kv_heads * a.group, x = (int64_t)blockIdx.x * RPB + (G > 1 ? 0 : t / TPR);
-  if (x >= a.tokens * hq_all) return;   // with groups, a whole workgroup
-  const int token = (int)(x / hq_all), hq = (int)(x - token * hq_all), h = hq / a.group, j = hq - h * a.group;
+  const int t = threadIdx.x, col = t % TPR, grp = G > 1 ? t / TPR : 0, hkv = (int)a.heads.d, g = (int)a.group.d, hq_all = hkv * g;
+  const int64_t x = (int64_t)blockIdx.x * RPB + (G > 1 ? 0 : t / TPR);
+  if (x >= (int64_t)a.tokens * hq_all) return;   // with groups, a whole workgroup
+  const int token = (int)(x / hq_all), hq = (int)(x - (int64_t)token * hq_all), h = divided(hq, a.group), j = hq - h * g;
   // segment of the token; the rows of a workgroup may belong to several
-  int s = 0;
-  for (int lo = 0, hi = a.segments; hi - lo > 1;) {
-    const int mid = (lo + hi) / 2;
-    if (token >= CKV_JOIN(first, mid)) lo = mid;
-    else hi = mid;
-    s = lo;
+  int s = token;
+  if (a.segments != a.tokens) {
+    s = 0;
+    for (int i = 1; i < a.segments; ++i) s += token >= kernarg_at<int32_t>(offsetof(JoinArgs, first), i) ? 1 : 0;
   }
-  const int nth = token - CKV_JOIN(first, s), own = CKV_JOIN(splits, s), all = own + CKV_JOIN(prefix_splits, s);
-  const int rows = CKV_JOIN(rows, s), prefix_rows = CKV_JOIN(prefix_rows, s);
-  const int64_t at = CKV_JOIN(part, s) + (int64_t)h * rows + (int64_t)nth * a.group + j;
-  const int64_t prefix_at = CKV_JOIN(prefix_part, s) + (int64_t)h * prefix_rows + CKV_JOIN(prefix_row0, s) + (int64_t)nth * a.group + j;
+  const size_t place = offsetof(JoinArgs, segment) + s * sizeof(JoinSegment);
+  auto number = [&](int i) { return kernarg_at<int32_t>(place, i); };
+  const JoinSegment seg = {number(0), number(1), number(2), number(3), number(4), number(5), number(6), number(7), kernarg_at<int64_t>(place + 32, 0)};
+  const int nth = a.segments != a.tokens ? token - kernarg_at<int32_t>(offsetof(JoinArgs, first), s) : 0;
+  const int own = seg.splits, all = own + seg.prefix_splits;
+  const int64_t at = seg.part + (int64_t)h * seg.rows + (int64_t)nth * g + j;
+  const int64_t prefix_at = seg.prefix_part + (int64_t)h * seg.prefix_rows + seg.prefix_row0 + (int64_t)nth * g + j;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float m = kPagedLowest, l = 0.f, le = 0.f;
   const float c1 = a.scale_log2e;
@@ -40,7 +39,7 @@ __global__ __launch_bounds__(kThreads) void rows_join_kernel(JoinArgs a) {
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       const int i = i0 + u * G < all ? i0 + u * G : i0;
-      const int64_t p = i < own ? at + (int64_t)i * a.n_kv_heads * rows : prefix_at + (int64_t)(i - own) * a.n_kv_heads * prefix_rows;
+      const int64_t p = i < own ? at + (int64_t)i * hkv * seg.rows : prefix_at + (int64_t)(i - own) * hkv * seg.prefix_rows;
       ml[u] = a.part_ml[p];
       o[u] = *(const f32x4 *)(a.part_o + p * HD + col * 4);
     }
@@ -80,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void rows_join_kernel(JoinArgs a) {
     m = M;
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  char *to = (char *)a.out + CKV_JOIN(out_base, s) + nth * a.out_tok + hq * a.out_head;
+  char *to = (char *)a.out + seg.out_base + nth * a.out_tok + hq * a.out_head;
   if constexpr (DT == CHUNKKV_F32) {
     *(f32x4 *)(to + col * 16) = acc * inv;
   } else if constexpr (DT == CHUNKKV_BF16) {
@@ -91,13 +90,13 @@ __global__ __launch_bounds__(kThreads) void rows_join_kernel(JoinArgs a) {
     *(f16x4 *)(to + col * 8) = __builtin_convertvector(acc * inv, f16x4);
   }
   if (a.lse != nullptr && col == 0)
-    a.lse[CKV_JOIN(lse_base, s) + (int64_t)nth * hq_all + hq] = le > 0.f ? __builtin_fmaf(m, a.scale, __builtin_log2f(le) * 0.6931471805599453f) : -__builtin_inff();
+    a.lse[(int64_t)(seg.token0 + nth) * hq_all + hq] = le > 0.f ? __builtin_fmaf(m, a.scale, __builtin_log2f(le) * 0.6931471805599453f) : -__builtin_inff();
 }
 
 template <int DT, int HD>
 int launch_join_of(const JoinArgs &a, hipStream_t s) {
   constexpr int TPR = HD / 4, G = kThreads / TPR;
-  const int64_t rows = (int64_t)a.tokens * a.n_kv_heads * a.group;
+  const int64_t rows = (int64_t)a.tokens * (int)(a.heads.d * a.group.d);
   if (rows <= 4096) hipLaunchKernelGGL((rows_join_kernel<DT, HD, G>), dim3((uint32_t)rows), dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((rows_join_kernel<DT, HD, 1>), dim3((uint32_t)((rows + G - 1) / G)), dim3(kThreads), 0, s, a);
   return hipGetLastError() == hipSuccess ? CHUNKKV_OK : CHUNKKV_ERR_LAUNCH;
