@@ -472,7 +472,7 @@ int chunkkv_cross_attention(const chunkkv_cross *cross, const int32_t *kv_len, c
  *   q            device [B][Hq][d], 16-byte aligned;  out  device [B][Hq][d] in the storage type;  lse  NULL or device float [B][Hq]
  *   workspace    chunkkv_shared_decode_workspace_bytes(prefix, pages, n_sharing) bytes (0 = invalid), contents scratch
  * No slot in either: out = 0, lse = -inf.  Pages that are not there, rows without a token and precision of weights and outputs as in
- * chunkkv_paged_decode_attention and chunkkv_cross_attention.  Two launches up to 64 sequences and 16 prefixes.                   */
+ * chunkkv_paged_decode_attention and chunkkv_cross_attention.  Two launches up to 64 sequences and 8 prefixes.                    */
 size_t chunkkv_shared_decode_workspace_bytes(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing);
 int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing,
                                     const int32_t *prefix_table, const int32_t *prefix_len, const int32_t *page_table, const int32_t *kv_len,

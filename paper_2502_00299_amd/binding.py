@@ -233,11 +233,6 @@ class _CCross(C.Structure):
     ]
 
 
-class _CRows(C.Structure):
-    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n_heads", C.c_int32), ("in_stride_seq", C.c_int64), ("in_stride_head", C.c_int64), ("in_stride_tok", C.c_int64),
-                ("out_stride_seq", C.c_int64), ("out_stride_head", C.c_int64), ("out_stride_tok", C.c_int64)]
-
-
 @dataclass
 class Cross(_KeepsStruct):
     """Python mirror of chunkkv_cross (see include/chunkkv.h for the meaning of every field).  Without bases queries and outputs are packed
@@ -780,49 +775,61 @@ def chunkkv_rotary_frequencies(rotary_dim: int, base: float, factor: float = 1.0
 _DTYPES = {kind: code for code, kind in _KINDS.items()}
 
 
-def _four(where: str, name: str, t: torch.Tensor):
-    """Shape and strides of rows as [seqs][tokens][heads][dim]."""
-    if t.dim() not in (3, 4):
-        raise ValueError(f"{where}: {name} is {tuple(t.shape)}, not [tokens][heads][dim] or [seqs][tokens][heads][dim]")
-    shape, strides = t.shape, t.stride()
-    return (shape, strides) if len(shape) == 4 else ((1, *shape), (0, *strides))
+def _refuse_rows(where: str, dev: int, name: str, x, y):
+    for t in (x, y):
+        if t.dim() not in (3, 4):
+            raise ValueError(f"{where}: {name} is {tuple(t.shape)}, not [tokens][heads][dim] or [seqs][tokens][heads][dim]")
+    raise ValueError(f"{where}: {name} is {x.dtype} {tuple(x.shape)} with strides {x.stride()} on device {x.get_device()}, its output {y.dtype} {tuple(y.shape)} "
+                     f"with strides {y.stride()} on device {y.get_device()}; the call runs on {dev}, rows have to be contiguous")
 
 
-def _rows(where: str, dev: int, name: str, x: torch.Tensor, y: Optional[torch.Tensor]):
-    """Struct of rows x and y, and their [seqs][tokens][dim], type."""
-    if y is None or x.shape != y.shape or x.dtype is not y.dtype or x.get_device() != dev or y.get_device() != dev:
-        raise ValueError(f"{where}: {name} is {x.dtype} {tuple(x.shape)} on device {x.get_device()}, its output "
-                         + ("missing" if y is None else f"{y.dtype} {tuple(y.shape)} on device {y.get_device()}") + f"; the call runs on {dev}")
-    (n, t, h, d), (xs, xt, xh, xe) = _four(where, name, x)
-    _, (ys, yt, yh, ye) = _four(where, name, y)
-    if x.numel() and (xe != 1 or ye != 1):
-        raise ValueError(f"{where}: {name} has rows that are not contiguous")
+def _rows(where: str, dev: int, name: str, x: torch.Tensor, y: torch.Tensor):
+    """The nine numbers of a chunkkv_rows, eight bytes each, of rows x and y; their shape [seqs][tokens][heads][dim]; their type."""
+    shape, kind, xs, ys = x.shape, x.dtype, x.stride(), y.stride()
+    if y.shape != shape or y.dtype is not kind or x.get_device() != dev or y.get_device() != dev:
+        _refuse_rows(where, dev, name, x, y)
+    if len(shape) == 4:
+        (n, t, h, _), (xn, xt, xh, xe), (yn, yt, yh, ye) = shape, xs, ys
+    elif len(shape) == 3:
+        (t, h, _), (xt, xh, xe), (yt, yh, ye) = shape, xs, ys
+        n = 1
+    else:
+        _refuse_rows(where, dev, name, x, y)
     # the stride of an axis of one entry can be anything
-    xs, ys = (xs, ys) if n > 1 else (0, 0)
-    xt, yt = (xt, yt) if t > 1 else (0, 0)
-    xh, yh = (xh, yh) if h > 1 else (0, 0)
-    return _CRows(x.data_ptr(), y.data_ptr(), h, xs, xh, xt, ys, yh, yt), (n, t, d), x.dtype
+    if n <= 1:
+        xn = yn = 0
+    if t <= 1:
+        xt = yt = 0
+    if h <= 1:
+        xh = yh = 0
+    if (xe != 1 or ye != 1) and x.numel():
+        _refuse_rows(where, dev, name, x, y)
+    return (x.data_ptr(), y.data_ptr(), h, xn, xh, xt, yn, yh, yt), n, t, shape[-1], kind
 
 
 def chunkkv_rotate(q, k, positions, inv_freq, interleaved: bool, magnitude: float, q_out, k_out, stream=None) -> None:
     """q, k and their outputs: [tokens][heads][head_dim] or [seqs][tokens][heads][head_dim], views of any strides, either None; an output may be the input
     itself.  rotary_dim is twice inv_freq's length."""
     where, dev = "chunkkv_rotate", _device()
-    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+    if (q is None) is not (q_out is None) or (k is None) is not (k_out is None):
         raise ValueError(f"{where}: rows without an output, or an output without rows")
-    a = b = None
-    shape, kind = None, None
     if q is not None:
-        a, shape, kind = _rows(where, dev, "q", q, q_out)
-    if k is not None:
-        b, other, kind_k = _rows(where, dev, "k", k, k_out)
-        if a is not None and (other != shape or kind_k is not kind):
-            raise ValueError(f"{where}: q is {kind} {tuple(q.shape)}, k {kind_k} {tuple(k.shape)}")
-        shape, kind = other, kind_k
-    if shape is None or kind not in _DTYPES:
-        raise ValueError(f"{where}: " + ("neither q nor k" if shape is None else f"{kind} rows"))
-    at, freq = _arrays(where, dev, ("positions", positions, _I32, shape[0] * shape[1]), ("inv_freq", inv_freq, _F32, 0))
-    _check(load_library().chunkkv_rotate(_DTYPES[kind], shape[2], shape[0], shape[1], a and C.byref(a), b and C.byref(b), at, freq,
+        numbers, n, t, d, kind = _rows(where, dev, "q", q, q_out)
+        if k is not None:
+            more, *rest = _rows(where, dev, "k", k, k_out)
+            if rest != [n, t, d, kind]:
+                raise ValueError(f"{where}: q is {kind} {tuple(q.shape)}, k {k.dtype} {tuple(k.shape)}")
+            numbers += more
+    elif k is not None:
+        numbers, n, t, d, kind = _rows(where, dev, "k", k, k_out)
+    else:
+        raise ValueError(f"{where}: neither q nor k")
+    if kind not in _DTYPES:
+        raise ValueError(f"{where}: {kind} rows")
+    at, freq = _arrays(where, dev, ("positions", positions, _I32, n * t), ("inv_freq", inv_freq, _F32, 0))
+    rows = array("Q", numbers)   # chunkkv_rows of q, then of k; read before the call returns
+    first = rows.buffer_info()[0]
+    _check(load_library().chunkkv_rotate(_DTYPES[kind], d, n, t, None if q is None else first, None if k is None else first + (72 if q is not None else 0), at, freq,
                                          0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0, magnitude, _stream(stream, dev)), where)
 
 

@@ -17,7 +17,9 @@
 // in it is as much as its own does (2^-8 of the weight's part in bf16).  They are normalised by the sum of the rounded ones, so they add up
 // to one; the log-sum-exp takes the sum before.  fp16 weights are held 2^9 times as large, so that the smallest normal one is 2^-23 of the
 // reference.  Scores, references, sums and outputs are fp32.
-// The reference of the online softmax is lazy: it moves when the weights of a row and tile add up to more than kOver.
+// The reference of the online softmax is lazy: weights are taken from the one there is, and only where 32 of them add up to kOver is the maximum
+// looked for and the reference moved.  Looking at it before every block instead: 1044 us rather than 988 for 4096 tokens over 16384 keys of a
+// head dimension of 128 with 32 query heads on 8, 198 rather than 189 for 64 sequences behind a prefix of 131072.
 #pragma once
 #include "decode_mfma.h"
 #include "rows.h"
@@ -215,23 +217,23 @@ struct RowsShape {
 template <int DT, int HD, bool LSE>
 struct Rows {
   using S = RowsShape<DT, HD>;
-  // fp16 weights are held 2^kOff times as large.  A reference moves when the 16 or 32 weights of a lane add up to kOver, which they do not
-  // where none is above the reference's own.
-  static constexpr float kOff = DT == CHUNKKV_F16 ? 9.f : 0.f, kOver = DT == CHUNKKV_F16 ? 32768.f : (DT == CHUNKKV_BF16 ? 256.f : 64.f);
+  // fp16 weights are held 2^kOff times as large.  A row's reference moves to its maximum when that is kRise above it in log2 units; kOver: more
+  // than the weights of 32 keys add up to where it is not, and no less than what a weight may be.
+  static constexpr float kOff = DT == CHUNKKV_F16 ? 9.f : 0.f, kRise = DT == CHUNKKV_F16 ? 1.f : 3.f, kOver = DT == CHUNKKV_F16 ? 65536.f : 512.f;
+  static_assert(kOver > 32.f * (DT == CHUNKKV_F16 ? 1024.f : 8.f), "sums");
   u32x4 qf[S::kQ];
   f32x16 acc[S::kD];
-  float m, mc, l, le, c1;
-  // Are the references in log2 units below 2^14: their rounding, 2^-24 of them, is then no more than the scores' own, and the difference to
-  // them one operation with the scale.
-  bool plain;
+  float m, l, le, c1;
+  float ref;                             // kOff - m c1
+  uint64_t rough;                        // not 0: that there is no such reference yet, or one too large to be rounded
 
   __device__ __forceinline__ void load(const char *from, int half, float scale_log2e) {
 #pragma unroll
     for (int i = 0; i < S::kQ; ++i) qf[i] = *(const u32x4 *)(from + (2 * i + half) * 16);
     m = kPagedLowest;
-    mc = l = le = 0.f;
-    plain = false;
+    l = le = ref = 0.f;
     c1 = scale_log2e;
+    rough = 1;
 #pragma unroll
     for (int i = 0; i < S::kD; ++i)
 #pragma unroll
@@ -256,73 +258,70 @@ struct Rows {
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = bits >> (8 * (e / 4) + e % 4) & 1 ? sc[e] : -__builtin_inff();
   }
-  // Weights of NKB blocks: p, and for 16-bit types pk, pairs rounded; the sums take them in.
-  template <int NKB, bool SHORT>
-  __device__ __forceinline__ void weigh(const f32x16 (&sc)[NKB], float (&p)[NKB][16], uint32_t (&pk)[NKB][8]) {
-    float sum, exact;
-    auto weights = [&](bool direct) __attribute__((always_inline)) {
-      if (direct) {
+  // Is a row's reference outgrown by the scores of NKB blocks?  mx: their maximum.
+  template <int NKB>
+  __device__ __forceinline__ bool rises(const f32x16 (&sc)[NKB], float &mx) const {
+    mx = sc[0][0];
 #pragma unroll
-        for (int b = 0; b < NKB; ++b)
+    for (int b = 0; b < NKB; ++b)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) p[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][e], c1, kOff - mc));
-      } else {
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[b][e]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32));  // of the other half's keys
+    return (mx - m) * c1 > kRise || m == kPagedLowest;
+  }
+  __device__ __forceinline__ void move(bool rise, float mx) {
+    const float m_new = rise ? fmaxf(mx, kPagedLowest) : m, f = __builtin_amdgcn_exp2f((m - m_new) * c1);
+    m = m_new;
+    l *= f;
+    if constexpr (LSE) le *= f;
 #pragma unroll
-        for (int b = 0; b < NKB; ++b)
+    for (int i = 0; i < S::kD; ++i) acc[i] *= f;
+  }
+  // Weights of NKB blocks: p, and for 16-bit types pk, pairs rounded; their sums.
+  template <int NKB, typename F>
+  static __device__ __forceinline__ void weights(F &&exponent, float (&p)[NKB][16], uint32_t (&pk)[NKB][8], float &sum, float &exact) {
+    float s4[4] = {0.f, 0.f, 0.f, 0.f}, e4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int e = 0; e < 16; ++e) p[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][e] - m, c1, kOff));
-      }
-      float s4[4] = {0.f, 0.f, 0.f, 0.f}, e4[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < NKB; ++b)
 #pragma unroll
-      for (int b = 0; b < NKB; ++b)
+      for (int e = 0; e < 16; ++e) p[b][e] = __builtin_amdgcn_exp2f(exponent(b, e));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if constexpr (DT == CHUNKKV_F32) {
-            s4[e % 4] += p[b][2 * e] + p[b][2 * e + 1];
-          } else {
-            pk[b][e] = pack2<DT>(p[b][2 * e], p[b][2 * e + 1]);
-            s4[e % 4] = add2<DT>(pk[b][e], s4[e % 4]);
-            if constexpr (LSE) e4[e % 4] += p[b][2 * e] + p[b][2 * e + 1];
-          }
+    for (int b = 0; b < NKB; ++b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (DT == CHUNKKV_F32) {
+          s4[e % 4] += p[b][2 * e] + p[b][2 * e + 1];
+        } else {
+          pk[b][e] = pack2<DT>(p[b][2 * e], p[b][2 * e + 1]);
+          s4[e % 4] = add2<DT>(pk[b][e], s4[e % 4]);
+          if constexpr (LSE) e4[e % 4] += p[b][2 * e] + p[b][2 * e + 1];
         }
-      sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-      exact = (e4[0] + e4[1]) + (e4[2] + e4[3]);
-    };
-    // moves the references of the rows that outgrew them, in both halves; no weight is above 1 then
-    auto move = [&]() __attribute__((always_inline)) {
-      float mx = sc[0][0];
-#pragma unroll
-      for (int b = 0; b < NKB; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[b][e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float over = fmaxf(sum, __shfl_xor(sum, 32));
-      const float m_new = over >= kOver ? fmaxf(mx, kPagedLowest) : m;
-      const float f = __builtin_amdgcn_exp2f((m - m_new) * c1);
-      m = m_new;
-      mc = m * c1;
-      plain = __builtin_amdgcn_ballot_w64(fabsf(mc) >= 0x1p14f) == 0;
-      l *= f;
-      if constexpr (LSE) le *= f;
-#pragma unroll
-      for (int i = 0; i < S::kD; ++i) acc[i] *= f;
-    };
-    if constexpr (SHORT) {   // as few instructions as can be: a short range runs them from cold
-      bool moved = m == kPagedLowest;    // the first keys: from their maximum
-      sum = moved ? kOver : 0.f;
-#pragma nounroll
-      for (;;) {                         // twice at most
-        if (__builtin_amdgcn_ballot_w64(sum >= kOver) != 0) move();
-        weights(false);
-        if (moved || __builtin_amdgcn_ballot_w64(sum >= kOver) == 0) break;
-        moved = true;
       }
-    } else {
-      weights(plain);
-      if (__builtin_amdgcn_ballot_w64(sum >= kOver) != 0) {
-        move();
-        weights(plain);
-      }
+    sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+    exact = (e4[0] + e4[1]) + (e4[2] + e4[3]);
+  }
+  // The weights, after the references have moved; the sums take them in.
+  template <int NKB>
+  __device__ __forceinline__ void weigh(const f32x16 (&sc)[NKB], float (&p)[NKB][16], uint32_t (&pk)[NKB][8]) {
+    float sum, exact, mx;
+    const bool rise = rises<NKB>(sc, mx);
+    if (__builtin_amdgcn_ballot_w64(rise) != 0) move(rise, mx);
+    weights<NKB>([&](int b, int e) __attribute__((always_inline)) { return __builtin_fmaf(sc[b][e] - m, c1, kOff); }, p, pk, sum, exact);
+    l += sum;
+    if constexpr (LSE) le += exact;
+  }
+  // The same where references seldom move: from the ones there are, without a look at the maximum, and again only if that was too low.
+  template <int NKB>
+  __device__ __forceinline__ void weigh_on(const f32x16 (&sc)[NKB], float (&p)[NKB][16], uint32_t (&pk)[NKB][8]) {
+    float sum, exact, mx;
+    weights<NKB>([&](int b, int e) __attribute__((always_inline)) { return __builtin_fmaf(sc[b][e], c1, ref); }, p, pk, sum, exact);
+    if ((__builtin_amdgcn_ballot_w64(sum >= kOver) | rough) != 0) {
+      const bool rise = rises<NKB>(sc, mx);
+      move(rise, mx);
+      weights<NKB>([&](int b, int e) __attribute__((always_inline)) { return __builtin_fmaf(sc[b][e] - m, c1, kOff); }, p, pk, sum, exact);
+      ref = kOff - m * c1;
+      // taken in log2 units, a reference is off by 2^-24 of it: below 2^14 no more than the scores themselves
+      rough = __builtin_amdgcn_ballot_w64(fabsf(m * c1) >= 0x1p14f);
     }
     l += sum;
     if constexpr (LSE) le += exact;
@@ -443,16 +442,19 @@ __device__ __forceinline__ void rows_finish(const R &r, const RowsWork &w, const
 }
 
 // The keys of a range: which there are, and loads of 16-row blocks of theirs.  They are looked up by windows of 64 blocks, a block to a
-// lane, one window ahead.
+// lane, one window ahead: a load then takes its block's place out of those registers.
 template <int DT, int HD, bool PAGED, bool MASK>
 struct RowsKeys {
   using S = RowsShape<DT, HD>;
   const RowsArgsOf<PAGED> &a;
   const RowsWork &w;
   int lane;
-  uint32_t tok, live = 0;                // live: keys of this lane's block that count
-  int32_t page = -1, page_next = -1;     // pages: entries of this window and of the next one
-  u32x4 mask_next = {0, 0, 0, 0};        // bytes of the mask
+  uint32_t tok;
+  uint32_t live = 0, at_lo = 0, at_hi = 0, span = 0;   // of this lane's block: keys that count; where it is in the pools; bytes to the end of its last
+                                                       // key, 0: none that counts
+  uint64_t full = 0;                     // blocks of the window all of whose keys count
+  int32_t page_next = -1;                // pages: entry of the next window's block
+  u32x4 mask_next = {0, 0, 0, 0};        // bytes of the mask, of the next window's block
   __device__ __forceinline__ RowsKeys(const RowsArgsOf<PAGED> &a_, const RowsWork &w_, int lane_) : a(a_), w(w_), lane(lane_), tok((uint32_t)a_.r.geom.tok) {
     if constexpr (PAGED) page_next = w.page;
     fetch_mask(0);
@@ -475,9 +477,10 @@ struct RowsKeys {
   __device__ __forceinline__ void open(int window) {
     const int blk = 64 * window + lane, left = w.len - 16 * blk;
     live = left >= 16 ? 0xFFFFu : (left > 0 ? (1u << left) - 1 : 0u);
+    int64_t at = (int64_t)(16 * blk) * tok;
     if constexpr (PAGED) {
-      page = page_next;
-      if (page < 0 || page >= a.r.geom.n_pages) live = 0;
+      at = block_offset(a.r.geom, page_next, w.h, (uint32_t)(w.r0 / 16 + blk));
+      if (at < 0) live = 0;
       page_next = left > 1024 ? w.table[page_of_block(a.r.geom, (uint32_t)(w.r0 / 16 + blk + 64))] : -1;
     }
     if constexpr (MASK) {
@@ -493,31 +496,36 @@ struct RowsKeys {
       live &= bits;
       fetch_mask(window + 1);
     }
+    at_lo = (uint32_t)at;
+    at_hi = (uint32_t)(at >> 32);
+    span = live == 0 ? 0u : ((left < 16 ? (uint32_t)left : 16u) - 1) * tok + S::kRow;
+    full = __builtin_amdgcn_ballot_w64(live == 0xFFFFu);
   }
   // Keys key0 .. key0 + 16 N - 1 that count, one bit each.
   template <int N>
   __device__ __forceinline__ uint64_t alive(int key0) const {
     const int blk = key0 / 16 & 63;
+    constexpr uint32_t kAll = (1u << N) - 1;
+    if (((uint32_t)(full >> blk) & kAll) == kAll) return N == 4 ? ~0ull : (1ull << (16 * N % 64)) - 1;
     uint64_t bits = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) bits |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)live, blk + i) << (16 * i);
     return bits;
   }
-  // N loads from the block of key key0, a multiple of 16, at this lane's offsets in it; `wanted` false: empty ones, which write zeros.
+  // Where the block of key key0 is, a multiple of 16 in the open window, and its span.
+  struct Place {
+    uint64_t at;
+    uint32_t span;
+  };
+  __device__ __forceinline__ Place place(int key0) const {
+    const int blk = key0 / 16 & 63;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)at_lo, blk), hi = (uint32_t)__builtin_amdgcn_readlane((int)at_hi, blk);
+    return {(uint64_t)hi << 32 | lo, (uint32_t)__builtin_amdgcn_readlane((int)span, blk)};
+  }
+  // N loads from a block, at this lane's offsets in it; rows past its span, all of one without, arrive as zeros.
   template <int N>
-  __device__ __forceinline__ void load(const char *base, int key0, bool wanted, const uint32_t *off, char *to) const {
-    const int left = w.len - key0, rows = left < 16 ? left : 16;
-    int64_t at = 0;
-    bool there = wanted && rows > 0;
-    if constexpr (PAGED) {
-      at = block_offset(a.r.geom, __builtin_amdgcn_readlane(page, key0 / 16 & 63), w.h, (uint32_t)((w.r0 + key0) / 16));
-      there = there && at >= 0;
-      at = there ? at : 0;
-    } else {
-      at = there ? key0 * a.r.geom.tok : 0;
-    }
-    const int span = there ? (int)((uint32_t)(rows - 1) * tok) + S::kRow : 0;
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(base + at), 0, span, 0x00020000);
+  static __device__ __forceinline__ void load(const char *base, const Place &p, const uint32_t *off, char *to) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(base + p.at), 0, (int)p.span, 0x00020000);
 #pragma unroll
     for (int j = 0; j < N; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(to + j * 1024), 16, off[j], 0, 0, 0);
   }
@@ -579,8 +587,9 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
     const uint64_t bits = keys.template alive<4>(kRowsTile * t);
     char *to = smem + stage * 2 * S::kTile + wave * 8 * S::kRow;
     const int key0 = kRowsTile * t + 16 * (wave / 2);
-    keys.template load<NL>(w.k, key0, bits != 0, koff, to);
-    keys.template load<NL>(w.v, key0, bits != 0, voff, to + S::kTile);
+    const auto place = keys.place(key0);
+    keys.template load<NL>(w.k, place, koff, to);
+    keys.template load<NL>(w.v, place, voff, to + S::kTile);
     return bits;
   };
   uint32_t kat, vat[S::kD];
@@ -639,7 +648,7 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
     }
     float p[NKB][16];
     uint32_t pk[NKB][8];
-    x.template weigh<NKB, false>(sc, p, pk);
+    x.template weigh_on<NKB>(sc, p, pk);
 #pragma unroll
     for (int b = 0; b < NKB; ++b) {
       const uint32_t at = base + (uint32_t)(S::kTile + b * 32 * S::kRow);
@@ -675,12 +684,20 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
   auto key_of = [&](int s) { return 32 * (wave + 4 * s); };
   const int steps_all = w.len > 0 ? (w.len + 31) / 32 : 0, steps = (steps_all - wave + 3) / 4;
   auto look = [&](int s) __attribute__((always_inline)) {   // keys of step s that count
-    if ((s & 7) == 0) keys.open(s / 8);              // V of step s is issued before the next look
+    if ((s & 7) == 0) keys.open(s / 8);
     return (uint32_t)keys.template alive<2>(key_of(s));
   };
-  auto issue = [&](const char *base, const uint32_t (&off)[NL], int s, bool wanted, char *to) __attribute__((always_inline)) {
+  typename RowsKeys<DT, HD, PAGED, MASK>::Place place[2];
+  auto issue_k = [&](int s) __attribute__((always_inline)) {   // V of a step has K's places
 #pragma unroll
-    for (int t = 0; t < 2; ++t) keys.template load<NL>(base, key_of(s) + 16 * t, wanted, off, to + t * NL * 1024);
+    for (int t = 0; t < 2; ++t) {
+      place[t] = keys.place(key_of(s) + 16 * t);
+      keys.template load<NL>(w.k, place[t], koff, kslot + t * NL * 1024);
+    }
+  };
+  auto issue_v = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) keys.template load<NL>(w.v, place[t], voff, vslot + t * NL * 1024);
   };
   uint32_t kat, vat[S::kD];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
@@ -689,8 +706,8 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
   Rows<DT, HD, LSE> x;
   x.load(rows_query(r, w, n), half, r.scale_log2e);
   uint32_t bits = look(0);
-  issue(w.k, koff, 0, bits != 0, kslot);
-  issue(w.v, voff, 0, bits != 0, vslot);
+  issue_k(0);
+  issue_v();
   x.settle();
   for (int s = 0; s < steps; ++s) {
     const uint32_t now = bits;
@@ -707,7 +724,7 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0xC07F);   // the fragments are in registers: the K slot is free
         bits = look(s + 1);
-        issue(w.k, koff, s + 1, bits != 0, kslot);
+        issue_k(s + 1);
       }
 #pragma unroll
       for (int i = 0; i < S::kAhead; ++i) x.product(kf[i], i0 + i, sc[0]);
@@ -716,7 +733,7 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
       if (now != ~0u) x.leave_out(sc[0], now, half);
       float p[1][16];
       uint32_t pk[1][8];
-      x.template weigh<1, true>(sc, p, pk);
+      x.template weigh<1>(sc, p, pk);
       __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL));
       if constexpr (MASK) {
         const int left = w.len - key_of(s);
@@ -733,7 +750,7 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
     }
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL) & 0xC07F);   // V of this step is there and read
-    issue(w.v, voff, s + 1, bits != 0, vslot);
+    issue_v();
   }
   __builtin_amdgcn_s_waitcnt(vm_imm(0));
   x.close();

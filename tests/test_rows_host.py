@@ -10,7 +10,6 @@ import pytest
 import torch
 
 import paper_2502_00299_amd as ckv
-from paper_2502_00299_amd import binding
 
 FAKE = C.c_void_p(0x1000)   # never dereferenced: every call below fails a check before a launch
 ODD = C.c_void_p(0x1008)
@@ -143,10 +142,15 @@ def test_a_prefix_is_counted_once():
 
 
 # ---- rotation ----
+class Rows(C.Structure):   # chunkkv_rows
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n_heads", C.c_int32), ("in_stride_seq", C.c_int64), ("in_stride_head", C.c_int64), ("in_stride_tok", C.c_int64),
+                ("out_stride_seq", C.c_int64), ("out_stride_head", C.c_int64), ("out_stride_tok", C.c_int64)]
+
+
 def rows(**kw):
     d = dict(in_=0x1000, out=0x2000, n_heads=4, in_stride_seq=0, in_stride_head=64, in_stride_tok=256, out_stride_seq=0, out_stride_head=64, out_stride_tok=256)
     d.update(kw)
-    return binding._CRows(*[d[name] for name, _ in binding._CRows._fields_])
+    return Rows(*[d[name] for name, _ in Rows._fields_])
 
 
 def rotate(lib, q=None, k=None, dtype=ckv.BF16, d=64, n=1, t=5, pos=FAKE, freq=FAKE, rotary=64, magnitude=1.0):
