@@ -205,6 +205,10 @@ struct RowsShape {
   static constexpr int kLds = kStages * 2 * kTile;
   static constexpr int kQ = DT == CHUNKKV_F32 ? HD / 8 : HD / 16, kD = HD / 32;    // 16-byte reads of a key by a lane, 32-dim output tiles
   static constexpr int kAhead = kQ < 8 ? kQ : 8;     // of which so many are in flight
+  // Two workgroups to a CU where 128 registers do, a block of 32 keys at a time: one's weights run beside the other's products.  512 (1024) query
+  // tokens of 16 heads over 8 x 1654 keys, fp16: 44 (87) us with one, which takes both blocks of a tile at a time, 46 (79) with two; under a
+  // mask with holes 63 (113) and 58 (89).
+  static constexpr bool kTwo = DT != CHUNKKV_F32 && HD == 64;
   static constexpr int kNarrow = rows_pairs(DT, HD);   // narrow tiles of a workgroup
   static_assert(kLds >= kNarrow * 4 * 2 * 32 * kRow, "slots of the wavefronts");
   static_assert(kLds >= 8 * 32 * HD * 4 && 2 * 32 * kRow >= 32 * HD * 4, "states of the wavefronts");
@@ -252,11 +256,16 @@ struct Rows {
       sc = mma32<DT>(kf, qf[i], sc);
     }
   }
-  // `bits`: keys of a 32-key block that count
-  static __device__ __forceinline__ void leave_out(f32x16 &sc, uint32_t bits, int half) {
-    bits >>= 4 * half;
+  // `bits`: keys of a 32-key block that count, the same for all lanes.  The condition of an element is two scalar instructions, one bit
+  // for either half of the wavefront.
+  static __device__ __forceinline__ void leave_out(f32x16 &sc, uint32_t bits) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sc[e] = bits >> (8 * (e / 4) + e % 4) & 1 ? sc[e] : -__builtin_inff();
+    for (int e = 0; e < 16; ++e) {
+      const int key = 8 * (e / 4) + e % 4;
+      const uint64_t lanes = (uint32_t)((int32_t)(bits << (31 - key)) >> 31) | (uint64_t)(uint32_t)((int32_t)(bits << (27 - key)) >> 31) << 32;
+      sc[e] = __builtin_amdgcn_inverse_ballot_w64(lanes) ? sc[e] : -__builtin_inff();
+      if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // or all conditions are made first, more than there are registers for
+    }
   }
   // Is a row's reference outgrown by the scores of NKB blocks?  mx: their maximum.
   template <int NKB>
@@ -280,7 +289,10 @@ struct Rows {
   // Weights of NKB blocks: p, and for 16-bit types pk, pairs rounded; their sums.
   template <int NKB, typename F>
   static __device__ __forceinline__ void weights(F &&exponent, float (&p)[NKB][16], uint32_t (&pk)[NKB][8], float &sum, float &exact) {
-    float s4[4] = {0.f, 0.f, 0.f, 0.f}, e4[4] = {0.f, 0.f, 0.f, 0.f};
+    constexpr int NS = LSE ? 2 : 4;      // sums in parallel, as registers allow
+    float s4[NS], e4[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) s4[i] = e4[i] = 0.f;
 #pragma unroll
     for (int b = 0; b < NKB; ++b)
 #pragma unroll
@@ -290,15 +302,16 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if constexpr (DT == CHUNKKV_F32) {
-          s4[e % 4] += p[b][2 * e] + p[b][2 * e + 1];
+          s4[e % NS] += p[b][2 * e] + p[b][2 * e + 1];
         } else {
           pk[b][e] = pack2<DT>(p[b][2 * e], p[b][2 * e + 1]);
-          s4[e % 4] = add2<DT>(pk[b][e], s4[e % 4]);
-          if constexpr (LSE) e4[e % 4] += p[b][2 * e] + p[b][2 * e + 1];
+          s4[e % NS] = add2<DT>(pk[b][e], s4[e % NS]);
+          if constexpr (LSE) e4[e % NS] += p[b][2 * e] + p[b][2 * e + 1];
         }
       }
-    sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-    exact = (e4[0] + e4[1]) + (e4[2] + e4[3]);
+    sum = s4[0] + s4[1];
+    exact = e4[0] + e4[1];
+    if constexpr (NS == 4) sum += s4[2] + s4[3];
   }
   // The weights, after the references have moved; the sums take them in.
   template <int NKB>
@@ -529,6 +542,15 @@ struct RowsKeys {
 #pragma unroll
     for (int j = 0; j < N; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(to + j * 1024), 16, off[j], 0, 0, 0);
   }
+  // The same of values: rows that the mask leaves out are asked for behind every span.  They are multiplied by weights of zero, whatever
+  // bits there are, so they have to arrive as zeros.  `bits`: which rows of these loads count.
+  template <int N>
+  __device__ __forceinline__ void load_values(const char *base, const Place &p, const uint32_t (&off)[N], char *to, uint32_t bits) const {
+    uint32_t at[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) at[j] = !MASK || bits >> (S::kRpl * j + lane / S::kSegs) & 1 ? off[j] : 0x80000000u;
+    load<N>(base, p, at, to);
+  }
 };
 
 // This lane's places in a block of 32 keys in LDS.  K: key n, segment 2 i + half is at kat ^ 32 i.  V, 16 bits: keys 4 half + (lane % 16) / 4 of
@@ -570,6 +592,7 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
   using S = RowsShape<DT, HD>;
   const auto &r = a.r;
   constexpr int NL = 8 / S::kRpl, NST = S::kStages, NKB = 2 / WK;   // loads of a wavefront's eight rows of a tile; 32-key blocks of a tile that it has
+  constexpr int NB = S::kTwo ? 1 : NKB;    // of which so many at a time
   const int n = lane & 31, half = lane >> 5, wk = WK == 2 ? wave & 1 : 0, wr = wave / WK;
   const bool idle = w.row0 + 32 * wr >= w.rows;      // this wavefront's rows are not there: it loads and waits with the others
   RowsKeys<DT, HD, PAGED, MASK> keys(a, w, lane);
@@ -589,7 +612,7 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
     const int key0 = kRowsTile * t + 16 * (wave / 2);
     const auto place = keys.place(key0);
     keys.template load<NL>(w.k, place, koff, to);
-    keys.template load<NL>(w.v, place, voff, to + S::kTile);
+    keys.template load_values<NL>(w.v, place, voff, to + S::kTile, (uint32_t)(bits >> (8 * wave)));
     return bits;
   };
   uint32_t kat, vat[S::kD];
@@ -606,54 +629,49 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
     const uint32_t base = (uint32_t)stage * 2 * S::kTile + (uint32_t)(32 * wk * S::kRow);
     __builtin_amdgcn_s_waitcnt(vm_imm((NST - 2) * 2 * NL));
     const uint64_t now = alive[0];
-    if constexpr (MASK) {
-      // values of keys that do not count are multiplied by weights of zero, whatever bits they are: each wavefront clears those it has loaded
-      const int left = w.len - kRowsTile * t - 8 * wave;
-      const uint32_t dead = ~(uint32_t)(now >> (8 * wave)) & (left >= 8 ? 0xFFu : (left > 0 ? (1u << left) - 1 : 0u));
-      if (dead != 0 && now != 0) {
-#pragma unroll
-        for (int j = 0; j < NL; ++j)
-          if (dead >> (S::kRpl * j + lane / S::kSegs) & 1) *(u32x4 *)(smem + stage * 2 * S::kTile + S::kTile + wave * 8 * S::kRow + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-      }
-    }
     rows_barrier();
 #pragma unroll
     for (int i = 0; i < NST - 2; ++i) alive[i] = alive[i + 1];
     alive[NST - 2] = issue(t + NST - 1, (t + NST - 1) % NST);
     if (now == 0 || idle) continue;
-    f32x16 sc[NKB];
-    u32x4 kf[S::kAhead];
-    auto read_k = [&](int j) __attribute__((always_inline)) {   // read j of the tile's, block by block
-      if (j < NKB * S::kQ) kf[j % S::kAhead] = *(const u32x4 *)(smem + base + ((kat ^ (uint32_t)(32 * (j % S::kQ))) + (uint32_t)(j / S::kQ * 32 * S::kRow)));
-    };
 #pragma unroll
-    for (int j = 0; j < S::kAhead; ++j) read_k(j);
-    __builtin_amdgcn_sched_barrier(0);
+    for (int b0 = 0; b0 < NKB; b0 += NB) {
+      const uint32_t at0 = base + (uint32_t)(b0 * 32 * S::kRow);
+      f32x16 sc[NB];
+      u32x4 kf[S::kAhead];
+      auto read_k = [&](int j) __attribute__((always_inline)) {   // read j of these blocks, one after the other
+        if (j < NB * S::kQ) kf[j % S::kAhead] = *(const u32x4 *)(smem + at0 + ((kat ^ (uint32_t)(32 * (j % S::kQ))) + (uint32_t)(j / S::kQ * 32 * S::kRow)));
+      };
 #pragma unroll
-    for (int b = 0; b < NKB; ++b) {
+      for (int j = 0; j < S::kAhead; ++j) read_k(j);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
+      for (int b = 0; b < NB; ++b) {
 #pragma unroll
-      for (int i = 0; i < S::kQ; ++i) {
-        x.product(kf[i % S::kAhead], i, sc[b]);
-        read_k(b * S::kQ + i + S::kAhead);
+        for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::kQ; ++i) {
+          x.product(kf[i % S::kAhead], i, sc[b]);
+          read_k(b * S::kQ + i + S::kAhead);
+        }
       }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    typename Rows<DT, HD, LSE>::Values vf;
-    x.read_values(base + (uint32_t)S::kTile, vat, vf);   // while the products run
-    if (now != ~0ull) {
+      __builtin_amdgcn_sched_barrier(0);
+      typename Rows<DT, HD, LSE>::Values vf;
+      x.read_values(at0 + (uint32_t)S::kTile, vat, vf);   // while the products run
+      if (now != ~0ull) {
 #pragma unroll
-      for (int b = 0; b < NKB; ++b) x.leave_out(sc[b], (uint32_t)(now >> (32 * (b + wk))), half);
-    }
-    float p[NKB][16];
-    uint32_t pk[NKB][8];
-    x.template weigh_on<NKB>(sc, p, pk);
+        for (int b = 0; b < NB; ++b) x.leave_out(sc[b], (uint32_t)(now >> (32 * (b0 + b + wk))));
+      }
+      float p[NB][16];
+      uint32_t pk[NB][8];
+      x.template weigh_on<NB>(sc, p, pk);
 #pragma unroll
-    for (int b = 0; b < NKB; ++b) {
-      const uint32_t at = base + (uint32_t)(S::kTile + b * 32 * S::kRow);
-      if (b > 0) x.read_values(at, vat, vf);
-      x.values(smem, at, vat, vf, p[b], pk[b]);
+      for (int b = 0; b < NB; ++b) {
+        const uint32_t at = at0 + (uint32_t)(S::kTile + b * 32 * S::kRow);
+        if (b > 0) x.read_values(at, vat, vf);
+        x.values(smem, at, vat, vf, p[b], pk[b]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   __builtin_amdgcn_s_waitcnt(vm_imm(0));   // the empty loads write into LDS too
@@ -695,9 +713,9 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
       keys.template load<NL>(w.k, place[t], koff, kslot + t * NL * 1024);
     }
   };
-  auto issue_v = [&]() __attribute__((always_inline)) {
+  auto issue_v = [&](uint32_t bits) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) keys.template load<NL>(w.v, place[t], voff, vslot + t * NL * 1024);
+    for (int t = 0; t < 2; ++t) keys.template load_values<NL>(w.v, place[t], voff, vslot + t * NL * 1024, bits >> (16 * t));
   };
   uint32_t kat, vat[S::kD];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
@@ -707,7 +725,7 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
   x.load(rows_query(r, w, n), half, r.scale_log2e);
   uint32_t bits = look(0);
   issue_k(0);
-  issue_v();
+  issue_v(bits);
   x.settle();
   for (int s = 0; s < steps; ++s) {
     const uint32_t now = bits;
@@ -730,27 +748,18 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
       for (int i = 0; i < S::kAhead; ++i) x.product(kf[i], i0 + i, sc[0]);
     }
     if (now != 0) {
-      if (now != ~0u) x.leave_out(sc[0], now, half);
+      if (now != ~0u) x.leave_out(sc[0], now);
       float p[1][16];
       uint32_t pk[1][8];
       x.template weigh<1>(sc, p, pk);
       __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL));
-      if constexpr (MASK) {
-        const int left = w.len - key_of(s);
-        const uint32_t dead = ~now & (left >= 32 ? ~0u : (1u << left) - 1);
-        if (dead != 0) {
-#pragma unroll
-          for (int j = 0; j < 2 * NL; ++j)
-            if (dead >> (S::kRpl * j + lane / S::kSegs) & 1) *(u32x4 *)(vslot + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-        }
-      }
       typename Rows<DT, HD, LSE>::Values vf;
       x.read_values(kbase + SLOT, vat, vf);
       x.values(smem, kbase + SLOT, vat, vf, p[0], pk[0]);
     }
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL) & 0xC07F);   // V of this step is there and read
-    issue_v();
+    issue_v(bits);
   }
   __builtin_amdgcn_s_waitcnt(vm_imm(0));
   x.close();
@@ -771,7 +780,7 @@ __device__ __forceinline__ RowsSegment rows_find(const R &r, int &s, int &x) {
 
 constexpr int kRowsThreads = 512;
 template <int DT, int HD, bool PAGED, bool MASK, bool LSE>
-__global__ __launch_bounds__(kRowsThreads, 2) void rows_kernel(RowsArgsOf<PAGED> a) {
+__global__ __launch_bounds__(kRowsThreads, (RowsShape<DT, HD>::kTwo ? 4 : 2)) void rows_kernel(RowsArgsOf<PAGED> a) {
   using S = RowsShape<DT, HD>;
   __shared__ __align__(16) char smem[S::kLds + 8 * 32 * sizeof(float4)];
   const auto &r = a.r;
