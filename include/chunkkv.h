@@ -404,7 +404,8 @@ int chunkkv_rotary_frequencies(int32_t rotary_dim, double base, double factor, d
 
 /* Rows of heads, in and out: row (sequence b, token t, head h) starts at element b*stride_seq + t*stride_tok + h*stride_head, its
  * head_dim elements are contiguous, rows are 16-byte aligned.  Rows of a fused projection and those of a cache both fit, in different
- * orders too.  In place (out == in) the strides have to be the same.                                                              */
+ * orders too.  In place (out == in) the strides have to be the same.  Rows that are written must not overlap each other: of the axes that
+ * have more than one entry, in the order of their strides, each steps over all before it (CHUNKKV_ERR_SHAPE).                      */
 typedef struct {
   const void *in;
   void *out;
@@ -432,9 +433,10 @@ int chunkkv_rotate(int32_t dtype, int32_t head_dim, int32_t n_seq, int32_t n_tok
  * i / g (g = Hq / Hkv):  out = sum_s softmax_s(scale * q . k_s) v_s.
  * Token t of query head h of sequence b starts at element q_base[b] + t*q_stride_tok + h*q_stride_head, its output at out_base[b] +
  * t*out_stride_tok + h*out_stride_head, state s of kv-head h of K and V at kv_base[b] + s*kv_stride_tok + h*kv_stride_head; rows have
- * head_dim contiguous elements and are 16-byte aligned.
+ * head_dim contiguous elements and are 16-byte aligned.  Outputs must not overlap each other: the larger of out's strides steps over all
+ * heads, or all tokens, of the smaller (CHUNKKV_ERR_SHAPE).
  * Limits: head_dim 64 or 128; up to 1023 kv-heads and 256 query heads per kv-head; up to 2^24 states of a sequence, up to 4 MB apart;
- * 2^30 tokens, and as many query rows (tokens times g) of a sequence.                                                             */
+ * 2^30 tokens, and as many query rows (tokens times g) of a sequence; 2^29 tokens times heads of 32 sequences.                   */
 typedef struct {
   int32_t batch, n_q_heads, n_kv_heads, head_dim;
   int32_t dtype;                /* chunkkv_dtype: of queries, states and outputs                               */

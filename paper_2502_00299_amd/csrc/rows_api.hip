@@ -2,6 +2,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "rows.h"
 
 namespace ckv {
@@ -11,6 +13,24 @@ constexpr int64_t kMostElements = (int64_t)1 << 56;   // strides and bases: what
 constexpr int kMaxQueryRows = 1 << 30;   // of a sequence (or prefix) and kv-head
 constexpr int kLaunchPrefixes = kSharedSegments - kJoinSegments;   // prefixes of a launch: the others of its segments are sequences
 constexpr int kRotateMaxHeads = 1 << 16;
+// Of a launch: a grid has less than 2^32 threads, 512 of a workgroup here, and up to 32 of a row of the join.
+constexpr int64_t kMostBlocks = ((int64_t)1 << 23) - 1, kMostPartials = ((int64_t)1 << 27) - 1;
+
+// Do rows of d elements that are written overlap?  Axes by stride, each behind all of the ones before; bounds checked before: no product overflows.
+struct Axis {
+  int64_t stride, n;
+};
+template <int N>
+bool overlap(Axis (&axis)[N], int64_t d) {
+  std::sort(axis, axis + N, [](const Axis &x, const Axis &y) { return x.stride < y.stride; });
+  __int128 end = d;
+  for (const Axis &x : axis) {
+    if (x.n <= 1) continue;
+    if (x.stride < end) return true;
+    end += (__int128)x.stride * (x.n - 1);
+  }
+  return false;
+}
 
 // ---- key ranges ---------------------------------------------------------------------------------------------------
 // Segments of a call, as the plan sees them.
@@ -150,15 +170,18 @@ int check_cross(const chunkkv_cross *c) {
     if (x > kMostElements) return CHUNKKV_ERR_UNSUPPORTED;
     if ((x * esz) % 16) return CHUNKKV_ERR_SHAPE;
   }
-  int64_t tokens = 0;
+  int64_t tokens = 0, most = 0;
   for (int b = 0; b < c->batch; ++b) {
     if (c->q_len[b] < 0 || c->seqlen[b] < 0 || c->q_base[b] < 0 || c->kv_base[b] < 0 || c->out_base[b] < 0) return CHUNKKV_ERR_SHAPE;
     if (c->q_base[b] > kMostElements || c->kv_base[b] > kMostElements || c->out_base[b] > kMostElements) return CHUNKKV_ERR_UNSUPPORTED;
     if ((c->q_base[b] * esz) % 16 || (c->kv_base[b] * esz) % 16 || (c->out_base[b] * esz) % 16) return CHUNKKV_ERR_SHAPE;
     if (c->seqlen[b] > kPagedMaxTokens || (int64_t)c->q_len[b] * g > kMaxQueryRows) return CHUNKKV_ERR_UNSUPPORTED;
     tokens += c->q_len[b];
+    most = c->q_len[b] > most ? c->q_len[b] : most;
   }
-  return tokens > kMaxQueryRows ? CHUNKKV_ERR_UNSUPPORTED : CHUNKKV_OK;
+  if (tokens > kMaxQueryRows) return CHUNKKV_ERR_UNSUPPORTED;
+  Axis axis[2] = {{c->out_stride_head, c->n_q_heads}, {c->out_stride_tok, most}};
+  return most > 0 && overlap(axis, c->head_dim) ? CHUNKKV_ERR_SHAPE : CHUNKKV_OK;
 }
 
 struct CrossPlan {
@@ -179,7 +202,7 @@ int cross_plan(const chunkkv_cross *c, CrossPlan *pl) {
       if (splits > 1) rows += (int64_t)splits * c->n_kv_heads * x.rows;
       items += blocks_of(x, pl->rows, c->n_kv_heads);
     }
-    if (rows > INT32_MAX || items > INT32_MAX) return CHUNKKV_ERR_UNSUPPORTED;
+    if (rows > kMostPartials || items > kMostBlocks) return CHUNKKV_ERR_UNSUPPORTED;
     pl->partials = rows > pl->partials ? rows : pl->partials;
   }
   pl->total = partial_bytes(pl->partials, c->head_dim, &pl->off_o);
@@ -227,7 +250,7 @@ int shared_plan(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *n
     items += blocks_of(x, pl->rows, p->n_kv_heads);
     if (i == w->batch - 1) pl->prefix_partials = pl->partials;
   }
-  if (pl->partials > INT32_MAX || items > INT32_MAX) return CHUNKKV_ERR_UNSUPPORTED;
+  if (pl->partials > kMostPartials || items > kMostBlocks) return CHUNKKV_ERR_UNSUPPORTED;
   pl->total = partial_bytes(pl->partials, p->head_dim, &pl->off_o);
   return CHUNKKV_OK;
 }
@@ -447,6 +470,11 @@ int chunkkv_rotate(int32_t dtype, int32_t head_dim, int32_t n_seq, int32_t n_tok
   if (heads == 0 || (a.tokens > 0 && !positions) || !inv_freq) return CHUNKKV_ERR_NULL;
   if (a.tokens > kPagedMaxTokens) return CHUNKKV_ERR_UNSUPPORTED;
   if (a.tokens == 0) return CHUNKKV_OK;
+  for (const chunkkv_rows *x : given) {
+    if (!x) continue;
+    Axis axis[3] = {{x->out_stride_seq, n_seq}, {x->out_stride_head, x->n_heads}, {x->out_stride_tok, n_tokens}};
+    if (overlap(axis, head_dim)) return CHUNKKV_ERR_SHAPE;
+  }
   a.positions = positions; a.inv_freq = inv_freq; a.n_tokens = n_tokens; a.rotary = rotary_dim;
   a.magnitude = magnitude == 0.f ? 1.f : magnitude;
   hipStream_t s = (hipStream_t)stream;

@@ -51,6 +51,20 @@ def test_cross_problems_that_are_refused(lib, kw, status):
         assert cross(lib, p) == status
 
 
+@pytest.mark.parametrize("kw,status", [
+    # outputs of two heads, or two tokens, in one place
+    (dict(out_base=[0, 0], out_stride_head=0, out_stride_tok=4096), SHAPE), (dict(out_base=[0, 0], out_stride_head=128, out_stride_tok=0), SHAPE),
+    (dict(out_base=[0, 0], out_stride_head=64, out_stride_tok=4096), SHAPE), (dict(out_base=[0, 0], out_stride_head=128, out_stride_tok=4096 - 8), SHAPE),
+    (dict(out_base=[0, 0], out_stride_head=699 * 128, out_stride_tok=128), SHAPE), (dict(out_base=[0, 0], out_stride_head=700 * 128, out_stride_tok=128), OK),
+    (dict(out_base=[0, 0], out_stride_head=128, out_stride_tok=0, q_len=[1, 0]), OK), (dict(out_base=[0, 0], out_stride_head=0, out_stride_tok=0, q_len=[0, 0]), OK),
+    (dict(out_base=[0, 0], out_stride_head=128, out_stride_tok=1 << 56), OK),
+    # more workgroups than a grid has threads for: 2^28 rows of 8 kv-heads are 2^23 workgroups of 256 rows, 2^32 threads
+    (dict(n_q_heads=8, q_len=[1 << 26, 0], seqlen=[1, 0]), OK), (dict(n_q_heads=8, q_len=[1 << 28, 0], seqlen=[1, 0]), UNSUPPORTED), (dict(n_q_heads=8, q_len=[1 << 28, 1 << 28], seqlen=[1, 1]), UNSUPPORTED),
+])
+def test_cross_outputs_and_grids(lib, kw, status):
+    test_cross_problems_that_are_refused(lib, kw, status)
+
+
 def test_cross_pointers_and_workspace(lib):
     p = good()
     need = ckv.chunkkv_cross_workspace_bytes(p)
@@ -172,6 +186,14 @@ def test_rotations_that_are_refused(lib, kw, status):
 ])
 def test_rows_that_are_refused(lib, kw, status):
     assert rotate(lib, rows(**kw)) == status and rotate(lib, rows(), rows(**kw)) == status
+
+
+def test_rotated_rows_that_overlap(lib):
+    for kw in (dict(out_stride_head=0), dict(out_stride_tok=0), dict(out_stride_tok=128), dict(out_stride_head=32), dict(out_stride_head=256 - 64), dict(out_stride_tok=64, out_stride_head=256),
+               dict(out=0x1000, in_stride_tok=0, out_stride_tok=0)):
+        assert rotate(lib, rows(**kw)) == SHAPE and rotate(lib, rows(out_stride_tok=64, out_stride_head=320), rows(**kw)) == SHAPE, kw
+    assert rotate(lib, rows(), n=2) == SHAPE
+    assert rotate(lib, rows(out_stride_head=0, out_stride_tok=0), t=0) == OK
 
 
 def test_rotation_of_nothing(lib):
