@@ -15,7 +15,7 @@ def attend(q, k, v, scale, dtype):
 
     Scores: d products and as many sums in fp32, so off by (d + 4) 2^-24 of sum |q_i k_i| at most, and the argument of the exponential by
     two roundings (2^-23) of the largest difference of scores, in natural units.  A weight is off by that, relatively; a sum of n weights by
-    n / 16 + 40 roundings (16 of a lane in four chains, tile after tile, ranges and halves).  An output is a mean of values, so an error e of
+    n / 16 + 40 roundings (16 of a lane in two or four chains, tile after tile, ranges and halves).  An output is a mean of values, so an error e of
     all weights (and of their sum) moves it by 2 e of the largest value.  Weights of 16 bits add their rounding u (fp16 2^-33 of the largest
     weight each beside it), the output its own."""
     n, d = k.shape

@@ -248,6 +248,31 @@ def test_uneven_scores(lib, dtype):
         assert torch.equal(job.result().cpu(), job.v[0].expand_as(job.result()))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d,rows", [(64, 3), (64, 150), (64, 600), (128, 150), (128, 600)])
+def test_references(lib, dtype, d, rows):
+    """Tiles whose weights add up to just what a reference stands, a little less and a little more, and single weights at the end of fp16."""
+    job = Job(15, dtype, 2, 2, d, [rows], [13 * 64], layout="heads", scale=math.log(2.0))
+    level = torch.zeros(13, 64, dtype=torch.float64)
+    level[1, 5] = level[2, 40] = 7.0     # one weight of 2^7, in fp16's scale 2^16; in tile 1 it is 2^(15.9995), which rounds to the largest number
+    for tile, x in ((3, 9.875), (4, 10.0), (5, 11.0), (6, 14.0), (7, 12.0), (8, -20.0), (9, 30.0), (10, 31.0), (11, 38.0), (12, 38.0)):
+        level[tile] = x
+    level[12, ::2] = -1000.0
+    k = torch.zeros(13 * 64, d, dtype=torch.float64)
+    k[:, 0] = level.flatten()
+    k[64 + 5, 1] = 1.0
+    k = k.to(KIND[dtype])
+    for h in range(2):
+        job.rows[0, h][0] = k.double()
+        at = job.base[0] + h * job.sh
+        job.k[at:at + k.numel()] = k.flatten()
+    job.q_all.zero_()
+    job.q_all[:, :, 0] = torch.tensor([1.0, 0.5, 2.0, -1.0, 0.0]).to(KIND[dtype])[torch.arange(rows) % 5][:, None]
+    job.q_all[:, 0, 1] = -0.0005         # 65513: to 65504
+    job.q_all[:, 1, 1] = -0.0002         # 65527: beyond it
+    job.check()
+
+
 def test_far_offsets(lib):
     """States, queries and outputs behind the first 4 GB of their arrays, keys 64 KB apart so that a sequence's span passes 32 bits."""
     d, hkv, n, far = 64, 2, 70000, 1 << 15
