@@ -52,12 +52,18 @@ int64_t blocks_of(const Shape &x, const RowsPlan &pl, int n_kv_heads) {
 }
 
 // Narrow segments alone: ranges that are a workgroup for each CU together, kLeastRange at least; a segment of up to kShortKeys has no launch
-// behind it where it need not.  Fewer and longer ones leave CUs idle, more of them cost more starts and partial rows.
+// behind it where it need not.  Fewer and longer ones leave CUs idle, more of them cost more starts and partial rows.  Eight tokens of 32 heads on
+// 8 over 13171 keys, bf16, d = 128: 16.4 us with ranges of 512, 18.4 with 256, 24.9 with 128; eight sequences of one token over 16384 keys each:
+// 95.5 with 4096, 98.5 with 1024, 107.6 with 8192; eight of up to 64 keys behind 848: 12.6 with 128, 14.9 with 1024.  One token over 512 (768)
+// keys in one launch, d = 128: 8.8 (10.7) us, in two 10.8 (10.7); d = 64: 7.7 (8.9) and 10.8 (10.6).
 //
 // Otherwise the ranges and the tile whose last workgroup ends first, by an estimate in microseconds: a workgroup costs kStart, kRow for each of
 // its rows where ranges are joined (written and read again), and its keys, by type and kind.  The launch ends when the longest workgroups have
-// gone through in rounds, when all CUs have done their share, or when all keys have come from memory, whichever is last.
-constexpr int kLeastRange = 128, kShortKeys = 512, kCUs = 256;
+// gone through in rounds, when all CUs have done their share, or when all keys have come from memory, whichever is last.  61 tokens of 32 heads
+// on 8 over 13171 keys, bf16, d = 128: 33 to 35 us as estimated (128 rows, ranges of 832), 36.7 with 256 rows and ranges of 448, 42.3 with 256 and
+// 832, 44.2 with 128 and 640; 64 sequences behind 131072 keys: 194 (256 rows, 4096), 200 (128, 8192), 230 (256, 8192).  Other sizes that were
+// swept lie within 4 % of their best.
+constexpr int kLeastRange = 128, kShortKeys = 768, kCUs = 256;
 constexpr float kStart = 5.f, kJoin = 3.5f, kRow = 0.05f, kBytes = 5.5e6f;
 constexpr float kKey[2][2][3] = {   // [fp32][d = 128][256 rows, 128, narrow]
     {{0.020f, 0.012f, 0.008f}, {0.030f, 0.018f, 0.016f}}, {{0.13f, 0.066f, 0.018f}, {0.25f, 0.13f, 0.034f}}};

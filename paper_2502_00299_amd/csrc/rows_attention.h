@@ -3,10 +3,21 @@
 //   out_r = sum_s softmax_s(scale * q_r . k_s) v_s
 //
 // A workgroup of eight wavefronts has a tile of a segment's query rows (rows.h) and a range of its keys.  Three ways:
-//   256 rows   every wavefront has 32 rows and all keys, which come in tiles of 64 through a ring in LDS that all share;
-//   128 rows   two wavefronts have the same 32 rows, each half of every tile's keys; their states are merged in the end;
+//   256 rows   every wavefront has 32 rows and all keys, which come in tiles of 64 through a ring in LDS that all share: the most products to
+//              a byte of LDS;
+//   128 rows   two wavefronts have the same 32 rows, each half of every tile's keys; their states are merged in the end.  Half as many partial
+//              rows where there are few rows, but every key is read twice as often;
 //   32 rows    what a decoding step has: either half of the workgroup has a tile and range of its own, and each of its four wavefronts 32 keys
 //              at a time, every fourth, through LDS slots of its own, without a barrier; four states are merged in the end.
+// The plan in rows_api.hip chooses.  Keys go from memory into LDS without passing registers, three tiles (one, for fp32 and d = 128) ahead of
+// their use; a barrier to a tile is all that wavefronts wait for.
+//
+// Measured (MI355X).  Wide, 16 bits: bound by issue, not by one unit: the matrix cores are busy for half of the cycles, exponentials, sums and
+// roundings take most of the rest, at the clock that this power allows: 4096 tokens over 16384 keys, 32 heads on 8, d = 128, bf16: 958 us,
+// 1150 TFLOP/s, where a matrix product of 8192^3 reaches 1175.  Wide fp32: by its products, 127 of 152 TFLOP/s a tile; short calls also by starts and
+// partial rows.  Narrow: by memory, eight tokens over 16384 keys each (537 MB) 95 us, 5.6 TB/s; a few hundred keys by latency, 7 us.
+// Tried and slower: scores of the next block beside the weights of this one in one stream of instructions (3 to 8 %), half of the wavefronts half
+// a block behind the others (4 %).  Wave priorities change nothing.
 //
 //   scores   S[key][row] = K Q^T by 32x32 products, keys the M dimension: a lane holds 16 keys of row lane % 32, so a row's
 //            statistics need no exchange but one between the two halves of a wavefront, at the end.
