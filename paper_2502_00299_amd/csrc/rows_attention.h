@@ -5,7 +5,7 @@
 // A workgroup of eight wavefronts has a tile of a segment's query rows (rows.h) and a range of its keys.  Three ways:
 //   256 rows   every wavefront has 32 rows and all keys, which come in tiles of 64 through a ring in LDS that all share: the most products to
 //              a byte of LDS;
-//   128 rows   two wavefronts have the same 32 rows, each half of every tile's keys; their states are merged in the end.  Half as many partial
+//   128 rows   two wavefronts have the same 32 rows, each half of the keys; their states are merged in the end.  Half as many partial
 //              rows where there are few rows, but every key is read twice as often;
 //   32 rows    what a decoding step has: either half of the workgroup has a tile and range of its own, and each of its four wavefronts 32 keys
 //              at a time, every fourth, through LDS slots of its own, without a barrier; four states are merged in the end.
@@ -602,7 +602,12 @@ template <int DT, int HD, bool PAGED, bool MASK, bool LSE, int WK>
 __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const RowsWork &w, char *smem, int wave, int lane) {
   using S = RowsShape<DT, HD>;
   const auto &r = a.r;
-  constexpr int NL = 8 / S::kRpl, NST = S::kStages, NKB = 2 / WK;   // loads of a wavefront's eight rows of a tile; 32-key blocks of a tile that it has
+  constexpr int NL = 8 / S::kRpl, NST = S::kStages;   // loads of a wavefront's eight rows of a tile
+  // Wavefronts that share rows have halves of a tile's keys, or every other tile: half as many barriers, with one step rather than three
+  // tiles on their way, which d = 64 has more of the gain than the loss of.  23 sequences behind prefixes of 20995, 4096 and 10460 keys, fp16: 20.4 ->
+  // 19.1 us, 4096 rows over 2048 keys 77.9 -> 73.5; with d = 128 28.1 -> 29.0.
+  constexpr int PAIR = WK == 2 && HD == 64 ? 2 : 1;    // tiles to a barrier
+  constexpr int NKB = 2 * PAIR / WK;       // 32-key blocks that a wavefront has of them
   constexpr int NB = S::kTwo ? 1 : NKB;    // of which so many at a time
   const int n = lane & 31, half = lane >> 5, wk = WK == 2 ? wave & 1 : 0, wr = wave / WK;
   const bool idle = w.row0 + 32 * wr >= w.rows;      // this wavefront's rows are not there: it loads and waits with the others
@@ -615,7 +620,7 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
     voff[j] = (uint32_t)in_block * keys.tok + (uint32_t)((pos ^ S::vswz(in_block)) * 16);
   }
   const int tiles = w.len > 0 ? (w.len + kRowsTile - 1) / kRowsTile : 0;
-  uint64_t alive[NST];                   // keys that count, of the tiles in flight
+  uint64_t alive[NST - PAIR];            // keys that count, of the tiles in flight
   auto issue = [&](int t, int stage) __attribute__((always_inline)) {   // tiles past the last one too: the number of loads in flight is known at every wait
     if ((t & 15) == 0) keys.open(t / 16);
     const uint64_t bits = keys.template alive<4>(kRowsTile * t);
@@ -632,18 +637,18 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
   Rows<DT, HD, LSE> x;
   x.load(rows_query(r, w, w.row0 + 32 * wr + n), half, r.scale_log2e);
 #pragma unroll
-  for (int t = 0; t < NST - 1; ++t) alive[t] = issue(t, t);
+  for (int t = 0; t < NST - PAIR; ++t) alive[t] = issue(t, t);
   x.settle();
-  alive[NST - 1] = 0;
-  for (int t = 0; t < tiles; ++t) {
-    const int stage = t % NST;
-    const uint32_t base = (uint32_t)stage * 2 * S::kTile + (uint32_t)(32 * wk * S::kRow);
-    __builtin_amdgcn_s_waitcnt(vm_imm((NST - 2) * 2 * NL));
-    const uint64_t now = alive[0];
+  for (int t = 0; t < tiles; t += PAIR) {
+    const int stage = (PAIR == 2 ? t + wk : t) % NST, first = PAIR == 2 ? 0 : 32 * wk;   // first: key of the tile
+    const uint32_t base = (uint32_t)stage * 2 * S::kTile + (uint32_t)(first * S::kRow);
+    __builtin_amdgcn_s_waitcnt(vm_imm((NST - 2 * PAIR) * 2 * NL));
+    const uint64_t now = PAIR == 2 && wk == 1 ? alive[1] : alive[0];
     rows_barrier();
 #pragma unroll
-    for (int i = 0; i < NST - 2; ++i) alive[i] = alive[i + 1];
-    alive[NST - 2] = issue(t + NST - 1, (t + NST - 1) % NST);
+    for (int i = 0; i < NST - 2 * PAIR; ++i) alive[i] = alive[i + PAIR];
+#pragma unroll
+    for (int i = NST - PAIR; i < NST; ++i) alive[i - PAIR] = issue(t + i, (t + i) % NST);
     if (now == 0 || idle) continue;
 #pragma unroll
     for (int b0 = 0; b0 < NKB; b0 += NB) {
@@ -671,7 +676,7 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
       x.read_values(at0 + (uint32_t)S::kTile, vat, vf);   // while the products run
       if (now != ~0ull) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) x.leave_out(sc[b], (uint32_t)(now >> (32 * (b0 + b + wk))));
+        for (int b = 0; b < NB; ++b) x.leave_out(sc[b], (uint32_t)(now >> (32 * (b0 + b) + first)));
       }
       float p[NB][16];
       uint32_t pk[NB][8];
