@@ -3,7 +3,10 @@
 // A row (one head of one token) is spread over LPR = d * element size / 16 lanes, 16 bytes each; a wavefront takes 64 / LPR rows of a
 // token at a time, query and key rows alike, with the next ones on their way.  Angles and pairs as in rotary.h: all rows of a token
 // share its angles, which a wavefront forms once.  Per row: rotation in fp32, one rounding, store.
-// Bound by HBM for prompts, by latency for single tokens.
+// Bound by HBM for prompts (32768 tokens of 40 heads, bf16, d = 128: 671 MB read and written in 125 us, 5.4 TB/s), by the chain position, angle, row
+// for a few thousand tokens (4503 of 32 heads, 74 MB: 18.4 us), by one launch for a step (3.4 us in a graph, 7.5 with the host's checks).
+// Twice (four times) as many wavefronts to a token: 4096 tokens 17.9 -> 18.0 (19.4) us, 9000 half-rotated ones 32.7 -> 32.6 (29.8); two rows ahead
+// instead of one: the same.
 #include "rotary.h"
 #include "rows.h"
 
