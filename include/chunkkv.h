@@ -404,8 +404,9 @@ int chunkkv_rotary_frequencies(int32_t rotary_dim, double base, double factor, d
 
 /* Rows of heads, in and out: row (sequence b, token t, head h) starts at element b*stride_seq + t*stride_tok + h*stride_head, its
  * head_dim elements are contiguous, rows are 16-byte aligned.  Rows of a fused projection and those of a cache both fit, in different
- * orders too.  In place (out == in) the strides have to be the same.  Rows that are written must not overlap each other: of the axes that
- * have more than one entry, in the order of their strides, each steps over all before it (CHUNKKV_ERR_SHAPE).                      */
+ * orders too.  In place (out == in) the strides have to be the same; otherwise nothing that is written may overlap what is read.  Rows
+ * that are written must not overlap each other: of the axes that have more than one entry, in the order of their strides, each steps
+ * over all before it (CHUNKKV_ERR_SHAPE).                                                                                         */
 typedef struct {
   const void *in;
   void *out;
@@ -451,7 +452,7 @@ typedef struct {
 /*   kv_len     device int32 [B][Hkv] or NULL: states that there are, clamped to [0, seqlen_b] (heads of a whole-chunk cache differ)
  *   kv_mask    device bytes [B][mask_pitch] or NULL: 0 takes a state out, for all heads.  K and V of a state that is taken out, by
  *              the mask or by kv_len, may hold any bits
- *   out        device, in the storage type; 0 where no state is left
+ *   out        device, in the storage type, apart from what is read; 0 where no state is left
  *   lse        NULL or device float [sum of q_len][Hq], tokens of sequence 0 first: natural log of the softmax denominator (-inf where no
  *              state is left).  With it, parts of an attention can be joined: over a cache here, among the tokens themselves elsewhere
  *   workspace  chunkkv_cross_workspace_bytes(cross) bytes (0 = invalid), contents scratch
