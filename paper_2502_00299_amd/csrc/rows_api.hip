@@ -137,9 +137,9 @@ RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bo
       return blocks;
     };
     attempt(whole);
-    for (int share : {kCUs / 2, kCUs, 2 * kCUs}) {
+    for (int share : {kCUs / 2, kCUs, 2 * kCUs, 3 * kCUs}) {
       int range = whole_tiles(wide_keys[k] * n_kv_heads / (float)share);
-      for (int again = 0; again < 2 && range < whole; ++again) {
+      for (int again = 0; again < 3 && range < whole; ++again) {
         if (range < kLeastRange) range = kLeastRange;
         const float blocks = attempt(range);
         if (blocks <= (float)share) break;

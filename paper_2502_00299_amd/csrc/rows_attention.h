@@ -350,7 +350,7 @@ struct Rows {
     l += sum;
     if constexpr (LSE) le += exact;
   }
-  // Values of 32 keys at `at` in LDS, this lane's place among them at vat[].  16 bits: read ahead of their use.
+  // Values of 32 keys at `at` in LDS, this lane's place among them at vat[].  16 bits: read ahead of their use.  `bits`: keys that count.
   struct Values {
     u32x4 v[2][S::kD];
   };
@@ -362,10 +362,11 @@ struct Rows {
       read_vt<S::kRow>(from, x.v);
     }
   }
-  __device__ __forceinline__ void values(const char *smem, uint32_t at, const uint32_t (&vat)[S::kD], const Values &x, const float (&p)[16], const uint32_t (&pk)[8]) {
+  __device__ __forceinline__ void values(const char *smem, uint32_t at, const uint32_t (&vat)[S::kD], const Values &x, const float (&p)[16], const uint32_t (&pk)[8], uint32_t bits) {
     if constexpr (DT == CHUNKKV_F32) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
+        if ((bits >> (8 * (e / 4)) & 0xFF) == 0) continue;   // keys of these four steps: none counts
         const char *from = smem + at + vat[0] + (8 * (e / 4) + e % 4) * S::kRow;
         float vf[S::kD];
         if constexpr (S::kD == 4) {
@@ -608,7 +609,7 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
   // 19.1 us, 4096 rows over 2048 keys 77.9 -> 73.5; with d = 128 28.1 -> 29.0.
   constexpr int PAIR = WK == 2 && HD == 64 ? 2 : 1;    // tiles to a barrier
   constexpr int NKB = 2 * PAIR / WK;       // 32-key blocks that a wavefront has of them
-  constexpr int NB = S::kTwo ? 1 : NKB;    // of which so many at a time
+  constexpr int NB = S::kTwo || DT == CHUNKKV_F32 ? 1 : NKB;    // of which so many at a time
   const int n = lane & 31, half = lane >> 5, wk = WK == 2 ? wave & 1 : 0, wr = wave / WK;
   const bool idle = w.row0 + 32 * wr >= w.rows;      // this wavefront's rows are not there: it loads and waits with the others
   RowsKeys<DT, HD, PAGED, MASK> keys(a, w, lane);
@@ -652,6 +653,9 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
     if (now == 0 || idle) continue;
 #pragma unroll
     for (int b0 = 0; b0 < NKB; b0 += NB) {
+      // fp32, whose products take the time, has none with keys that do not count: 600 tokens over one key 27 -> 17 us (d = 64: 17 -> 11), over 4000
+      // keys 1 % slower
+      if (DT == CHUNKKV_F32 && (uint32_t)(now >> (32 * b0 + first)) == 0) continue;
       const uint32_t at0 = base + (uint32_t)(b0 * 32 * S::kRow);
       f32x16 sc[NB];
       u32x4 kf[S::kAhead];
@@ -685,7 +689,7 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
       for (int b = 0; b < NB; ++b) {
         const uint32_t at = at0 + (uint32_t)(S::kTile + b * 32 * S::kRow);
         if (b > 0) x.read_values(at, vat, vf);
-        x.values(smem, at, vat, vf, p[b], pk[b]);
+        x.values(smem, at, vat, vf, p[b], pk[b], (uint32_t)(now >> (32 * (b0 + b) + first)));
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -771,7 +775,7 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
       __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL));
       typename Rows<DT, HD, LSE>::Values vf;
       x.read_values(kbase + SLOT, vat, vf);
-      x.values(smem, kbase + SLOT, vat, vf, p[0], pk[0]);
+      x.values(smem, kbase + SLOT, vat, vf, p[0], pk[0], now);
     }
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL) & 0xC07F);   // V of this step is there and read
