@@ -775,6 +775,20 @@ def chunkkv_rotary_frequencies(rotary_dim: int, base: float, factor: float = 1.0
 _DTYPES = {kind: code for code, kind in _KINDS.items()}
 
 
+def _refuse_pitch(where: str, name: str, t: torch.Tensor, rows: int, pitch: int):
+    raise ValueError(f"{where}: {name} is {tuple(t.shape)}, not [{rows}][{pitch}]; a row of another width has to be the handle's pitch")
+
+
+def _pitched(where: str, name: str, t: Optional[torch.Tensor], rows: int, pitch: int):
+    """An array of rows has to have them `pitch` wide, one axis of rows: the library would read all but the first from another place.  A flat array and
+    a single row can be anything long enough."""
+    if t is None or rows < 2 or t.dim() < 2:
+        return
+    shape = t.shape
+    if shape[-1] != pitch or (len(shape) > 2 and sum(n != 1 for n in shape[:-1]) > 1):
+        _refuse_pitch(where, name, t, rows, pitch)
+
+
 def _refuse_rows(where: str, dev: int, name: str, x, y):
     for t in (x, y):
         if t.dim() not in (3, 4):
@@ -838,7 +852,8 @@ def chunkkv_cross_workspace_bytes(cross: Cross) -> int:
 
 
 def chunkkv_cross_attention(cross: Cross, kv_len, kv_mask, q, k, v, out, lse, workspace, stream=None) -> None:
-    """q, k, v, out: tensors whose first element the offsets of `cross` count from; kv_mask: [batch][mask_pitch] of torch.bool or torch.uint8."""
+    """q, k, v, out: tensors whose first element the offsets of `cross` count from; kv_mask: [batch][mask_pitch] of torch.bool or torch.uint8, the pitch that of
+    `cross` (the longest sequence's states, unless given)."""
     where, dev, kind = "chunkkv_cross_attention", _device(), _KINDS.get(cross.dtype)
     cp = cross._c()
     q_room, kv_room, out_room, tokens, mask_bytes = cross._kept[3]
@@ -846,6 +861,7 @@ def chunkkv_cross_attention(cross: Cross, kv_len, kv_mask, q, k, v, out, lse, wo
     mask = None
     if kv_mask is not None:
         mask, = _arrays(where, dev, ("kv_mask", kv_mask, kv_mask.dtype if kv_mask.dtype in (torch.bool, torch.uint8) else torch.bool, mask_bytes))
+        _pitched(where, "kv_mask", kv_mask, cross.batch, cross.mask_pitch)
     _check(load_library().chunkkv_cross_attention(
         cp, length, mask, _pool(where, dev, "q", q, kind, q_room), _pool(where, dev, "k", k, kind, kv_room), _pool(where, dev, "v", v, kind, kv_room),
         _pool(where, dev, "out", out, kind, out_room), norm, *_scratch(where, dev, workspace), _stream(stream, dev)), where)
