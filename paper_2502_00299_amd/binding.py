@@ -888,6 +888,8 @@ def chunkkv_shared_decode_attention(prefix: Pages, pages: Pages, n_sharing: Sequ
         where, dev, ("prefix_table", prefix_table, _I32, prefix.batch * prefix.table_pitch), ("prefix_len", prefix_len, _I32, prefix.batch * hkv),
         ("page_table", page_table, _I32, batch * pages.table_pitch), ("kv_len", kv_len, _I32, batch * hkv), ("q", q, kind, rows * pages.head_dim),
         ("out", out, kind, rows * pages.head_dim), ("lse", lse, _F32, rows))
+    _pitched(where, "prefix_table", prefix_table, prefix.batch, prefix.table_pitch)
+    _pitched(where, "page_table", page_table, batch, pages.table_pitch)
     _check(load_library().chunkkv_shared_decode_attention(
         whole, cp, _sharing(where, prefix, pages, n_sharing), ptable, plength, table, length, qp, _pool(where, dev, "k_pages", k_pages, kind, room),
         _pool(where, dev, "v_pages", v_pages, kind, room), op, lp, *_scratch(where, dev, workspace), _stream(stream, dev)), where)

@@ -38,3 +38,29 @@ def test_masks_as_wide_as_the_pitch(seqlen, shape, kw):
     with pytest.raises(ckv.ChunkKVError) as e:
         masked(seqlen, torch.ones(shape, dtype=torch.bool), **kw)
     assert e.value.status == NULL
+
+
+def behind(prefix, own, prefix_table, table, **kw):
+    whole, pages = (ckv.Pages(4, 2, 64, ckv.BF16, 16, 100, n, **kw) for n in (prefix, own))
+    tables = [torch.zeros(x, dtype=torch.int32) for x in (prefix_table, table)]
+    sharing = [len(own)] + [0] * (len(prefix) - 1)
+    ckv.chunkkv_shared_decode_attention(whole, pages, sharing, tables[0], None, tables[1], None, None, None, None, None, None, None, stream=STREAM)
+
+
+@pytest.mark.parametrize("prefix,own,prefix_table,table,name", [
+    ([100, 30], [5, 6, 7], (2, 8), (3, 1), "prefix_table"), ([100, 30], [5, 6, 7], (14, 1), (3, 1), "prefix_table"), ([100], [5, 40, 7], (1, 7), (3, 4), "page_table"),
+    ([100], [5, 40, 7], (7,), (3, 3, 3), "page_table"),
+])
+def test_tables_of_another_width(prefix, own, prefix_table, table, name):
+    """A second prefix's, or a second sequence's, pages would be read from the middle of the row before."""
+    with pytest.raises(ValueError, match=name):
+        behind(prefix, own, prefix_table, table)
+
+
+@pytest.mark.parametrize("prefix,own,prefix_table,table,kw", [
+    ([100, 30], [5, 6, 7], (2, 7), (3, 1), {}), ([100], [5], (1, 9), (1, 3), {}), ([100, 30], [5, 40, 7], (14,), (9,), {}), ([100, 30], [5, 6, 7], (2, 9), (4, 9), dict(table_pitch=9)),
+])
+def test_tables_as_wide_as_the_pitch(prefix, own, prefix_table, table, kw):
+    with pytest.raises(ckv.ChunkKVError) as e:
+        behind(prefix, own, prefix_table, table, **kw)
+    assert e.value.status == NULL
