@@ -435,7 +435,7 @@ int chunkkv_rotate(int32_t dtype, int32_t head_dim, int32_t n_seq, int32_t n_tok
  * Token t of query head h of sequence b starts at element q_base[b] + t*q_stride_tok + h*q_stride_head, its output at out_base[b] +
  * t*out_stride_tok + h*out_stride_head, state s of kv-head h of K and V at kv_base[b] + s*kv_stride_tok + h*kv_stride_head; rows have
  * head_dim contiguous elements and are 16-byte aligned.  Outputs must not overlap each other: the larger of out's strides steps over all
- * heads, or all tokens, of the smaller (CHUNKKV_ERR_SHAPE).
+ * heads, or all tokens, of the smaller, and no output row of a sequence lies on one of another's (CHUNKKV_ERR_SHAPE, the latter from the call).
  * Limits: head_dim 64 or 128; up to 1023 kv-heads and 256 query heads per kv-head; up to 2^24 states of a sequence, up to 4 MB apart;
  * 2^30 tokens, and as many query rows (tokens times g) of a sequence; 2^29 tokens times heads of 32 sequences.                   */
 typedef struct {

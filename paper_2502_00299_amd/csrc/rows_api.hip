@@ -3,6 +3,8 @@
 #include <string.h>
 
 #include <algorithm>
+#include <memory>
+#include <new>
 
 #include "rows.h"
 
@@ -28,6 +30,78 @@ bool overlap(Axis (&axis)[N], int64_t d) {
     if (x.n <= 1) continue;
     if (x.stride < end) return true;
     end += (__int128)x.stride * (x.n - 1);
+  }
+  return false;
+}
+
+// Rows of two axes at bases of their own, one lattice for each of n sequences: count[0] rows on the small axis, count[1] on the large one, both 0 or
+// neither.  overlap() has passed for the largest counts, so a lattice's rows do not overlap each other; do those of two?
+struct Lattice {
+  int64_t base, count[2];
+};
+struct Lattices {
+  int64_t small, large, d;               // strides; elements of a row
+
+  // Ends of x: of its rows on the small axis, of all.
+  __int128 end(const Lattice &x, bool all) const { return (__int128)x.base + (x.count[0] - 1) * (__int128)small + (all ? (x.count[1] - 1) * (__int128)large : 0) + d; }
+  // Is there a pair of rows less than d apart?  Steps i of the large axis and j of the small one lie between a row of x and one of y: only few i leave
+  // the rest within reach of the small axis, and of the j the two nearest to it.
+  bool meet(const Lattice &x, const Lattice &y) const {
+    const __int128 apart = (__int128)y.base - x.base;     // apart + i large + j small = 0, nearly
+    const int64_t j0 = -(x.count[0] - 1), j1 = y.count[0] - 1, i0 = -(x.count[1] - 1), i1 = y.count[1] - 1;
+    auto floor_div = [](__int128 a, int64_t b) { return a >= 0 ? a / b : -((-a + b - 1) / b); };
+    auto near = [&](__int128 rest) {                      // some j: |rest + j small| < d
+      __int128 j = small > 0 ? floor_div(-rest, small) : 0;
+      for (int e = 0; e < 2; ++e, ++j) {
+        const __int128 k = j < j0 ? j0 : (j > j1 ? j1 : j), gap = rest + k * small;
+        if (gap < d && gap > -d) return true;
+      }
+      return false;
+    };
+    if (large == 0) return near(apart);
+    // -apart - j small within d of i large, for j in [j0, j1]
+    __int128 lo = floor_div(-apart - j1 * (__int128)small - d, large), hi = floor_div(-apart - j0 * (__int128)small + d, large) + 1;
+    lo = lo < i0 ? i0 : lo;
+    hi = hi > i1 ? i1 : hi;
+    for (__int128 i = lo; i <= hi; ++i)
+      if (near(apart + i * large)) return true;
+    return false;
+  }
+};
+// One behind the other in the order of nth, as they mostly are: each whole, or (sequences between the rows of one another's large axis) within one step of it.
+template <typename F>
+bool lattices_in_line(int n, F &&nth, const Lattices &l) {
+  __int128 whole = 0, step = 0;
+  int64_t lowest = -1;
+  bool apart = true, beside = true;
+  for (int i = 0; i < n && (apart || beside); ++i) {
+    const Lattice x = nth(i);
+    if (x.count[0] == 0) continue;
+    apart &= x.base >= whole;
+    beside &= x.base >= step;
+    whole = l.end(x, true);
+    step = l.end(x, false);
+    if (lowest < 0) lowest = x.base;
+  }
+  return apart || (beside && step - lowest <= l.large);
+}
+template <typename F>
+bool lattices_meet(int n, F &&nth, const Lattices &l) {
+  if (lattices_in_line(n, nth, l)) return false;
+  const std::unique_ptr<int32_t[]> order(new (std::nothrow) int32_t[n]);   // by base; without memory every pair is looked at
+  auto sorted = [&](int i) { return nth(order ? order[i] : i); };
+  if (order) {
+    for (int i = 0; i < n; ++i) order[i] = i;
+    std::sort(order.get(), order.get() + n, [&](int x, int y) { return nth(x).base < nth(y).base; });
+    if (lattices_in_line(n, sorted, l)) return false;
+  }
+  for (int i = 0; i < n; ++i) {
+    const Lattice x = sorted(i);
+    for (int j = i + 1; x.count[0] > 0 && j < n; ++j) {
+      const Lattice y = sorted(j);
+      if (order && l.end(x, true) <= y.base) break;
+      if (y.count[0] > 0 && l.meet(x, y)) return true;
+    }
   }
   return false;
 }
@@ -191,6 +265,20 @@ int check_cross(const chunkkv_cross *c) {
   return most > 0 && overlap(axis, c->head_dim) ? CHUNKKV_ERR_SHAPE : CHUNKKV_OK;
 }
 
+// Outputs of two sequences in one place: whichever workgroup came last would have written them.
+bool cross_outputs_meet(const chunkkv_cross *c) {
+  int64_t most = 0;
+  for (int b = 0; b < c->batch; ++b) most = c->q_len[b] > most ? c->q_len[b] : most;
+  const bool heads_small = most <= 1 || (c->n_q_heads > 1 && c->out_stride_head < c->out_stride_tok);
+  // the stride of an axis of one entry can be anything
+  const int64_t head = c->n_q_heads > 1 ? c->out_stride_head : 0, tok = most > 1 ? c->out_stride_tok : 0;
+  const Lattices l = {heads_small ? head : tok, heads_small ? tok : head, c->head_dim};
+  return lattices_meet(c->batch, [&](int b) {
+    const int64_t n = c->q_len[b], heads = n > 0 ? c->n_q_heads : 0;
+    return heads_small ? Lattice{c->out_base[b], {heads, n}} : Lattice{c->out_base[b], {n, heads}};
+  }, l);
+}
+
 struct CrossPlan {
   RowsPlan rows;
   int64_t partials;
@@ -281,6 +369,8 @@ int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const
   if (rc) return rc;
   CrossPlan pl;
   if ((rc = cross_plan(c, &pl))) return rc;
+  if (pl.partials > 0 && (!workspace || workspace_bytes < pl.total || misaligned(workspace))) return CHUNKKV_ERR_WORKSPACE;
+  if (cross_outputs_meet(c)) return CHUNKKV_ERR_SHAPE;
   int64_t tokens = 0;
   int longest = 0;
   for (int b = 0; b < c->batch; ++b) {
@@ -290,7 +380,6 @@ int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const
   if (tokens > 0 && (!q || !out || (longest > 0 && (!k || !v)))) return CHUNKKV_ERR_NULL;   // arrays of no tokens may be anything
   if (kv_mask && c->mask_pitch < longest) return CHUNKKV_ERR_SHAPE;
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out)) return CHUNKKV_ERR_SHAPE;
-  if (pl.partials > 0 && (!workspace || workspace_bytes < pl.total || misaligned(workspace))) return CHUNKKV_ERR_WORKSPACE;
   if (tokens == 0) return CHUNKKV_OK;
   hipStream_t s = (hipStream_t)stream;
   const int esz = elem_bytes(c->dtype), g = c->n_q_heads / c->n_kv_heads;

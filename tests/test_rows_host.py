@@ -4,6 +4,7 @@ import ctypes as C
 import math
 import os
 import pickle
+import random
 import subprocess
 
 import pytest
@@ -231,3 +232,66 @@ def test_argument_checks_and_plans_are_clean_under_asan_and_ubsan(tmp_path):
     out = r.stdout + r.stderr
     assert r.returncode == 0 and "HOST SANITIZER RUN OK" in r.stdout, out[-4000:]
     assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
+
+
+def rows_of(p, b):
+    t, h = torch.meshgrid(torch.arange(p.q_len[b]), torch.arange(p.n_q_heads), indexing="ij")
+    return (p.out_base[b] + t * p.out_stride_tok + h * p.out_stride_head).flatten()
+
+
+def meet(p):
+    """Any two output rows of different sequences less than a row apart."""
+    rows = [rows_of(p, b) for b in range(p.batch)]
+    return any(len(x) and len(y) and bool(((x[:, None] - y).abs() < p.head_dim).any()) for i, x in enumerate(rows) for y in rows[:i])
+
+
+def outputs(q_len, base, head, tok, heads=4, d=64):
+    return ckv.Cross(heads, 2, d, ckv.BF16, q_len, [9] * len(q_len), [0] * len(q_len), d, 2 * d, out_base=base, out_stride_head=head, out_stride_tok=tok)
+
+
+@pytest.mark.parametrize("q_len,base,head,tok,status", [
+    ([3, 7], [0, 0], 64, 256, SHAPE), ([3, 7], [0, 2 * 256], 64, 256, SHAPE), ([3, 7], [0, 3 * 256 - 8], 64, 256, SHAPE), ([3, 7], [0, 3 * 256], 64, 256, NULL), ([3, 7], [7 * 256, 0], 64, 256, NULL),
+    ([3, 7], [7 * 256 - 64, 0], 64, 256, SHAPE), ([3, 0], [0, 0], 64, 256, NULL), ([1, 1], [0, 0], 64, 0, SHAPE), ([1, 1], [0, 256], 64, 0, NULL), ([1, 1, 1], [512, 0, 256], 64, 0, NULL),
+    # by head: sequences side by side in every head's row of tokens, one too long for it, in another order, one round the end
+    ([3, 7], [0, 3 * 64], 640, 64, NULL), ([3, 8], [0, 3 * 64], 640, 64, SHAPE), ([3, 7], [7 * 64, 0], 640, 64, NULL), ([3, 7], [0, 3 * 64 - 8], 640, 64, SHAPE), ([3, 7], [640, 3 * 64], 640, 64, NULL),
+    ([3, 7], [8 * 64, 0], 640, 64, SHAPE), ([3, 7], [8 * 64, 64], 640, 64, NULL),
+    # between one another's tokens, and heads
+    ([5, 5], [0, 256], 64, 512, NULL), ([5, 5], [0, 192], 64, 512, SHAPE), ([5, 5], [0, 64], 128, 512, NULL), ([5, 5], [0, 56], 128, 512, SHAPE), ([5, 5], [0, 512 + 64], 128, 512, NULL),
+    ([5, 5], [0, 1 << 55], 64, 1 << 55, SHAPE), ([5, 5], [1 << 55, 256], 64, 1 << 55, NULL),
+])
+def test_cross_outputs_of_two_sequences(lib, q_len, base, head, tok, status):
+    """In one place they would be whichever workgroup's came last; the call refuses before it misses the queries."""
+    p = outputs(q_len, base, head, tok)
+    assert meet(p) == (status == SHAPE) and cross(lib, p, q=None) == status
+
+
+def test_cross_outputs_of_many_sequences(lib):
+    rng, seen = random.Random(3), [0, 0]
+    for _ in range(3000):
+        heads, n = rng.choice([2, 4, 6]), rng.randint(2, 5)
+        q_len = [rng.choice([0, 1, 1, 2, 3, 5]) for _ in range(n)]
+        small = 64 + 8 * rng.choice([0, 0, 1, 8, 9, 20])
+        by_head = rng.random() < 0.5
+        span = ((heads if not by_head else max(q_len)) - 1) * small + 64 if max(q_len) else 64
+        large = span + 8 * rng.choice([0, 0, 1, 8, 30, 60, 400])
+        room = rng.choice([200, 1000, 4000])
+        base = [8 * rng.randrange(room) for _ in range(n)] if rng.random() < 0.7 else [i * rng.choice([64, small, large, span]) for i in rng.sample(range(n), n)]
+        p = outputs(q_len, base, *((large, small) if by_head else (small, large)), heads=heads)
+        want = meet(p)
+        seen[want] += 1
+        assert cross(lib, p, q=None) == (SHAPE if want else NULL if sum(q_len) else OK), p
+    assert min(seen) > 300, seen
+
+
+def test_cross_outputs_of_thousands_of_sequences(lib):
+    """Any order of them, in time: by sequence, by head, and one that meets another."""
+    n, t = 4000, [1 + i % 3 for i in range(4000)]
+    at = [sum(t[:i]) for i in range(n)]
+    order = random.Random(4).sample(range(n), n)
+    for scale, head, tok in ((256, 64, 256), (64, 64 * sum(t), 64)):
+        base = [x * scale for x in at]
+        assert cross(lib, outputs(t, base, head, tok), q=None) == NULL
+        q_len, shuffled = [t[i] for i in order], [base[i] for i in order]
+        assert cross(lib, outputs(q_len, shuffled, head, tok), q=None) == NULL
+        shuffled[17] = shuffled[3999] + (t[order[3999]] - 1) * tok
+        assert cross(lib, outputs(q_len, shuffled, head, tok), q=None) == SHAPE
