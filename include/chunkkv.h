@@ -467,7 +467,7 @@ int chunkkv_cross_attention(const chunkkv_cross *cross, const int32_t *kv_len, c
 /* chunkkv_paged_decode_attention for sequences that share a prefix: sequence b attends to all slots of its prefix and to those of
  * its own, and a prefix is read once for all sequences that share it.  Sequences are ordered by prefix: the first n_sharing[0] share prefix 0.
  *   prefix       geometry of the prefixes: batch is their number, max_tokens their slots; pages of the same pools, so heads, head_dim,
- *                dtype, softmax_scale, page_tokens, n_pages and strides are those of `pages` (CHUNKKV_ERR_SHAPE).  slot_pitch is not used
+ *                dtype, softmax_scale, page_tokens, n_pages and strides are those of `pages` (CHUNKKV_ERR_SHAPE).  slot_pitch of either is not used
  *   pages        geometry of the sequences' own slots
  *   n_sharing    HOST int32 [prefixes], each >= 0; their sum is pages->batch
  *   prefix_table device int32 [prefixes][prefix->table_pitch];  prefix_len  device int32 [prefixes][Hkv], or NULL: max_tokens

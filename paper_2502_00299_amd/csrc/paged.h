@@ -223,7 +223,7 @@ struct PagedEvictArgs {
 
 // ---- host side, shared by the entry points
 bool fine_scale(float x);
-int check_pages(const chunkkv_pages *p);
+int check_pages(const chunkkv_pages *p, bool slots = true);   // slots: the call has arrays of slots, and their pitch counts
 PageGeom geometry(const chunkkv_pages *p, const int32_t *table);
 int launch_paged_append(int dtype, int head_dim, const PagedAppendArgs &a, hipStream_t s);
 int launch_paged_len(const PagedLenArgs &a, hipStream_t s);

@@ -13,9 +13,9 @@ bool fine_scale(float x) {
   return u < 0x7F800000u || u == 0x80000000u;
 }
 
-int check_pages(const chunkkv_pages *p) {
+int check_pages(const chunkkv_pages *p, bool slots) {
   if (!p || !p->max_tokens) return CHUNKKV_ERR_NULL;
-  if (p->batch < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_pages < 1 || p->table_pitch < 1 || p->slot_pitch < 1) return CHUNKKV_ERR_SHAPE;
+  if (p->batch < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_pages < 1 || p->table_pitch < 1 || (slots && p->slot_pitch < 1)) return CHUNKKV_ERR_SHAPE;
   if (p->n_q_heads % p->n_kv_heads != 0) return CHUNKKV_ERR_SHAPE;
   if (!fine_scale(p->softmax_scale)) return CHUNKKV_ERR_SHAPE;
   if (p->dtype != CHUNKKV_F32 && p->dtype != CHUNKKV_BF16 && p->dtype != CHUNKKV_F16) return CHUNKKV_ERR_UNSUPPORTED;
@@ -30,7 +30,7 @@ int check_pages(const chunkkv_pages *p) {
     const int64_t n = p->max_tokens[b];
     if (n < 0) return CHUNKKV_ERR_SHAPE;
     if (n > kPagedMaxTokens) return CHUNKKV_ERR_UNSUPPORTED;
-    if (n > p->slot_pitch || n > (int64_t)p->table_pitch * p->page_tokens) return CHUNKKV_ERR_SHAPE;
+    if ((slots && n > p->slot_pitch) || n > (int64_t)p->table_pitch * p->page_tokens) return CHUNKKV_ERR_SHAPE;
   }
   return CHUNKKV_OK;
 }

@@ -306,9 +306,9 @@ int cross_plan(const chunkkv_cross *c, CrossPlan *pl) {
 
 // ---- attention behind shared prefixes -------------------------------------------------------------------------------
 int check_shared(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *n_sharing) {
-  int rc = check_pages(w);
+  int rc = check_pages(w, false);
   if (rc) return rc;
-  if ((rc = check_pages(p))) return rc;
+  if ((rc = check_pages(p, false))) return rc;
   if (!n_sharing) return CHUNKKV_ERR_NULL;
   if (w->n_q_heads != p->n_q_heads || w->n_kv_heads != p->n_kv_heads || w->head_dim != p->head_dim || w->dtype != p->dtype || w->page_tokens != p->page_tokens ||
       w->n_pages != p->n_pages || w->table_pitch < 1 || w->stride_page != p->stride_page || w->stride_head != p->stride_head || w->stride_tok != p->stride_tok ||

@@ -295,3 +295,20 @@ def test_cross_outputs_of_thousands_of_sequences(lib):
         assert cross(lib, outputs(q_len, shuffled, head, tok), q=None) == NULL
         shuffled[17] = shuffled[3999] + (t[order[3999]] - 1) * tok
         assert cross(lib, outputs(q_len, shuffled, head, tok), q=None) == SHAPE
+
+
+@pytest.mark.parametrize("pitch", [1, 16, 847])
+@pytest.mark.parametrize("whose", ["prefix", "pages"])
+def test_shared_uses_no_slot_arrays(lib, whose, pitch):
+    """Nor their pitch: of a prefix, or of the sequences' own slots, it may be less than there are slots, and nothing at all."""
+    w, p = pages([848, 30]), pages([5, 6, 900])
+    need, sharing = ckv.chunkkv_shared_decode_workspace_bytes(w, p, [2, 1]), (C.c_int32 * 2)(2, 1)
+    structs = {"prefix": w.as_c(), "pages": p.as_c()}
+    for n in (pitch, 0, -1):
+        structs[whose].slot_pitch = n
+        a, b = C.byref(structs["prefix"]), C.byref(structs["pages"])
+        assert lib.chunkkv_shared_decode_workspace_bytes(a, b, sharing) == need > 256
+        assert lib.chunkkv_shared_decode_attention(a, b, sharing, FAKE, None, FAKE, None, FAKE, FAKE, FAKE, FAKE, None, FAKE, need - 1, None) == WORKSPACE
+    # where there are such arrays it counts
+    structs["pages"].slot_pitch = 0
+    assert lib.chunkkv_paged_decode_workspace_bytes(C.byref(structs["pages"]), 0) == 0
