@@ -526,7 +526,7 @@ int chunkkv_rotary_frequencies(int32_t rotary_dim, double base, double factor, d
   if (rotary_dim < 2 || rotary_dim % 2 != 0 || base <= 1.0 || factor < 1.0 || slow < 0.0 || fast < slow || trained_tokens < 0.0) return CHUNKKV_ERR_SHAPE;
   for (int i = 0; i < rotary_dim / 2; ++i) {
     const double f = pow(base, -2.0 * i / rotary_dim), turns = trained_tokens * f / 6.283185307179586;
-    const double stay = turns >= fast ? 1.0 : (turns <= slow ? 0.0 : (turns - slow) / (fast - slow));
+    const double stay = trained_tokens == 0.0 ? 0.0 : (turns >= fast ? 1.0 : (turns <= slow ? 0.0 : (turns - slow) / (fast - slow)));
     inv_freq[i] = (float)(f * stay + f / factor * (1.0 - stay));
   }
   return CHUNKKV_OK;

@@ -312,3 +312,14 @@ def test_shared_uses_no_slot_arrays(lib, whose, pitch):
     # where there are such arrays it counts
     structs["pages"].slot_pitch = 0
     assert lib.chunkkv_paged_decode_workspace_bytes(C.byref(structs["pages"]), 0) == 0
+
+
+@pytest.mark.parametrize("slow,fast", [(1.0, 32.0), (0.0, 32.0), (0.0, 0.0), (2.0, 2.0)])
+def test_frequencies_without_a_trained_length(slow, fast):
+    """trained_tokens 0 divides every frequency, whatever the ramp, also one that begins and ends at 0 turns."""
+    want = 10000.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64) / 64) / 4
+    got = ckv.chunkkv_rotary_frequencies(64, 10000.0, 4.0, slow, fast, 0.0).double()
+    assert ((got - want).abs() <= 2.0 ** -24 * want).all()
+    if fast == 0.0:   # with one, every frequency turns: none is divided
+        got = ckv.chunkkv_rotary_frequencies(64, 10000.0, 4.0, slow, fast, 1.0).double()
+        assert ((got - 4 * want).abs() <= 4 * 2.0 ** -24 * want).all()
