@@ -323,3 +323,13 @@ def test_frequencies_without_a_trained_length(slow, fast):
     if fast == 0.0:   # with one, every frequency turns: none is divided
         got = ckv.chunkkv_rotary_frequencies(64, 10000.0, 4.0, slow, fast, 1.0).double()
         assert ((got - 4 * want).abs() <= 4 * 2.0 ** -24 * want).all()
+
+
+@pytest.mark.parametrize("sequences,fits", [(32767, True), (32768, False), (65536, False)])
+def test_partial_rows_that_a_launch_cannot_number(lib, sequences, fits):
+    """A prefix of one slot and own ones of one: 2048 query heads of both are 4096 partial rows a sequence, of less than 2^27."""
+    kw = dict(n_q_heads=2048, n_kv_heads=8, table_pitch=1)
+    w, p = pages([1], **kw), pages([1] * sequences, **kw)
+    need = ckv.chunkkv_shared_decode_workspace_bytes(w, p, [sequences])
+    assert need >= 4096 * sequences * (16 + 512) if fits else need == 0
+    assert shared(lib, w, p, n=(sequences,), size=need - 1 if fits else 1 << 50) == (WORKSPACE if fits else UNSUPPORTED)
