@@ -111,6 +111,7 @@ bool lattices_meet(int n, F &&nth, const Lattices &l) {
 struct Shape {
   int rows, most;
 };
+constexpr int kKeptPlans = 16;   // of a call's first launches, between its size and its launches; those of later ones are made again
 struct RowsPlan {
   int tile, pairs;       // rows of a wide workgroup, kRowsNarrow: there is none; narrow tiles of a workgroup
   int range[2];          // keys of a range of a wide segment, of a narrow one; a multiple of kRowsTile
@@ -137,13 +138,17 @@ int64_t blocks_of(const Shape &x, const RowsPlan &pl, int n_kv_heads) {
 // on 8 over 13171 keys, bf16, d = 128: 33 to 35 us as estimated (128 rows, ranges of 832), 36.7 with 256 rows and ranges of 448, 42.3 with 256 and
 // 832, 44.2 with 128 and 640; 64 sequences behind 131072 keys: 194 (256 rows, 4096), 200 (128, 8192), 230 (256, 8192).  Other sizes that were
 // swept lie within 4 % of their best.
+//
+// A plan is that of one launch: a call's launches run one behind the other.  128 sequences of one token, one kv-head and 16384 keys, bf16, d = 128: 365 us
+// with ranges for the sum of all, 202 so; 64 prefixes of 8192 slots with 16 sequences of 32 heads on 8 each 937 and 650; 300 sequences behind 5000
+// slots 122 and 143, 127 with `of_many`, which is why ranges for the wide segments alone are tried there.
 constexpr int kLeastRange = 128, kShortKeys = 768, kCUs = 256;
 constexpr float kStart = 5.f, kJoin = 3.5f, kRow = 0.05f, kBytes = 5.5e6f;
 constexpr float kKey[2][2][3] = {   // [fp32][d = 128][256 rows, 128, narrow]
     {{0.020f, 0.012f, 0.008f}, {0.030f, 0.018f, 0.016f}}, {{0.13f, 0.066f, 0.018f}, {0.25f, 0.13f, 0.034f}}};
 int whole_tiles(float keys) { return keys < (float)kPagedMaxTokens ? ((int)keys + kRowsTile - 1) / kRowsTile * kRowsTile : kPagedMaxTokens; }
 template <typename F>
-RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bool always_joined) {
+RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bool always_joined, bool of_many) {
   float keys = 0.f, wide_keys[2] = {0.f, 0.f};   // of all segments; of wide ones times their workgroups, 256 rows and 128
   int most = 1, rows_most = 0;
   for (int i = 0; i < n; ++i) {
@@ -180,11 +185,11 @@ RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bo
   const float *rate = kKey[dtype == CHUNKKV_F32][head_dim == 128];
   for (int k = 0; k < 2; ++k) {
     const float tile = 1.f / (float)(kRowsWide << (1 - k));
-    // tries ranges of so many keys; -> workgroups
-    auto attempt = [&](int range) {
+    // tries ranges of so many keys; -> workgroups, of all segments or of the wide ones
+    auto attempt = [&](int range, bool all = true) {
       RowsPlan pl = {kRowsWide << (1 - k), pairs, {range, whole_tiles((float)range * rate[k] / rate[2])}};
       const float per[2] = {1.f / (float)pl.range[0], 1.f / (float)pl.range[1]};
-      float total = 0.f, blocks = 0.f, full = 0.f, longest[2] = {0.f, 0.f};
+      float total = 0.f, blocks = 0.f, wide = 0.f, full = 0.f, longest[2] = {0.f, 0.f};
       bool joined = always_joined;
       for (int i = 0; i < n; ++i) {
         const Shape x = shape(i);
@@ -195,6 +200,7 @@ RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bo
         const float cost = (float)(cut ? pl.range[narrow] : x.most) * rate[narrow ? 2 : k] + kStart + (cut ? (float)rows * kRow : 0.f);
         total += count * cost;
         blocks += count;
+        wide += narrow ? 0.f : count;
         longest[narrow] = cost > longest[narrow] ? cost : longest[narrow];
         full += !narrow && 2 * x.most > pl.range[0] ? count : 0.f;
         joined |= cut;
@@ -208,7 +214,7 @@ RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bo
         least = end;
         best = pl;
       }
-      return blocks;
+      return all ? blocks : wide * (float)n_kv_heads;
     };
     attempt(whole);
     // half a workgroup to a CU, one, two or three; the last for segments of unlike length (three of 41 to 418 fp32 tokens: 227 us, 266 without)
@@ -219,6 +225,16 @@ RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bo
         const float blocks = attempt(range);
         if (blocks <= (float)share) break;
         range = whole_tiles((float)range * blocks / (float)share);   // ends of segments are more workgroups than that
+      }
+    }
+    // a launch of a call that has more: its wide segments alone so many, where narrow ones are half of it or more
+    for (int share : {kCUs / 2, kCUs, 2 * kCUs}) {
+      int range = whole_tiles(wide_keys[k] * n_kv_heads / (float)share);
+      for (int again = 0; of_many && again < 3 && range < whole; ++again) {
+        if (range < kLeastRange) range = kLeastRange;
+        const float blocks = attempt(range, false);
+        if (blocks <= (float)share) break;
+        range = whole_tiles((float)range * blocks / (float)share);
       }
     }
   }
@@ -279,23 +295,28 @@ bool cross_outputs_meet(const chunkkv_cross *c) {
   }, l);
 }
 
+// The launches of a call follow one another on the stream and share the workspace; each is planned for the whole card.
 struct CrossPlan {
-  RowsPlan rows;
+  RowsPlan kept[kKeptPlans];
   int64_t partials;
   size_t off_o, total;
 };
 Shape cross_shape(const chunkkv_cross *c, int b) { return {c->q_len[b] * (c->n_q_heads / c->n_kv_heads), c->seqlen[b]}; }
-// The launches of a call follow one another on the stream and share the workspace.
+int cross_count(const chunkkv_cross *c, int b0) { return c->batch - b0 < kCrossSegments ? c->batch - b0 : kCrossSegments; }
+RowsPlan cross_launch_plan(const chunkkv_cross *c, int b0) {   // of the sequences from b0 on
+  return plan_rows(cross_count(c, b0), [&](int i) { return cross_shape(c, b0 + i); }, c->n_kv_heads, c->dtype, c->head_dim, false, c->batch > kCrossSegments);
+}
 int cross_plan(const chunkkv_cross *c, CrossPlan *pl) {
-  pl->rows = plan_rows(c->batch, [&](int b) { return cross_shape(c, b); }, c->n_kv_heads, c->dtype, c->head_dim, false);
   pl->partials = 0;
   for (int b0 = 0; b0 < c->batch; b0 += kCrossSegments) {
+    const RowsPlan plan = cross_launch_plan(c, b0);
+    if (b0 / kCrossSegments < kKeptPlans) pl->kept[b0 / kCrossSegments] = plan;
     int64_t rows = 0, items = 0;
-    for (int b = b0; b < c->batch && b < b0 + kCrossSegments; ++b) {
-      const Shape x = cross_shape(c, b);
-      const int splits = ranges_of(x, pl->rows);
+    for (int i = 0; i < cross_count(c, b0); ++i) {
+      const Shape x = cross_shape(c, b0 + i);
+      const int splits = ranges_of(x, plan);
       if (splits > 1) rows += (int64_t)splits * c->n_kv_heads * x.rows;
-      items += blocks_of(x, pl->rows, c->n_kv_heads);
+      items += blocks_of(x, plan, c->n_kv_heads);
     }
     if (rows > kMostPartials || items > kMostBlocks) return CHUNKKV_ERR_UNSUPPORTED;
     pl->partials = rows > pl->partials ? rows : pl->partials;
@@ -323,30 +344,51 @@ int check_shared(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *
   return (int64_t)p->batch * (p->n_q_heads / p->n_kv_heads) > kMaxQueryRows ? CHUNKKV_ERR_UNSUPPORTED : CHUNKKV_OK;
 }
 
+// Launch l has up to kLaunchPrefixes prefixes and kJoinSegments sequences of a call, and is planned for the whole card.
 struct SharedPlan {
-  RowsPlan rows;
+  RowsPlan kept[kKeptPlans];
   int64_t partials, prefix_partials;
   size_t off_o, total;
 };
-// Segment i: prefix i, or sequence i - prefixes; one without keys has no rows.
-Shape shared_shape(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *n_sharing, int i) {
-  const int g = p->n_q_heads / p->n_kv_heads;
-  if (i < w->batch) return {w->max_tokens[i] > 0 ? n_sharing[i] * g : 0, w->max_tokens[i]};
-  return {p->max_tokens[i - w->batch] > 0 ? g : 0, p->max_tokens[i - w->batch]};
-}
-int shared_plan(const chunkkv_pages *w, const chunkkv_pages *p, const int32_t *n_sharing, SharedPlan *pl) {
-  const int n = w->batch + p->batch;
-  pl->rows = plan_rows(n, [&](int i) { return shared_shape(w, p, n_sharing, i); }, p->n_kv_heads, p->dtype, p->head_dim, true);
-  pl->partials = 0;
-  int64_t items = 0;
-  for (int i = 0; i < n; ++i) {
-    const Shape x = shared_shape(w, p, n_sharing, i);
-    pl->partials += (int64_t)ranges_of(x, pl->rows) * p->n_kv_heads * x.rows;
-    items += blocks_of(x, pl->rows, p->n_kv_heads);
-    if (i == w->batch - 1) pl->prefix_partials = pl->partials;
+struct SharedCall {
+  const chunkkv_pages *w, *p;
+  const int32_t *n_sharing;
+
+  // Prefix i, sequence b; one without keys has no rows.
+  Shape prefix(int i) const { return {w->max_tokens[i] > 0 ? n_sharing[i] * (p->n_q_heads / p->n_kv_heads) : 0, w->max_tokens[i]}; }
+  Shape sequence(int b) const { return {p->max_tokens[b] > 0 ? p->n_q_heads / p->n_kv_heads : 0, p->max_tokens[b]}; }
+  static int part(int n, int each, int l) { return (int64_t)l * each >= n ? 0 : (n - l * each < each ? n - l * each : each); }
+  int prefixes(int l) const { return part(w->batch, kLaunchPrefixes, l); }
+  int sequences(int l) const { return part(p->batch, kJoinSegments, l); }
+  // Segment i of launch l, which has np prefixes: those, then its sequences.
+  Shape segment(int l, int np, int i) const { return i < np ? prefix(l * kLaunchPrefixes + i) : sequence(l * kJoinSegments + i - np); }
+  RowsPlan plan(int l) const {
+    const int np = prefixes(l), g = p->n_q_heads / p->n_kv_heads;
+    const int i0 = np > 0 ? l * kLaunchPrefixes : 0, b0 = sequences(l) > 0 ? l * kJoinSegments : 0;
+    const int32_t *whole = w->max_tokens + i0, *sharing = n_sharing + i0, *own = p->max_tokens + b0;
+    auto shape = [&](int i) {   // as segment()
+      const int most = i < np ? whole[i] : own[i - np];
+      return Shape{most > 0 ? (i < np ? sharing[i] * g : g) : 0, most};
+    };
+    return plan_rows(np + sequences(l), shape, p->n_kv_heads, p->dtype, p->head_dim, true, prefixes(1) + sequences(1) > 0);
   }
+};
+int shared_plan(const SharedCall &c, SharedPlan *pl) {
+  int64_t rows[2] = {0, 0}, items = 0;   // partial rows of prefixes, of sequences
+  for (int l = 0; c.prefixes(l) + c.sequences(l) > 0; ++l) {
+    const RowsPlan plan = c.plan(l);
+    if (l < kKeptPlans) pl->kept[l] = plan;
+    const int np = c.prefixes(l), n = np + c.sequences(l);
+    for (int i = 0; i < n; ++i) {
+      const Shape x = c.segment(l, np, i);
+      rows[i >= np] += (int64_t)ranges_of(x, plan) * c.p->n_kv_heads * x.rows;
+      items += blocks_of(x, plan, c.p->n_kv_heads);
+    }
+  }
+  pl->prefix_partials = rows[0];
+  pl->partials = rows[0] + rows[1];
   if (pl->partials > kMostPartials || items > kMostBlocks) return CHUNKKV_ERR_UNSUPPORTED;
-  pl->total = partial_bytes(pl->partials, p->head_dim, &pl->off_o);
+  pl->total = partial_bytes(pl->partials, c.p->head_dim, &pl->off_o);
   return CHUNKKV_OK;
 }
 
@@ -385,7 +427,8 @@ int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const
   const int esz = elem_bytes(c->dtype), g = c->n_q_heads / c->n_kv_heads;
   int token0 = 0;
   for (int b0 = 0; b0 < c->batch; b0 += kCrossSegments) {
-    const int nb = c->batch - b0 < kCrossSegments ? c->batch - b0 : kCrossSegments;
+    const int nb = cross_count(c, b0);
+    const RowsPlan plan = b0 / kCrossSegments < kKeptPlans ? pl.kept[b0 / kCrossSegments] : cross_launch_plan(c, b0);
     CrossArgs a;
     JoinArgs j;
     memset(&a, 0, sizeof(a));
@@ -396,7 +439,7 @@ int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const
     r.q = q; r.k = k; r.v = v; r.out = out; r.lse = lse;
     r.part_ml = (float4 *)workspace; r.part_o = (float *)((char *)workspace + pl.off_o);
     r.q_tok = c->q_stride_tok * esz; r.q_head = c->q_stride_head * esz; r.out_tok = c->out_stride_tok * esz; r.out_head = c->out_stride_head * esz;
-    r.heads = divisor(c->n_kv_heads); r.group = divisor(g); r.segments = nb; r.seq0 = b0; r.tile = pl.rows.tile;
+    r.heads = divisor(c->n_kv_heads); r.group = divisor(g); r.segments = nb; r.seq0 = b0; r.tile = plan.tile;
     set_scale(c->softmax_scale, c->head_dim, &r.scale, &r.scale_log2e);
     for (int &x : r.first) x = INT32_MAX;
     j.part_ml = r.part_ml; j.part_o = r.part_o; j.out = out; j.lse = lse; j.out_tok = r.out_tok; j.out_head = r.out_head;
@@ -406,10 +449,10 @@ int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const
     for (int i = 0; i < nb; ++i) {
       const int b = b0 + i;
       const Shape x = cross_shape(c, b);
-      const int splits = ranges_of(x, pl.rows);
+      const int splits = ranges_of(x, plan);
       RowsSegment &seg = r.segment[i];
       r.first[i] = items;
-      seg.rows = x.rows; seg.most = x.most; seg.row0 = token0; seg.splits = splits; seg.tiles = tiles_of(x, pl.rows); seg.part = -1;
+      seg.rows = x.rows; seg.most = x.most; seg.row0 = token0; seg.splits = splits; seg.tiles = tiles_of(x, plan); seg.part = -1;
       a.q_base[i] = c->q_base[b] * esz; a.kv_base[i] = c->kv_base[b] * esz; a.out_base[i] = c->out_base[b] * esz;
       if (splits > 1 && x.rows > 0) {
         seg.part = parts;
@@ -419,7 +462,7 @@ int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const
         j.tokens += c->q_len[b];
         parts += splits * c->n_kv_heads * x.rows;
       }
-      items += (int)blocks_of(x, pl.rows, c->n_kv_heads);
+      items += (int)blocks_of(x, plan, c->n_kv_heads);
       token0 += c->q_len[b];
     }
     r.first[nb] = items;
@@ -434,7 +477,7 @@ int chunkkv_cross_attention(const chunkkv_cross *c, const int32_t *kv_len, const
 
 size_t chunkkv_shared_decode_workspace_bytes(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing) {
   SharedPlan pl;
-  if (check_shared(prefix, pages, n_sharing) || shared_plan(prefix, pages, n_sharing, &pl)) return 0;
+  if (check_shared(prefix, pages, n_sharing) || shared_plan({prefix, pages, n_sharing}, &pl)) return 0;
   return pl.total > 256 ? pl.total : 256;
 }
 
@@ -445,20 +488,22 @@ int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_p
   if (rc) return rc;
   if (!prefix_table || !page_table || !q || !k_pages || !v_pages || !out) return CHUNKKV_ERR_NULL;
   if (misaligned(q) || misaligned(k_pages) || misaligned(v_pages) || misaligned(out)) return CHUNKKV_ERR_SHAPE;
+  const SharedCall c = {prefix, pages, n_sharing};
   SharedPlan pl;
-  if ((rc = shared_plan(prefix, pages, n_sharing, &pl))) return rc;
+  if ((rc = shared_plan(c, &pl))) return rc;
   if (pl.partials > 0 && (!workspace || workspace_bytes < pl.total || misaligned(workspace))) return CHUNKKV_ERR_WORKSPACE;
+  auto plan_of = [&](int l) { return l < kKeptPlans ? pl.kept[l] : c.plan(l); };
   hipStream_t s = (hipStream_t)stream;
   const int d = pages->head_dim, esz = elem_bytes(pages->dtype), g = pages->n_q_heads / pages->n_kv_heads, hkv = pages->n_kv_heads;
   float4 *part_ml = (float4 *)workspace;
   float *part_o = (float *)((char *)workspace + pl.off_o);
   float scale, scale_log2e;
   set_scale(pages->softmax_scale, d, &scale, &scale_log2e);
-  // Partial rows: those of the prefixes, then those of the sequences.  A launch has up to kLaunchPrefixes prefixes and kJoinSegments sequences.
+  // Partial rows: those of the prefixes, then those of the sequences.
   int parts[2] = {0, (int)pl.prefix_partials}, before = 0;   // before: sequences of the prefixes before
-  for (int i0 = 0, b0 = 0; i0 < prefix->batch || b0 < pages->batch; i0 += kLaunchPrefixes, b0 += kJoinSegments) {
-    const int np = i0 >= prefix->batch ? 0 : (prefix->batch - i0 < kLaunchPrefixes ? prefix->batch - i0 : kLaunchPrefixes);
-    const int nb = b0 >= pages->batch ? 0 : (pages->batch - b0 < kJoinSegments ? pages->batch - b0 : kJoinSegments);
+  for (int l = 0; c.prefixes(l) + c.sequences(l) > 0; ++l) {
+    const int np = c.prefixes(l), nb = c.sequences(l), i0 = l * kLaunchPrefixes, b0 = l * kJoinSegments;
+    const RowsPlan plan = plan_of(l);
     SharedArgs a;
     memset(&a, 0, sizeof(a));
     auto &r = a.r;
@@ -468,19 +513,19 @@ int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_p
     r.q = q; r.k = k_pages; r.v = v_pages; r.out = out; r.lse = lse;
     r.part_ml = part_ml; r.part_o = part_o;
     r.q_tok = r.out_tok = (int64_t)pages->n_q_heads * d * esz; r.q_head = r.out_head = (int64_t)d * esz;
-    r.heads = divisor(hkv); r.group = divisor(g); r.segments = np + nb; r.prefixes = np; r.prefix0 = i0; r.seq0 = b0; r.tile = pl.rows.tile;
+    r.heads = divisor(hkv); r.group = divisor(g); r.segments = np + nb; r.prefixes = np; r.prefix0 = i0; r.seq0 = b0; r.tile = plan.tile;
     r.scale = scale; r.scale_log2e = scale_log2e;
     for (int &x : r.first) x = INT32_MAX;
     int items = 0;
     for (int i = 0; i < np + nb; ++i) {
       const bool own = i >= np;
-      const Shape x = shared_shape(prefix, pages, n_sharing, own ? prefix->batch + b0 + i - np : i0 + i);
-      const int splits = ranges_of(x, pl.rows);
+      const Shape x = c.segment(l, np, i);
+      const int splits = ranges_of(x, plan);
       RowsSegment &seg = r.segment[i];
       r.first[i] = items;
-      seg.rows = x.rows; seg.most = x.most; seg.row0 = own ? b0 + i - np : before; seg.splits = splits; seg.tiles = tiles_of(x, pl.rows); seg.part = parts[own];
+      seg.rows = x.rows; seg.most = x.most; seg.row0 = own ? b0 + i - np : before; seg.splits = splits; seg.tiles = tiles_of(x, plan); seg.part = parts[own];
       if (!own) before += n_sharing[i0 + i];
-      items += (int)blocks_of(x, pl.rows, hkv);
+      items += (int)blocks_of(x, plan, hkv);
       parts[own] += splits * hkv * x.rows;
     }
     r.first[np + nb] = items;
@@ -489,22 +534,27 @@ int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_p
     rc = pages->dtype == CHUNKKV_BF16 ? launch_shared_bf16(d, a, s) : (pages->dtype == CHUNKKV_F16 ? launch_shared_f16(d, a, s) : launch_shared_f32(d, a, s));
     if (rc) return rc;
   }
-  // every sequence's own ranges and those of its prefix, in the order in which their rows were numbered
+  // every sequence's own ranges and those of its prefix, in the order in which their rows were numbered: each by the plan of its launch
   int i = 0, nth = 0, prefix_part = 0, own_part = (int)pl.prefix_partials;
-  for (int b0 = 0; b0 < pages->batch; b0 += kJoinSegments) {
-    const int nb = pages->batch - b0 < kJoinSegments ? pages->batch - b0 : kJoinSegments;
+  RowsPlan of_prefix = plan_of(0);
+  for (int l = 0; c.sequences(l) > 0; ++l) {
+    const int nb = c.sequences(l), b0 = l * kJoinSegments;
+    const RowsPlan plan = plan_of(l);
     JoinArgs j;
     memset(&j, 0, sizeof(j));
     j.part_ml = part_ml; j.part_o = part_o; j.out = out; j.lse = lse; j.out_tok = (int64_t)pages->n_q_heads * d * esz; j.out_head = (int64_t)d * esz;
     j.heads = divisor(hkv); j.group = divisor(g); j.scale = scale; j.scale_log2e = scale_log2e; j.segments = j.tokens = nb;
     for (int n = 0; n < kJoinSegments; ++n) j.first[n] = n < nb ? n : INT32_MAX;
     for (int n = 0; n < nb; ++n, ++nth) {
-      for (; nth == n_sharing[i]; ++i, nth = 0) {
-        const Shape x = shared_shape(prefix, pages, n_sharing, i);
-        prefix_part += ranges_of(x, pl.rows) * hkv * x.rows;
+      while (nth == n_sharing[i]) {
+        const Shape x = c.prefix(i);
+        prefix_part += ranges_of(x, of_prefix) * hkv * x.rows;
+        ++i;
+        nth = 0;
+        if (i % kLaunchPrefixes == 0) of_prefix = plan_of(i / kLaunchPrefixes);
       }
-      const Shape whole = shared_shape(prefix, pages, n_sharing, i), own = shared_shape(prefix, pages, n_sharing, prefix->batch + b0 + n);
-      j.segment[n] = {own_part, ranges_of(own, pl.rows), own.rows, b0 + n, prefix_part, ranges_of(whole, pl.rows), whole.rows, nth * g, (b0 + n) * j.out_tok};
+      const Shape whole = c.prefix(i), own = c.sequence(b0 + n);
+      j.segment[n] = {own_part, ranges_of(own, plan), own.rows, b0 + n, prefix_part, ranges_of(whole, of_prefix), whole.rows, nth * g, (b0 + n) * j.out_tok};
       own_part += j.segment[n].splits * hkv * own.rows;
     }
     Timed t(kDecode, s);

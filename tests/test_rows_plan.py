@@ -202,3 +202,23 @@ def test_shapes_of_many_segments(ask, dt, d):
     a, = ask([shared(dt, 8, 2, d, prefix, sharing, own)])
     check_shared(a, dt, 8, 2, d, prefix, sharing, own)
     assert [x["kind"] for x in a["launches"]].count("rows") >= 3
+
+
+@pytest.mark.parametrize("dt,d", TYPES)
+def test_every_launch_is_planned_for_all_of_the_card(ask, dt, d):
+    """More segments than a launch has: the launches run one behind the other, so each of them is cut as a call of its segments alone."""
+    calls = [(8, 4, [1] * 64, [16384] * 64), (1, 1, [1] * 128, [16384] * 128), (32, 8, [40] * 70, [9000] * 70), (32, 8, [1 + i % 3 for i in range(100)], [200 + 199 * i for i in range(100)])]
+    for hq, hkv, q_len, states in calls:
+        launches = [x for x in ask([cross(dt, hq, hkv, d, q_len, states)])[0]["launches"] if x["kind"] == "rows"]
+        assert len(launches) == -(-len(q_len) // 32)
+        for i, launch in enumerate(launches):
+            part = slice(32 * i, 32 * i + 32)
+            alone = ask([cross(dt, hq, hkv, d, q_len[part], states[part])])[0]["launches"][0]
+            assert launch["tile"] == alone["tile"] and launch["blocks"] == alone["blocks"] and [x[4] for x in launch["segments"]] == [x[4] for x in alone["segments"]]
+    # long prefixes, eight to a launch: a workgroup to every second CU at least, which an eighth of that was
+    for sharing in ([16] * 64, [1] * 64):
+        own = [16] * sum(sharing)
+        a, = ask([shared(dt, 32, 8, d, [8192] * 64, sharing, own)])
+        check_shared(a, dt, 32, 8, d, [8192] * 64, sharing, own)
+        for launch in (x for x in a["launches"] if x["kind"] == "rows" and x["prefixes"]):
+            assert sum(n[4] * 8 for n in launch["segments"][:8]) >= 128
