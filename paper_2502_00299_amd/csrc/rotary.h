@@ -58,10 +58,11 @@ __device__ __forceinline__ float other_half(float x) {
   }
 }
 
-// How rows turn: not at all, whole heads by halves, the front of a head by halves, neighbours.
+// How rows turn: not at all (new tokens of a cache alone), whole heads by halves, the front of a head by halves, neighbours.
 enum Turn { kNone, kWhole, kFront, kNeighbours };
 
-// Cosine and sine of position * inv_freq, formed as in paged_append.hip, which says how far off they are.
+// Cosine and sine of position * inv_freq, by the steps of paged_append.hip, which says how far off they are.  That kernel keeps a text of its own of these
+// steps and of the pairs' below: with this one the compiler joins other products and sums, which moves a last bit here and there of what it has always stored.
 struct Turned {
   float cos, sin;
 };
@@ -74,10 +75,9 @@ __device__ __forceinline__ Turned turned(int32_t position, float inv_freq) {
   return {__builtin_fmaf(-s, rest, c), __builtin_fmaf(c, rest, s)};
 }
 
-
 // Angles that a lane holds, and those of this lane: element e turns by (cs[e], sn[e]) with its partner's value (neighbours: elements 2 e and
 // 2 e + 1); the second of a pair adds what the first subtracts.  The 64 / LPR row groups of a wavefront form a share of them each.
-__host__ __device__ constexpr int lane_angles(int turn, int epl) { return turn == kNone ? 1 : (turn == kNeighbours ? epl / 2 : epl); }
+__host__ __device__ constexpr int lane_angles(int turn, int epl) { return turn == kNeighbours ? epl / 2 : epl; }
 template <int TURN, int LPR, int EPL>
 __device__ __forceinline__ void form_angles(int32_t position, const float *inv_freq, int rotary, int lane, float (&cs)[lane_angles(TURN, EPL)], float (&sn)[lane_angles(TURN, EPL)]) {
   constexpr int RPW = 64 / LPR, NA = lane_angles(TURN, EPL);
@@ -116,7 +116,7 @@ __device__ __forceinline__ void turn_row(float (&y)[EPL], const float (&cs)[lane
       y[e] = __builtin_fmaf(p, c, -q * s);
       y[e + 1] = __builtin_fmaf(q, c, p * s);
     }
-  } else if constexpr (TURN != kNone) {
+  } else {
     float z[EPL];
 #pragma unroll
     for (int e = 0; e < EPL; ++e) z[e] = TURN == kWhole ? other_half<LPR>(y[e]) : __shfl(y[e], partner);

@@ -51,7 +51,7 @@ struct RowsArgs {
   const void *q, *k, *v;
   void *out;
   float *lse;
-  float4 *part_ml;                       // (reference in log2 units, sum of the weights as multiplied, sum before their rounding, -) of every partial row
+  float4 *part_ml;                       // (reference before the scale, sum of the weights as multiplied, sum before their rounding, -) of every partial row
   float *part_o;                         // [d] of every partial row
   int64_t q_tok, q_head, out_tok, out_head;        // bytes
   Divisor heads, group;                  // kv-heads; query heads of one

@@ -510,9 +510,9 @@ int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_p
     r.geom = geometry(pages, page_table);
     r.prefix_table = prefix_table; r.prefix_pitch = prefix->table_pitch;
     r.kv_len = kv_len; r.prefix_len = prefix_len;
-    r.q = q; r.k = k_pages; r.v = v_pages; r.out = out; r.lse = lse;
+    r.q = q; r.k = k_pages; r.v = v_pages; r.lse = lse;   // lse: whether there is one; the join writes it, and the outputs
     r.part_ml = part_ml; r.part_o = part_o;
-    r.q_tok = r.out_tok = (int64_t)pages->n_q_heads * d * esz; r.q_head = r.out_head = (int64_t)d * esz;
+    r.q_tok = (int64_t)pages->n_q_heads * d * esz; r.q_head = (int64_t)d * esz;
     r.heads = divisor(hkv); r.group = divisor(g); r.segments = np + nb; r.prefixes = np; r.prefix0 = i0; r.seq0 = b0; r.tile = plan.tile;
     r.scale = scale; r.scale_log2e = scale_log2e;
     for (int &x : r.first) x = INT32_MAX;

@@ -135,8 +135,8 @@ struct RowsWork {
   const char *k, *v;                        // keys in a row: of (segment, kv-head), key r0
   const uint8_t *mask;                      // of key r0, or null
   const char *q;                            // of the segment's first token
-  char *out;
-  float *lse;
+  char *out;                                // keys in a row: of the segment's first token
+  float *lse;                               // and of that, or null
 };
 
 template <bool PAGED>
@@ -188,17 +188,17 @@ __device__ __forceinline__ RowsWork rows_work(const RowsArgsOf<PAGED> &a, const 
     if (range != full) w.page = entry(w.r0, w.r0 + w.len);
   }
   w.q = (const char *)r.q;
-  w.out = (char *)r.out;
+  w.out = nullptr;
   w.k = (const char *)r.k;
   w.v = (const char *)r.v;
   w.mask = nullptr;
-  w.lse = r.lse != nullptr ? r.lse + (int64_t)tok0 * (int)(r.heads.d * r.group.d) : nullptr;
+  w.lse = nullptr;
   if constexpr (PAGED) {
     w.q += tok0 * r.q_tok;
-    w.out += tok0 * r.out_tok;
   } else {
     w.q += kernarg_at<int64_t>(offsetof(CrossArgs, q_base), s);
-    w.out += kernarg_at<int64_t>(offsetof(CrossArgs, out_base), s);
+    w.out = (char *)r.out + kernarg_at<int64_t>(offsetof(CrossArgs, out_base), s);
+    if (r.lse != nullptr) w.lse = r.lse + (int64_t)tok0 * (int)(r.heads.d * r.group.d);
     const int64_t at = kernarg_at<int64_t>(offsetof(CrossArgs, kv_base), s) + w.h * r.geom.head + w.r0 * r.geom.tok;
     w.k += at;
     w.v += at;
@@ -423,8 +423,8 @@ struct Rows {
   }
 };
 
-// States of wavefronts in LDS, W of them of the same 32 rows, to outputs or partial rows; eight threads to a row.
-template <int DT, int HD, bool LSE, int W, typename R>
+// States of wavefronts in LDS, W of them of the same 32 rows, to outputs or, behind shared prefixes always, partial rows; eight threads to a row.
+template <int DT, int HD, bool PAGED, bool LSE, int W, typename R>
 __device__ __forceinline__ void rows_finish(const R &r, const RowsWork &w, const float *o, const float4 *ml, int rows, int t, int threads) {
   const int heads = (int)(r.heads.d * r.group.d), first = t % 8 * 4;   // every eighth 16-byte piece of a row
   for (int i = t / 8; i < rows; i += threads / 8) {
@@ -449,7 +449,7 @@ __device__ __forceinline__ void rows_finish(const R &r, const RowsWork &w, const
 #pragma unroll
       for (int k = 0; k < W; ++k) x[j] += *(const f32x4 *)(o + Rows<DT, HD, LSE>::piece(wave + k, n, first + 32 * j)) * f[k];
     }
-    if (w.part < 0) {
+    if (!PAGED && w.part < 0) {
       const int token = divided(row, r.group), head = w.h * (int)r.group.d + (row - token * (int)r.group.d);
       const float inv = l > 0.f ? 1.f / l : 0.f;
       char *to = w.out + token * r.out_tok + head * r.out_head + first * RowsShape<DT, HD>::kEsz;
@@ -700,7 +700,7 @@ __device__ __forceinline__ void rows_wide(const RowsArgsOf<PAGED> &a, const Rows
   if (!idle) x.put((float *)smem, (float4 *)(smem + S::kLds), wave, n, half);
   __syncthreads();
   const int left = w.rows - w.row0, most = 256 / WK;
-  rows_finish<DT, HD, LSE, WK>(r, w, (const float *)smem, (const float4 *)(smem + S::kLds), left < most ? left : most, wave * 64 + lane, 512);
+  rows_finish<DT, HD, PAGED, LSE, WK>(r, w, (const float *)smem, (const float4 *)(smem + S::kLds), left < most ? left : most, wave * 64 + lane, 512);
 }
 
 // 32 rows, by four wavefronts.
@@ -786,7 +786,7 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
   __syncthreads();                         // the other wavefronts' slots are read
   if (n < w.rows) x.put((float *)smem, ml, wave, n, half);
   __syncthreads();
-  rows_finish<DT, HD, LSE, 4>(r, w, (const float *)smem, ml, w.rows, wave * 64 + lane, 256);
+  rows_finish<DT, HD, PAGED, LSE, 4>(r, w, (const float *)smem, ml, w.rows, wave * 64 + lane, 256);
 }
 
 // Segment of this workgroup, and its number in it.
