@@ -456,9 +456,10 @@ typedef struct {
  *   lse        NULL or device float [sum of q_len][Hq], tokens of sequence 0 first: natural log of the softmax denominator (-inf where no
  *              state is left).  With it, parts of an attention can be joined: over a cache here, among the tokens themselves elsewhere
  *   workspace  chunkkv_cross_workspace_bytes(cross) bytes (0 = invalid), contents scratch
- * Products and sums in fp32.  Softmax weights of 16-bit types are rounded to that type once, to nearest, and normalised by the sum of
- * the rounded ones (fp16: those below 2^-23 of the largest lose bits, down to 2^-33); outputs are rounded once more, lse not at all below
- * fp32.  The same call on the same inputs gives the same bits.  A NaN or an infinity in a state that counts gives undefined outputs of
+ * Products and sums in fp32.  Softmax weights of 16-bit types: those of a sequence with up to 32 query rows (tokens times g) are multiplied to
+ * 2^-16 (fp16 2^-22, and 2^-34 of the largest); with more, they are rounded to the type once, to nearest, and normalised by the sum of the rounded
+ * ones (fp16: those below 2^-23 of the largest lose bits, down to 2^-33).  Outputs are rounded to the storage type, lse not at all below fp32.
+ * The same call on the same inputs gives the same bits.  A NaN or an infinity in a state that counts gives undefined outputs of
  * its kv-head's query heads.  One or two launches per 32 sequences.                                                                  */
 size_t chunkkv_cross_workspace_bytes(const chunkkv_cross *cross);
 int chunkkv_cross_attention(const chunkkv_cross *cross, const int32_t *kv_len, const uint8_t *kv_mask, const void *q, const void *k,
@@ -474,8 +475,9 @@ int chunkkv_cross_attention(const chunkkv_cross *cross, const int32_t *kv_len, c
  *   page_table   device int32 [B][pages->table_pitch];          kv_len      device int32 [B][Hkv], or NULL: max_tokens
  *   q            device [B][Hq][d], 16-byte aligned;  out  device [B][Hq][d] in the storage type;  lse  NULL or device float [B][Hq]
  *   workspace    chunkkv_shared_decode_workspace_bytes(prefix, pages, n_sharing) bytes (0 = invalid), contents scratch
- * No slot in either: out = 0, lse = -inf.  Pages that are not there, rows without a token and precision of weights and outputs as in
- * chunkkv_paged_decode_attention and chunkkv_cross_attention.  Two launches up to 64 sequences and 8 prefixes.                    */
+ * No slot in either: out = 0, lse = -inf.  Pages that are not there and rows without a token as in chunkkv_paged_decode_attention.  Outputs, which
+ * have the storage type here, and the precision of weights as in chunkkv_cross_attention: a prefix has n_sharing times g query rows, a sequence's own
+ * slots g.  Two launches up to 64 sequences and 8 prefixes.                                                                         */
 size_t chunkkv_shared_decode_workspace_bytes(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing);
 int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_pages *pages, const int32_t *n_sharing,
                                     const int32_t *prefix_table, const int32_t *prefix_len, const int32_t *page_table, const int32_t *kv_len,

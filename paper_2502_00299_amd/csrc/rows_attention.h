@@ -24,10 +24,12 @@
 //   output   O^T[dim][row] = V^T P^T: the order in which keys are summed is free, so the weights are the B operand where the scores left
 //            them, and V^T comes out of LDS in that order, by transposing reads (16 bits) or as rows (fp32).
 //
-// Weights of 16-bit types are rounded to that type once, to nearest: the output has that type, and what the rounding of a weight leaves
-// in it is as much as its own does (2^-8 of the weight's part in bf16).  They are normalised by the sum of the rounded ones, so they add up
-// to one; the log-sum-exp takes the sum before.  fp16 weights are held 2^9 times as large, so that the smallest normal one is 2^-23 of the
-// reference.  Scores, references, sums and outputs are fp32.
+// Weights of 16-bit types.  32 rows, which are bound by memory and latency: a weight is two numbers of the type, it rounded and what that leaves, both multiplied
+// (2^-16 of it in bf16, 2^-22 in fp16), so outputs are as good as their own rounding; normalised by the sum of the weights.  One number instead: eight tokens over
+// up to 2048 masked keys 13.7 us rather than 14.1, others the same within 1 %, with errors of 1.94e-3 rather than 1.67e-3 of the outputs, which is
+// their rounding alone.  More rows, which are bound by issue and products: rounded to the type once, to nearest (1.95e-3 to 2.14e-3), as the second product would cost as much
+// as the scores; normalised by the sum of the rounded ones, so they add up to one; the log-sum-exp takes the sum before.  fp16 weights are held 2^9 times as large, so
+// that the smallest normal one is 2^-23 of the reference.  Scores, references, sums and outputs are fp32.
 // The reference of the online softmax is lazy: weights are taken from the one there is, and only where 32 of them add up to kOver is the maximum
 // looked for and the reference moved.  Looking at it before every block instead: 1044 us rather than 988 for 4096 tokens over 16384 keys of a
 // head dimension of 128 with 32 query heads on 8, 198 rather than 189 for 64 sequences behind a prefix of 131072.
@@ -60,6 +62,12 @@ template <int DT>
 __device__ __forceinline__ float add2(uint32_t pair, float x) {
   if constexpr (DT == CHUNKKV_BF16) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), x, false);
   else return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), __builtin_bit_cast(f16x2, 0x3C003C00u), x, false);
+}
+// Number i of such a pair.
+template <int DT>
+__device__ __forceinline__ float part(uint32_t pair, int i) {
+  if constexpr (DT == CHUNKKV_BF16) return __uint_as_float(i == 0 ? pair << 16 : pair & 0xFFFF0000u);
+  else return (float)__builtin_bit_cast(f16x2, pair)[i];
 }
 
 // Four numbers as four elements of a row.
@@ -229,9 +237,12 @@ struct RowsShape {
 };
 
 // A wavefront's 32 query rows and what they have seen: row n = lane % 32 in both halves of the wavefront.
-template <int DT, int HD, bool LSE>
+template <int DT, int HD, bool LSE, bool FINE = false>
 struct Rows {
   using S = RowsShape<DT, HD>;
+  // FINE: weights of 16-bit types are two numbers, kParts.  kWhole: they are multiplied as they are, so there is one sum of them.
+  static constexpr bool kWhole = DT == CHUNKKV_F32 || FINE;
+  static constexpr int kParts = DT != CHUNKKV_F32 && FINE ? 2 : 1;
   // fp16 weights are held 2^kOff times as large.  A row's reference moves to its maximum when that is kRise above it in log2 units; kOver: more
   // than the weights of 32 keys add up to where it is not, and no less than what a weight may be.
   static constexpr float kOff = DT == CHUNKKV_F16 ? 9.f : 0.f, kRise = DT == CHUNKKV_F16 ? 1.f : 3.f, kOver = DT == CHUNKKV_F16 ? 65536.f : 512.f;
@@ -293,13 +304,13 @@ struct Rows {
     const float m_new = rise ? fmaxf(mx, kPagedLowest) : m, f = __builtin_amdgcn_exp2f((m - m_new) * c1);
     m = m_new;
     l *= f;
-    if constexpr (LSE) le *= f;
+    if constexpr (LSE && !kWhole) le *= f;
 #pragma unroll
     for (int i = 0; i < S::kD; ++i) acc[i] *= f;
   }
-  // Weights of NKB blocks: p, and for 16-bit types pk, pairs rounded; their sums.
+  // Weights of NKB blocks: p, and for 16-bit types pk, pairs rounded, and behind them what that leaves; their sums.
   template <int NKB, typename F>
-  static __device__ __forceinline__ void weights(F &&exponent, float (&p)[NKB][16], uint32_t (&pk)[NKB][8], float &sum, float &exact) {
+  static __device__ __forceinline__ void weights(F &&exponent, float (&p)[NKB][16], uint32_t (&pk)[NKB][8 * kParts], float &sum, float &exact) {
     constexpr int NS = LSE ? 2 : 4;      // sums in parallel, as registers allow
     float s4[NS], e4[NS];
 #pragma unroll
@@ -314,6 +325,11 @@ struct Rows {
       for (int e = 0; e < 8; ++e) {
         if constexpr (DT == CHUNKKV_F32) {
           s4[e % NS] += p[b][2 * e] + p[b][2 * e + 1];
+        } else if constexpr (FINE) {
+          const float x = p[b][2 * e], y = p[b][2 * e + 1];
+          pk[b][e] = pack2<DT>(x, y);
+          pk[b][8 + e] = pack2<DT>(x - part<DT>(pk[b][e], 0), y - part<DT>(pk[b][e], 1));
+          s4[e % NS] += x + y;
         } else {
           pk[b][e] = pack2<DT>(p[b][2 * e], p[b][2 * e + 1]);
           s4[e % NS] = add2<DT>(pk[b][e], s4[e % NS]);
@@ -326,17 +342,17 @@ struct Rows {
   }
   // The weights, after the references have moved; the sums take them in.
   template <int NKB>
-  __device__ __forceinline__ void weigh(const f32x16 (&sc)[NKB], float (&p)[NKB][16], uint32_t (&pk)[NKB][8]) {
+  __device__ __forceinline__ void weigh(const f32x16 (&sc)[NKB], float (&p)[NKB][16], uint32_t (&pk)[NKB][8 * kParts]) {
     float sum, exact, mx;
     const bool rise = rises<NKB>(sc, mx);
     if (__builtin_amdgcn_ballot_w64(rise) != 0) move(rise, mx);
     weights<NKB>([&](int b, int e) __attribute__((always_inline)) { return __builtin_fmaf(sc[b][e] - m, c1, kOff); }, p, pk, sum, exact);
     l += sum;
-    if constexpr (LSE) le += exact;
+    if constexpr (LSE && !kWhole) le += exact;
   }
   // The same where references seldom move: from the ones there are, without a look at the maximum, and again only if that was too low.
   template <int NKB>
-  __device__ __forceinline__ void weigh_on(const f32x16 (&sc)[NKB], float (&p)[NKB][16], uint32_t (&pk)[NKB][8]) {
+  __device__ __forceinline__ void weigh_on(const f32x16 (&sc)[NKB], float (&p)[NKB][16], uint32_t (&pk)[NKB][8 * kParts]) {
     float sum, exact, mx;
     weights<NKB>([&](int b, int e) __attribute__((always_inline)) { return __builtin_fmaf(sc[b][e], c1, ref); }, p, pk, sum, exact);
     if ((__builtin_amdgcn_ballot_w64(sum >= kOver) | rough) != 0) {
@@ -348,7 +364,7 @@ struct Rows {
       rough = __builtin_amdgcn_ballot_w64(fabsf(m * c1) >= 0x1p14f);
     }
     l += sum;
-    if constexpr (LSE) le += exact;
+    if constexpr (LSE && !kWhole) le += exact;
   }
   // Values of 32 keys at `at` in LDS, this lane's place among them at vat[].  16 bits: read ahead of their use.  `bits`: keys that count.
   struct Values {
@@ -362,7 +378,7 @@ struct Rows {
       read_vt<S::kRow>(from, x.v);
     }
   }
-  __device__ __forceinline__ void values(const char *smem, uint32_t at, const uint32_t (&vat)[S::kD], const Values &x, const float (&p)[16], const uint32_t (&pk)[8], uint32_t bits) {
+  __device__ __forceinline__ void values(const char *smem, uint32_t at, const uint32_t (&vat)[S::kD], const Values &x, const float (&p)[16], const uint32_t (&pk)[8 * kParts], uint32_t bits) {
     if constexpr (DT == CHUNKKV_F32) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -384,17 +400,20 @@ struct Rows {
     } else {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        const u32x4 pf = {pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]};
 #pragma unroll
-        for (int i = 0; i < S::kD; ++i) acc[i] = mma32<DT>(x.v[ks][i], pf, acc[i]);
+        for (int j = 0; j < kParts; ++j) {
+          const u32x4 pf = {pk[8 * j + 4 * ks], pk[8 * j + 4 * ks + 1], pk[8 * j + 4 * ks + 2], pk[8 * j + 4 * ks + 3]};
+#pragma unroll
+          for (int i = 0; i < S::kD; ++i) acc[i] = mma32<DT>(x.v[ks][i], pf, acc[i]);
+        }
       }
     }
   }
   // Halves of a row together; fp16 weights back to their size.
   __device__ __forceinline__ void close() {
     l += __shfl_xor(l, 32);
-    if constexpr (LSE) le += __shfl_xor(le, 32);
-    if constexpr (DT == CHUNKKV_F32) le = l;
+    if constexpr (LSE && !kWhole) le += __shfl_xor(le, 32);
+    if constexpr (kWhole) le = l;
     if constexpr (kOff != 0.f) {
       l *= 0x1p-9f;
       le *= 0x1p-9f;
@@ -741,7 +760,8 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
   rows_places<DT, HD>(lane, lds0, kat, vat);
   const uint32_t kbase = (uint32_t)(wave * 2 * SLOT);
-  Rows<DT, HD, LSE> x;
+  using X = Rows<DT, HD, LSE, true>;
+  X x;
   x.load(rows_query(r, w, n), half, r.scale_log2e);
   uint32_t bits = look(0);
   issue_k(0);
@@ -770,10 +790,10 @@ __device__ __forceinline__ void rows_narrow(const RowsArgsOf<PAGED> &a, const Ro
     if (now != 0) {
       if (now != ~0u) x.leave_out(sc[0], now);
       float p[1][16];
-      uint32_t pk[1][8];
+      uint32_t pk[1][8 * X::kParts];
       x.template weigh<1>(sc, p, pk);
       __builtin_amdgcn_s_waitcnt(vm_imm(2 * NL));
-      typename Rows<DT, HD, LSE>::Values vf;
+      typename X::Values vf;
       x.read_values(kbase + SLOT, vat, vf);
       x.values(smem, kbase + SLOT, vat, vf, p[0], pk[0], now);
     }
