@@ -13,8 +13,8 @@
 // their use; a barrier to a tile is all that wavefronts wait for.
 //
 // Measured (MI355X).  Wide, 16 bits: bound by issue, not by one unit: the matrix cores are busy for half of the cycles, exponentials, sums and
-// roundings take most of the rest, at the clock that this power allows: 4096 tokens over 16384 keys, 32 heads on 8, d = 128, bf16: 958 us,
-// 1150 TFLOP/s, where a matrix product of 8192^3 reaches 1175.  Wide fp32: by its products, 129 of 152 TFLOP/s a tile; short calls also by starts and
+// roundings take most of the rest, at the clock that this power allows: 4096 tokens over 16384 keys, 32 heads on 8, d = 128, bf16: 955 to 1005 us
+// by the card, 1150 to 1095 TFLOP/s, where a matrix product of 8192^3 reaches 1175 to 1200.  Wide fp32: by its products, 129 of 152 TFLOP/s a tile; short calls also by starts and
 // partial rows.  Narrow: by memory, eight tokens over 16384 keys each (537 MB) 95 us, 5.6 TB/s; a few hundred keys by latency, 7 us.
 // Tried and slower: scores of the next block beside the weights of this one in one stream of instructions (3 to 8 %), half of the wavefronts half
 // a block behind the others (4 %).  Wave priorities change nothing.
