@@ -406,7 +406,7 @@ int chunkkv_rotary_frequencies(int32_t rotary_dim, double base, double factor, d
  * head_dim elements are contiguous, rows are 16-byte aligned.  Rows of a fused projection and those of a cache both fit, in different
  * orders too.  In place (out == in) the strides have to be the same; otherwise nothing that is written may overlap what is read.  Rows
  * that are written must not overlap each other: of the axes that have more than one entry, in the order of their strides, each steps
- * over all before it (CHUNKKV_ERR_SHAPE).                                                                                         */
+ * over all before it (CHUNKKV_ERR_SHAPE).  Outputs of queries and of keys are the caller's to keep apart.                          */
 typedef struct {
   const void *in;
   void *out;

@@ -141,7 +141,7 @@ int64_t blocks_of(const Shape &x, const RowsPlan &pl, int n_kv_heads) {
 //
 // A plan is that of one launch: a call's launches run one behind the other.  128 sequences of one token, one kv-head and 16384 keys, bf16, d = 128: 365 us
 // with ranges for the sum of all, 202 so; 64 prefixes of 8192 slots with 16 sequences of 32 heads on 8 each 937 and 650; 300 sequences behind 5000
-// slots 122 and 143, 127 with `of_many`, which is why ranges for the wide segments alone are tried there.
+// slots 122 and 127 (143 without `of_many`, which tries ranges for the wide segments alone too).
 constexpr int kLeastRange = 128, kShortKeys = 768, kCUs = 256;
 constexpr float kStart = 5.f, kJoin = 3.5f, kRow = 0.05f, kBytes = 5.5e6f;
 constexpr float kKey[2][2][3] = {   // [fp32][d = 128][256 rows, 128, narrow]
@@ -227,7 +227,7 @@ RowsPlan plan_rows(int n, F &&shape, int n_kv_heads, int dtype, int head_dim, bo
         range = whole_tiles((float)range * blocks / (float)share);   // ends of segments are more workgroups than that
       }
     }
-    // a launch of a call that has more: its wide segments alone so many, where narrow ones are half of it or more
+    // a launch of a call that has others: so many workgroups of its wide segments, beside which narrow ones may be most of the launch
     for (int share : {kCUs / 2, kCUs, 2 * kCUs}) {
       int range = whole_tiles(wide_keys[k] * n_kv_heads / (float)share);
       for (int again = 0; of_many && again < 3 && range < whole; ++again) {
@@ -502,7 +502,7 @@ int chunkkv_shared_decode_attention(const chunkkv_pages *prefix, const chunkkv_p
   // Partial rows: those of the prefixes, then those of the sequences.
   int parts[2] = {0, (int)pl.prefix_partials}, before = 0;   // before: sequences of the prefixes before
   for (int l = 0; c.prefixes(l) + c.sequences(l) > 0; ++l) {
-    const int np = c.prefixes(l), nb = c.sequences(l), i0 = l * kLaunchPrefixes, b0 = l * kJoinSegments;
+    const int np = c.prefixes(l), nb = c.sequences(l), i0 = np > 0 ? l * kLaunchPrefixes : 0, b0 = nb > 0 ? l * kJoinSegments : 0;
     const RowsPlan plan = plan_of(l);
     SharedArgs a;
     memset(&a, 0, sizeof(a));
